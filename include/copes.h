@@ -175,7 +175,8 @@ enum { COPES_COEF_PAPER = 0, COPES_COEF_OPENAI = 1 };
 /* -------------------------------------------------------------------- host utilities */
 
 /* Version string of the library (static storage).  0.2 added copes_params.w3 / w4 and
- * copes_perturb_two_pairs: callers built against 0.1's copes_params must be rebuilt. */
+ * copes_perturb_two_pairs: callers built against 0.1's copes_params must be rebuilt.  0.3
+ * added the calls from copes_cache_workspace_bytes on and changed none. */
 const char *copes_version(void);
 
 /* Copies the calling thread's last error message into buf (NUL-terminated, truncated to
@@ -453,6 +454,122 @@ int copes_backup_restore(const copes_backup_params *p, const copes_subspace *S, 
 int copes_backup_update(const copes_backup_params *p, const copes_subspace *S, int n_members,
                         const int32_t *noise_id, const int8_t *sign, const float *fitness,
                         int n_noise, const uint64_t *seeds, float coef, cudaStream_t stream);
+
+/* --------------------------------------------------------- answering with the weights
+ * What a member's evaluation runs on the perturbed weights beside the model's matrix
+ * products: a paged key-value cache for its rollouts, the attention of one new token over
+ * it, and the log probabilities that a scored answer's reward is read from.  Evolution
+ * strategies take no gradients, so these have a forward form only. */
+
+/* A key-value cache in pages, shared by all layers of a model.
+ *  pool:   device [n_pages][n_layers][2][n_kv_heads][page_size][head_dim] of dtype, keys at
+ *          index 0 and values at 1 of the third axis; 16-byte aligned.  A page holds page_size
+ *          tokens of every layer in one piece.
+ *  table:  device int32 [n_slots][table_width]: the pages of each sequence (a "slot") in
+ *          order; token t is in page table[slot][t / page_size] at place t % page_size.
+ *  length: device int32 [n_slots]: the tokens of each sequence, 0 for an empty slot.
+ *  refs:   device int32 [n_pages]: how many table entries name the page; 0: free.
+ * The caller owns the four arrays, which must be disjoint, and an all-zero length and refs
+ * are an empty cache.  The calls below keep them consistent: a page is free, or held by one
+ * slot, or full and shared by several (copes_cache_fork).  Only pages of tokens below a
+ * slot's length are ever read.  An id in table outside [0, n_pages) is not followed (its tokens
+ * read as zeros) and is reported by copes_check (bit 32).
+ * head_dim is a multiple of 8 and at most COPES_MAX_HEAD_DIM; n_pages is at most
+ * COPES_MAX_PAGES; table_width * page_size and n_slots * table_width are below 2^31. */
+enum { COPES_MAX_HEAD_DIM = 256, COPES_MAX_PAGES = 1 << 22, COPES_MAX_TOP = 32 };
+typedef struct {
+  void *pool;
+  int dtype;        /* COPES_BF16 or COPES_FP32 */
+  int n_pages;
+  int n_layers;
+  int n_kv_heads;
+  int page_size;    /* tokens of a page, any number >= 1 */
+  int head_dim;
+  int32_t *table;
+  int n_slots;
+  int table_width;  /* pages a sequence may have */
+  int32_t *length;
+  int32_t *refs;
+} copes_kv_cache;
+
+/* Device workspace of copes_cache_grow, _fork and _compact (16-byte aligned; its contents
+ * need not be kept or cleared).  Calls that share a cache run in one stream's order. */
+size_t copes_cache_workspace_bytes(const copes_kv_cache *c);
+
+/* Grows n distinct slots (device int32 [n]) by add[i] >= 0 tokens (device int32 [n]), or by
+ * add_all each where add is NULL, and gives them the pages these need: the free pages with
+ * the lowest ids, in the order of the list, then of the tokens.  The new tokens' keys and
+ * values are whatever the pages hold until copes_cache_append writes them.
+ * All or nothing: an id outside the cache or named twice, a negative count or more tokens than
+ * table_width * page_size (copes_check bit 32), or too few free pages (bit 64) leave the whole
+ * cache as it was. */
+int copes_cache_grow(const copes_kv_cache *c, const int32_t *slots, int n, const int32_t *add, int add_all,
+                     void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* Writes keys and values of one layer: row i (head h at k + i k_row + h k_head, elements;
+ * likewise v; head_dim values in a row) goes to token position[i] of slots[i]; where position
+ * is NULL, to the slot's last token, and where slots is NULL, to slot i.  Slots may repeat
+ * (a prompt's tokens); of rows that name one token (through a shared page, or twice) each value
+ * is one of theirs.  A row that is not a token of its slot is skipped and reported (bit 32). */
+int copes_cache_append(const copes_kv_cache *c, int layer, const int32_t *slots, const int32_t *position, int n,
+                       const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                       int64_t v_head, cudaStream_t stream);
+
+/* Fork: the empty slot children[i] becomes a copy of parents[i] (device int32 [n], children
+ * distinct and none of them a parent, parents may repeat).  Full pages are shared (refs grows by one); a partly filled
+ * last page is copied whole, in all layers, to the free page with the lowest id, in the order
+ * of the list.  All or nothing as copes_cache_grow; a child that is not empty is bit 32. */
+int copes_cache_fork(const copes_kv_cache *c, const int32_t *parents, const int32_t *children, int n,
+                     void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* Empties n slots: length 0, their table entries -1, and each of their pages' refs lowered
+ * by one.  An empty slot, or one named twice, loses nothing more.  An id outside the cache is
+ * skipped and reported (bit 32). */
+int copes_cache_free(const copes_kv_cache *c, const int32_t *slots, int n, cudaStream_t stream);
+
+/* Moves the pages in use to ids 0 .. U-1, U their number: those at U and above move, in
+ * ascending order, to the free ids below U in ascending order; table and refs follow, and the
+ * ids they leave are free.  counts (device int32 [2], or NULL) gets U and the number moved. */
+int copes_cache_compact(const copes_kv_cache *c, int32_t *counts, void *workspace, size_t workspace_bytes,
+                        cudaStream_t stream);
+
+/* pool[dst[i]] = pool[src[i]], whole pages of all layers (device int32 [n]); table, length
+ * and refs stay.  No page may be in dst twice, or in both.  A pair with an id outside the
+ * cache is skipped and reported (bit 32). */
+int copes_cache_copy_pages(const copes_kv_cache *c, const int32_t *src, const int32_t *dst, int n,
+                           cudaStream_t stream);
+
+/* Attention of one new token per row over its slot's pages of one layer.  Row i reads slot
+ * slots[i] (device int32 [n]; NULL: slot i); query head h (q + i q_row + h q_head, elements)
+ * reads key-value head h / (q_heads / n_kv_heads), and with s_t = scale q . k_t over the
+ * slot's tokens t < length:
+ *   out[i][h] = sum_t softmax(s)_t v_t   ([n][q_heads][head_dim] of dtype),
+ *   lse[i][h] = ln sum_t exp(s_t)        (fp32 [n][q_heads], or NULL).
+ * The new token's own key and value are in the cache before the call (grow, append).  A slot
+ * without tokens gives 0 and -inf, and so does an id outside the cache (bit 32).
+ * Scores, softmax and sums are fp32, with every product of bf16 values exact.
+ * workspace: copes_paged_attention_workspace_bytes(c, n, q_heads) bytes, 16-byte aligned,
+ * all zero before its first use: a call leaves its counters zero again, so one buffer serves
+ * any number of calls in one stream's order, of any sizes it is large enough for. */
+size_t copes_paged_attention_workspace_bytes(const copes_kv_cache *c, int n, int q_heads);
+int copes_paged_attention(const copes_kv_cache *c, int layer, const int32_t *slots, int n, const void *q,
+                          int64_t q_row, int64_t q_head, int q_heads, float scale, void *out, float *lse,
+                          void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* Log probabilities under softmax(x), x = scale * logits, of each row of logits (row i at
+ * logits + i row elements, vocab values of dtype; scale > 0, an inverse temperature):
+ *   logprob[i] = x[target[i]] - ln sum_j exp(x_j)       (fp32 [n]),
+ *   entropy[i] = -sum_j p_j ln p_j                      (fp32 [n], or NULL),
+ *   top_ids[i], top_logprobs[i]: the top largest logits (int64 and fp32 [n][top]; NULL with
+ *     top = 0), largest first, equal ones by ascending id; 0 <= top <= min(vocab, COPES_MAX_TOP).
+ * target: device int64 [n]; a negative one is padding (logprob 0), one past the vocabulary
+ * gives NaN and is reported by copes_check (bit 32).  A logit of -inf is a masked token: no
+ * probability, and nothing in the entropy.  A row of nothing else has logprob -inf, entropy
+ * 0 and the lowest ids as alternatives, at -inf.  A NaN or +inf in a row makes its
+ * outputs NaN, but for top_ids, which order NaN above +inf, and logprob 0 of padding. */
+int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_t row, const int64_t *target,
+                         float scale, int top, float *logprob, float *entropy, int64_t *top_ids,
+                         float *top_logprobs, cudaStream_t stream);
 
 /* ------------------------------------------------------------------- debug exports */
 

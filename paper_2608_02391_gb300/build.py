@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcopes.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.cu", "es_kernels.cu", "elem_ragged.cu", "replay_kernels.cu", "backup_kernels.cu", "shape_kernels.cu",
-           "partition_kernels.cu", "hash_static.cu"]
+           "partition_kernels.cu", "hash_static.cu", "answer_api.cu", "cache_kernels.cu", "attend_kernels.cu",
+           "logprob_kernels.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-Xptxas", "-warn-spills"]

@@ -24,6 +24,7 @@ ERR_INVALID_ARG, ERR_ALIGNMENT, ERR_SIZE, ERR_WORKSPACE, ERR_CUDA, ERR_DEVICE_CH
 BF16, FP32 = 0, 1
 TAG_NOISE, TAG_INIT, TAG_PARTITION, TAG_SEED, TAG_CHUNK = 0, 1, 2, 3, 4
 MAX_MEMBERS, MAX_NOISE, MAX_K, TILE_MAX = 256, 256, 64, 1 << 20
+MAX_HEAD_DIM, MAX_PAGES, MAX_TOP = 256, 1 << 22, 32
 SUBSPACE_TILES, SUBSPACE_INDICES, SUBSPACE_HASH_REPLAY = 0, 1, 2
 PART_CONTIGUOUS, PART_TENSOR_GROUPS, PART_HASH, PART_RANDOM_CHUNKS = 0, 1, 2, 3
 SHAPE_NONE, SHAPE_ZSCORE, SHAPE_ZSCORE_GROUPED, SHAPE_CENTERED_RANK = 0, 1, 2, 3
@@ -68,12 +69,20 @@ class PartitionSpec(ctypes.Structure):
                 ("chunk", ctypes.c_uint64), ("group_of", ctypes.c_void_p)]
 
 
+class KVCacheDesc(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("dtype", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("n_layers", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("table", ctypes.c_void_p), ("n_slots", ctypes.c_int),
+                ("table_width", ctypes.c_int), ("length", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
 _lib = None
 
 # name -> (restype, argtypes); every function declared in include/copes.h.
 _VP, _U64, _U32, _I32, _F32, _F64, _SZ = (ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32,
                                           ctypes.c_int, ctypes.c_float, ctypes.c_double,
                                           ctypes.c_size_t)
+_I64 = ctypes.c_int64
 SIGNATURES = {
     "copes_version": (ctypes.c_char_p, []),
     "copes_last_error": (_I32, [_VP, _SZ]),
@@ -111,6 +120,16 @@ SIGNATURES = {
     "copes_backup_perturb_partner": (_I32, [_VP, _VP, _VP, _U64, _U64, _VP]),
     "copes_backup_restore": (_I32, [_VP, _VP, _VP]),
     "copes_backup_update": (_I32, [_VP, _VP, _I32, _VP, _VP, _VP, _I32, _VP, _F32, _VP]),
+    "copes_cache_workspace_bytes": (_SZ, [_VP]),
+    "copes_cache_grow": (_I32, [_VP, _VP, _I32, _VP, _I32, _VP, _SZ, _VP]),
+    "copes_cache_append": (_I32, [_VP, _I32, _VP, _VP, _I32, _VP, _I64, _I64, _VP, _I64, _I64, _VP]),
+    "copes_cache_fork": (_I32, [_VP, _VP, _VP, _I32, _VP, _SZ, _VP]),
+    "copes_cache_free": (_I32, [_VP, _VP, _I32, _VP]),
+    "copes_cache_compact": (_I32, [_VP, _VP, _VP, _SZ, _VP]),
+    "copes_cache_copy_pages": (_I32, [_VP, _VP, _VP, _I32, _VP]),
+    "copes_paged_attention_workspace_bytes": (_SZ, [_VP, _I32, _I32]),
+    "copes_paged_attention": (_I32, [_VP, _I32, _VP, _I32, _VP, _I64, _I64, _I32, _F32, _VP, _VP, _VP, _SZ, _VP]),
+    "copes_token_logprobs": (_I32, [_VP, _I32, _I32, _I32, _I64, _VP, _F32, _I32, _VP, _VP, _VP, _VP, _VP]),
     "copes_debug_philox": (_I32, [_U64, _U64, _U64, _U32, _U32, _VP, _VP]),
     "copes_debug_normals": (_I32, [_U64, _U32, _U64, _U64, _VP, _VP]),
     "copes_debug_transform": (_I32, [_VP, _U64, _VP, _VP]),
@@ -541,6 +560,175 @@ def update(arena: Arena, sub: SubspaceHandle, noise_id: np.ndarray, sign: np.nda
     _check(load().copes_update(ctypes.byref(arena.params), ctypes.byref(S), nid.size, _np_ptr(nid),
                                _np_ptr(sg), _ptr(fitness), sd.size, _np_ptr(sd), coef,
                                int(fuse_commit), _stream(stream)))
+
+
+# ------------------------------------------------------------ answering with the weights
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """An output of a call on `stream`, allocated in that stream's order."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class KVCache:
+    """A paged key-value cache (copes_kv_cache): pool [n_pages, n_layers, 2, n_kv_heads,
+    page_size, head_dim] (bf16 or fp32), table [n_slots, table_width], length [n_slots] and
+    refs [n_pages] (int32).  The tensors are the caller's and may be read at any time; the
+    cache_* calls change them in stream order.  KVCache.empty allocates an empty cache.  The
+    handle keeps the calls' workspaces: its calls run in one stream's order."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, refs: torch.Tensor):
+        assert pool.dim() == 6 and pool.shape[2] == 2 and table.dim() == 2
+        assert length.shape == (table.shape[0],) and refs.shape == (pool.shape[0],)
+        for t in (pool, table, length, refs):
+            assert t.is_cuda and t.is_contiguous() and t.device == pool.device
+        assert all(t.dtype == torch.int32 for t in (table, length, refs))
+        self.pool, self.table, self.length, self.refs = pool, table, length, refs
+        self.dtype = {torch.bfloat16: BF16, torch.float32: FP32}[pool.dtype]
+        n_pages, n_layers, _, kv, ps, d = pool.shape
+        self.desc = KVCacheDesc(pool.data_ptr(), self.dtype, n_pages, n_layers, kv, ps, d, table.data_ptr(),
+                                table.shape[0], table.shape[1], length.data_ptr(), refs.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+        self.workspace_bytes = load().copes_cache_workspace_bytes(self.ref)
+        if self.workspace_bytes == 0:
+            raise CopesError(ERR_INVALID_ARG, last_error())
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=pool.device)
+        self.attend_workspace = None  # paged_attention's: zero between calls
+        self._attend_bytes = {}       # (rows, query heads) -> bytes of it
+
+    @classmethod
+    def empty(cls, n_pages: int, n_layers: int, n_kv_heads: int, page_size: int, head_dim: int, n_slots: int,
+              table_width: int, dtype=torch.bfloat16, device="cuda") -> "KVCache":
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.empty((n_pages, n_layers, 2, n_kv_heads, page_size, head_dim), dtype=dtype, device=device),
+                   torch.full((n_slots, table_width), -1, **i32), torch.zeros(n_slots, **i32),
+                   torch.zeros(n_pages, **i32))
+
+    def _ids(self, t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
+        """The address of a list of int32 ids on the cache's device."""
+        if t is None:
+            return None
+        assert t.dtype == torch.int32 and t.device == self.pool.device and t.is_contiguous() and t.dim() == 1
+        assert n is None or t.numel() == n
+        return t.data_ptr()
+
+    def attend_space(self, n: int, q_heads: int, stream=None) -> Tuple[int, int]:
+        """paged_attention's workspace (address, bytes), allocated and zeroed where it has to grow."""
+        need = self._attend_bytes.get((n, q_heads))
+        if need is None:
+            need = load().copes_paged_attention_workspace_bytes(self.ref, n, q_heads)
+            if need == 0:
+                raise CopesError(ERR_INVALID_ARG, last_error())
+            self._attend_bytes[n, q_heads] = need
+        ws = self.attend_workspace
+        if ws is None or ws.numel() < need:
+            if ws is not None and stream is not None:
+                ws.record_stream(stream)
+            ws = self.attend_workspace = _empty((need,), torch.uint8, self.pool.device, stream)
+            with torch.cuda.stream(stream):
+                ws.zero_()
+        return ws.data_ptr(), ws.numel()
+
+
+def cache_grow(cache: KVCache, slots: torch.Tensor, add, stream=None) -> None:
+    """copes_cache_grow: `add` tokens (an int, or an int32 tensor by slot) more for each of `slots`."""
+    n = slots.numel()
+    each, every = (cache._ids(add, n), 0) if isinstance(add, torch.Tensor) else (None, add)
+    _check(load().copes_cache_grow(cache.ref, cache._ids(slots), n, each, every, cache.workspace.data_ptr(),
+                                   cache.workspace_bytes, _stream(stream)))
+
+
+def cache_append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                 position: Optional[torch.Tensor] = None, stream=None) -> None:
+    """copes_cache_append: rows of k and v [n, n_kv_heads, head_dim] (any strides over rows and
+    heads) into tokens `position` (default: the last ones) of `slots` (default: 0 .. n-1)."""
+    n, want = k.shape[0], cache.pool.shape
+    for t in (k, v):
+        assert t.shape == (n, want[3], want[5]) and t.dtype == cache.pool.dtype and t.device == cache.pool.device
+        assert t.stride(2) == 1
+    _check(load().copes_cache_append(cache.ref, layer, cache._ids(slots, n), cache._ids(position, n), n, k.data_ptr(),
+                                     k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                                     _stream(stream)))
+
+
+def cache_fork(cache: KVCache, parents: torch.Tensor, children: torch.Tensor, stream=None) -> None:
+    """copes_cache_fork: the empty slot children[i] becomes a copy of parents[i]."""
+    n = parents.numel()
+    _check(load().copes_cache_fork(cache.ref, cache._ids(parents), cache._ids(children, n), n,
+                                   cache.workspace.data_ptr(), cache.workspace_bytes, _stream(stream)))
+
+
+def cache_free(cache: KVCache, slots: torch.Tensor, stream=None) -> None:
+    """copes_cache_free: empties `slots`."""
+    _check(load().copes_cache_free(cache.ref, cache._ids(slots), slots.numel(), _stream(stream)))
+
+
+def cache_compact(cache: KVCache, counts: Optional[torch.Tensor] = None, stream=None) -> None:
+    """copes_cache_compact: the pages in use move to the lowest ids; `counts` (int32 [2], device)
+    gets their number and how many moved."""
+    _check(load().copes_cache_compact(cache.ref, cache._ids(counts, 2), cache.workspace.data_ptr(),
+                                      cache.workspace_bytes, _stream(stream)))
+
+
+def cache_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """copes_cache_copy_pages: pool[dst[i]] = pool[src[i]]."""
+    n = src.numel()
+    _check(load().copes_cache_copy_pages(cache.ref, cache._ids(src), cache._ids(dst, n), n, _stream(stream)))
+
+
+def paged_attention(cache: KVCache, layer: int, q: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """copes_paged_attention: q [n, q_heads, head_dim] (any strides over rows and heads), row i
+    over slot slots[i] (default: i), scale 1 / sqrt(head_dim) by default.  Returns (out, lse):
+    [n, q_heads, head_dim] and fp32 [n, q_heads]."""
+    n, heads, d = q.shape
+    assert d == cache.desc.head_dim and q.dtype == cache.pool.dtype and q.device == cache.pool.device
+    assert q.stride(2) == 1
+    if out is None:
+        out = _empty((n, heads, d), q.dtype, q.device, stream)
+    else:
+        assert out.shape == q.shape and out.dtype == q.dtype and out.device == q.device and out.is_contiguous()
+    if lse is None:
+        lse = _empty((n, heads), torch.float32, q.device, stream)
+    else:
+        assert lse.shape == (n, heads) and lse.dtype == torch.float32 and lse.device == q.device and lse.is_contiguous()
+    ws, nbytes = cache.attend_space(n, heads, stream)
+    _check(load().copes_paged_attention(cache.ref, layer, cache._ids(slots, n), n, q.data_ptr(), q.stride(0),
+                                        q.stride(1), heads, d ** -0.5 if scale is None else scale, out.data_ptr(),
+                                        lse.data_ptr(), ws, nbytes, _stream(stream)))
+    return out, lse
+
+
+@dataclass
+class TokenLogprobs:
+    """token_logprobs' result: fp32 [n] logprob and entropy, and the alternatives, int64 and
+    fp32 [n, top]."""
+    logprob: torch.Tensor
+    entropy: torch.Tensor
+    top_ids: torch.Tensor
+    top_logprobs: torch.Tensor
+
+
+def token_logprobs(logits: torch.Tensor, target: torch.Tensor, top: int = 0, scale: float = 1.0,
+                   stream=None) -> TokenLogprobs:
+    """copes_token_logprobs: log probability of target[i] (int64, negative: padding) and entropy
+    under softmax(scale * logits[i]), and the `top` likeliest tokens; logits [n, vocab] (bf16 or
+    fp32, any stride over rows)."""
+    n, vocab = logits.shape
+    device = logits.device
+    assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
+    assert target.shape == (n,) and target.dtype == torch.int64 and target.device == device and target.is_contiguous()
+    dtype = {torch.bfloat16: BF16, torch.float32: FP32}[logits.dtype]
+    both = _empty((2, n), torch.float32, device, stream)
+    ids = _empty((n, top), torch.int64, device, stream)
+    top_logprobs = _empty((n, top), torch.float32, device, stream)
+    logprob, entropy = both[0], both[1]
+    _check(load().copes_token_logprobs(logits.data_ptr(), dtype, n, vocab, logits.stride(0), target.data_ptr(), scale,
+                                       top, logprob.data_ptr(), entropy.data_ptr(), ids.data_ptr(),
+                                       top_logprobs.data_ptr(), _stream(stream)))
+    return TokenLogprobs(logprob, entropy, ids, top_logprobs)
 
 
 # ----------------------------------------------------------------------------- debug

@@ -274,7 +274,7 @@ void copes::set_last_error(const char *message) { g_message = message; }
 
 extern "C" {
 
-const char *copes_version(void) { return "copes-gb300 0.2 (sm_103a)"; }
+const char *copes_version(void) { return "copes-gb300 0.3 (sm_103a)"; }
 
 int copes_last_error(char *buf, size_t len) {
   if (buf && len) {
@@ -290,14 +290,17 @@ int copes_check(cudaStream_t stream) {
   if (e != cudaSuccess) return cuda_fail(e, "copes_check");
   const unsigned bits = copes::read_and_clear_es_errors() | copes::read_and_clear_ragged_errors() |
                         copes::read_and_clear_partition_errors() |
-                        copes::read_and_clear_replay_errors() | copes::read_and_clear_backup_errors();
+                        copes::read_and_clear_replay_errors() | copes::read_and_clear_backup_errors() |
+                        copes::read_and_clear_cache_errors() | copes::read_and_clear_attend_errors() |
+                        copes::read_and_clear_logprob_errors();
   if ((e = cudaGetLastError()) != cudaSuccess) return cuda_fail(e, "copes_check");
   if (bits)
     return fail(COPES_ERR_DEVICE_CHECK,
                 "copes_check: a kernel's own check failed and it skipped the work (bits 0x%x: 1 = tile "
                 "outside the arena, 2 = gather index outside the arena, 4 = inconsistent partition "
                 "workspace or replay table, 8 = a bulk-copy wait ran out, 16 = an element outside "
-                "the partner buffer)",
+                "the partner buffer, 32 = a slot, page, token or target id outside its range or named "
+                "twice, 64 = too few free pages)",
                 bits);
   return COPES_OK;
 }

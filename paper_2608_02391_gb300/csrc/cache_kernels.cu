@@ -1,0 +1,369 @@
+// Pages of a key-value cache: growing, writing, forking, freeing, moving together and copying.
+//
+// Which page goes where is decided by one block (the free pages in ascending order against the
+// list's needs, by prefix sums), so that the same calls give the same pages; what has to be
+// copied then is copied by as many blocks as fill the GPU.  The plan is bound by latency, the
+// copies by HBM.
+#include "answer.h"
+
+namespace copes {
+
+__device__ unsigned g_cache_error;
+static std::atomic<bool> g_used{false};
+__device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_cache_error, bit); }
+
+constexpr int kPlanThreads = 1024;
+
+// Exclusive prefix sum of v over the block and the block's total.  `s` holds 33 ints.
+__device__ __forceinline__ int block_scan(int v, int *s, int *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();  // s may still be read by a previous scan
+  if (lane == 31) s[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int w = s[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, w, d);
+      if (lane >= d) w += y;
+    }
+    s[lane] = w;
+  }
+  __syncthreads();
+  *total = s[31];
+  return x - v + (warp ? s[warp - 1] : 0);
+}
+
+__device__ __forceinline__ int pages_of(int tokens, int page_size) {
+  return tokens / page_size + (tokens % page_size != 0);
+}
+
+// Grow and fork: what every listed slot needs, checked, and the lowest free pages given out.
+template <bool kFork>
+__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(Cache c, const int32_t *slots, const int32_t *parents,
+                                                                  const int32_t *add, int add_all, int n, int32_t *ws) {
+  __shared__ int s_scan[32];
+  __shared__ unsigned s_bad;
+  const int tid = threadIdx.x;
+  int32_t *first = ws + kPlanHeader;       // rank of slot i's first new page
+  int32_t *mark = first + c.n_slots;       // by slot: its place in the list
+  int32_t *fresh = mark + c.n_slots;       // the free pages given out, ascending
+  if (tid == 0) s_bad = 0;
+  for (int i = tid; i < n; i += kPlanThreads)
+    if ((unsigned)slots[i] < (unsigned)c.n_slots) mark[slots[i]] = -1;
+  if (kFork)
+    for (int i = tid; i < n; i += kPlanThreads)
+      if ((unsigned)parents[i] < (unsigned)c.n_slots) mark[parents[i]] = -1;
+  __syncthreads();
+
+  int total = 0;
+  for (int base = 0; base < n; base += kPlanThreads) {
+    const int i = base + tid;
+    int need = 0;
+    if (i < n) {
+      const int slot = slots[i];
+      bool ok = (unsigned)slot < (unsigned)c.n_slots && atomicCAS(&mark[slot], -1, i) == -1;
+      if (kFork) {
+        const int parent = parents[i];
+        ok = ok && (unsigned)parent < (unsigned)c.n_slots && slot_tokens(c, slot) == 0;
+        if (ok) need = slot_tokens(c, parent) % c.page_size != 0;
+      } else if (ok) {
+        const int more = add ? add[i] : add_all;
+        const int64_t now = (int64_t)slot_tokens(c, slot) + more;
+        ok = more >= 0 && now <= (int64_t)c.table_width * c.page_size;
+        if (ok) need = pages_of((int)now, c.page_size) - pages_of(slot_tokens(c, slot), c.page_size);
+      }
+      if (!ok) atomicOr(&s_bad, kErrCacheId);
+    }
+    int sum;
+    const int at = block_scan(need, s_scan, &sum);
+    if (i < n) first[i] = total + at;
+    total += sum;
+  }
+  __syncthreads();
+  if (kFork)  // a child's table is written while the parents' are read
+    for (int i = tid; i < n; i += kPlanThreads)
+      if ((unsigned)parents[i] < (unsigned)c.n_slots && mark[parents[i]] != -1) atomicOr(&s_bad, kErrCacheId);
+  __syncthreads();
+  if (s_bad) {
+    if (tid == 0) {
+      ws[kPlanDone] = 0;
+      flag_error(s_bad);
+    }
+    return;
+  }
+  int found = 0;
+  for (int base = 0; base < c.n_pages && found < total; base += kPlanThreads) {
+    const int p = base + tid;
+    const int free = p < c.n_pages && c.refs[p] == 0;
+    int sum;
+    const int at = block_scan(free, s_scan, &sum);
+    if (free && found + at < total) fresh[found + at] = p;
+    found += sum;
+  }
+  if (found < total) {
+    if (tid == 0) {
+      ws[kPlanDone] = 0;
+      flag_error(kErrCacheFull);
+    }
+    return;
+  }
+  __syncthreads();  // fresh and first, for every thread
+  for (int r = tid; r < total; r += kPlanThreads) {
+    const int page = fresh[r];
+    c.refs[page] = 1;
+    if (kFork) continue;  // the copy's blocks write the children's tables
+    int lo = 0, hi = n - 1;  // the last slot whose first page's rank is at most r
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first[mid] <= r) lo = mid;
+      else hi = mid - 1;
+    }
+    const int slot = slots[lo];
+    c.table[(int64_t)slot * c.table_width + pages_of(slot_tokens(c, slot), c.page_size) + (r - first[lo])] = page;
+  }
+  __syncthreads();  // lengths are read above
+  for (int i = tid; i < n; i += kPlanThreads)
+    c.length[slots[i]] = kFork ? slot_tokens(c, parents[i]) : slot_tokens(c, slots[i]) + (add ? add[i] : add_all);
+  if (tid == 0) ws[kPlanDone] = 1;
+}
+
+// 16-byte pieces [begin, end) of a page.
+__device__ __forceinline__ void copy_pieces(const Cache &c, int to, int from, uint64_t begin, uint64_t end) {
+  const int4 *a = reinterpret_cast<const int4 *>(c.pool + (uint64_t)from * c.page_bytes);
+  int4 *b = reinterpret_cast<int4 *>(c.pool + (uint64_t)to * c.page_bytes);
+  for (uint64_t i = begin + threadIdx.x; i < end; i += blockDim.x) b[i] = a[i];
+}
+
+// Children's tables, the shared pages' refs and the copies of partly filled pages: `parts`
+// blocks work on each child.
+__global__ void __launch_bounds__(256) fork_copy_kernel(Cache c, const int32_t *parents, const int32_t *children,
+                                                        int parts, const int32_t *ws) {
+  if (!ws[kPlanDone]) return;
+  const int i = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int32_t *first = ws + kPlanHeader, *fresh = first + 2 * (size_t)c.n_slots;
+  const int32_t *from = c.table + (int64_t)parents[i] * c.table_width;
+  int32_t *to = c.table + (int64_t)children[i] * c.table_width;
+  const int tokens = slot_tokens(c, parents[i]), full = tokens / c.page_size;
+  for (int j = part * blockDim.x + threadIdx.x; j < full; j += parts * blockDim.x) {
+    const int page = from[j];
+    to[j] = page;
+    if ((unsigned)page < (unsigned)c.n_pages) atomicAdd(&c.refs[page], 1);
+    else flag_error(kErrCacheId);
+  }
+  if (tokens % c.page_size == 0) return;
+  const int page = from[full], copy = fresh[first[i]];
+  if (part == 0 && threadIdx.x == 0) to[full] = copy;
+  if ((unsigned)page >= (unsigned)c.n_pages) {
+    if (threadIdx.x == 0) flag_error(kErrCacheId);
+    return;
+  }
+  const uint64_t pieces = c.page_bytes / 16;
+  copy_pieces(c, copy, page, pieces * part / parts, pieces * (part + 1) / parts);
+}
+
+// One block per slot.  The exchange of the length makes one of a slot's blocks the one that frees it.
+__global__ void __launch_bounds__(256) cache_free_kernel(Cache c, const int32_t *slots) {
+  __shared__ int s_tokens;
+  const int slot = slots[blockIdx.x];
+  if ((unsigned)slot >= (unsigned)c.n_slots) {
+    if (threadIdx.x == 0) flag_error(kErrCacheId);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    const int len = atomicExch(&c.length[slot], 0), most = c.table_width * c.page_size;
+    s_tokens = len < 0 ? 0 : (len < most ? len : most);
+  }
+  __syncthreads();
+  int32_t *row = c.table + (int64_t)slot * c.table_width;
+  for (int j = threadIdx.x; j < pages_of(s_tokens, c.page_size); j += blockDim.x) {
+    const int page = row[j];
+    row[j] = -1;
+    if ((unsigned)page < (unsigned)c.n_pages) atomicSub(&c.refs[page], 1);
+    else flag_error(kErrCacheId);
+  }
+}
+
+// Compact: counts the pages in use (U) and pairs those at U and above with the free ids below.
+// ws: to[r] and from[r] of move r (the list of fresh pages' place and the one after it).
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(Cache c, int32_t *counts, int32_t *ws) {
+  __shared__ int s_scan[32];
+  const int tid = threadIdx.x;
+  int32_t *to = ws + kPlanHeader + 2 * (size_t)c.n_slots, *from = to + c.n_pages;
+  int mine = 0, used, sum;
+  for (int p = tid; p < c.n_pages; p += kPlanThreads) mine += c.refs[p] != 0;
+  block_scan(mine, s_scan, &used);
+  int holes = 0, movers = 0;
+  for (int base = 0; base < used; base += kPlanThreads) {
+    const int p = base + tid;
+    const int hole = p < used && c.refs[p] == 0;
+    const int at = block_scan(hole, s_scan, &sum);
+    if (hole) to[holes + at] = p;
+    holes += sum;
+  }
+  for (int base = used; base < c.n_pages; base += kPlanThreads) {
+    const int p = base + tid;
+    const int mover = p < c.n_pages && c.refs[p] != 0;
+    const int at = block_scan(mover, s_scan, &sum);
+    if (mover) from[movers + at] = p;
+    movers += sum;
+  }
+  __syncthreads();
+  for (int r = tid; r < movers; r += kPlanThreads) {  // as many holes as movers
+    c.refs[to[r]] = c.refs[from[r]];
+    c.refs[from[r]] = 0;
+  }
+  if (tid == 0) {
+    ws[kPlanTotal] = movers;
+    if (counts) {
+      counts[0] = used;
+      counts[1] = movers;
+    }
+  }
+}
+
+// The moves' copies, in pieces of 16 bytes over the whole grid, and the tables' new ids.
+__global__ void __launch_bounds__(256) compact_move_kernel(Cache c, const int32_t *ws) {
+  const int moves = ws[kPlanTotal];
+  if (moves == 0) return;
+  const int32_t *to = ws + kPlanHeader + 2 * (size_t)c.n_slots, *from = to + c.n_pages;
+  const int lowest = from[0];  // the moves' sources ascend
+  for (int slot = blockIdx.x; slot < c.n_slots; slot += gridDim.x) {
+    int32_t *row = c.table + (int64_t)slot * c.table_width;
+    const int pages = pages_of(slot_tokens(c, slot), c.page_size);
+    for (int j = threadIdx.x; j < pages; j += blockDim.x) {
+      const int page = row[j];
+      if (page < lowest) continue;
+      int lo = 0, hi = moves - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (from[mid] < page) lo = mid + 1;
+        else hi = mid;
+      }
+      if (from[lo] == page) row[j] = to[lo];
+    }
+  }
+  const uint64_t pieces = c.page_bytes / 16, share = 2048, parts = (pieces + share - 1) / share;
+  for (uint64_t job = blockIdx.x; job < parts * moves; job += gridDim.x) {
+    const uint64_t r = job / parts, begin = job % parts * share;
+    copy_pieces(c, to[r], from[r], begin, begin + share < pieces ? begin + share : pieces);
+  }
+}
+
+__global__ void __launch_bounds__(256) copy_pages_kernel(Cache c, const int32_t *src, const int32_t *dst, int parts) {
+  const int i = blockIdx.x / parts, part = blockIdx.x % parts, from = src[i], to = dst[i];
+  if ((unsigned)from >= (unsigned)c.n_pages || (unsigned)to >= (unsigned)c.n_pages) {
+    if (threadIdx.x == 0) flag_error(kErrCacheId);
+    return;
+  }
+  const uint64_t pieces = c.page_bytes / 16;
+  copy_pieces(c, to, from, pieces * part / parts, pieces * (part + 1) / parts);
+}
+
+// A warp per (row, key-value head, key or value).
+template <typename T>
+__global__ void __launch_bounds__(256) append_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position,
+                                                     int n, const T *k, int64_t k_row, int64_t k_head, const T *v,
+                                                     int64_t v_row, int64_t v_head) {
+  const int64_t job = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (job >= (int64_t)n * c.n_kv_heads * 2) return;
+  const int which = (int)(job & 1), h = (int)((job >> 1) % c.n_kv_heads), i = (int)((job >> 1) / c.n_kv_heads);
+  const int slot = slots ? slots[i] : i;
+  bool ok = (unsigned)slot < (unsigned)c.n_slots;
+  int page = 0, t = 0;
+  if (ok) {
+    const int tokens = slot_tokens(c, slot);
+    t = position ? position[i] : tokens - 1;
+    ok = t >= 0 && t < tokens;
+    if (ok) page = c.table[(int64_t)slot * c.table_width + t / c.page_size];
+    ok = ok && (unsigned)page < (unsigned)c.n_pages;
+  }
+  if (!ok) {
+    if (lane == 0) flag_error(kErrCacheId);
+    return;
+  }
+  const T *from = which ? v + i * v_row + h * v_head : k + i * k_row + h * k_head;
+  T *to = reinterpret_cast<T *>(c.pool + (uint64_t)page * c.page_bytes) + (uint64_t)layer * c.layer_elems +
+          (uint64_t)(which * c.n_kv_heads + h) * c.head_elems + (uint64_t)(t % c.page_size) * c.head_dim;
+  for (int d = lane; d < c.head_dim; d += 32) to[d] = from[d];
+}
+
+cudaError_t launch_cache_grow(const Cache &c, const int32_t *slots, int n, const int32_t *add, int add_all, int32_t *ws,
+                              cudaStream_t s) {
+  if (n == 0) return cudaSuccess;
+  g_used = true;
+  cache_plan_kernel<false><<<1, kPlanThreads, 0, s>>>(c, slots, nullptr, add, add_all, n, ws);
+  return cudaGetLastError();
+}
+
+// Blocks a page's copy is cut into: enough for the GPU over `pages` of them, none under 32 KB.
+static int copy_parts(const Cache &c, int pages) {
+  const uint64_t most = (c.page_bytes + (32 << 10) - 1) / (32 << 10), want = (152 * 8 + pages - 1) / pages;
+  return (int)(want < most ? want : most);
+}
+
+cudaError_t launch_cache_fork(const Cache &c, const int32_t *parents, const int32_t *children, int n, int32_t *ws,
+                              cudaStream_t s) {
+  if (n == 0) return cudaSuccess;
+  g_used = true;
+  cache_plan_kernel<true><<<1, kPlanThreads, 0, s>>>(c, children, parents, nullptr, 0, n, ws);
+  const int parts = copy_parts(c, n);
+  fork_copy_kernel<<<(unsigned)n * parts, 256, 0, s>>>(c, parents, children, parts, ws);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache_free(const Cache &c, const int32_t *slots, int n, cudaStream_t s) {
+  if (n == 0) return cudaSuccess;
+  g_used = true;
+  cache_free_kernel<<<n, 256, 0, s>>>(c, slots);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache_compact(const Cache &c, int32_t *counts, int32_t *ws, cudaStream_t s) {
+  g_used = true;
+  compact_plan_kernel<<<1, kPlanThreads, 0, s>>>(c, counts, ws);
+  compact_move_kernel<<<152 * 8, 256, 0, s>>>(c, ws);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache_copy(const Cache &c, const int32_t *src, const int32_t *dst, int n, cudaStream_t s) {
+  if (n == 0) return cudaSuccess;
+  g_used = true;
+  const int parts = copy_parts(c, n);
+  copy_pages_kernel<<<(unsigned)n * parts, 256, 0, s>>>(c, src, dst, parts);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n,
+                                const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                                int64_t v_head, cudaStream_t s) {
+  if (n == 0) return cudaSuccess;
+  g_used = true;
+  const unsigned blocks = (unsigned)(((int64_t)n * c.n_kv_heads * 2 + 7) / 8);
+  if (c.elem == 2)
+    append_kernel<uint16_t><<<blocks, 256, 0, s>>>(c, layer, slots, position, n, (const uint16_t *)k, k_row, k_head,
+                                                   (const uint16_t *)v, v_row, v_head);
+  else
+    append_kernel<uint32_t><<<blocks, 256, 0, s>>>(c, layer, slots, position, n, (const uint32_t *)k, k_row, k_head,
+                                                   (const uint32_t *)v, v_row, v_head);
+  return cudaGetLastError();
+}
+
+// Read only once a kernel of this file was launched: copes_check of a program without a cache
+// takes as long as before.
+unsigned read_and_clear_cache_errors() {
+  if (!g_used) return 0;
+  unsigned v = 0, zero = 0;
+  cudaMemcpyFromSymbol(&v, g_cache_error, sizeof(v));
+  if (v) cudaMemcpyToSymbol(g_cache_error, &zero, sizeof(zero));
+  return v;
+}
+
+}  // namespace copes

@@ -1,0 +1,135 @@
+"""Refusals of the answering operators' C entries: every case fails its checks before any CUDA
+call, with a message that names the entry; the fake addresses are never read."""
+import copy
+import ctypes
+import os
+
+import pytest
+
+import answer_model as model
+
+GOOD = dict(pool=0x1000000, dtype=0, n_pages=8, n_layers=2, n_kv_heads=2, page_size=16, head_dim=64, table=0x9000000,
+            n_slots=4, table_width=5, length=0xA000000, refs=0xB000000)
+WS, BIG = 0xC000000, 1 << 30
+
+
+@pytest.fixture(scope="module")
+def copes():
+    from paper_2608_02391_gb300 import build, copes as c
+    if not os.path.exists(c.LIB_PATH):
+        build.build()
+    c.load()
+    return c
+
+
+def cache(copes, **kw):
+    f = copy.copy(GOOD)
+    f.update(kw)
+    return ctypes.byref(copes.KVCacheDesc(*[f[name] for name, _ in copes.KVCacheDesc._fields_]))
+
+
+def calls(copes, c):
+    """Every entry that takes a cache, with arguments that are fine where the cache is."""
+    L = copes.load()
+    return {
+        "copes_cache_grow": lambda: L.copes_cache_grow(c, 0x100, 1, None, 1, WS, BIG, None),
+        "copes_cache_append": lambda: L.copes_cache_append(c, 0, 0x100, None, 1, 0x100, 64, 64, 0x100, 64, 64, None),
+        "copes_cache_fork": lambda: L.copes_cache_fork(c, 0x100, 0x200, 1, WS, BIG, None),
+        "copes_cache_free": lambda: L.copes_cache_free(c, 0x100, 1, None),
+        "copes_cache_compact": lambda: L.copes_cache_compact(c, None, WS, BIG, None),
+        "copes_cache_copy_pages": lambda: L.copes_cache_copy_pages(c, 0x100, 0x200, 1, None),
+        "copes_paged_attention": lambda: L.copes_paged_attention(c, 0, None, 1, 0x100, 256, 64, 4, 0.1, 0xD000000, None,
+                                                                 WS, BIG, None),
+    }
+
+
+def refused(copes, rc, code, name):
+    assert rc == code, (name, rc, copes.last_error())
+    assert name in copes.last_error()
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(pool=None), -1), (dict(table=None), -1), (dict(length=None), -1), (dict(refs=None), -1), (dict(dtype=2), -1),
+    (dict(n_pages=0), -1), (dict(n_layers=0), -1), (dict(n_kv_heads=-1), -1), (dict(page_size=0), -1), (dict(n_slots=0), -1),
+    (dict(table_width=0), -1), (dict(head_dim=60), -3), (dict(head_dim=264), -3), (dict(head_dim=0), -3),
+    (dict(n_pages=(1 << 22) + 1), -3), (dict(table_width=1 << 28), -3), (dict(n_slots=1 << 30, table_width=2), -3),
+    (dict(n_layers=1 << 20), -3), (dict(page_size=1 << 24, head_dim=256, table_width=1, n_pages=1), -3),
+    (dict(page_size=1 << 22, n_kv_heads=60000, n_layers=60000, table_width=1), -3),
+    (dict(pool=0x1000008), -2), (dict(table=0x9000002), -2), (dict(length=0xA000001), -2), (dict(refs=0xB000003), -2),
+    (dict(length=0x9000010), -1), (dict(refs=0x1000100), -1)])
+def test_caches_that_are_refused(copes, change, code):
+    c = cache(copes, **change)
+    for name, call in calls(copes, c).items():
+        refused(copes, call(), code, name)
+    assert copes.load().copes_cache_workspace_bytes(c) == 0
+    assert copes.load().copes_paged_attention_workspace_bytes(c, 1, 4) == 0
+
+
+def test_a_null_cache_is_refused(copes):
+    for name, call in calls(copes, None).items():
+        refused(copes, call(), -1, name)
+
+
+def test_arguments_that_are_refused(copes):
+    L, c = copes.load(), cache(copes)
+    ws = L.copes_cache_workspace_bytes(c)
+    assert ws >= 4 * (2 * 8 + 2 * 4)
+
+    def grow(slots=0x100, n=1, add=None, add_all=1, work=WS, size=BIG):
+        return L.copes_cache_grow(c, slots, n, add, add_all, work, size, None)
+
+    for kw, code in [(dict(slots=None), -1), (dict(n=-1), -1), (dict(n=5), -3), (dict(slots=0x102), -2), (dict(add=0x101), -2),
+                     (dict(add_all=-1), -1), (dict(work=None), -4), (dict(size=ws - 1), -4), (dict(work=WS + 4), -2)]:
+        refused(copes, grow(**kw), code, "copes_cache_grow")
+    for kw, code in [((None, 0x200, 1), -1), ((0x100, None, 1), -1), ((0x100, 0x200, 5), -3), ((0x100, 0x201, 1), -2)]:
+        refused(copes, L.copes_cache_fork(c, *kw, WS, BIG, None), code, "copes_cache_fork")
+    refused(copes, L.copes_cache_fork(c, 0x100, 0x200, 1, WS, ws - 1, None), -4, "copes_cache_fork")
+    refused(copes, L.copes_cache_free(c, None, 1, None), -1, "copes_cache_free")
+    refused(copes, L.copes_cache_free(c, 0x100, -2, None), -1, "copes_cache_free")
+    refused(copes, L.copes_cache_compact(c, 0x101, WS, BIG, None), -2, "copes_cache_compact")
+    refused(copes, L.copes_cache_compact(c, None, WS, 16, None), -4, "copes_cache_compact")
+    refused(copes, L.copes_cache_copy_pages(c, 0x100, None, 1, None), -1, "copes_cache_copy_pages")
+
+    def append(layer=0, slots=0x100, position=None, n=1, k=0x100, v=0x100):
+        return L.copes_cache_append(c, layer, slots, position, n, k, 64, 64, v, 64, 64, None)
+
+    for kw, code in [(dict(layer=2), -1), (dict(layer=-1), -1), (dict(slots=None, n=5), -3), (dict(position=0x102), -2),
+                     (dict(k=None), -1), (dict(v=None), -1), (dict(k=0x101), -2), (dict(n=-1), -1)]:
+        refused(copes, append(**kw), code, "copes_cache_append")
+
+    need = L.copes_paged_attention_workspace_bytes(c, 4, 8)
+    assert need > 0 and L.copes_paged_attention_workspace_bytes(c, 4, 7) == 0
+    assert L.copes_paged_attention_workspace_bytes(c, -1, 8) == 0
+
+    def attend(layer=0, slots=None, n=4, q=0x100, heads=8, scale=0.1, out=0xD000000, lse=None, work=WS, size=BIG):
+        return L.copes_paged_attention(c, layer, slots, n, q, 512, 64, heads, scale, out, lse, work, size, None)
+
+    for kw, code in [(dict(layer=2), -1), (dict(n=5), -3), (dict(n=-1), -1), (dict(q=None), -1), (dict(out=None), -1),
+                     (dict(heads=7), -1), (dict(heads=0), -1), (dict(heads=70000), -3), (dict(scale=float("nan")), -1),
+                     (dict(scale=float("inf")), -1), (dict(q=0x101), -2), (dict(out=0xD000008), -2), (dict(lse=0xE000002), -2),
+                     (dict(out=0x1000010), -1), (dict(lse=0x1000010), -1), (dict(lse=0xD000010), -1), (dict(slots=0x102), -2),
+                     (dict(work=None), -4), (dict(size=need - 1), -4), (dict(work=WS + 8), -2)]:
+        refused(copes, attend(**kw), code, "copes_paged_attention")
+
+    def logprobs(logits=0x100, dtype=0, n=1, vocab=100, target=0x1000, scale=1.0, top=2, lp=0x2000, ent=None, ids=0x3000,
+                 tlp=0x4000):
+        return L.copes_token_logprobs(logits, dtype, n, vocab, 100, target, scale, top, lp, ent, ids, tlp, None)
+
+    for kw, code in [(dict(dtype=2), -1), (dict(n=-1), -1), (dict(vocab=0), -1), (dict(vocab=(1 << 30) + 1), -3), (dict(scale=0.0), -1),
+                     (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(top=-1), -3),
+                     (dict(top=33), -3), (dict(vocab=1), -3), (dict(logits=None), -1), (dict(target=None), -1), (dict(lp=None), -1),
+                     (dict(ids=None), -1), (dict(tlp=None), -1), (dict(logits=0x101), -2), (dict(target=0x1004), -2),
+                     (dict(ids=0x3004), -2), (dict(lp=0x2002), -2), (dict(ent=0x5001), -2)]:
+        refused(copes, logprobs(**kw), code, "copes_token_logprobs")
+
+
+def test_the_model_of_the_pages():
+    """The bookkeeping that the GPU tests compare with, on a small case by hand."""
+    m = model.CacheModel(n_pages=6, page_size=4, n_slots=4, width=3)
+    assert m.grow([2, 0], [5, 1]) == 0
+    assert m.pages == [[2], [], [0, 1], []] and m.refs == [1, 1, 1, 0, 0, 0]
+    assert m.fork([2, 2], [1, 3]) == 0
+    assert m.pages == [[2], [0, 3], [0, 1], [0, 4]] and m.copies == [(1, 3), (1, 4)] and m.refs == [3, 1, 1, 1, 1, 0]
+    assert m.grow([0, 1], [8, 4]) == 64 and m.grow([0], [12]) == 32 and m.fork([0], [1]) == 32
+    assert m.free([2, 2, 9]) == 32 and m.refs == [2, 0, 1, 1, 1, 0]
+    assert m.compact() == (4, 1) and m.pages == [[2], [0, 3], [], [0, 1]] and m.refs == [2, 1, 1, 1, 0, 0]
