@@ -1,4 +1,29 @@
 // Attention of one new token per sequence over a paged key-value cache.
+//
+// For a row's query heads h of one key-value head, over its tokens t:
+//   s_t = scale q.k_t,  out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),  m = max_t s_t.
+// Every key and value is read once, for up to 8 or 16 query heads together: 2 flops per value
+// and head, 32 flops a byte at 8 heads of bf16.  That is past the fp32 units at the rate of HBM
+// (54 TFLOP/s at 6.8 TB/s), and 3% of the tensor cores': the bound is HBM, and mma.sync on
+// registers filled from shared memory is enough (tcgen05 takes 64 rows or more of one operand;
+// a group of query heads has 1 to 16).
+//
+// Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
+// are shared out evenly among as many blocks as the GPU runs at once, whatever the lengths are.
+// A (row, head group) whose tiles lie in several blocks is joined by the block that is done last
+// with its part, over the parts in order: the result does not depend on which that is.
+//
+// A tile.  Each warp keeps 16 of a tile's tokens to itself, from the copy into shared memory to
+// its own running maximum, sum and output, so that the warps need each other only at the end of
+// a row.  Keys are the rows of the first product and the query heads its columns,
+// S^T[token][head] = K Q^T, and in the second O^T[d][head] = V^T P^T: 8 heads fill a tile of the
+// matrix unit, where heads as rows would fill half of 16.  P^T is S^T's registers transposed in
+// 8 x 8 blocks (movmatrix).
+//
+// Precision.  Scores, maxima, sums and outputs are fp32.  bf16: products are exact, and a weight
+// p goes into the second product as two bf16 terms (2^-16 of it lost; one term would lose 2^-8
+// where the tensor cores have room for both).  fp32: every factor is split into two tf32 terms
+// and three of the four products are taken (2^-21 lost).
 #include <math.h>
 
 #include "answer.h"
@@ -9,81 +34,614 @@ __device__ unsigned g_attend_error;
 static std::atomic<bool> g_used{false};
 __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_attend_error, bit); }
 
-constexpr int kAttendThreads = 128;
+constexpr int kSMs = 152;
+constexpr unsigned kAll = 0xffffffffu;
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_float(float x, float *to) { *to = x; }
-__device__ __forceinline__ void from_float(float x, __nv_bfloat16 *to) { *to = __float2bfloat16_rn(x); }
+// What a kernel variant is made of: T of the cache, head_dim padded to DP, NT x 8 query heads.
+template <typename T, int DP_, int NT_>
+struct Shape {
+  static constexpr bool kFp32 = sizeof(T) == 4;
+  static constexpr int DP = DP_, NT = NT_;
+  static constexpr int kWarps = kFp32 ? 2 : 4;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kTile = kWarps * 16;               // tokens
+  static constexpr int kChunks = DP * (int)sizeof(T) / 16;  // 16-byte pieces of a token's row
+  static constexpr int kPart = 16 * kChunks * 16;         // a warp's keys (or values) of a tile, bytes
+  static constexpr int kStage = 2 * kPart * kWarps;
+  static constexpr int kHeads = 8 * NT;                   // query heads of a block at a time
+  static constexpr int kRow = DP + 4;                     // row of s_o: heads 2j begin 8 banks apart
+  static constexpr int kFixed = (kWarps * 8 * kRow + kWarps * 16) * 4;
+  // three tiles in flight or more where two blocks fit on an SM, else what one block can have
+  static constexpr int kStages = kStage <= 16384 ? 4 : 3;
+  static constexpr int kSmem = kStages * kStage + kFixed;
+  static constexpr int kPerSm = kSmem <= 74 * 1024 ? 3 : kSmem <= 113 * 1024 ? 2 : 1;
+  static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
+};
 
-// A block per (row, query head): a chunk of tokens at a time, a thread per token for the scores
-// and a thread per value component for the sums, with the running maximum and sum of the softmax.
-template <typename T>
-__global__ void __launch_bounds__(kAttendThreads) attend_simple_kernel(AttendArgs a) {
-  __shared__ float s_q[COPES_MAX_HEAD_DIM], s_p[kAttendThreads], s_red[kAttendThreads];
-  __shared__ int s_page[kAttendThreads];
-  const Cache &c = a.c;
-  const int tid = threadIdx.x, i = blockIdx.x / a.q_heads, h = blockIdx.x % a.q_heads;
-  const int g = h / (a.q_heads / c.n_kv_heads), D = c.head_dim;
-  const int slot = a.slots ? a.slots[i] : i;
-  int tokens = 0;
-  if ((unsigned)slot < (unsigned)c.n_slots) tokens = slot_tokens(c, slot);
-  else if (tid == 0) flag_error(kErrCacheId);
-  const T *q = (const T *)a.q + i * a.q_row + h * a.q_head;
-  for (int d = tid; d < D; d += kAttendThreads) s_q[d] = to_float(q[d]) * a.scale;
-  float m = -INFINITY, l = 0.0f, o[COPES_MAX_HEAD_DIM / kAttendThreads] = {};
-  const uint64_t k_at = (uint64_t)a.layer * c.layer_elems + (uint64_t)g * c.head_elems;
-  const uint64_t v_at = k_at + (uint64_t)c.n_kv_heads * c.head_elems;
-  for (int base = 0; base < tokens; base += kAttendThreads) {
-    const int t = base + tid, here = min(kAttendThreads, tokens - base);
-    __syncthreads();
-    float s = -INFINITY;
-    if (t < tokens) {
-      int page = c.table[(int64_t)slot * c.table_width + t / c.page_size];
-      if ((unsigned)page >= (unsigned)c.n_pages) {
-        flag_error(kErrCacheId);
-        page = -1;
-      }
-      s_page[tid] = page;
-      s = 0.0f;
-      if (page >= 0) {
-        const T *k = (const T *)(c.pool + (uint64_t)page * c.page_bytes) + k_at + (uint64_t)(t % c.page_size) * D;
-        for (int d = 0; d < D; ++d) s = fmaf(to_float(k[d]), s_q[d], s);
-      }
-    }
-    s_red[tid] = s;
-    __syncthreads();
-    float top = m;
-    for (int j = 0; j < here; ++j) top = fmaxf(top, s_red[j]);
-    const float p = t < tokens ? expf(s - top) : 0.0f, keep = expf(m - top);
-    s_p[tid] = p;
-    __syncthreads();
-    m = top;
-    l *= keep;
-    for (int j = 0; j < here; ++j) l += s_p[j];
-    for (int r = 0, d = tid; d < D; d += kAttendThreads, ++r) {
-      float x = o[r] * keep;
-      for (int j = 0; j < here; ++j)
-        if (s_page[j] >= 0)
-          x = fmaf(s_p[j], to_float(((const T *)(c.pool + (uint64_t)s_page[j] * c.page_bytes))[
-                                v_at + (uint64_t)((base + j) % c.page_size) * D + d]), x);
-      o[r] = x;
-    }
-  }
-  T *out = (T *)a.out + ((int64_t)i * a.q_heads + h) * D;
-  for (int r = 0, d = tid; d < D; d += kAttendThreads, ++r) from_float(tokens ? o[r] / l : 0.0f, out + d);
-  if (tid == 0 && a.lse) a.lse[(int64_t)i * a.q_heads + h] = tokens ? m + logf(l) : -INFINITY;
+// Where a block is in the line of tiles: row by row, head group by head group, tile by tile.
+struct Cursor {
+  int row, unit, tile, tiles, tokens, slot;
+};
+
+__device__ __forceinline__ int row_slot(const AttendArgs &a, int row) { return a.slots ? a.slots[row] : row; }
+
+__device__ __forceinline__ int row_tokens(const AttendArgs &a, int slot) {
+  return (unsigned)slot < (unsigned)a.c.n_slots ? slot_tokens(a.c, slot) : 0;
 }
 
-size_t attend_workspace_bytes(const Cache &, int, int) { return 16; }
+// An empty row has one tile, of no tokens, so that somebody writes its output.
+template <int kTile>
+__device__ __forceinline__ int row_tiles(int tokens) {
+  return tokens ? (tokens - 1) / kTile + 1 : 1;
+}
 
-cudaError_t launch_paged_attention(int dtype, const AttendArgs &a, void *, cudaStream_t s) {
+template <int kTile>
+__device__ __forceinline__ void enter_row(const AttendArgs &a, Cursor &c) {
+  if (c.row >= a.n) return;
+  c.slot = row_slot(a, c.row);
+  c.tokens = row_tokens(a, c.slot);
+  c.tiles = row_tiles<kTile>(c.tokens);
+}
+
+template <int kTile>
+__device__ __forceinline__ void advance(const AttendArgs &a, int units, Cursor &c) {
+  if (++c.tile < c.tiles) return;
+  c.tile = 0;
+  if (++c.unit < units) return;
+  c.unit = 0;
+  ++c.row;
+  enter_row<kTile>(a, c);
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void ldmatrix(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// x as a tf32 term and what it leaves (whose own tf32 term is within 2^-21 of x).
+__device__ __forceinline__ void split_tf32(uint32_t x, uint32_t &hi, uint32_t &lo) {
+  hi = x & 0xFFFFE000u;
+  lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi));
+}
+
+// c += a b, with both factors in two tf32 terms: the product of the small terms is left out.
+__device__ __forceinline__ void mma_split(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  uint32_t ah[4], al[4], bh[2], bl[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split_tf32(a[i], ah[i], al[i]);
+  split_tf32(b0, bh[0], bl[0]);
+  split_tf32(b1, bh[1], bl[1]);
+  mma_tf32(c, al, bh[0], bh[1]);
+  mma_tf32(c, ah, bl[0], bl[1]);
+  mma_tf32(c, ah, bh[0], bh[1]);
+}
+
+// A 16-byte piece's place in a row of a tile is its number xor this, so that what one load
+// instruction reads lies in different banks.
+template <bool kFp32>
+__device__ __forceinline__ int swizzle(int row) {
+  return kFp32 ? (row & 6) ^ ((row & 1) << 2) : row & 7;
+}
+
+// Factor of a part with maximum m and sum l in a whole with maximum M (both of log2).  A part
+// without weight counts 0; a NaN stays one.
+__device__ __forceinline__ float part_weight(float m, float l, float M) {
+  return m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : exp2_fast(m - M);
+}
+
+// A warp's state of one (row, head group): heads 8 nt + 2 (lane % 4) + {0, 1}.
+template <typename S>
+struct Running {
+  float m[S::NT][2], l[S::NT][2];     // of log2; l of this lane's tokens alone
+  float o[S::DP / 16][S::NT][4];      // O^T: two values of d x two heads each
+  __device__ void clear() {
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+      m[j][0] = m[j][1] = -INFINITY;
+      l[j][0] = l[j][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < S::DP / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
+    }
+  }
+};
+
+// Query heads as the columns of the first product's second factor.
+template <typename S>
+struct Queries {
+  uint32_t b[S::DP / 16][S::NT][S::kFp32 ? 4 : 2];
+};
+
+template <typename T, typename S>
+__device__ __forceinline__ void load_queries(const AttendArgs &a, int row, int first_head, int heads, Queries<S> &q) {
+  const int lane = threadIdx.x & 31, D = a.c.head_dim;
+#pragma unroll
+  for (int j = 0; j < S::NT; ++j) {
+    const int h = j * 8 + (lane >> 2);
+    const T *from = (const T *)a.q + row * a.q_row + (first_head + h) * a.q_head;
+#pragma unroll
+    for (int k = 0; k < S::DP / 16; ++k) {
+      if constexpr (S::kFp32) {
+        // one 16-byte piece of a key's row is the four k of two products: a lane's are d .. d + 3
+        const int d = k * 16 + (lane & 3) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q.b[k][j][e] = h < heads && d < D ? __float_as_uint(from[d + e]) : 0u;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int d = k * 16 + (lane & 3) * 2 + e * 8;
+          uint32_t x = 0;
+          if (h < heads && d < D) {
+            const uint16_t *u = reinterpret_cast<const uint16_t *>(from + d);
+            x = u[0] | (uint32_t)u[1] << 16;
+          }
+          q.b[k][j][e] = x;
+        }
+      }
+    }
+  }
+}
+
+// One warp's 16 tokens: scores, the running maximum and sum, and the weighted values.
+// `left`: how many of the 16 are tokens.
+template <typename S>
+__device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int left, float scale, const Queries<S> &q,
+                                          Running<S> &r) {
+  constexpr int NT = S::NT, KS = S::DP / 16, kPitch = S::kChunks * 16;
+  const int lane = threadIdx.x & 31;
+  float s[NT][4] = {};
+  if constexpr (S::kFp32) {
+    const int row = lane >> 2;
+    const uint32_t at = keys + row * kPitch;
+    const int x = swizzle<true>(row);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const uint32_t off = (uint32_t)(((k * 4 + (lane & 3)) ^ x) * 16);
+      uint32_t u[4], v[4];
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(at + off) : "memory");
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                   : "r"(at + off + 8 * kPitch) : "memory");
+      const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        mma_split(s[j], a0, q.b[k][j][0], q.b[k][j][1]);
+        mma_split(s[j], a1, q.b[k][j][2], q.b[k][j][3]);
+      }
+    }
+  } else {
+    const int row = lane & 15, x = swizzle<false>(row);
+    const uint32_t at = keys + row * kPitch;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      uint32_t a[4];
+      ldmatrix(a, at + (uint32_t)(((k * 2 + (lane >> 4)) ^ x) * 16));
+#pragma unroll
+      for (int j = 0; j < NT; ++j) mma_bf16(s[j], a, q.b[k][j][0], q.b[k][j][1]);
+    }
+  }
+
+  // tokens lane / 4 (s[.][0], s[.][1]) and lane / 4 + 8
+  const bool here[2] = {(lane >> 2) < left, (lane >> 2) + 8 < left};
+  bool grown = false;
+  float keep[NT][2];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      s[j][e] = here[0] ? s[j][e] * scale : -INFINITY;
+      s[j][2 + e] = here[1] ? s[j][2 + e] * scale : -INFINITY;
+      float top = fmaxf(s[j][e], s[j][2 + e]);
+      top = fmaxf(top, __shfl_xor_sync(kAll, top, 4));
+      top = fmaxf(top, __shfl_xor_sync(kAll, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(kAll, top, 16));
+      const float m = fmaxf(r.m[j][e], top);
+      keep[j][e] = m == r.m[j][e] ? 1.0f : exp2_fast(r.m[j][e] - m);
+      grown |= m != r.m[j][e];
+      r.m[j][e] = m;
+      const float base = m == -INFINITY ? 0.0f : m;
+      s[j][e] = exp2_fast(s[j][e] - base);
+      s[j][2 + e] = exp2_fast(s[j][2 + e] - base);
+      r.l[j][e] = r.l[j][e] * keep[j][e] + (s[j][e] + s[j][2 + e]);
+    }
+  if (__any_sync(kAll, grown)) {
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.o[i][j][e] *= keep[j][e & 1];
+  }
+
+  if constexpr (S::kFp32) {
+    // P^T: 8 tokens x 8 heads at a time, in 16-bit halves.  A lane then has tokens 2j and 2j + 1
+    // (j = lane % 4) as the k of one product: its values are read from those rows.
+    uint32_t p[NT][2][2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t u = __float_as_uint(s[j][2 * e]), v = __float_as_uint(s[j][2 * e + 1]);
+        const uint32_t lo = transpose8(__byte_perm(u, v, 0x5410)), hi = transpose8(__byte_perm(u, v, 0x7632));
+        p[j][e][0] = __byte_perm(lo, hi, 0x5410);
+        p[j][e][1] = __byte_perm(lo, hi, 0x7632);
+      }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = e * 8 + (lane & 3) * 2;
+      const uint32_t at = values + row * kPitch;
+#pragma unroll
+      for (int g = 0; g < S::DP / 32; ++g) {
+        const int piece = g * 8 + (lane >> 2);  // d = 32 g + 4 (lane / 4) + 0 .. 3
+        uint32_t u[4], v[4];
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                     : "r"(at + (uint32_t)((piece ^ swizzle<true>(row)) * 16)) : "memory");
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                     : "r"(at + kPitch + (uint32_t)((piece ^ swizzle<true>(row + 1)) * 16)) : "memory");
+        const uint32_t a0[4] = {u[0], u[1], v[0], v[1]}, a1[4] = {u[2], u[3], v[2], v[3]};
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          mma_split(r.o[2 * g][j], a0, p[j][e][0], p[j][e][1]);
+          mma_split(r.o[2 * g + 1][j], a1, p[j][e][0], p[j][e][1]);
+        }
+      }
+    }
+  } else {
+    uint32_t p[NT][2], rest[NT][2];  // tokens 0 .. 7 and 8 .. 15, in two bf16 terms
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float u = s[j][2 * e], v = s[j][2 * e + 1];
+        const uint32_t hi = pack_bf16(u, v);
+        p[j][e] = transpose8(hi);
+        rest[j][e] = transpose8(pack_bf16(u - __uint_as_float(hi << 16), v - __uint_as_float(hi & 0xFFFF0000u)));
+      }
+    const int row = (lane & 7) + (lane >> 4) * 8, x = swizzle<false>(row);
+    const uint32_t at = values + row * kPitch;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      uint32_t a[4];
+      ldmatrix_trans(a, at + (uint32_t)(((i * 2 + ((lane >> 3) & 1)) ^ x) * 16));
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        mma_bf16(r.o[i][j], a, rest[j][0], rest[j][1]);
+        mma_bf16(r.o[i][j], a, p[j][0], p[j][1]);
+      }
+    }
+  }
+}
+
+// The d of r.o[i][.][2 half + .].
+template <typename S>
+__device__ __forceinline__ int output_d(int i, int half) {
+  const int lane = threadIdx.x & 31;
+  return S::kFp32 ? (i >> 1) * 32 + (lane >> 2) * 4 + (i & 1) * 2 + half : i * 16 + (lane >> 2) + half * 8;
+}
+
+__device__ __forceinline__ void store(float x, float *to) { *to = x; }
+__device__ __forceinline__ void store(float x, __nv_bfloat16 *to) { *to = __float2bfloat16_rn(x); }
+
+// The workspace: counters of the joins (`counter`), one per row and head group, then the parts:
+// block w's at 2 w (of a row that begins before the block's share) and 2 w + 1 (of one that ends
+// after it), each kHeads maxima, kHeads sums and kHeads x head_dim values.
+template <typename T, typename S>
+__global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendArgs a, int *counter, float *part,
+                                                                        int units, int groups) {
+  extern __shared__ __align__(128) char smem[];
+  __shared__ int s_row, s_last;
+  __shared__ int64_t s_before, s_sum[S::kWarps];
+  constexpr int TILE = S::kTile;
+  const Cache &c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = c.head_dim;
+  const int group = a.q_heads / c.n_kv_heads;
+
+  // the line's length and this block's share [lo, hi) of it
+  const int each = (a.n + S::kThreads - 1) / S::kThreads, r0 = min(a.n, tid * each), r1 = min(a.n, r0 + each);
+  int64_t mine = 0;
+  for (int i = r0; i < r1; ++i) mine += row_tiles<TILE>(row_tokens(a, row_slot(a, i)));
+  int64_t before = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(kAll, before, d);
+    if (lane >= d) before += y;
+  }
+  if (lane == 31) s_sum[warp] = before;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < S::kWarps; ++w) {
+    if (w < warp) before += s_sum[w];
+    total += s_sum[w];
+  }
+  total *= units;
+  const int64_t blocks = min((int64_t)gridDim.x, total);  // each has a tile at least
+  if (blockIdx.x >= blocks) return;
+  const int64_t lo = total * blockIdx.x / blocks, hi = total * (blockIdx.x + 1) / blocks;
+  before -= mine;
+  if (before * units <= lo && lo < (before + mine) * units) {
+    int i = r0;
+    for (; i + 1 < r1; ++i) {
+      const int t = row_tiles<TILE>(row_tokens(a, row_slot(a, i)));
+      if (lo < (before + t) * units) break;
+      before += t;
+    }
+    s_row = i;
+    s_before = before * units;
+  }
+  __syncthreads();
+  Cursor at;
+  at.row = s_row;
+  enter_row<TILE>(a, at);
+  at.unit = (int)((lo - s_before) / at.tiles);
+  at.tile = (int)((lo - s_before) % at.tiles);
+  Cursor ahead = at;
+
+  float *s_o = reinterpret_cast<float *>(smem + S::kStages * S::kStage);  // [warp][8][kRow]
+  float *s_m = s_o + S::kWarps * 8 * S::kRow, *s_l = s_m + S::kWarps * 8;
+  const uint32_t stages = smem_addr(smem) + warp * 2 * S::kPart;
+  const int count = (int)(hi - lo);
+
+  // page of token (16 warp + lane % 16) of the next tile to be asked for, -1 for none
+  const auto page_ahead = [&]() {
+    const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
+    return t < ahead.tokens ? c.table[(int64_t)ahead.slot * c.table_width + t / c.page_size] : -1;
+  };
+  int page = page_ahead();
+  const auto ask = [&](int stage) {
+    const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
+    const char *from = nullptr;
+    if ((unsigned)page < (unsigned)c.n_pages)
+      from = c.pool + (uint64_t)page * c.page_bytes +
+             ((uint64_t)a.layer * c.layer_elems + (uint64_t)(ahead.unit / groups) * c.head_elems +
+              (uint64_t)(t % c.page_size) * D) * sizeof(T);
+    else if (t < ahead.tokens) flag_error(kErrCacheId);
+    const uint64_t to_values = (uint64_t)c.n_kv_heads * c.head_elems * sizeof(T);
+    const uint32_t to = stages + stage * S::kStage;
+#pragma unroll
+    for (int i = 0; i < S::kChunks / 2; ++i) {
+      const int row = (i * 32 + lane) / S::kChunks, piece = (i * 32 + lane) % S::kChunks;
+      const char *src = reinterpret_cast<const char *>(__shfl_sync(kAll, (unsigned long long)from, row));
+      const int bytes = src && piece * 16 < D * (int)sizeof(T) ? 16 : 0;  // 0: zeros
+      src = bytes ? src + piece * 16 : c.pool;
+      const uint32_t dst = to + (row * S::kChunks + (piece ^ swizzle<S::kFp32>(row))) * 16;
+      copy_async(dst, src, bytes);
+      copy_async(dst + S::kPart, bytes ? src + to_values : src, bytes);
+    }
+    advance<TILE>(a, units, ahead);
+  };
+
+  int asked = 0;
+#pragma unroll
+  for (int s = 0; s < S::kStages - 1; ++s) {
+    if (asked < count) {
+      ask(s);
+      if (++asked < count) page = page_ahead();
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+
+  Running<S> r;
+  Queries<S> q;
+  const float scale = a.scale * 1.44269504088896340736f;  // of log2
+  bool fresh = true;
+  for (int j = 0; j < count; ++j) {
+    if (asked < count) {
+      ask(asked % S::kStages);
+      if (++asked < count) page = page_ahead();
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const int g = at.unit / groups, skip = at.unit % groups * S::kHeads;
+    const int first_head = g * group + skip, heads = min(S::kHeads, group - skip);
+    if (fresh) {
+      load_queries<T, S>(a, at.row, first_head, heads, q);
+      r.clear();
+      fresh = false;
+    }
+    asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
+    __syncwarp();
+    const int left = at.tokens - at.tile * TILE - warp * 16;
+    const uint32_t tile = stages + j % S::kStages * S::kStage;
+    if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
+    __syncwarp();
+
+    const bool ends = at.tile + 1 == at.tiles;
+    if (ends || j + 1 == count) {
+      // the warps' states together
+      const int64_t x0 = lo + j - at.tile, x1 = x0 + at.tiles - 1;
+      const int64_t w0 = ((x0 + 1) * blocks - 1) / total, w1 = ((x1 + 1) * blocks - 1) / total;
+      const bool whole = w0 == w1;
+      if (tid == 0 && (unsigned)at.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
+      const int id = 2 * (int)blockIdx.x + (lo > x0 ? 0 : 1);
+      const int slot_floats = S::kHeads * (D + 2);
+      float *mine_part = part + (int64_t)id * slot_floats;
+#pragma unroll
+      for (int nt = 0; nt < S::NT; ++nt) {
+        __syncthreads();  // s_o may still be read
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float l = r.l[nt][e];
+          l += __shfl_xor_sync(kAll, l, 4);
+          l += __shfl_xor_sync(kAll, l, 8);
+          l += __shfl_xor_sync(kAll, l, 16);
+          if (lane < 4) {
+            s_m[warp * 8 + lane * 2 + e] = r.m[nt][e];
+            s_l[warp * 8 + lane * 2 + e] = l;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < S::DP / 16; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s_o[(warp * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e];
+        __syncthreads();
+        for (int h = 0; h < 8 && nt * 8 + h < heads; ++h) {
+          float M = -INFINITY, L = 0.0f, weight[S::kWarps];
+#pragma unroll
+          for (int w = 0; w < S::kWarps; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+#pragma unroll
+          for (int w = 0; w < S::kWarps; ++w) {
+            weight[w] = part_weight(s_m[w * 8 + h], s_l[w * 8 + h], M);
+            L += weight[w] * s_l[w * 8 + h];
+          }
+          const int64_t head = (int64_t)at.row * a.q_heads + first_head + nt * 8 + h;
+          for (int d = tid; d < D; d += S::kThreads) {
+            float x = 0.0f;
+#pragma unroll
+            for (int w = 0; w < S::kWarps; ++w) x += weight[w] * s_o[(w * 8 + h) * S::kRow + d];
+            if (whole) store(L == 0.0f ? 0.0f : x / L, (T *)a.out + head * D + d);
+            else mine_part[2 * S::kHeads + (nt * 8 + h) * D + d] = x;
+          }
+          if (tid == 0) {
+            if (!whole) {
+              mine_part[nt * 8 + h] = M;
+              mine_part[S::kHeads + nt * 8 + h] = L;
+            } else if (a.lse) {
+              a.lse[head] = L == 0.0f ? -INFINITY : 0.6931471805599453094f * M + logf(L);
+            }
+          }
+        }
+      }
+      if (!whole) {
+        __threadfence();
+        __syncthreads();
+        int *seen = counter + (int64_t)at.row * units + at.unit;
+        if (tid == 0) s_last = atomicAdd(seen, 1) == (int)(w1 - w0);
+        __syncthreads();
+        if (s_last) {
+          __threadfence();
+          for (int v = tid; v < heads * (D / 4); v += S::kThreads) {
+            const int h = v / (D / 4), d = v % (D / 4) * 4;
+            float M = -INFINITY, L = 0.0f;
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int64_t w = w0; w <= w1; ++w) {
+              const float *p = part + (2 * w + (w == w0 ? 1 : 0)) * slot_floats;
+              const float m = __ldcg(p + h), l = __ldcg(p + S::kHeads + h);
+              const float4 x = __ldcg(reinterpret_cast<const float4 *>(p + 2 * S::kHeads + h * D + d));
+              const float N = fmaxf(M, m), keep = part_weight(M, L, N), weight = part_weight(m, l, N);
+              M = N;
+              L = L * keep + l * weight;
+              o.x = o.x * keep + x.x * weight;
+              o.y = o.y * keep + x.y * weight;
+              o.z = o.z * keep + x.z * weight;
+              o.w = o.w * keep + x.w * weight;
+            }
+            const int64_t head = (int64_t)at.row * a.q_heads + first_head + h;
+            T *out = (T *)a.out + head * D + d;
+            const float f = L == 0.0f ? 0.0f : 1.0f / L;
+            store(o.x * f, out);
+            store(o.y * f, out + 1);
+            store(o.z * f, out + 2);
+            store(o.w * f, out + 3);
+            if (d == 0 && a.lse) a.lse[head] = L == 0.0f ? -INFINITY : 0.6931471805599453094f * M + logf(L);
+          }
+          if (tid == 0) *seen = 0;
+        }
+      }
+      fresh = true;
+    }
+    advance<TILE>(a, units, at);
+  }
+}
+
+namespace {
+
+// Blocks that the GPU runs at once, and how many of them the tiles that the tables have room for
+// can feed.
+template <typename S>
+unsigned attend_blocks(const Cache &c, int n, int units) {
+  const int64_t room = (int64_t)c.table_width * c.page_size, tiles = (room + S::kTile - 1) / S::kTile;
+  const int64_t most = (int64_t)n * units * tiles, run = (int64_t)kSMs * S::kPerSm;
+  return (unsigned)(most < run ? most : run);
+}
+
+size_t counters_bytes(int n, int q_heads) { return ((size_t)n * q_heads * 4 + 15) / 16 * 16; }
+
+template <typename T, int DP, int NT>
+cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
+  using S = Shape<T, DP, NT>;
+  const int group = a.q_heads / a.c.n_kv_heads, groups = (group + S::kHeads - 1) / S::kHeads;
+  const int units = a.c.n_kv_heads * groups;
+  const unsigned blocks = attend_blocks<S>(a.c, a.n, units);
+  if (bytes) {
+    *bytes = counters_bytes(a.n, a.q_heads) + (size_t)2 * blocks * S::kHeads * (a.c.head_dim + 2) * 4;
+    return cudaSuccess;
+  }
+  const cudaError_t e = allow_smem((const void *)attend_kernel<T, S>, S::kSmem, S::kSmem);
+  if (e != cudaSuccess) return e;
+  attend_kernel<T, S><<<blocks, S::kThreads, S::kSmem, s>>>(
+      a, (int *)ws, (float *)((char *)ws + counters_bytes(a.n, a.q_heads)), units, groups);
+  return cudaGetLastError();
+}
+
+// Up to 8 query heads of a key-value head at a time, or 16 where it has more (each further group
+// reads the keys and values again); 8 for head_dim past 128, whose state would not fit in
+// registers twice.
+template <typename T>
+cudaError_t by_shape(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
+  const bool many = a.q_heads / a.c.n_kv_heads > 8;
+  if (a.c.head_dim <= 64) return many ? launch<T, 64, 2>(a, ws, s, bytes) : launch<T, 64, 1>(a, ws, s, bytes);
+  if (a.c.head_dim <= 128) return many ? launch<T, 128, 2>(a, ws, s, bytes) : launch<T, 128, 1>(a, ws, s, bytes);
+  return launch<T, 256, 1>(a, ws, s, bytes);
+}
+
+cudaError_t dispatch(int dtype, const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
+  return dtype == COPES_BF16 ? by_shape<__nv_bfloat16>(a, ws, s, bytes) : by_shape<float>(a, ws, s, bytes);
+}
+
+}  // namespace
+
+size_t attend_workspace_bytes(const Cache &c, int n, int q_heads) {
+  AttendArgs a{};
+  a.c = c;
+  a.n = n;
+  a.q_heads = q_heads;
+  size_t bytes = 0;
+  dispatch(c.elem == 2 ? COPES_BF16 : COPES_FP32, a, nullptr, 0, &bytes);
+  return bytes ? bytes : 16;
+}
+
+cudaError_t launch_paged_attention(int dtype, const AttendArgs &a, void *ws, cudaStream_t s) {
   if (a.n == 0) return cudaSuccess;
   g_used = true;
-  const unsigned blocks = (unsigned)a.n * a.q_heads;
-  if (dtype == COPES_BF16) attend_simple_kernel<__nv_bfloat16><<<blocks, kAttendThreads, 0, s>>>(a);
-  else attend_simple_kernel<float><<<blocks, kAttendThreads, 0, s>>>(a);
-  return cudaGetLastError();
+  return dispatch(dtype, a, ws, s, nullptr);
 }
 
 unsigned read_and_clear_attend_errors() {
