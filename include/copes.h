@@ -557,7 +557,8 @@ int copes_paged_attention(const copes_kv_cache *c, int layer, const int32_t *slo
                           void *workspace, size_t workspace_bytes, cudaStream_t stream);
 
 /* Log probabilities under softmax(x), x = scale * logits, of each row of logits (row i at
- * logits + i row elements, vocab values of dtype; scale > 0, an inverse temperature):
+ * logits + i row elements, vocab values of dtype; 0 < scale <= 1e38, an inverse
+ * temperature):
  *   logprob[i] = x[target[i]] - ln sum_j exp(x_j)       (fp32 [n]),
  *   entropy[i] = -sum_j p_j ln p_j                      (fp32 [n], or NULL),
  *   top_ids[i], top_logprobs[i]: the top largest logits (int64 and fp32 [n][top]; NULL with

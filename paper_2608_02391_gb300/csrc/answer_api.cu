@@ -237,7 +237,8 @@ int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_
     return fail(COPES_ERR_INVALID_ARG, "%s: dtype %d is neither COPES_BF16 nor COPES_FP32", who, dtype);
   if (n < 0 || vocab < 1) return fail(COPES_ERR_INVALID_ARG, "%s: n is negative or vocab below 1", who);
   if (vocab > (1 << 30)) return fail(COPES_ERR_SIZE, "%s: a vocabulary of more than 2^30", who);
-  if (!(scale > 0.0f) || !isfinite(scale)) return fail(COPES_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  if (!(scale > 0.0f) || !(scale <= 1e38f))
+    return fail(COPES_ERR_INVALID_ARG, "%s: scale must be positive and at most 1e38", who);
   if (top < 0 || top > COPES_MAX_TOP || top > vocab)
     return fail(COPES_ERR_SIZE, "%s: top %d of a vocabulary of %d, at most %d", who, top, vocab, COPES_MAX_TOP);
   if (n && (!logits || !target || !logprob)) return fail(COPES_ERR_INVALID_ARG, "%s: logits, target or logprob is NULL", who);
