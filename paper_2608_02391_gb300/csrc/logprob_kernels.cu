@@ -10,13 +10,15 @@
 // 75% of the special-function units and the whole half of the issue slots, and HBM bounds it.
 //
 // The alternatives need no second pass over the row: while it is read, the maximum of every cell
-// (a few adjacent 16-byte pieces) is kept in shared memory.  Cells are dealt into 32 groups; the
-// k-th largest of the groups' maxima is a bound that k logits at least reach, so only cells that
-// reach it hold alternatives.  They are about k to 4 k of 1,024 at most, and are read again, from
-// L2.  Their logits that reach the bound are ranked by counting.
+// (a thread's pieces of one step, or of a few) is kept in shared memory, and each thread's over
+// all in two halves.  The halves of one lane number are a group: the k-th largest of the 64 groups'
+// maxima is a bound that k logits at least reach, so only cells that reach it hold alternatives.
+// To fill k of 64 groups takes 64 (1/64 + ... + 1/(65 - k)) random logits, 24 for k = 20 and 44 for
+// k = 32 (of 32 groups it would be 31 and 130): so many cells of thousands are read again, from L2,
+// and their logits that reach the bound are ranked by counting.
 //
-// A row is read by one block, or, where there are few rows, by a cluster of up to 8 blocks whose
-// first joins the others' sums and alternatives through its shared memory.
+// A row is read by one block, or, where rows alone would leave SMs without work, by a cluster of
+// up to 8 blocks whose first joins the others' sums and alternatives through its shared memory.
 #include <float.h>
 #include <math.h>
 
@@ -29,11 +31,13 @@ static std::atomic<bool> g_used{false};
 __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_logprob_error, bit); }
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kThreads_ = 256, kWarps_ = kThreads_ / 32;
-constexpr int kCells = 1024;      // of a block's part of a row, at most
-constexpr int kCandidates = 512;  // at most, by the fast way
+constexpr int kMostThreads = 256, kMostWarps = kMostThreads / 32, kPerSm = 4;
+constexpr int kCells = 8192;       // of a block, at most
+constexpr int kReached = 1024;     // cells read again by the fast way, at most
+constexpr int kCandidates = 512;   // logits ranked by counting, at most
 constexpr int kClusterMost = 8;
-constexpr int kLoads = 4;         // 16-byte pieces of a lane in one step
+constexpr int kLoads = 4;          // 16-byte pieces of a lane in one step
+constexpr int kStep = kLoads * 32;  // pieces of a warp in one step
 
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -43,6 +47,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float warp_max_nan(float x) {
+  float r;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -116,6 +125,14 @@ __device__ __forceinline__ float max_of(const Piece<T> &p) {
   }
 }
 
+template <typename T>
+__device__ __forceinline__ Piece<T> load_piece(const void *at) {
+  Piece<T> p;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(p.r[0]), "=r"(p.r[1]), "=r"(p.r[2]), "=r"(p.r[3]) : "l"(at));
+  return p;
+}
+
 // A row in aligned pieces of 16 bytes: piece v holds logits v kN - shift and on; the first and
 // the last may hold fewer than kN.
 template <typename T>
@@ -124,16 +141,16 @@ struct Row {
   int vocab, shift;
   __device__ Row(const T *row, int n) : x(row), vocab(n), shift((int)(((uintptr_t)row & 15) / sizeof(T))) {}
   __device__ int pieces() const { return (int)(((int64_t)shift + vocab + Piece<T>::kN - 1) / Piece<T>::kN); }
+  // pieces [first_full(), end_full()) are whole
+  __device__ int first_full() const { return shift ? 1 : 0; }
+  __device__ int end_full() const { return (int)(((int64_t)shift + vocab) / Piece<T>::kN); }
+  __device__ const char *at(int v) const { return reinterpret_cast<const char *>(x - shift) + (int64_t)v * 16; }
   __device__ int first(int v) const { return v * Piece<T>::kN - shift; }
   // what lies outside the row reads as -inf
   __device__ __forceinline__ Piece<T> load(int v) const {
     Piece<T> p;
     const int j = first(v);
-    if (j >= 0 && j + Piece<T>::kN <= vocab) {
-      asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
-                   : "=r"(p.r[0]), "=r"(p.r[1]), "=r"(p.r[2]), "=r"(p.r[3]) : "l"(x + j));
-      return p;
-    }
+    if (j >= 0 && j + Piece<T>::kN <= vocab) return load_piece<T>(x + j);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (sizeof(T) == 2) {
@@ -184,141 +201,96 @@ __device__ __forceinline__ uint32_t in_first(const void *p) {
 }
 
 struct LogprobShared {
-  int cell[kCells];                // maxima, as order_of
-  uint16_t reached[kCells];        // cells that reach the bound
+  uint16_t reached[kReached];  // cells that reach the bound
   uint64_t candidate[kCandidates];
   uint64_t top[COPES_MAX_TOP];
   uint64_t theirs[kClusterMost * COPES_MAX_TOP];  // of the cluster's blocks, in the first
   Sums sums[kClusterMost];
-  int group[kWarps_][32];
-  Sums warp[kWarps_];
-  uint64_t best[kWarps_];
+  int group[2][kMostThreads];
+  int bound;
+  Sums warp[kMostWarps];
+  uint64_t best[kMostWarps];
   int n_reached, n_candidates;
 };
 
-// top[0 .. k): the k largest of list[0 .. n), 0 past them.  By counting: the numbers differ.
+// top[0 .. k): the k largest of list[0 .. n), untouched past them.  By counting: the numbers differ.
 __device__ __forceinline__ void rank_by_counting(const uint64_t *list, int n, int k, uint64_t *top) {
-  for (int i = threadIdx.x; i < n; i += kThreads_) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const uint64_t mine = list[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) rank += list[j] > mine;
     if (rank < k && mine) top[rank] = mine;
   }
 }
 
-// The block's alternatives into sh.top, from the cells' maxima of pieces [v0, v0 + n).
-template <typename T>
-__device__ void find_top(LogprobShared &sh, const Row<T> &row, int v0, int n, int cell_log, int k) {
+// visit(a logit's order, its index) for the logits of piece v whose order is `least` or above.
+template <typename T, typename Visit>
+__device__ __forceinline__ void visit_piece(const Row<T> &row, int v, int least, Visit visit) {
   constexpr int N = Piece<T>::kN;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int cells = (n + (1 << cell_log) - 1) >> cell_log;
-  int best = kNone;
-  for (int i = tid; i < cells; i += kThreads_) best = max(best, sh.cell[i]);
-  sh.group[warp][lane] = best;
-  __syncthreads();
+  const Piece<T> p = row.load(v);
+  if (order_of(max_of(p)) < least) return;
+  const int j = row.first(v);
 #pragma unroll
-  for (int w = 0; w < kWarps_; ++w) best = max(best, sh.group[w][lane]);
-  int rank = 0;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const int other = __shfl_sync(kAll, best, i);
-    rank += other > best || (other == best && i < lane);
+  for (int e = 0; e < N; ++e) {
+    float x[2];
+    pair_of(p, e / 2, x[0], x[1]);
+    const int o = order_of(x[e & 1]);
+    if (o >= least && (unsigned)(j + e) < (unsigned)row.vocab) visit(o, (uint32_t)(j + e));
   }
-  const int bound = __shfl_sync(kAll, best, __ffs(__ballot_sync(kAll, rank == k - 1)) - 1);
-  for (int i = tid; i < cells; i += kThreads_)
-    if (sh.cell[i] >= bound) sh.reached[atomicAdd(&sh.n_reached, 1)] = (uint16_t)i;
-  __syncthreads();
-  const int items = sh.n_reached << cell_log;  // a cell's pieces are at most n, cells at most kCells
+}
 
-  // visit(logit's order, its index) for every logit of the cells that reach the bound
-  const auto each = [&](auto visit) {
-    for (int i = tid; i < items; i += kThreads_) {
-      const int v = ((int)sh.reached[i >> cell_log] << cell_log) + (i & ((1 << cell_log) - 1));
-      if (v >= n) continue;
-      const Piece<T> p = row.load(v0 + v);
-      const int j = row.first(v0 + v);
-#pragma unroll
-      for (int e = 0; e < N / 2; ++e) {
-        float x[2];
-        pair_of(p, e, x[0], x[1]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          if ((unsigned)(j + 2 * e + u) < (unsigned)row.vocab) visit(order_of(x[u]), (uint32_t)(j + 2 * e + u));
-      }
-    }
-  };
-  const auto push = [&](int order, uint32_t index) {
-    const int at = atomicAdd(&sh.n_candidates, 1);
-    if (at < kCandidates) sh.candidate[at] = ranked(order, index);
-  };
-  each([&](int order, uint32_t index) {
-    if (order >= bound) push(order, index);
-  });
+// The k largest of pieces [v0, v0 + n) where the logits that reach the bound are too many to be
+// listed.  Where most of them equal it (masked tokens, with fewer than k others): those that surpass
+// it and, in the order of the indices, the first that equal it.  Else one after the other.
+template <typename T>
+__device__ __noinline__ void find_top_slowly(LogprobShared &sh, const Row<T> &row, int v0, int n, int bound, int k) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   __syncthreads();
-  int found = sh.n_candidates;
-  if (found > kCandidates) {
-    // Many equal the bound (masked tokens where fewer than k are left), or many surpass it (logits
-    // in order).  The former: those that surpass it, and the first k that equal it.
-    __syncthreads();
-    if (tid == 0) sh.n_candidates = 0;
-    __syncthreads();
-    each([&](int order, uint32_t index) {
-      if (order > bound) push(order, index);
-    });
-    __syncthreads();
-    found = sh.n_candidates;
-    if (found <= kCandidates - COPES_MAX_TOP) {
-      if (warp == 0) {
-        int equal = 0;
-        for (int v = lane; equal < k && v - lane < n; v += 32) {  // in the order of the indices
-          const bool here = v < n && sh.cell[v >> cell_log] >= bound;
-          if (!__any_sync(kAll, here)) continue;
-          float x[N];
-          int j = 0, mine = 0;
-          if (here) {
-            const Piece<T> p = row.load(v0 + v);
-            j = row.first(v0 + v);
+  if (tid == 0) sh.n_candidates = 0;
+  __syncthreads();
+  if (bound != 0x7FFFFFFF)
+    for (int v = tid; v < n; v += blockDim.x)
+      visit_piece(row, v0 + v, bound + 1, [&](int order, uint32_t index) {
+        const int at = atomicAdd(&sh.n_candidates, 1);
+        if (at < kCandidates) sh.candidate[at] = ranked(order, index);
+      });
+  __syncthreads();
+  const int above = sh.n_candidates;
+  if (above <= kCandidates - COPES_MAX_TOP) {
+    if (warp == 0) {
+      int equal = 0;
+      for (int v = lane; equal < k && v - lane < n; v += 32) {
+        int mine = 0;
+        if (v < n) visit_piece(row, v0 + v, bound, [&](int order, uint32_t) { mine += order == bound; });
+        int before = mine;
 #pragma unroll
-            for (int e = 0; e < N / 2; ++e) pair_of(p, e, x[2 * e], x[2 * e + 1]);
-#pragma unroll
-            for (int e = 0; e < N; ++e) mine += (unsigned)(j + e) < (unsigned)row.vocab && order_of(x[e]) == bound;
-          }
-          int before = mine;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(kAll, before, d);
-            if (lane >= d) before += y;
-          }
-          const int sum = __shfl_sync(kAll, before, 31);
-          int at = equal + before - mine;
-          if (here) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-              if ((unsigned)(j + e) < (unsigned)row.vocab && order_of(x[e]) == bound) {
-                if (at < k) sh.candidate[found + at] = ranked(bound, (uint32_t)(j + e));
-                ++at;
-              }
-          }
-          equal += sum;
+        for (int d = 1; d < 32; d <<= 1) {
+          const int y = __shfl_up_sync(kAll, before, d);
+          if (lane >= d) before += y;
         }
-        if (lane == 0) sh.n_candidates = found + min(equal, k);
+        int at = equal + before - mine;
+        equal += __shfl_sync(kAll, before, 31);
+        if (mine && at < k)
+          visit_piece(row, v0 + v, bound, [&](int order, uint32_t index) {
+            if (order == bound && at < k) sh.candidate[above + at++] = ranked(bound, index);
+          });
       }
-      __syncthreads();
-      found = sh.n_candidates;
+      if (lane == 0) sh.n_candidates = above + min(equal, k);
     }
-  }
-  if (found <= kCandidates) {
-    rank_by_counting(sh.candidate, found, k, sh.top);
+    __syncthreads();
+    rank_by_counting(sh.candidate, sh.n_candidates, k, sh.top);
     __syncthreads();
     return;
   }
-  uint64_t last = ~0ull;  // one after the other
+  uint64_t last = ~0ull;
   for (int r = 0; r < k; ++r) {
     uint64_t next = 0;
-    each([&](int order, uint32_t index) {
-      const uint64_t key = ranked(order, index);
-      if (key < last && key > next) next = key;
-    });
+    for (int v = tid; v < n; v += blockDim.x)
+      visit_piece(row, v0 + v, bound, [&](int order, uint32_t index) {
+        const uint64_t key = ranked(order, index);
+        if (key < last && key > next) next = key;
+      });
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
       const uint64_t y = __shfl_xor_sync(kAll, next, d);
@@ -326,8 +298,7 @@ __device__ void find_top(LogprobShared &sh, const Row<T> &row, int v0, int n, in
     }
     if (lane == 0) sh.best[warp] = next;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWarps_; ++w)
+    for (int w = 0; w < warps; ++w)
       if (sh.best[w] > next) next = sh.best[w];
     if (tid == 0) sh.top[r] = next;
     last = next;
@@ -335,34 +306,115 @@ __device__ void find_top(LogprobShared &sh, const Row<T> &row, int v0, int n, in
   }
 }
 
-// Block (or cluster of `parts` blocks) per row; a cell is 2^cell_log pieces.
+// The k-th largest (1 <= k <= 32) of a warp's 64 numbers: a bitonic sort, the largest in a of lane 0.
+__device__ __forceinline__ int kth_of_64(int a, int b, int k) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll 1
+    for (int d = size >> 1; d; d >>= 1) {
+      const int u = __shfl_xor_sync(kAll, a, d), v = __shfl_xor_sync(kAll, b, d);
+      const bool lower = (lane & d) == 0;
+      const bool down = size == 32 || (lane & size) == 0;  // a's second halves and, last, all of b ascend
+      a = down == lower ? max(a, u) : min(a, u);
+      b = (size == 32 ? false : down) == lower ? max(b, v) : min(b, v);
+    }
+  int top = max(a, b);  // the 32 largest, in some order
+#pragma unroll 1
+  for (int d = 16; d; d >>= 1) {
+    const int u = __shfl_xor_sync(kAll, top, d);
+    top = (lane & d) == 0 ? max(top, u) : min(top, u);
+  }
+  return __shfl_sync(kAll, top, k - 1);
+}
+
+// The block's alternatives into sh.top, from the cells' maxima of pieces [v0, v0 + n) and `own`,
+// this thread's over all, in two halves.  cell[j blockDim + tid]: steps j 2^merge and on of the thread.
+template <typename T>
+__device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, const Row<T> &row, int v0, int n, int merge,
+                                         const float (&own)[2], int k) {
+  const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
+  sh.group[0][tid] = order_of(own[0]);
+  sh.group[1][tid] = order_of(own[1]);
+  __syncthreads();
+  if (tid < 32) {
+    int u = sh.group[0][lane], v = sh.group[1][lane];
+    for (int w = 1; w < warps; ++w) {
+      u = max(u, sh.group[0][w * 32 + lane]);
+      v = max(v, sh.group[1][w * 32 + lane]);
+    }
+    u = kth_of_64(u, v, k);
+    if (lane == 0) sh.bound = u;
+  }
+  __syncthreads();
+  const int bound = sh.bound;
+  if (order_of(max_nan(own[0], own[1])) >= bound) {
+    const int steps = (n + kStep * warps - 1) / (kStep * warps), cells = (steps + (1 << merge) - 1) >> merge;
+#pragma unroll 4
+    for (int j = 0; j < cells; ++j)
+      if (order_of(cell[j * threads + tid]) >= bound) {
+        const int at = atomicAdd(&sh.n_reached, 1);
+        if (at < kReached) sh.reached[at] = (uint16_t)(j * threads + tid);
+      }
+  }
+  __syncthreads();
+  const int reached = sh.n_reached;
+  bool listed = reached <= kReached;
+  if (listed) {
+    const int sub = 2 + merge, shift = 31 - __clz(threads);  // 2^sub pieces in a cell
+    for (int i = tid; i < reached << sub; i += threads) {
+      const int id = sh.reached[i >> sub], part = i & ((1 << sub) - 1);
+      const int step = ((id >> shift) << merge) + (part >> 2), thread = id & (threads - 1);
+      const int v = ((step * warps + (thread >> 5)) * kLoads + (part & 3)) * 32 + (thread & 31);
+      if (v < n)
+        visit_piece(row, v0 + v, bound, [&](int order, uint32_t index) {
+          const int at = atomicAdd(&sh.n_candidates, 1);
+          if (at < kCandidates) sh.candidate[at] = ranked(order, index);
+        });
+    }
+    __syncthreads();
+    const int found = sh.n_candidates;
+    listed = found <= kCandidates;
+    if (listed) {
+      rank_by_counting(sh.candidate, found, k, sh.top);
+      __syncthreads();
+    }
+  }
+  if (!listed) find_top_slowly(sh, row, v0, n, bound, k);
+}
+
+// Block (or cluster of `parts` blocks) per row; a cell is 2^merge steps of a thread.
 template <typename T, bool kTop>
-__global__ void __launch_bounds__(kThreads_, 4) logprob_kernel(LogprobArgs a, int parts, int cell_log) {
+__global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobArgs a, int parts, int merge) {
+  extern __shared__ float cell[];
   __shared__ LogprobShared sh;
   constexpr int N = Piece<T>::kN;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int i = blockIdx.x / parts, part = blockIdx.x % parts;
   if (parts > 1) cluster_arrive();
   const Row<T> row((const T *)a.logits + (int64_t)i * a.row, a.vocab);
   const int all = row.pieces();
   const int v0 = (int)((int64_t)all * part / parts), n = (int)((int64_t)all * (part + 1) / parts) - v0;
+  const int full0 = row.first_full() - v0, full1 = min(n, row.end_full() - v0);
+  const char *at = row.at(v0) + lane * 16;
   const float c = a.scale * 1.44269504088896340736f;
   const int64_t target = a.target[i];
   if (kTop) {
-    const int cells = (n + (1 << cell_log) - 1) >> cell_log;
     if (tid < COPES_MAX_TOP) sh.top[tid] = 0;
     if (tid == 0) sh.n_reached = sh.n_candidates = 0;
-    if (cell_log > 5)
-      for (int j = tid; j < cells; j += kThreads_) sh.cell[j] = kNone;
-    __syncthreads();
   }
 
   Sums t{-FLT_MAX, 0.0f, 0.0f};
+  float own[2] = {-INFINITY, -INFINITY};
   uint64_t s2 = 0, h2 = 0;
   const uint64_t c2 = pack2(c, c);
-  constexpr int kStep = kLoads * 32;
-  Piece<T> now[kLoads];
+  Piece<T> now[kLoads], next[kLoads];
   const auto fetch = [&](int base, Piece<T> (&to)[kLoads]) {
+    if (base >= full0 && base + kStep <= full1) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) to[u] = load_piece<T>(at + (int64_t)base * 16 + u * 512);
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
       const int v = base + u * 32 + lane;
@@ -374,30 +426,20 @@ __global__ void __launch_bounds__(kThreads_, 4) logprob_kernel(LogprobArgs a, in
       }
     }
   };
+  const int stride = warps * kStep;
   if (warp * kStep < n) fetch(warp * kStep, now);
-  for (int base = warp * kStep; base < n; base += kWarps_ * kStep) {
-    Piece<T> next[kLoads];
-    if (base + kWarps_ * kStep < n) fetch(base + kWarps_ * kStep, next);
-    float most[kLoads];
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) most[u] = max_of(now[u]);
+  int step = 0;
+  for (int base = warp * kStep; base < n; base += stride, ++step) {
+    if (base + stride < n) fetch(base + stride, next);
+    const float half[2] = {max_nan(max_of(now[0]), max_of(now[1])), max_nan(max_of(now[2]), max_of(now[3]))};
+    const float most = max_nan(half[0], half[1]);
     if (kTop) {
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int v = base + u * 32 + lane;
-        int o = order_of(most[u]);
-        if (cell_log >= 5) o = __reduce_max_sync(kAll, o);
-        else
-          for (int d = 1; d < (1 << cell_log); d <<= 1) o = max(o, __shfl_xor_sync(kAll, o, d));
-        if (cell_log > 5) {
-          if (lane == 0 && v < n) atomicMax(&sh.cell[v >> cell_log], o);
-        } else if ((v & ((1 << cell_log) - 1)) == 0 && v < n) {
-          sh.cell[v >> cell_log] = o;
-        }
-      }
+      own[0] = max_nan(own[0], half[0]);
+      own[1] = max_nan(own[1], half[1]);
+      float *to = cell + (step >> merge) * blockDim.x + tid;
+      *to = step & ((1 << merge) - 1) ? max_nan(*to, most) : most;
     }
-    const float lane_most = max_nan(max_nan(most[0], most[1]), max_nan(most[2], most[3]));
-    const float M = max_nan(t.m, value_of(__reduce_max_sync(kAll, order_of(lane_most))));
+    const float M = max_nan(t.m, warp_max_nan(most));
     if (!(M == t.m)) {  // the same for the whole warp
       float s0, s1, h0, h1;
       unpack2(s2, s0, s1);
@@ -416,16 +458,19 @@ __global__ void __launch_bounds__(kThreads_, 4) logprob_kernel(LogprobArgs a, in
       for (int e = 0; e < N / 2; ++e) {
         float x, y;
         pair_of(now[u], e, x, y);
-        float d0, d1;
-        unpack2(mul2(add2(pack2(x, y), minus_m), c2), d0, d1);
-        d0 = max_nan(d0, kLeast);
-        d1 = max_nan(d1, kLeast);
-        const uint64_t p = pack2(exp2_fast(d0), exp2_fast(d1));
+        unpack2(mul2(add2(pack2(x, y), minus_m), c2), x, y);
+        x = max_nan(x, kLeast);
+        y = max_nan(y, kLeast);
+        const uint64_t p = pack2(exp2_fast(x), exp2_fast(y));
         s2 = add2(s2, p);
-        h2 = fma2(p, pack2(d0, d1), h2);
+        h2 = fma2(p, pack2(x, y), h2);
       }
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) now[u] = next[u];
+  }
+  if (kTop) {  // a thread's steps past its last hold nothing
+    const int steps = (n + stride - 1) / stride, cells = (steps + (1 << merge) - 1) >> merge;
+    for (int j = (step + (1 << merge) - 1) >> merge; j < cells; ++j) cell[j * blockDim.x + tid] = -INFINITY;
   }
   float odd_s, odd_h;
   unpack2(s2, t.s, odd_s);
@@ -439,10 +484,9 @@ __global__ void __launch_bounds__(kThreads_, 4) logprob_kernel(LogprobArgs a, in
   }
   if (lane == 0) sh.warp[warp] = t;
   __syncthreads();
+  if (kTop) find_top(sh, cell, row, v0, n, merge, own, a.top);
   t = sh.warp[0];
-#pragma unroll
-  for (int w = 1; w < kWarps_; ++w) t = join(t, sh.warp[w], c);
-  if (kTop) find_top(sh, row, v0, n, cell_log, a.top);
+  for (int w = 1; w < warps; ++w) t = join(t, sh.warp[w], c);
 
   if (parts > 1) {
     cluster_wait();  // the first block has begun
@@ -457,8 +501,7 @@ __global__ void __launch_bounds__(kThreads_, 4) logprob_kernel(LogprobArgs a, in
     t = sh.sums[0];
     for (int p = 1; p < parts; ++p) t = join(t, sh.sums[p], c);
     if (kTop) {
-      __syncthreads();  // sh.top was read above
-      rank_by_counting(sh.theirs, parts * a.top, a.top, sh.top);
+      rank_by_counting(sh.theirs, parts * a.top, a.top, sh.top);  // sh.top was read before the barrier
       __syncthreads();
     }
   }
@@ -486,15 +529,33 @@ __global__ void __launch_bounds__(kThreads_, 4) logprob_kernel(LogprobArgs a, in
 
 template <typename T, bool kTop>
 static cudaError_t launch(const LogprobArgs &a, cudaStream_t s) {
-  // blocks for the whole GPU (152 SMs, 4 blocks each) from few rows, none with less than 4 KB
   const int64_t pieces = (int64_t)a.vocab / Piece<T>::kN + 2;
+  // Parts of a row: the waves of blocks over the GPU times a part's pieces, and what a block costs
+  // besides, about 2,000 pieces' time on a full GPU.  734 rows of 18,992 pieces: 71 us as two waves
+  // of whole rows, TODO us as rows in four.
+  const int64_t slots = 152 * kPerSm;
   int parts = 1;
-  while (parts < kClusterMost && (int64_t)a.n * parts * 2 <= 152 * 4 && pieces / (parts * 2) >= 256) parts *= 2;
-  int cell_log = 0;
-  while ((pieces / parts + 1) >> cell_log >= kCells) ++cell_log;
+  int64_t best = INT64_MAX;
+  for (int p = 1; p <= kClusterMost && (p == 1 || pieces / p >= 256); p *= 2) {
+    const int64_t waves = ((int64_t)a.n * p + slots - 1) / slots, cost = waves * (pieces / p + 2000);
+    if (cost < best) {
+      best = cost;
+      parts = p;
+    }
+  }
+  int threads = 32;
+  while (threads < kMostThreads && pieces / parts >= threads * 2 * kLoads) threads *= 2;
+  const int64_t steps = (pieces / parts + 1 + threads * kLoads - 1) / (threads * kLoads);
+  int merge = 0;
+  while ((((steps + (1 << merge) - 1) >> merge) * threads) > kCells) ++merge;
+  const uint32_t bytes = kTop ? (uint32_t)((steps + (1 << merge) - 1) >> merge) * threads * 4 : 0;
+  const uint32_t fixed = sizeof(LogprobShared);
+  const cudaError_t e = allow_smem((const void *)logprob_kernel<T, kTop>, bytes + fixed, kCells * 4);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)a.n * parts);
-  cfg.blockDim = dim3(kThreads_);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -502,7 +563,7 @@ static cudaError_t launch(const LogprobArgs &a, cudaStream_t s) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop>, a, parts, cell_log);
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop>, a, parts, merge);
 }
 
 cudaError_t launch_token_logprobs(int dtype, const LogprobArgs &a, cudaStream_t s) {
