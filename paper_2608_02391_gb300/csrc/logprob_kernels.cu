@@ -90,7 +90,6 @@ __device__ __forceinline__ int order_of(float x) {
   return x != x ? 0x7FFFFFFF : o;
 }
 __device__ __forceinline__ float value_of(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7FFFFFFF)); }
-constexpr int kNone = (int)0x80000000;  // below every logit
 
 // A logit and its index as one number: larger logits are larger, then lower indices.  0: none.
 __device__ __forceinline__ uint64_t ranked(int order, uint32_t index) {
@@ -179,18 +178,6 @@ __device__ __forceinline__ void rebase(float &s, float &h, float m, float M, flo
   s = f * s;
 }
 
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
-  const float M = max_nan(a.m, b.m);
-  rebase(a.s, a.h, a.m, M, c);
-  rebase(b.s, b.h, b.m, M, c);
-  return {M, a.s + b.s, a.h + b.h};
-}
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 // The address of the cluster's first block's copy of a shared variable.
@@ -200,11 +187,26 @@ __device__ __forceinline__ uint32_t in_first(const void *p) {
   return r;
 }
 
+// n <= 8 sums together, to the same bits in every lane.
+__device__ __forceinline__ Sums warp_join(const Sums *from, int n, float c) {
+  const int lane = threadIdx.x & 31;
+  Sums t = lane < n ? from[lane] : Sums{-FLT_MAX, 0.0f, 0.0f};
+  const float M = warp_max_nan(t.m);
+  rebase(t.s, t.h, t.m, M, c);
+#pragma unroll
+  for (int d = 1; d < kMostWarps; d <<= 1) {
+    t.s += __shfl_xor_sync(kAll, t.s, d);
+    t.h += __shfl_xor_sync(kAll, t.h, d);
+  }
+  return {M, __shfl_sync(kAll, t.s, 0), __shfl_sync(kAll, t.h, 0)};
+}
+static_assert(kMostWarps <= 8 && kClusterMost <= 8, "warp_join adds up 8 lanes");
+
 struct LogprobShared {
-  uint16_t reached[kReached];  // cells that reach the bound
-  uint64_t candidate[kCandidates];
+  alignas(16) uint64_t candidate[kCandidates];
+  alignas(16) uint64_t theirs[kClusterMost * COPES_MAX_TOP];  // of the cluster's blocks, in the first
   uint64_t top[COPES_MAX_TOP];
-  uint64_t theirs[kClusterMost * COPES_MAX_TOP];  // of the cluster's blocks, in the first
+  uint16_t reached[kReached];  // cells that reach the bound
   Sums sums[kClusterMost];
   int group[2][kMostThreads];
   int bound;
@@ -217,11 +219,29 @@ struct LogprobShared {
 __device__ __forceinline__ void rank_by_counting(const uint64_t *list, int n, int k, uint64_t *top) {
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const uint64_t mine = list[i];
-    int rank = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += list[j] > mine;
+    int rank = n & 1 ? list[n - 1] > mine : 0;
+#pragma unroll 8
+    for (int j = 0; j < n / 2; ++j) {
+      const ulonglong2 two = reinterpret_cast<const ulonglong2 *>(list)[j];
+      rank += (two.x > mine) + (two.y > mine);
+    }
     if (rank < k && mine) top[rank] = mine;
   }
+}
+
+// A place for `mine` entries of each lane in a list of which *n are taken.
+__device__ __forceinline__ int warp_reserve(int mine, int *n) {
+  if (!__any_sync(kAll, mine)) return 0;
+  const int lane = threadIdx.x & 31;
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(kAll, upto, d);
+    if (lane >= d) upto += y;
+  }
+  int at = 0;
+  if (lane == 31) at = atomicAdd(n, upto);
+  return __shfl_sync(kAll, at, 31) + upto - mine;
 }
 
 // visit(a logit's order, its index) for the logits of piece v whose order is `least` or above.
@@ -309,9 +329,9 @@ __device__ __noinline__ void find_top_slowly(LogprobShared &sh, const Row<T> &ro
 // The k-th largest (1 <= k <= 32) of a warp's 64 numbers: a bitonic sort, the largest in a of lane 0.
 __device__ __forceinline__ int kth_of_64(int a, int b, int k) {
   const int lane = threadIdx.x & 31;
-#pragma unroll 1
+#pragma unroll
   for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll 1
+#pragma unroll
     for (int d = size >> 1; d; d >>= 1) {
       const int u = __shfl_xor_sync(kAll, a, d), v = __shfl_xor_sync(kAll, b, d);
       const bool lower = (lane & d) == 0;
@@ -320,7 +340,7 @@ __device__ __forceinline__ int kth_of_64(int a, int b, int k) {
       b = (size == 32 ? false : down) == lower ? max(b, v) : min(b, v);
     }
   int top = max(a, b);  // the 32 largest, in some order
-#pragma unroll 1
+#pragma unroll
   for (int d = 16; d; d >>= 1) {
     const int u = __shfl_xor_sync(kAll, top, d);
     top = (lane & d) == 0 ? max(top, u) : min(top, u);
@@ -333,6 +353,7 @@ __device__ __forceinline__ int kth_of_64(int a, int b, int k) {
 template <typename T>
 __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, const Row<T> &row, int v0, int n, int merge,
                                          const float (&own)[2], int k) {
+  constexpr int N = Piece<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
   sh.group[0][tid] = order_of(own[0]);
   sh.group[1][tid] = order_of(own[1]);
@@ -348,29 +369,50 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
   }
   __syncthreads();
   const int bound = sh.bound;
-  if (order_of(max_nan(own[0], own[1])) >= bound) {
-    const int steps = (n + kStep * warps - 1) / (kStep * warps), cells = (steps + (1 << merge) - 1) >> merge;
+  {
+    unsigned mine = 0;  // which of the thread's cells: at most kCells / kMostThreads = 32 (fewer threads have fewer)
+    if (order_of(max_nan(own[0], own[1])) >= bound) {
+      const int steps = (n + kStep * warps - 1) / (kStep * warps), cells = (steps + (1 << merge) - 1) >> merge;
 #pragma unroll 4
-    for (int j = 0; j < cells; ++j)
-      if (order_of(cell[j * threads + tid]) >= bound) {
-        const int at = atomicAdd(&sh.n_reached, 1);
-        if (at < kReached) sh.reached[at] = (uint16_t)(j * threads + tid);
-      }
+      for (int j = 0; j < cells; ++j) mine |= (unsigned)(order_of(cell[j * threads + tid]) >= bound) << j;
+    }
+    int at = warp_reserve(__popc(mine), &sh.n_reached);
+    for (; mine; mine &= mine - 1, ++at)
+      if (at < kReached) sh.reached[at] = (uint16_t)((__ffs(mine) - 1) * threads + tid);
   }
   __syncthreads();
   const int reached = sh.n_reached;
   bool listed = reached <= kReached;
   if (listed) {
-    const int sub = 2 + merge, shift = 31 - __clz(threads);  // 2^sub pieces in a cell
-    for (int i = tid; i < reached << sub; i += threads) {
-      const int id = sh.reached[i >> sub], part = i & ((1 << sub) - 1);
-      const int step = ((id >> shift) << merge) + (part >> 2), thread = id & (threads - 1);
-      const int v = ((step * warps + (thread >> 5)) * kLoads + (part & 3)) * 32 + (thread & 31);
-      if (v < n)
-        visit_piece(row, v0 + v, bound, [&](int order, uint32_t index) {
-          const int at = atomicAdd(&sh.n_candidates, 1);
-          if (at < kCandidates) sh.candidate[at] = ranked(order, index);
-        });
+    const int sub = 2 + merge, shift = 31 - __clz(threads), items = reached << sub;  // 2^sub pieces in a cell
+    for (int base = tid & ~31; base < items; base += threads) {
+      const int i = base + lane;
+      Piece<T> p;
+      int j = 0, mine = 0;
+      if (i < items) {
+        const int id = sh.reached[i >> sub], part = i & ((1 << sub) - 1);
+        const int step = ((id >> shift) << merge) + (part >> 2), thread = id & (threads - 1);
+        const int v = ((step * warps + (thread >> 5)) * kLoads + (part & 3)) * 32 + (thread & 31);
+        if (v < n) {
+          p = row.load(v0 + v);
+          j = row.first(v0 + v);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            float x[2];
+            pair_of(p, e / 2, x[0], x[1]);
+            mine |= (order_of(x[e & 1]) >= bound && (unsigned)(j + e) < (unsigned)row.vocab) << e;
+          }
+        }
+      }
+      int at = warp_reserve(__popc(mine), &sh.n_candidates);
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (mine >> e & 1) {
+          float x[2];
+          pair_of(p, e / 2, x[0], x[1]);
+          if (at < kCandidates) sh.candidate[at] = ranked(order_of(x[e & 1]), (uint32_t)(j + e));
+          ++at;
+        }
     }
     __syncthreads();
     const int found = sh.n_candidates;
@@ -383,33 +425,34 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
   if (!listed) find_top_slowly(sh, row, v0, n, bound, k);
 }
 
-// Block (or cluster of `parts` blocks) per row; a cell is 2^merge steps of a thread.
+// A block, or a cluster of `parts` blocks, per row; a cell is 2^merge steps of a thread.  Before it
+// looks for a row's alternatives a block asks for the first kAhead bytes of what a block `apart`
+// rows on reads, whose turn is near, into L2, so that HBM is not idle meanwhile.
+constexpr int kAhead = 48 << 10;
+
 template <typename T, bool kTop>
-__global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobArgs a, int parts, int merge) {
+__global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobArgs a, int parts, int merge, int apart) {
   extern __shared__ float cell[];
   __shared__ LogprobShared sh;
   constexpr int N = Piece<T>::kN;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  const int i = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, stride = warps * kStep;
+  const int part = blockIdx.x % parts;
+  const int64_t i = blockIdx.x / parts;
+  const float c = a.scale * 1.44269504088896340736f;
+  const uint64_t c2 = pack2(c, c);
   if (parts > 1) cluster_arrive();
-  const Row<T> row((const T *)a.logits + (int64_t)i * a.row, a.vocab);
+  const Row<T> row((const T *)a.logits + i * a.row, a.vocab);
   const int all = row.pieces();
   const int v0 = (int)((int64_t)all * part / parts), n = (int)((int64_t)all * (part + 1) / parts) - v0;
   const int full0 = row.first_full() - v0, full1 = min(n, row.end_full() - v0);
   const char *at = row.at(v0) + lane * 16;
-  const float c = a.scale * 1.44269504088896340736f;
   const int64_t target = a.target[i];
-  if (kTop) {
-    if (tid < COPES_MAX_TOP) sh.top[tid] = 0;
-    if (tid == 0) sh.n_reached = sh.n_candidates = 0;
-  }
 
   Sums t{-FLT_MAX, 0.0f, 0.0f};
   float own[2] = {-INFINITY, -INFINITY};
   uint64_t s2 = 0, h2 = 0;
-  const uint64_t c2 = pack2(c, c);
   Piece<T> now[kLoads], next[kLoads];
-  const auto fetch = [&](int base, Piece<T> (&to)[kLoads]) {
+  const auto fetch = [&](int base, Piece<T>(&to)[kLoads]) {
     if (base >= full0 && base + kStep <= full1) {
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) to[u] = load_piece<T>(at + (int64_t)base * 16 + u * 512);
@@ -426,8 +469,11 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
       }
     }
   };
-  const int stride = warps * kStep;
   if (warp * kStep < n) fetch(warp * kStep, now);
+  if (kTop) {
+    if (tid < COPES_MAX_TOP) sh.top[tid] = 0;
+    if (tid == 0) sh.n_reached = sh.n_candidates = 0;
+  }
   int step = 0;
   for (int base = warp * kStep; base < n; base += stride, ++step) {
     if (base + stride < n) fetch(base + stride, next);
@@ -468,6 +514,12 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) now[u] = next[u];
   }
+  if (tid == 0 && i + apart < a.n) {
+    const Row<T> then((const T *)a.logits + (i + apart) * a.row, a.vocab);
+    const int v = max((int)((int64_t)then.pieces() * part / parts), then.first_full());
+    const int bytes = min(min(n, then.end_full() - v), kAhead / 16) * 16;
+    if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(then.at(v)), "r"(bytes) : "memory");
+  }
   if (kTop) {  // a thread's steps past its last hold nothing
     const int steps = (n + stride - 1) / stride, cells = (steps + (1 << merge) - 1) >> merge;
     for (int j = (step + (1 << merge) - 1) >> merge; j < cells; ++j) cell[j * blockDim.x + tid] = -INFINITY;
@@ -484,22 +536,22 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
   }
   if (lane == 0) sh.warp[warp] = t;
   __syncthreads();
+  t = warp_join(sh.warp, warps, c);
   if (kTop) find_top(sh, cell, row, v0, n, merge, own, a.top);
-  t = sh.warp[0];
-  for (int w = 1; w < warps; ++w) t = join(t, sh.warp[w], c);
 
   if (parts > 1) {
     cluster_wait();  // the first block has begun
     const uint32_t to = in_first(&sh.sums[part]);
     if (tid < 3)
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * tid), "f"(tid == 0 ? t.m : tid == 1 ? t.s : t.h) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * tid), "f"(tid == 0 ? t.m : tid == 1 ? t.s : t.h)
+                   : "memory");
     if (kTop && tid < a.top)
-      asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(in_first(&sh.theirs[part * a.top + tid])), "l"(sh.top[tid]) : "memory");
+      asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(in_first(&sh.theirs[part * a.top + tid])), "l"(sh.top[tid])
+                   : "memory");
     cluster_arrive();
     cluster_wait();
     if (part) return;
-    t = sh.sums[0];
-    for (int p = 1; p < parts; ++p) t = join(t, sh.sums[p], c);
+    t = warp_join(sh.sums, parts, c);
     if (kTop) {
       rank_by_counting(sh.theirs, parts * a.top, a.top, sh.top);  // sh.top was read before the barrier
       __syncthreads();
@@ -522,8 +574,8 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
   }
   if (kTop && tid < a.top) {
     const uint64_t r = sh.top[tid];
-    a.top_ids[(int64_t)i * a.top + tid] = index_in(r);
-    a.top_logprobs[(int64_t)i * a.top + tid] = empty ? -INFINITY : (value_of(order_in(r)) - t.m) * a.scale - log_sum;
+    a.top_ids[i * a.top + tid] = index_in(r);
+    a.top_logprobs[i * a.top + tid] = empty ? -INFINITY : (value_of(order_in(r)) - t.m) * a.scale - log_sum;
   }
 }
 
@@ -553,6 +605,7 @@ static cudaError_t launch(const LogprobArgs &a, cudaStream_t s) {
   const cudaError_t e = allow_smem((const void *)logprob_kernel<T, kTop>, bytes + fixed, kCells * 4);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
+  const int apart = (int)(slots * kMostThreads / threads / parts);  // rows at a time
   cfg.gridDim = dim3((unsigned)a.n * parts);
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = bytes;
@@ -563,7 +616,7 @@ static cudaError_t launch(const LogprobArgs &a, cudaStream_t s) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop>, a, parts, merge);
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop>, a, parts, merge, apart);
 }
 
 cudaError_t launch_token_logprobs(int dtype, const LogprobArgs &a, cudaStream_t s) {
