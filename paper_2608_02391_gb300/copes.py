@@ -563,6 +563,9 @@ def update(arena: Arena, sub: SubspaceHandle, noise_id: np.ndarray, sign: np.nda
 
 
 # ------------------------------------------------------------ answering with the weights
+_DTYPE_CODES = {torch.bfloat16: BF16, torch.float32: FP32}
+
+
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
     """An output of a call on `stream`, allocated in that stream's order."""
     if stream is None:
@@ -585,7 +588,7 @@ class KVCache:
             assert t.is_cuda and t.is_contiguous() and t.device == pool.device
         assert all(t.dtype == torch.int32 for t in (table, length, refs))
         self.pool, self.table, self.length, self.refs = pool, table, length, refs
-        self.dtype = {torch.bfloat16: BF16, torch.float32: FP32}[pool.dtype]
+        self.dtype = _DTYPE_CODES[pool.dtype]
         n_pages, n_layers, _, kv, ps, d = pool.shape
         self.desc = KVCacheDesc(pool.data_ptr(), self.dtype, n_pages, n_layers, kv, ps, d, table.data_ptr(),
                                 table.shape[0], table.shape[1], length.data_ptr(), refs.data_ptr())
@@ -720,11 +723,10 @@ def token_logprobs(logits: torch.Tensor, target: torch.Tensor, top: int = 0, sca
     device = logits.device
     assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
     assert target.shape == (n,) and target.dtype == torch.int64 and target.device == device and target.is_contiguous()
-    dtype = {torch.bfloat16: BF16, torch.float32: FP32}[logits.dtype]
-    both = _empty((2, n), torch.float32, device, stream)
+    dtype = _DTYPE_CODES[logits.dtype]
+    logprob, entropy = _empty((2, n), torch.float32, device, stream).unbind(0)
     ids = _empty((n, top), torch.int64, device, stream)
     top_logprobs = _empty((n, top), torch.float32, device, stream)
-    logprob, entropy = both[0], both[1]
     _check(load().copes_token_logprobs(logits.data_ptr(), dtype, n, vocab, logits.stride(0), target.data_ptr(), scale,
                                        top, logprob.data_ptr(), entropy.data_ptr(), ids.data_ptr(),
                                        top_logprobs.data_ptr(), _stream(stream)))

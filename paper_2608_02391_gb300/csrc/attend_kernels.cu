@@ -58,9 +58,11 @@ struct Shape {
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
 };
 
-// Where a block is in the line of tiles: row by row, head group by head group, tile by tile.
+// Where a block is in the line of tiles: row by row, key-value head by head, group of query heads
+// by group, tile by tile.
 struct Cursor {
-  int row, unit, tile, tiles, tokens, slot;
+  int row, slot, tokens, tiles;  // of the row
+  int kv, sub, tile;
 };
 
 __device__ __forceinline__ int row_slot(const AttendArgs &a, int row) { return a.slots ? a.slots[row] : row; }
@@ -76,22 +78,29 @@ __device__ __forceinline__ int row_tiles(int tokens) {
 }
 
 template <int kTile>
-__device__ __forceinline__ void enter_row(const AttendArgs &a, Cursor &c) {
-  if (c.row >= a.n) return;
+__device__ __forceinline__ void advance(const AttendArgs &a, int groups, Cursor &c) {
+  if (++c.tile < c.tiles) return;
+  c.tile = 0;
+  if (++c.sub < groups) return;
+  c.sub = 0;
+  if (++c.kv < a.c.n_kv_heads) return;
+  c.kv = 0;
+  if (++c.row >= a.n) return;
   c.slot = row_slot(a, c.row);
   c.tokens = row_tokens(a, c.slot);
   c.tiles = row_tiles<kTile>(c.tokens);
 }
 
-template <int kTile>
-__device__ __forceinline__ void advance(const AttendArgs &a, int units, Cursor &c) {
-  if (++c.tile < c.tiles) return;
-  c.tile = 0;
-  if (++c.unit < units) return;
-  c.unit = 0;
-  ++c.row;
-  enter_row<kTile>(a, c);
-}
+// The line shared out: each block has `each` tiles, the first `more` of them one more.
+struct Shares {
+  int each, more;
+  __device__ Shares(int total, int blocks) : each(total / blocks), more(total % blocks) {}
+  __device__ int begin(int block) const { return block * each + min(block, more); }
+  __device__ int owner(int x) const {
+    const int longer = more * (each + 1);
+    return x < longer ? x / (each + 1) : more + (x - longer) / each;
+  }
+};
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -153,6 +162,18 @@ __device__ __forceinline__ void mma_split(float (&c)[4], const uint32_t (&a)[4],
   mma_tf32(c, ah, bh[0], bh[1]);
 }
 
+// The same into a sum of its own for each term: three short chains instead of a long one.
+__device__ __forceinline__ void mma_split3(float (&c)[3][4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  uint32_t ah[4], al[4], bh[2], bl[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split_tf32(a[i], ah[i], al[i]);
+  split_tf32(b0, bh[0], bl[0]);
+  split_tf32(b1, bh[1], bl[1]);
+  mma_tf32(c[0], al, bh[0], bh[1]);
+  mma_tf32(c[1], ah, bl[0], bl[1]);
+  mma_tf32(c[2], ah, bh[0], bh[1]);
+}
+
 // A 16-byte piece's place in a row of a tile is its number xor this, so that what one load
 // instruction reads lies in different banks.
 template <bool kFp32>
@@ -160,11 +181,9 @@ __device__ __forceinline__ int swizzle(int row) {
   return kFp32 ? (row & 6) ^ ((row & 1) << 2) : row & 7;
 }
 
-// Factor of a part with maximum m and sum l in a whole with maximum M (both of log2).  A part
-// without weight counts 0; a NaN stays one.
-__device__ __forceinline__ float part_weight(float m, float l, float M) {
-  return m == -INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : exp2_fast(m - M);
-}
+// Factor of a part with maximum m (of log2) in a whole with maximum M.  A part without weight has
+// m = -inf and zeros; where its scores are NaN its sums are, and 0 times them still is.
+__device__ __forceinline__ float part_weight(float m, float M) { return m == -INFINITY ? 0.0f : exp2_fast(m - M); }
 
 // A warp's state of one (row, head group): heads 8 nt + 2 (lane % 4) + {0, 1}.
 template <typename S>
@@ -227,8 +246,10 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
                                           Running<S> &r) {
   constexpr int NT = S::NT, KS = S::DP / 16, kPitch = S::kChunks * 16;
   const int lane = threadIdx.x & 31;
-  float s[NT][4] = {};
+  float s[NT][4];
   if constexpr (S::kFp32) {
+    constexpr int kSums = NT == 1 ? 2 : 1;  // one for each of the two products of a piece, registers permitting
+    float part[NT][kSums][3][4] = {};
     const int row = lane >> 2;
     const uint32_t at = keys + row * kPitch;
     const int x = swizzle<true>(row);
@@ -242,11 +263,23 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
       const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        mma_split(s[j], a0, q.b[k][j][0], q.b[k][j][1]);
-        mma_split(s[j], a1, q.b[k][j][2], q.b[k][j][3]);
+        mma_split3(part[j][0], a0, q.b[k][j][0], q.b[k][j][1]);
+        mma_split3(part[j][kSums - 1], a1, q.b[k][j][2], q.b[k][j][3]);
       }
     }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float small = part[j][0][0][e] + part[j][0][1][e], large = part[j][0][2][e];
+        if constexpr (kSums == 2) {
+          small += part[j][1][0][e] + part[j][1][1][e];
+          large += part[j][1][2][e];
+        }
+        s[j][e] = large + small;
+      }
   } else {
+    float part[NT][2][4] = {};
     const int row = lane & 15, x = swizzle<false>(row);
     const uint32_t at = keys + row * kPitch;
 #pragma unroll
@@ -254,8 +287,12 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
       uint32_t a[4];
       ldmatrix(a, at + (uint32_t)(((k * 2 + (lane >> 4)) ^ x) * 16));
 #pragma unroll
-      for (int j = 0; j < NT; ++j) mma_bf16(s[j], a, q.b[k][j][0], q.b[k][j][1]);
+      for (int j = 0; j < NT; ++j) mma_bf16(part[j][k & 1], a, q.b[k][j][0], q.b[k][j][1]);
     }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][e] = part[j][0][e] + part[j][1][e];
   }
 
   // tokens lane / 4 (s[.][0], s[.][1]) and lane / 4 + 8
@@ -356,84 +393,119 @@ __device__ __forceinline__ int output_d(int i, int half) {
   return S::kFp32 ? (i >> 1) * 32 + (lane >> 2) * 4 + (i & 1) * 2 + half : i * 16 + (lane >> 2) + half * 8;
 }
 
-__device__ __forceinline__ void store(float x, float *to) { *to = x; }
-__device__ __forceinline__ void store(float x, __nv_bfloat16 *to) { *to = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void store(float4 x, float *to) { *reinterpret_cast<float4 *>(to) = x; }
+__device__ __forceinline__ void store(float4 x, __nv_bfloat16 *to) {
+  *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+}
+__device__ __forceinline__ void fma4(float4 &o, float f, const float4 &x) {
+  o.x = fmaf(f, x.x, o.x);
+  o.y = fmaf(f, x.y, o.y);
+  o.z = fmaf(f, x.z, o.z);
+  o.w = fmaf(f, x.w, o.w);
+}
+// o / L, 0 of an empty row.
+__device__ __forceinline__ float4 normalised(const float4 &o, float L) {
+  if (L == 0.0f) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  return make_float4(o.x / L, o.y / L, o.z / L, o.w / L);
+}
+__device__ __forceinline__ float log_sum(float M, float L) {
+  return L == 0.0f ? -INFINITY : fmaf(0.6931471805599453094f, M, logf(L));
+}
+
+// t / d by a product: t < 2^31, m = ceil(2^(31 + s) / d) with 2^s >= d, so m d = 2^(31 + s) + e with
+// e < 2^s, and t e < 2^(31 + s) adds nothing to the quotient.
+struct Divisor {
+  uint32_t m;
+  int s;
+  __host__ explicit Divisor(uint32_t d) : s(0) {
+    while ((1ull << s) < d) ++s;
+    m = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+  }
+  __device__ __forceinline__ int quotient(int t) const { return (int)(((uint64_t)(uint32_t)t * m) >> (31 + s)); }
+};
 
 // The workspace: counters of the joins (`counter`), one per row and head group, then the parts:
 // block w's at 2 w (of a row that begins before the block's share) and 2 w + 1 (of one that ends
 // after it), each kHeads maxima, kHeads sums and kHeads x head_dim values.
 template <typename T, typename S>
 __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendArgs a, int *counter, float *part,
-                                                                        int units, int groups) {
+                                                                        int groups, Divisor by_page) {
   extern __shared__ __align__(128) char smem[];
-  __shared__ int s_row, s_last;
-  __shared__ int64_t s_before, s_sum[S::kWarps];
+  __shared__ Cursor s_at;
+  __shared__ int s_sum[S::kWarps], s_last;
   constexpr int TILE = S::kTile;
   const Cache &c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = c.head_dim;
-  const int group = a.q_heads / c.n_kv_heads;
+  const int group = a.q_heads / c.n_kv_heads, units = c.n_kv_heads * groups;
 
   // the line's length and this block's share [lo, hi) of it
-  const int each = (a.n + S::kThreads - 1) / S::kThreads, r0 = min(a.n, tid * each), r1 = min(a.n, r0 + each);
-  int64_t mine = 0;
+  const int rows = (a.n + S::kThreads - 1) / S::kThreads, r0 = min(a.n, tid * rows), r1 = min(a.n, r0 + rows);
+  int mine = 0;
   for (int i = r0; i < r1; ++i) mine += row_tiles<TILE>(row_tokens(a, row_slot(a, i)));
-  int64_t before = mine;
+  int before = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t y = __shfl_up_sync(kAll, before, d);
+    const int y = __shfl_up_sync(kAll, before, d);
     if (lane >= d) before += y;
   }
   if (lane == 31) s_sum[warp] = before;
   __syncthreads();
-  int64_t total = 0;
+  int total = 0;
 #pragma unroll
   for (int w = 0; w < S::kWarps; ++w) {
     if (w < warp) before += s_sum[w];
     total += s_sum[w];
   }
   total *= units;
-  const int64_t blocks = min((int64_t)gridDim.x, total);  // each has a tile at least
+  const int blocks = min((int)gridDim.x, total);  // each has a tile at least
   if (blockIdx.x >= blocks) return;
-  const int64_t lo = total * blockIdx.x / blocks, hi = total * (blockIdx.x + 1) / blocks;
+  const Shares shares(total, blocks);
+  const int lo = shares.begin(blockIdx.x), count = shares.begin(blockIdx.x + 1) - lo;
   before -= mine;
   if (before * units <= lo && lo < (before + mine) * units) {
-    int i = r0;
-    for (; i + 1 < r1; ++i) {
-      const int t = row_tiles<TILE>(row_tokens(a, row_slot(a, i)));
-      if (lo < (before + t) * units) break;
-      before += t;
+    Cursor at;
+    at.row = r0;
+    for (;; ++at.row) {
+      at.slot = row_slot(a, at.row);
+      at.tokens = row_tokens(a, at.slot);
+      at.tiles = row_tiles<TILE>(at.tokens);
+      if (at.row + 1 >= r1 || lo < (before + at.tiles) * units) break;
+      before += at.tiles;
     }
-    s_row = i;
-    s_before = before * units;
+    const int unit = (lo - before * units) / at.tiles;
+    at.tile = (lo - before * units) % at.tiles;
+    at.kv = unit / groups;
+    at.sub = unit % groups;
+    s_at = at;
   }
   __syncthreads();
-  Cursor at;
-  at.row = s_row;
-  enter_row<TILE>(a, at);
-  at.unit = (int)((lo - s_before) / at.tiles);
-  at.tile = (int)((lo - s_before) % at.tiles);
-  Cursor ahead = at;
+  Cursor at = s_at, ahead = at;
 
   float *s_o = reinterpret_cast<float *>(smem + S::kStages * S::kStage);  // [warp][8][kRow]
   float *s_m = s_o + S::kWarps * 8 * S::kRow, *s_l = s_m + S::kWarps * 8;
   const uint32_t stages = smem_addr(smem) + warp * 2 * S::kPart;
-  const int count = (int)(hi - lo);
+  const char *pool = c.pool + (uint64_t)a.layer * c.layer_elems * sizeof(T);
+  const uint64_t head_bytes = (uint64_t)c.head_elems * sizeof(T), to_values = c.n_kv_heads * head_bytes;
 
-  // page of token (16 warp + lane % 16) of the next tile to be asked for, -1 for none
-  const auto page_ahead = [&]() {
+  // where token (16 warp + lane % 16) of the next tile to be asked for is: its page (-1 for none, -2 for
+  // one outside the pool) and its place there
+  int page, place;
+  const auto look_up = [&]() {
     const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
-    return t < ahead.tokens ? c.table[(int64_t)ahead.slot * c.table_width + t / c.page_size] : -1;
+    page = -1;
+    place = 0;
+    if (t < ahead.tokens) {
+      const int at_page = by_page.quotient(t);
+      place = t - at_page * c.page_size;
+      page = c.table[(int64_t)ahead.slot * c.table_width + at_page];
+      if ((unsigned)page >= (unsigned)c.n_pages) page = -2;
+    }
   };
-  int page = page_ahead();
+  look_up();
   const auto ask = [&](int stage) {
-    const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
     const char *from = nullptr;
-    if ((unsigned)page < (unsigned)c.n_pages)
-      from = c.pool + (uint64_t)page * c.page_bytes +
-             ((uint64_t)a.layer * c.layer_elems + (uint64_t)(ahead.unit / groups) * c.head_elems +
-              (uint64_t)(t % c.page_size) * D) * sizeof(T);
-    else if (t < ahead.tokens) flag_error(kErrCacheId);
-    const uint64_t to_values = (uint64_t)c.n_kv_heads * c.head_elems * sizeof(T);
+    if (page >= 0) from = pool + (uint64_t)page * c.page_bytes + ahead.kv * head_bytes + (uint64_t)place * D * sizeof(T);
+    else if (page == -2) flag_error(kErrCacheId);
     const uint32_t to = stages + stage * S::kStage;
 #pragma unroll
     for (int i = 0; i < S::kChunks / 2; ++i) {
@@ -445,7 +517,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       copy_async(dst, src, bytes);
       copy_async(dst + S::kPart, bytes ? src + to_values : src, bytes);
     }
-    advance<TILE>(a, units, ahead);
+    advance<TILE>(a, groups, ahead);
   };
 
   int asked = 0;
@@ -453,7 +525,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   for (int s = 0; s < S::kStages - 1; ++s) {
     if (asked < count) {
       ask(s);
-      if (++asked < count) page = page_ahead();
+      if (++asked < count) look_up();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
@@ -465,11 +537,10 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   for (int j = 0; j < count; ++j) {
     if (asked < count) {
       ask(asked % S::kStages);
-      if (++asked < count) page = page_ahead();
+      if (++asked < count) look_up();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    const int g = at.unit / groups, skip = at.unit % groups * S::kHeads;
-    const int first_head = g * group + skip, heads = min(S::kHeads, group - skip);
+    const int first_head = at.kv * group + at.sub * S::kHeads, heads = min(S::kHeads, group - at.sub * S::kHeads);
     if (fresh) {
       load_queries<T, S>(a, at.row, first_head, heads, q);
       r.clear();
@@ -482,16 +553,15 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
     __syncwarp();
 
-    const bool ends = at.tile + 1 == at.tiles;
-    if (ends || j + 1 == count) {
+    if (at.tile + 1 == at.tiles || j + 1 == count) {
       // the warps' states together
-      const int64_t x0 = lo + j - at.tile, x1 = x0 + at.tiles - 1;
-      const int64_t w0 = ((x0 + 1) * blocks - 1) / total, w1 = ((x1 + 1) * blocks - 1) / total;
+      const int x0 = lo + j - at.tile, w0 = shares.owner(x0), w1 = shares.owner(x0 + at.tiles - 1);
       const bool whole = w0 == w1;
-      if (tid == 0 && (unsigned)at.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
-      const int id = 2 * (int)blockIdx.x + (lo > x0 ? 0 : 1);
+      constexpr int kD4 = S::DP / 4;
       const int slot_floats = S::kHeads * (D + 2);
-      float *mine_part = part + (int64_t)id * slot_floats;
+      float *mine_part = part + (int64_t)(2 * (int)blockIdx.x + (lo > x0 ? 0 : 1)) * slot_floats;
+      const int64_t first = (int64_t)at.row * a.q_heads + first_head;
+      if (tid == 0 && (unsigned)at.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
 #pragma unroll
       for (int nt = 0; nt < S::NT; ++nt) {
         __syncthreads();  // s_o may still be read
@@ -512,29 +582,27 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
           for (int e = 0; e < 4; ++e)
             s_o[(warp * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e];
         __syncthreads();
-        for (int h = 0; h < 8 && nt * 8 + h < heads; ++h) {
-          float M = -INFINITY, L = 0.0f, weight[S::kWarps];
+        for (int v = tid; v < 8 * kD4; v += S::kThreads) {
+          const int h = v / kD4, d = v % kD4 * 4;
+          if (nt * 8 + h >= heads || d >= D) continue;
+          float M = -INFINITY, L = 0.0f;
 #pragma unroll
           for (int w = 0; w < S::kWarps; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+          float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
           for (int w = 0; w < S::kWarps; ++w) {
-            weight[w] = part_weight(s_m[w * 8 + h], s_l[w * 8 + h], M);
-            L += weight[w] * s_l[w * 8 + h];
+            const float weight = part_weight(s_m[w * 8 + h], M);
+            L = fmaf(weight, s_l[w * 8 + h], L);
+            fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + d));
           }
-          const int64_t head = (int64_t)at.row * a.q_heads + first_head + nt * 8 + h;
-          for (int d = tid; d < D; d += S::kThreads) {
-            float x = 0.0f;
-#pragma unroll
-            for (int w = 0; w < S::kWarps; ++w) x += weight[w] * s_o[(w * 8 + h) * S::kRow + d];
-            if (whole) store(L == 0.0f ? 0.0f : x / L, (T *)a.out + head * D + d);
-            else mine_part[2 * S::kHeads + (nt * 8 + h) * D + d] = x;
-          }
-          if (tid == 0) {
-            if (!whole) {
+          if (whole) {
+            store(normalised(o, L), (T *)a.out + (first + nt * 8 + h) * D + d);
+            if (d == 0 && a.lse) a.lse[first + nt * 8 + h] = log_sum(M, L);
+          } else {
+            *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
+            if (d == 0) {
               mine_part[nt * 8 + h] = M;
               mine_part[S::kHeads + nt * 8 + h] = L;
-            } else if (a.lse) {
-              a.lse[head] = L == 0.0f ? -INFINITY : 0.6931471805599453094f * M + logf(L);
             }
           }
         }
@@ -542,42 +610,56 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       if (!whole) {
         __threadfence();
         __syncthreads();
-        int *seen = counter + (int64_t)at.row * units + at.unit;
-        if (tid == 0) s_last = atomicAdd(seen, 1) == (int)(w1 - w0);
+        int *seen = counter + (int64_t)at.row * units + at.kv * groups + at.sub;
+        if (tid == 0) s_last = atomicAdd(seen, 1) == w1 - w0;
         __syncthreads();
         if (s_last) {
           __threadfence();
-          for (int v = tid; v < heads * (D / 4); v += S::kThreads) {
-            const int h = v / (D / 4), d = v % (D / 4) * 4;
+          const auto part_of = [&](int w) { return part + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * slot_floats; };
+          for (int h = warp; h < heads; h += S::kWarps) {
             float M = -INFINITY, L = 0.0f;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int64_t w = w0; w <= w1; ++w) {
-              const float *p = part + (2 * w + (w == w0 ? 1 : 0)) * slot_floats;
-              const float m = __ldcg(p + h), l = __ldcg(p + S::kHeads + h);
-              const float4 x = __ldcg(reinterpret_cast<const float4 *>(p + 2 * S::kHeads + h * D + d));
-              const float N = fmaxf(M, m), keep = part_weight(M, L, N), weight = part_weight(m, l, N);
-              M = N;
-              L = L * keep + l * weight;
-              o.x = o.x * keep + x.x * weight;
-              o.y = o.y * keep + x.y * weight;
-              o.z = o.z * keep + x.z * weight;
-              o.w = o.w * keep + x.w * weight;
+            for (int w = w0 + lane; w <= w1; w += 32) M = fmaxf(M, __ldcg(part_of(w) + h));
+#pragma unroll
+            for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
+            for (int w = w0 + lane; w <= w1; w += 32)
+              L = fmaf(part_weight(__ldcg(part_of(w) + h), M), __ldcg(part_of(w) + S::kHeads + h), L);
+#pragma unroll
+            for (int d = 16; d; d >>= 1) L += __shfl_xor_sync(kAll, L, d);
+            if (lane == 0) {
+              s_m[h] = M;
+              s_l[h] = L;
+              if (a.lse) a.lse[first + h] = log_sum(M, L);
             }
-            const int64_t head = (int64_t)at.row * a.q_heads + first_head + h;
-            T *out = (T *)a.out + head * D + d;
-            const float f = L == 0.0f ? 0.0f : 1.0f / L;
-            store(o.x * f, out);
-            store(o.y * f, out + 1);
-            store(o.z * f, out + 2);
-            store(o.w * f, out + 3);
-            if (d == 0 && a.lse) a.lse[head] = L == 0.0f ? -INFINITY : 0.6931471805599453094f * M + logf(L);
           }
+          __syncthreads();
+          for (int v = tid; v < S::kHeads * kD4; v += S::kThreads) {
+            const int h = v / kD4, d = v % kD4 * 4;
+            if (h >= heads || d >= D) continue;
+            const float M = s_m[h];
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            constexpr int kBatch = 8;  // parts on their way at once
+            for (int w = w0; w <= w1; w += kBatch) {
+              float m[kBatch];
+              float4 x[kBatch];
+#pragma unroll
+              for (int u = 0; u < kBatch; ++u) {
+                const float *p = part_of(min(w + u, w1));
+                m[u] = w + u <= w1 ? __ldcg(p + h) : -INFINITY;
+                x[u] = __ldcg(reinterpret_cast<const float4 *>(p + 2 * S::kHeads + h * D + d));
+              }
+#pragma unroll
+              for (int u = 0; u < kBatch; ++u)
+                if (w + u <= w1) fma4(o, part_weight(m[u], M), x[u]);
+            }
+            store(normalised(o, s_l[h]), (T *)a.out + (first + h) * D + d);
+          }
+          __syncthreads();  // s_m and s_l are written at the next row's end
           if (tid == 0) *seen = 0;
         }
       }
       fresh = true;
     }
-    advance<TILE>(a, units, at);
+    advance<TILE>(a, groups, at);
   }
 }
 
@@ -598,8 +680,7 @@ template <typename T, int DP, int NT>
 cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   using S = Shape<T, DP, NT>;
   const int group = a.q_heads / a.c.n_kv_heads, groups = (group + S::kHeads - 1) / S::kHeads;
-  const int units = a.c.n_kv_heads * groups;
-  const unsigned blocks = attend_blocks<S>(a.c, a.n, units);
+  const unsigned blocks = attend_blocks<S>(a.c, a.n, a.c.n_kv_heads * groups);
   if (bytes) {
     *bytes = counters_bytes(a.n, a.q_heads) + (size_t)2 * blocks * S::kHeads * (a.c.head_dim + 2) * 4;
     return cudaSuccess;
@@ -607,7 +688,7 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
   const cudaError_t e = allow_smem((const void *)attend_kernel<T, S>, S::kSmem, S::kSmem);
   if (e != cudaSuccess) return e;
   attend_kernel<T, S><<<blocks, S::kThreads, S::kSmem, s>>>(
-      a, (int *)ws, (float *)((char *)ws + counters_bytes(a.n, a.q_heads)), units, groups);
+      a, (int *)ws, (float *)((char *)ws + counters_bytes(a.n, a.q_heads)), groups, Divisor(a.c.page_size));
   return cudaGetLastError();
 }
 
