@@ -548,9 +548,8 @@ int copes_cache_copy_pages(const copes_kv_cache *c, const int32_t *src, const in
  * The new token's own key and value are in the cache before the call (grow, append).  A slot
  * without tokens gives 0 and -inf, and so does an id outside the cache (bit 32).
  * Scores, softmax and sums are fp32, with every product of bf16 values exact.
- * workspace: copes_paged_attention_workspace_bytes(c, n, q_heads) bytes, 16-byte aligned,
- * all zero before its first use: a call leaves its counters zero again, so one buffer serves
- * any number of calls in one stream's order, of any sizes it is large enough for. */
+ * workspace: copes_paged_attention_workspace_bytes(c, n, q_heads) bytes, 16-byte aligned; its
+ * contents need not be kept or cleared, and calls may share it in one stream's order. */
 size_t copes_paged_attention_workspace_bytes(const copes_kv_cache *c, int n, int q_heads);
 int copes_paged_attention(const copes_kv_cache *c, int layer, const int32_t *slots, int n, const void *q,
                           int64_t q_row, int64_t q_head, int q_heads, float scale, void *out, float *lse,

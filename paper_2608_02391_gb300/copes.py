@@ -597,7 +597,7 @@ class KVCache:
         if self.workspace_bytes == 0:
             raise CopesError(ERR_INVALID_ARG, last_error())
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=pool.device)
-        self.attend_workspace = None  # paged_attention's: zero between calls
+        self.attend_workspace = None  # paged_attention's
         self._attend_bytes = {}       # (rows, query heads) -> bytes of it
 
     @classmethod
@@ -617,7 +617,7 @@ class KVCache:
         return t.data_ptr()
 
     def attend_space(self, n: int, q_heads: int, stream=None) -> Tuple[int, int]:
-        """paged_attention's workspace (address, bytes), allocated and zeroed where it has to grow."""
+        """paged_attention's workspace (address, bytes), allocated where it has to grow."""
         need = self._attend_bytes.get((n, q_heads))
         if need is None:
             need = load().copes_paged_attention_workspace_bytes(self.ref, n, q_heads)
@@ -629,8 +629,6 @@ class KVCache:
             if ws is not None and stream is not None:
                 ws.record_stream(stream)
             ws = self.attend_workspace = _empty((need,), torch.uint8, self.pool.device, stream)
-            with torch.cuda.stream(stream):
-                ws.zero_()
         return ws.data_ptr(), ws.numel()
 
 

@@ -10,8 +10,10 @@
 //
 // Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
 // are shared out evenly among as many blocks as the GPU runs at once, whatever the lengths are.
-// A (row, head group) whose tiles lie in several blocks is joined by the block that is done last
-// with its part, over the parts in order: the result does not depend on which that is.
+// A (row, head group) whose tiles lie in several blocks is joined, over the parts in order, by a
+// second kernel, which is on the GPU by the time the first ends (a dependent launch).  (Joined by
+// the last of its blocks, counted by an atomic, 60 parts of 16 heads took that block 25 us, and
+// few parts 3 us.)
 //
 // A tile.  Each warp keeps 16 of a tile's tokens to itself, from the copy into shared memory to
 // its own running maximum, sum and output, so that the warps need each other only at the end of
@@ -42,7 +44,11 @@ template <typename T, int DP_, int NT_>
 struct Shape {
   static constexpr bool kFp32 = sizeof(T) == 4;
   static constexpr int DP = DP_, NT = NT_;
-  static constexpr int kWarps = kFp32 ? 2 : 4;
+  // Warps of a block and tiles in shared memory, two or more of them on their way: what lets the
+  // most warps run on an SM.  (fp32 takes twice the room and three times the products, and wants
+  // warps more than tiles ahead.)
+  static constexpr int kWarps = !kFp32 ? 4 : DP <= 128 ? 2 : DP <= 192 ? 4 : 3;
+  static constexpr int kStages = kFp32 ? 2 : DP <= 96 ? 4 : 3;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kTile = kWarps * 16;               // tokens
   static constexpr int kChunks = DP * (int)sizeof(T) / 16;  // 16-byte pieces of a token's row
@@ -51,10 +57,11 @@ struct Shape {
   static constexpr int kHeads = 8 * NT;                   // query heads of a block at a time
   static constexpr int kRow = DP + 4;                     // row of s_o: heads 2j begin 8 banks apart
   static constexpr int kFixed = (kWarps * 8 * kRow + kWarps * 16) * 4;
-  // three tiles in flight or more where two blocks fit on an SM, else what one block can have
-  static constexpr int kStages = kStage <= 16384 ? 4 : 3;
   static constexpr int kSmem = kStages * kStage + kFixed;
-  static constexpr int kPerSm = kSmem <= 74 * 1024 ? 3 : kSmem <= 113 * 1024 ? 2 : 1;
+  // blocks of an SM by its 228 KB, 1 KB of them taken for each block, and by its registers
+  static constexpr int kFit = 228 * 1024 / (kSmem + 1280);
+  static constexpr int kByRegs = 65536 / (kThreads * (DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
+  static constexpr int kPerSm = kFit < kByRegs ? kFit : kByRegs;
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
 };
 
@@ -175,10 +182,11 @@ __device__ __forceinline__ void mma_split3(float (&c)[3][4], const uint32_t (&a)
 }
 
 // A 16-byte piece's place in a row of a tile is its number xor this, so that what one load
-// instruction reads lies in different banks.
-template <bool kFp32>
+// instruction reads lies in different banks.  (Rows of 4 pieces more than a multiple of 8 begin at
+// one of two places in the banks, by turns.)
+template <typename S>
 __device__ __forceinline__ int swizzle(int row) {
-  return kFp32 ? (row & 6) ^ ((row & 1) << 2) : row & 7;
+  return S::kFp32 ? (row & 6) ^ ((row & 1) << 2) : S::kChunks % 8 ? (row >> 1) & 3 : row & 7;
 }
 
 // Factor of a part with maximum m (of log2) in a whole with maximum M.  A part without weight has
@@ -252,7 +260,7 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
     float part[NT][kSums][3][4] = {};
     const int row = lane >> 2;
     const uint32_t at = keys + row * kPitch;
-    const int x = swizzle<true>(row);
+    const int x = swizzle<S>(row);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       const uint32_t off = (uint32_t)(((k * 4 + (lane & 3)) ^ x) * 16);
@@ -280,7 +288,7 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
       }
   } else {
     float part[NT][2][4] = {};
-    const int row = lane & 15, x = swizzle<false>(row);
+    const int row = lane & 15, x = swizzle<S>(row);
     const uint32_t at = keys + row * kPitch;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -349,9 +357,9 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
         const int piece = g * 8 + (lane >> 2);  // d = 32 g + 4 (lane / 4) + 0 .. 3
         uint32_t u[4], v[4];
         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                     : "r"(at + (uint32_t)((piece ^ swizzle<true>(row)) * 16)) : "memory");
+                     : "r"(at + (uint32_t)((piece ^ swizzle<S>(row)) * 16)) : "memory");
         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                     : "r"(at + kPitch + (uint32_t)((piece ^ swizzle<true>(row + 1)) * 16)) : "memory");
+                     : "r"(at + kPitch + (uint32_t)((piece ^ swizzle<S>(row + 1)) * 16)) : "memory");
         const uint32_t a0[4] = {u[0], u[1], v[0], v[1]}, a1[4] = {u[2], u[3], v[2], v[3]};
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -371,7 +379,7 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
         p[j][e] = transpose8(hi);
         rest[j][e] = transpose8(pack_bf16(u - __uint_as_float(hi << 16), v - __uint_as_float(hi & 0xFFFF0000u)));
       }
-    const int row = (lane & 7) + (lane >> 4) * 8, x = swizzle<false>(row);
+    const int row = (lane & 7) + (lane >> 4) * 8, x = swizzle<S>(row);
     const uint32_t at = values + row * kPitch;
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
@@ -424,20 +432,25 @@ struct Divisor {
   __device__ __forceinline__ int quotient(int t) const { return (int)(((uint64_t)(uint32_t)t * m) >> (31 + s)); }
 };
 
-// The workspace: counters of the joins (`counter`), one per row and head group, then the parts:
-// block w's at 2 w (of a row that begins before the block's share) and 2 w + 1 (of one that ends
-// after it), each kHeads maxima, kHeads sums and kHeads x head_dim values.
+// The workspace: a Split for every block, then the parts: block w's at 2 w (of a row that begins
+// before the block's share) and 2 w + 1 (of one that ends after it), each kHeads maxima, kHeads sums
+// and kHeads x head_dim values.
+struct Split {  // what begins in block w and goes on to block `last`; row -1: nothing
+  int row, kv, sub, last;
+};
+
 template <typename T, typename S>
-__global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendArgs a, int *counter, float *part,
+__global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendArgs a, Split *split, float *part,
                                                                         int groups, Divisor by_page) {
   extern __shared__ __align__(128) char smem[];
   __shared__ Cursor s_at;
-  __shared__ int s_sum[S::kWarps], s_last;
+  __shared__ int s_sum[S::kWarps];
   constexpr int TILE = S::kTile;
   const Cache &c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = c.head_dim;
   const int group = a.q_heads / c.n_kv_heads, units = c.n_kv_heads * groups;
 
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // the line's length and this block's share [lo, hi) of it
   const int rows = (a.n + S::kThreads - 1) / S::kThreads, r0 = min(a.n, tid * rows), r1 = min(a.n, r0 + rows);
   int mine = 0;
@@ -458,7 +471,10 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   }
   total *= units;
   const int blocks = min((int)gridDim.x, total);  // each has a tile at least
-  if (blockIdx.x >= blocks) return;
+  if (blockIdx.x >= blocks) {
+    if (tid == 0) split[blockIdx.x] = Split{-1, 0, 0, 0};
+    return;
+  }
   const Shares shares(total, blocks);
   const int lo = shares.begin(blockIdx.x), count = shares.begin(blockIdx.x + 1) - lo;
   before -= mine;
@@ -487,25 +503,30 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   const char *pool = c.pool + (uint64_t)a.layer * c.layer_elems * sizeof(T);
   const uint64_t head_bytes = (uint64_t)c.head_elems * sizeof(T), to_values = c.n_kv_heads * head_bytes;
 
-  // where token (16 warp + lane % 16) of the next tile to be asked for is: its page (-1 for none, -2 for
-  // one outside the pool) and its place there
-  int page, place;
+  // Where token (16 warp + lane % 16) of a tile is: its page (-1 for none, -2 for one outside the
+  // pool), its place there and the tile's key-value head.  Tables are read two tiles ahead of the
+  // tile that is asked for, so that nothing waits for them.
+  struct Place {
+    int page, place, kv;
+  };
+  int looked = 0;
   const auto look_up = [&]() {
+    Place p{-1, 0, ahead.kv};
+    if (looked == count) return p;
     const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
-    page = -1;
-    place = 0;
     if (t < ahead.tokens) {
       const int at_page = by_page.quotient(t);
-      place = t - at_page * c.page_size;
-      page = c.table[(int64_t)ahead.slot * c.table_width + at_page];
-      if ((unsigned)page >= (unsigned)c.n_pages) page = -2;
+      p.place = t - at_page * c.page_size;
+      p.page = c.table[(int64_t)ahead.slot * c.table_width + at_page];
+      if ((unsigned)p.page >= (unsigned)c.n_pages) p.page = -2;
     }
+    if (++looked < count) advance<TILE>(a, groups, ahead);
+    return p;
   };
-  look_up();
-  const auto ask = [&](int stage) {
+  const auto ask = [&](int stage, const Place &p) {
     const char *from = nullptr;
-    if (page >= 0) from = pool + (uint64_t)page * c.page_bytes + ahead.kv * head_bytes + (uint64_t)place * D * sizeof(T);
-    else if (page == -2) flag_error(kErrCacheId);
+    if (p.page >= 0) from = pool + (uint64_t)p.page * c.page_bytes + p.kv * head_bytes + (uint64_t)p.place * D * sizeof(T);
+    else if (p.page == -2) flag_error(kErrCacheId);
     const uint32_t to = stages + stage * S::kStage;
 #pragma unroll
     for (int i = 0; i < S::kChunks / 2; ++i) {
@@ -513,39 +534,45 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       const char *src = reinterpret_cast<const char *>(__shfl_sync(kAll, (unsigned long long)from, row));
       const int bytes = src && piece * 16 < D * (int)sizeof(T) ? 16 : 0;  // 0: zeros
       src = bytes ? src + piece * 16 : c.pool;
-      const uint32_t dst = to + (row * S::kChunks + (piece ^ swizzle<S::kFp32>(row))) * 16;
+      const uint32_t dst = to + (row * S::kChunks + (piece ^ swizzle<S>(row))) * 16;
       copy_async(dst, src, bytes);
       copy_async(dst + S::kPart, bytes ? src + to_values : src, bytes);
     }
-    advance<TILE>(a, groups, ahead);
   };
+  Place next = look_up();
+  Queries<S> q;
+  const auto queries_of = [&](const Cursor &x) {
+    load_queries<T, S>(a, x.row, x.kv * group + x.sub * S::kHeads, min(S::kHeads, group - x.sub * S::kHeads), q);
+  };
+  queries_of(at);
+  Place after = look_up();
 
   int asked = 0;
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s) {
     if (asked < count) {
-      ask(s);
-      if (++asked < count) look_up();
+      ask(s, next);
+      ++asked;
+      next = after;
+      after = look_up();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
 
   Running<S> r;
-  Queries<S> q;
+  r.clear();
   const float scale = a.scale * 1.44269504088896340736f;  // of log2
-  bool fresh = true;
+  constexpr int kD4 = S::DP / 4;
+  const int slot_floats = S::kHeads * (D + 2);
+  Split begun{-1, 0, 0, 0};
   for (int j = 0; j < count; ++j) {
     if (asked < count) {
-      ask(asked % S::kStages);
-      if (++asked < count) look_up();
+      ask(asked % S::kStages, next);
+      ++asked;
+      next = after;
+      after = look_up();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    const int first_head = at.kv * group + at.sub * S::kHeads, heads = min(S::kHeads, group - at.sub * S::kHeads);
-    if (fresh) {
-      load_queries<T, S>(a, at.row, first_head, heads, q);
-      r.clear();
-      fresh = false;
-    }
     asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
     __syncwarp();
     const int left = at.tokens - at.tile * TILE - warp * 16;
@@ -553,114 +580,137 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
     __syncwarp();
 
-    if (at.tile + 1 == at.tiles || j + 1 == count) {
-      // the warps' states together
-      const int x0 = lo + j - at.tile, w0 = shares.owner(x0), w1 = shares.owner(x0 + at.tiles - 1);
-      const bool whole = w0 == w1;
-      constexpr int kD4 = S::DP / 4;
-      const int slot_floats = S::kHeads * (D + 2);
-      float *mine_part = part + (int64_t)(2 * (int)blockIdx.x + (lo > x0 ? 0 : 1)) * slot_floats;
-      const int64_t first = (int64_t)at.row * a.q_heads + first_head;
-      if (tid == 0 && (unsigned)at.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
+    const Cursor was = at;
+    if (j + 1 < count) advance<TILE>(a, groups, at);
+    if (was.tile + 1 < was.tiles && j + 1 < count) continue;
+    if (j + 1 < count) queries_of(at);  // on their way during what follows
+
+    // the warps' states together
+    const int x0 = lo + j - was.tile, w0 = shares.owner(x0), w1 = shares.owner(x0 + was.tiles - 1);
+    const int first_head = was.kv * group + was.sub * S::kHeads, heads = min(S::kHeads, group - was.sub * S::kHeads);
+    const bool whole = w0 == w1;
+    float *mine_part = part + (int64_t)(2 * (int)blockIdx.x + (lo > x0 ? 0 : 1)) * slot_floats;
+    const int64_t first = (int64_t)was.row * a.q_heads + first_head;
+    if (tid == 0 && (unsigned)was.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
 #pragma unroll
-      for (int nt = 0; nt < S::NT; ++nt) {
-        __syncthreads();  // s_o may still be read
+    for (int nt = 0; nt < S::NT; ++nt) {
+      __syncthreads();  // s_o may still be read
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float l = r.l[nt][e];
-          l += __shfl_xor_sync(kAll, l, 4);
-          l += __shfl_xor_sync(kAll, l, 8);
-          l += __shfl_xor_sync(kAll, l, 16);
-          if (lane < 4) {
-            s_m[warp * 8 + lane * 2 + e] = r.m[nt][e];
-            s_l[warp * 8 + lane * 2 + e] = l;
-          }
+      for (int e = 0; e < 2; ++e) {
+        float l = r.l[nt][e];
+        l += __shfl_xor_sync(kAll, l, 4);
+        l += __shfl_xor_sync(kAll, l, 8);
+        l += __shfl_xor_sync(kAll, l, 16);
+        if (lane < 4) {
+          s_m[warp * 8 + lane * 2 + e] = r.m[nt][e];
+          s_l[warp * 8 + lane * 2 + e] = l;
         }
+      }
 #pragma unroll
-        for (int i = 0; i < S::DP / 16; ++i)
+      for (int i = 0; i < S::DP / 16; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            s_o[(warp * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e];
-        __syncthreads();
-        for (int v = tid; v < 8 * kD4; v += S::kThreads) {
-          const int h = v / kD4, d = v % kD4 * 4;
-          if (nt * 8 + h >= heads || d >= D) continue;
-          float M = -INFINITY, L = 0.0f;
+        for (int e = 0; e < 4; ++e)
+          s_o[(warp * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e];
+      __syncthreads();
+      for (int v = tid; v < 8 * kD4; v += S::kThreads) {
+        const int h = v / kD4, d = v % kD4 * 4;
+        if (nt * 8 + h >= heads || d >= D) continue;
+        float M = -INFINITY, L = 0.0f;
 #pragma unroll
-          for (int w = 0; w < S::kWarps; ++w) M = fmaxf(M, s_m[w * 8 + h]);
-          float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int w = 0; w < S::kWarps; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-          for (int w = 0; w < S::kWarps; ++w) {
-            const float weight = part_weight(s_m[w * 8 + h], M);
-            L = fmaf(weight, s_l[w * 8 + h], L);
-            fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + d));
-          }
-          if (whole) {
-            store(normalised(o, L), (T *)a.out + (first + nt * 8 + h) * D + d);
-            if (d == 0 && a.lse) a.lse[first + nt * 8 + h] = log_sum(M, L);
-          } else {
-            *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
-            if (d == 0) {
-              mine_part[nt * 8 + h] = M;
-              mine_part[S::kHeads + nt * 8 + h] = L;
-            }
+        for (int w = 0; w < S::kWarps; ++w) {
+          const float weight = part_weight(s_m[w * 8 + h], M);
+          L = fmaf(weight, s_l[w * 8 + h], L);
+          fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + d));
+        }
+        if (whole) {
+          store(normalised(o, L), (T *)a.out + (first + nt * 8 + h) * D + d);
+          if (d == 0 && a.lse) a.lse[first + nt * 8 + h] = log_sum(M, L);
+        } else {
+          *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
+          if (d == 0) {
+            mine_part[nt * 8 + h] = M;
+            mine_part[S::kHeads + nt * 8 + h] = L;
           }
         }
       }
-      if (!whole) {
-        __threadfence();
-        __syncthreads();
-        int *seen = counter + (int64_t)at.row * units + at.kv * groups + at.sub;
-        if (tid == 0) s_last = atomicAdd(seen, 1) == w1 - w0;
-        __syncthreads();
-        if (s_last) {
-          __threadfence();
-          const auto part_of = [&](int w) { return part + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * slot_floats; };
-          for (int h = warp; h < heads; h += S::kWarps) {
-            float M = -INFINITY, L = 0.0f;
-            for (int w = w0 + lane; w <= w1; w += 32) M = fmaxf(M, __ldcg(part_of(w) + h));
-#pragma unroll
-            for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
-            for (int w = w0 + lane; w <= w1; w += 32)
-              L = fmaf(part_weight(__ldcg(part_of(w) + h), M), __ldcg(part_of(w) + S::kHeads + h), L);
-#pragma unroll
-            for (int d = 16; d; d >>= 1) L += __shfl_xor_sync(kAll, L, d);
-            if (lane == 0) {
-              s_m[h] = M;
-              s_l[h] = L;
-              if (a.lse) a.lse[first + h] = log_sum(M, L);
-            }
-          }
-          __syncthreads();
-          for (int v = tid; v < S::kHeads * kD4; v += S::kThreads) {
-            const int h = v / kD4, d = v % kD4 * 4;
-            if (h >= heads || d >= D) continue;
-            const float M = s_m[h];
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            constexpr int kBatch = 8;  // parts on their way at once
-            for (int w = w0; w <= w1; w += kBatch) {
-              float m[kBatch];
-              float4 x[kBatch];
-#pragma unroll
-              for (int u = 0; u < kBatch; ++u) {
-                const float *p = part_of(min(w + u, w1));
-                m[u] = w + u <= w1 ? __ldcg(p + h) : -INFINITY;
-                x[u] = __ldcg(reinterpret_cast<const float4 *>(p + 2 * S::kHeads + h * D + d));
-              }
-#pragma unroll
-              for (int u = 0; u < kBatch; ++u)
-                if (w + u <= w1) fma4(o, part_weight(m[u], M), x[u]);
-            }
-            store(normalised(o, s_l[h]), (T *)a.out + (first + h) * D + d);
-          }
-          __syncthreads();  // s_m and s_l are written at the next row's end
-          if (tid == 0) *seen = 0;
-        }
-      }
-      fresh = true;
     }
-    advance<TILE>(a, groups, at);
+    if (!whole && lo <= x0) begun = Split{was.row, was.kv, was.sub, w1};
+    r.clear();
   }
+
+  if (tid == 0) split[blockIdx.x] = begun;
+}
+
+// Joins the parts of what begins in one block and goes on in others: `per` blocks for each block of
+// attend_kernel, one for a head (of the kheads that a part has room for).  Warps (pairs of them for more than 128 components) take the parts by turns.
+constexpr int kJoinThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(AttendArgs a, const Split *split, const float *part,
+                                                            int kheads, int per) {
+  __shared__ float4 s_o[kJoinThreads];
+  __shared__ float s_m[kJoinThreads / 32], s_l[kJoinThreads / 32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int w0 = blockIdx.x / per, h = blockIdx.x % per, D = a.c.head_dim;
+  const Split x = split[w0];
+  const int group = a.q_heads / a.c.n_kv_heads;
+  if (x.row < 0 || h >= min(kheads, group - x.sub * kheads)) return;
+  const int wide = D > 128 ? 64 : 32, groups = kJoinThreads / wide, mine = threadIdx.x / wide;
+  const int d = threadIdx.x % wide * 4, slot_floats = kheads * (D + 2);
+  float M = -INFINITY, L = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kBatch = 8;  // parts on their way at once
+  for (int w = w0 + mine; w <= x.last; w += groups * kBatch) {
+    float m[kBatch], l[kBatch];
+    float4 y[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int from = w + u * groups;
+      m[u] = -INFINITY;
+      l[u] = 0.0f;
+      y[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (from <= x.last) {
+        const float *p = part + (int64_t)(2 * from + (from == w0 ? 1 : 0)) * slot_floats;
+        m[u] = p[h];
+        l[u] = p[kheads + h];
+        if (d < D) y[u] = *reinterpret_cast<const float4 *>(p + 2 * kheads + h * D + d);
+      }
+    }
+    float N = M;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) N = fmaxf(N, m[u]);
+    const float keep = part_weight(M, N);
+    L *= keep;
+    o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const float weight = part_weight(m[u], N);
+      L = fmaf(weight, l[u], L);
+      fma4(o, weight, y[u]);
+    }
+    M = N;
+  }
+  s_o[threadIdx.x] = o;
+  if (threadIdx.x % wide == 0) {
+    s_m[mine] = M;
+    s_l[mine] = L;
+  }
+  __syncthreads();
+  if (threadIdx.x >= wide || d >= D) return;
+  M = -INFINITY;
+  L = 0.0f;
+  o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int g = 0; g < groups; ++g) M = fmaxf(M, s_m[g]);
+  for (int g = 0; g < groups; ++g) {
+    const float weight = part_weight(s_m[g], M);
+    L = fmaf(weight, s_l[g], L);
+    fma4(o, weight, s_o[g * wide + threadIdx.x]);
+  }
+  const int64_t head = (int64_t)x.row * a.q_heads + x.kv * group + x.sub * kheads + h;
+  store(normalised(o, L), (T *)a.out + head * D + d);
+  if (d == 0 && a.lse) a.lse[head] = log_sum(M, L);
 }
 
 namespace {
@@ -674,22 +724,33 @@ unsigned attend_blocks(const Cache &c, int n, int units) {
   return (unsigned)(most < run ? most : run);
 }
 
-size_t counters_bytes(int n, int q_heads) { return ((size_t)n * q_heads * 4 + 15) / 16 * 16; }
-
 template <typename T, int DP, int NT>
 cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   using S = Shape<T, DP, NT>;
   const int group = a.q_heads / a.c.n_kv_heads, groups = (group + S::kHeads - 1) / S::kHeads;
   const unsigned blocks = attend_blocks<S>(a.c, a.n, a.c.n_kv_heads * groups);
   if (bytes) {
-    *bytes = counters_bytes(a.n, a.q_heads) + (size_t)2 * blocks * S::kHeads * (a.c.head_dim + 2) * 4;
+    *bytes = blocks * sizeof(Split) + (size_t)2 * blocks * S::kHeads * (a.c.head_dim + 2) * 4;
     return cudaSuccess;
   }
-  const cudaError_t e = allow_smem((const void *)attend_kernel<T, S>, S::kSmem, S::kSmem);
+  cudaError_t e = allow_smem((const void *)attend_kernel<T, S>, S::kSmem, S::kSmem);
   if (e != cudaSuccess) return e;
-  attend_kernel<T, S><<<blocks, S::kThreads, S::kSmem, s>>>(
-      a, (int *)ws, (float *)((char *)ws + counters_bytes(a.n, a.q_heads)), groups, Divisor(a.c.page_size));
-  return cudaGetLastError();
+  Split *split = (Split *)ws;
+  float *part = (float *)(split + blocks);
+  attend_kernel<T, S><<<blocks, S::kThreads, S::kSmem, s>>>(a, split, part, groups, Divisor(a.c.page_size));
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  if ((int64_t)a.c.table_width * a.c.page_size <= S::kTile) return cudaSuccess;  // a row is one tile
+  cudaLaunchConfig_t cfg{};
+  const int per = S::kHeads < group ? S::kHeads : group;
+  cfg.gridDim = dim3(blocks * per);
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, join_kernel<T>, a, (const Split *)split, (const float *)part, S::kHeads, per);
 }
 
 // Up to 8 query heads of a key-value head at a time, or 16 where it has more (each further group
@@ -699,7 +760,9 @@ template <typename T>
 cudaError_t by_shape(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   const bool many = a.q_heads / a.c.n_kv_heads > 8;
   if (a.c.head_dim <= 64) return many ? launch<T, 64, 2>(a, ws, s, bytes) : launch<T, 64, 1>(a, ws, s, bytes);
+  if (a.c.head_dim <= 96) return many ? launch<T, 96, 2>(a, ws, s, bytes) : launch<T, 96, 1>(a, ws, s, bytes);
   if (a.c.head_dim <= 128) return many ? launch<T, 128, 2>(a, ws, s, bytes) : launch<T, 128, 1>(a, ws, s, bytes);
+  if (a.c.head_dim <= 192) return launch<T, 192, 1>(a, ws, s, bytes);
   return launch<T, 256, 1>(a, ws, s, bytes);
 }
 

@@ -263,7 +263,6 @@ def test_attention_split_over_long_and_many_sequences(copes, n, longest, heads, 
     for _ in range(3):  # joined in one order: the same bits again, on the same workspace
         again = copes.paged_attention(cache, 0, q)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
-    assert not cache.attend_workspace[:4 * n * heads].any() if cache.attend_workspace.numel() > 4 * n * heads else True
     assert error_bits(copes) == 0
 
 
