@@ -10,6 +10,9 @@
 //
 // Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
 // are shared out evenly among as many blocks as the GPU runs at once, whatever the lengths are.
+// The end of a (row, head group) costs about a tile's time and counts as a step of the line, too
+// (not where every tile has a block of its own): 32 rows of up to 4,096 tokens took 61 us without
+// it, a block with many short rows 67 us where the others took 39.
 // A (row, head group) whose tiles lie in several blocks is joined, over the parts in order, by a
 // second kernel, which is on the GPU by the time the first ends (a dependent launch).  (Joined by
 // the last of its blocks, counted by an atomic, 60 parts of 16 heads took that block 25 us, and
@@ -69,7 +72,7 @@ struct Shape {
 // by group, tile by tile.
 struct Cursor {
   int row, slot, tokens, tiles;  // of the row
-  int kv, sub, tile;
+  int kv, sub, tile;  // tile == tiles: the step that stands for the end
 };
 
 __device__ __forceinline__ int row_slot(const AttendArgs &a, int row) { return a.slots ? a.slots[row] : row; }
@@ -85,8 +88,8 @@ __device__ __forceinline__ int row_tiles(int tokens) {
 }
 
 template <int kTile>
-__device__ __forceinline__ void advance(const AttendArgs &a, int groups, Cursor &c) {
-  if (++c.tile < c.tiles) return;
+__device__ __forceinline__ void advance(const AttendArgs &a, int groups, int ends, Cursor &c) {
+  if (++c.tile < c.tiles + ends) return;
   c.tile = 0;
   if (++c.sub < groups) return;
   c.sub = 0;
@@ -98,7 +101,7 @@ __device__ __forceinline__ void advance(const AttendArgs &a, int groups, Cursor 
   c.tiles = row_tiles<kTile>(c.tokens);
 }
 
-// The line shared out: each block has `each` tiles, the first `more` of them one more.
+// The line shared out: each block has `each` steps, the first `more` of them one more.
 struct Shares {
   int each, more;
   __device__ Shares(int total, int blocks) : each(total / blocks), more(total % blocks) {}
@@ -469,15 +472,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if (w < warp) before += s_sum[w];
     total += s_sum[w];
   }
-  total *= units;
-  const int blocks = min((int)gridDim.x, total);  // each has a tile at least
+  const int ends = total * units > (int)gridDim.x;  // 1: an end is a step
+  before += r0 * ends - mine;
+  mine += (r1 - r0) * ends;
+  total = (total + a.n * ends) * units;
+  const int blocks = min((int)gridDim.x, total);  // each has a step at least
   if (blockIdx.x >= blocks) {
     if (tid == 0) split[blockIdx.x] = Split{-1, 0, 0, 0};
     return;
   }
   const Shares shares(total, blocks);
   const int lo = shares.begin(blockIdx.x), count = shares.begin(blockIdx.x + 1) - lo;
-  before -= mine;
   if (before * units <= lo && lo < (before + mine) * units) {
     Cursor at;
     at.row = r0;
@@ -485,11 +490,11 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       at.slot = row_slot(a, at.row);
       at.tokens = row_tokens(a, at.slot);
       at.tiles = row_tiles<TILE>(at.tokens);
-      if (at.row + 1 >= r1 || lo < (before + at.tiles) * units) break;
-      before += at.tiles;
+      if (at.row + 1 >= r1 || lo < (before + at.tiles + ends) * units) break;
+      before += at.tiles + ends;
     }
-    const int unit = (lo - before * units) / at.tiles;
-    at.tile = (lo - before * units) % at.tiles;
+    const int unit = (lo - before * units) / (at.tiles + ends);
+    at.tile = (lo - before * units) % (at.tiles + ends);
     at.kv = unit / groups;
     at.sub = unit % groups;
     s_at = at;
@@ -514,16 +519,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     Place p{-1, 0, ahead.kv};
     if (looked == count) return p;
     const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
-    if (t < ahead.tokens) {
+    if (ahead.tile < ahead.tiles && t < ahead.tokens) {
       const int at_page = by_page.quotient(t);
       p.place = t - at_page * c.page_size;
       p.page = c.table[(int64_t)ahead.slot * c.table_width + at_page];
       if ((unsigned)p.page >= (unsigned)c.n_pages) p.page = -2;
     }
-    if (++looked < count) advance<TILE>(a, groups, ahead);
+    if (++looked < count) advance<TILE>(a, groups, ends, ahead);
     return p;
   };
   const auto ask = [&](int stage, const Place &p) {
+    if (!__any_sync(kAll, p.page != -1)) return;  // nothing of this warp's is read
     const char *from = nullptr;
     if (p.page >= 0) from = pool + (uint64_t)p.page * c.page_bytes + p.kv * head_bytes + (uint64_t)p.place * D * sizeof(T);
     else if (p.page == -2) flag_error(kErrCacheId);
@@ -541,10 +547,14 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   };
   Place next = look_up();
   Queries<S> q;
-  const auto queries_of = [&](const Cursor &x) {
+  const auto queries_of = [&](Cursor x, int steps) {  // of the first tile of the next `steps` steps, from x on
+    if (x.tile == x.tiles) {
+      if (steps < 2) return;
+      advance<TILE>(a, groups, ends, x);
+    }
     load_queries<T, S>(a, x.row, x.kv * group + x.sub * S::kHeads, min(S::kHeads, group - x.sub * S::kHeads), q);
   };
-  queries_of(at);
+  queries_of(at, count);
   Place after = look_up();
 
   int asked = 0;
@@ -575,15 +585,15 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     asm volatile("cp.async.commit_group;" ::: "memory");
     asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
     __syncwarp();
-    const int left = at.tokens - at.tile * TILE - warp * 16;
+    const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - warp * 16 : 0;
     const uint32_t tile = stages + j % S::kStages * S::kStage;
     if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
     __syncwarp();
 
     const Cursor was = at;
-    if (j + 1 < count) advance<TILE>(a, groups, at);
-    if (was.tile + 1 < was.tiles && j + 1 < count) continue;
-    if (j + 1 < count) queries_of(at);  // on their way during what follows
+    if (j + 1 < count) advance<TILE>(a, groups, ends, at);
+    if (was.tile == was.tiles || (was.tile + 1 < was.tiles && j + 1 < count)) continue;
+    if (j + 1 < count) queries_of(at, count - j - 1);  // on their way during what follows
 
     // the warps' states together
     const int x0 = lo + j - was.tile, w0 = shares.owner(x0), w1 = shares.owner(x0 + was.tiles - 1);
