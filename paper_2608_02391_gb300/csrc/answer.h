@@ -27,11 +27,15 @@ __device__ __forceinline__ int slot_tokens(const Cache &c, int slot) {
   return len < 0 ? 0 : (len < most ? len : most);
 }
 
-// Workspace of the page plans, in int32: a header (kPlan...), per listed slot its first new
-// page's rank and its new page, per slot a mark, and three lists of up to n_pages ids.
+// Workspace of the page plans, in int32: a header (kPlan...), by listed slot the rank of its first new
+// page, by slot its place in the list, and two lists of pages.
 enum { kPlanDone = 0, kPlanTotal = 1, kPlanHeader = 4 };
 inline size_t cache_workspace_ints(int n_pages, int n_slots) {
   return (size_t)kPlanHeader + 2 * (size_t)n_slots + 2 * (size_t)n_pages;
+}
+template <typename Int>
+__device__ __forceinline__ Int *plan_pages(const Cache &c, Int *ws) {
+  return ws + kPlanHeader + 2 * (size_t)c.n_slots;
 }
 
 cudaError_t launch_cache_grow(const Cache &c, const int32_t *slots, int n, const int32_t *add, int add_all,
