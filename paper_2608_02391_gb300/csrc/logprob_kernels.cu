@@ -31,7 +31,9 @@ static std::atomic<bool> g_used{false};
 __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_logprob_error, bit); }
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kMostThreads = 256, kMostWarps = kMostThreads / 32, kPerSm = 4;
+constexpr int kMostThreads = 256, kMostWarps = kMostThreads / 32;
+// blocks of an SM: with a thread's next step on its way (shallow), or the next two (deep)
+constexpr int per_sm(bool deep) { return deep ? 3 : 4; }
 constexpr int kCells = 8192;       // of a block, at most
 constexpr int kReached = 1024;     // cells read again by the fast way, at most
 constexpr int kCandidates = 512;   // logits ranked by counting, at most
@@ -430,8 +432,8 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
 // rows on reads, whose turn is near, into L2, so that HBM is not idle meanwhile.
 constexpr int kAhead = 48 << 10;
 
-template <typename T, bool kTop>
-__global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobArgs a, int parts, int merge, int apart) {
+template <typename T, bool kTop, bool kDeep>
+__global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(LogprobArgs a, int parts, int merge, int apart) {
   extern __shared__ float cell[];
   __shared__ LogprobShared sh;
   constexpr int N = Piece<T>::kN;
@@ -451,7 +453,7 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
   Sums t{-FLT_MAX, 0.0f, 0.0f};
   float own[2] = {-INFINITY, -INFINITY};
   uint64_t s2 = 0, h2 = 0;
-  Piece<T> now[kLoads], next[kLoads];
+  Piece<T> now[kLoads], next[kLoads], then[kDeep ? kLoads : 1];
   const auto fetch = [&](int base, Piece<T>(&to)[kLoads]) {
     if (base >= full0 && base + kStep <= full1) {
 #pragma unroll
@@ -470,13 +472,19 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
     }
   };
   if (warp * kStep < n) fetch(warp * kStep, now);
+  if constexpr (kDeep)
+    if (warp * kStep + stride < n) fetch(warp * kStep + stride, next);
   if (kTop) {
     if (tid < COPES_MAX_TOP) sh.top[tid] = 0;
     if (tid == 0) sh.n_reached = sh.n_candidates = 0;
   }
   int step = 0;
   for (int base = warp * kStep; base < n; base += stride, ++step) {
-    if (base + stride < n) fetch(base + stride, next);
+    if constexpr (kDeep) {
+      if (base + 2 * stride < n) fetch(base + 2 * stride, then);
+    } else {
+      if (base + stride < n) fetch(base + stride, next);
+    }
     const float half[2] = {max_nan(max_of(now[0]), max_of(now[1])), max_nan(max_of(now[2]), max_of(now[3]))};
     const float most = max_nan(half[0], half[1]);
     if (kTop) {
@@ -512,13 +520,16 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
         h2 = fma2(p, pack2(x, y), h2);
       }
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) now[u] = next[u];
+    for (int u = 0; u < kLoads; ++u) {
+      now[u] = next[u];
+      if constexpr (kDeep) next[u] = then[u];
+    }
   }
   if (tid == 0 && i + apart < a.n) {
-    const Row<T> then((const T *)a.logits + (i + apart) * a.row, a.vocab);
-    const int v = max((int)((int64_t)then.pieces() * part / parts), then.first_full());
-    const int bytes = min(min(n, then.end_full() - v), kAhead / 16) * 16;
-    if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(then.at(v)), "r"(bytes) : "memory");
+    const Row<T> later((const T *)a.logits + (i + apart) * a.row, a.vocab);
+    const int v = max((int)((int64_t)later.pieces() * part / parts), later.first_full());
+    const int bytes = min(min(n, later.end_full() - v), kAhead / 16) * 16;
+    if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(later.at(v)), "r"(bytes) : "memory");
   }
   if (kTop) {  // a thread's steps past its last hold nothing
     const int steps = (n + stride - 1) / stride, cells = (steps + (1 << merge) - 1) >> merge;
@@ -579,51 +590,67 @@ __global__ void __launch_bounds__(kMostThreads, kPerSm) logprob_kernel(LogprobAr
   }
 }
 
-template <typename T, bool kTop>
-static cudaError_t launch(const LogprobArgs &a, cudaStream_t s) {
-  const int64_t pieces = (int64_t)a.vocab / Piece<T>::kN + 2;
-  // Parts of a row: the waves of blocks over the GPU times a part's pieces, and what a block costs
-  // besides, about 2,000 pieces' time on a full GPU.  734 rows of 18,992 pieces: 71 us as two waves
-  // of whole rows, TODO us as rows in four.
-  const int64_t slots = 152 * kPerSm;
-  int parts = 1;
-  int64_t best = INT64_MAX;
-  for (int p = 1; p <= kClusterMost && (p == 1 || pieces / p >= 256); p *= 2) {
-    const int64_t waves = ((int64_t)a.n * p + slots - 1) / slots, cost = waves * (pieces / p + 2000);
-    if (cost < best) {
-      best = cost;
-      parts = p;
-    }
-  }
-  int threads = 32;
-  while (threads < kMostThreads && pieces / parts >= threads * 2 * kLoads) threads *= 2;
-  const int64_t steps = (pieces / parts + 1 + threads * kLoads - 1) / (threads * kLoads);
-  int merge = 0;
-  while ((((steps + (1 << merge) - 1) >> merge) * threads) > kCells) ++merge;
-  const uint32_t bytes = kTop ? (uint32_t)((steps + (1 << merge) - 1) >> merge) * threads * 4 : 0;
-  const uint32_t fixed = sizeof(LogprobShared);
-  const cudaError_t e = allow_smem((const void *)logprob_kernel<T, kTop>, bytes + fixed, kCells * 4);
+// How a call is cut: blocks of a row, threads of a block, steps that share a cell.
+struct Cut {
+  int parts, threads, merge, apart;
+  uint32_t cell_bytes;
+};
+
+// Parts of a row: as many as leave at most 400 blocks, two or three of an SM, and each 256 pieces.
+// us for rows of 151,936 bf16 logits with 5 alternatives in 1, 2, 4 and 8 parts: 38 rows 15.1, 12.1,
+// 10.7, 10.3; 120 rows 18.4, 15.8, 20.6, 26.1; 300 rows 23.5, 32.1, 35.2, 53.2.
+// Threads: a step for each at least.
+static Cut cut_of(int64_t n, int64_t pieces, bool deep) {
+  Cut c{1, 32, 0, 0, 0};
+  while (c.parts < kClusterMost && n * c.parts * 2 <= 400 && pieces / (c.parts * 2) >= 256) c.parts *= 2;
+  const int64_t mine = pieces / c.parts + 1;
+  while (c.threads < kMostThreads && mine > c.threads * 2 * kLoads) c.threads *= 2;
+  const int64_t steps = (mine + c.threads * kLoads - 1) / (c.threads * kLoads);
+  while (((steps + (1 << c.merge) - 1) >> c.merge) * c.threads > kCells) ++c.merge;
+  c.cell_bytes = (uint32_t)((steps + (1 << c.merge) - 1) >> c.merge) * c.threads * 4;
+  c.apart = 152 * per_sm(deep) * kMostThreads / c.threads / c.parts;  // rows at a time
+  return c;
+}
+
+template <typename T, bool kTop, bool kDeep>
+static cudaError_t launch(const LogprobArgs &a, const Cut &c, cudaStream_t s) {
+  const auto kernel = logprob_kernel<T, kTop, kDeep>;
+  const uint32_t bytes = kTop ? c.cell_bytes : 0, fixed = sizeof(LogprobShared);
+  const cudaError_t e = allow_smem((const void *)kernel, bytes + fixed, kCells * 4);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  const int apart = (int)(slots * kMostThreads / threads / parts);  // rows at a time
-  cfg.gridDim = dim3((unsigned)a.n * parts);
-  cfg.blockDim = dim3(threads);
+  cfg.gridDim = dim3((unsigned)a.n * c.parts);
+  cfg.blockDim = dim3(c.threads);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = parts;
+  attr.val.clusterDim.x = c.parts;
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
-  cfg.numAttrs = parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop>, a, parts, merge, apart);
+  cfg.numAttrs = c.parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, a, c.parts, c.merge, c.apart);
+}
+
+// Three blocks of an SM with two steps on their way where a thread has three steps or more, else
+// four blocks with one: 301 rows of 32,003 fp32 logits take 12.3 us deep and 13.2 shallow, 4,096 rows
+// of 7,500 bf16 logits (two steps) 37 and 32.  Four blocks, too, where their last wave is so much
+// fuller: 500 rows of 151,936 in one wave 38 us, in two of three blocks 45 (734 rows: 58 and 47).
+template <typename T, bool kTop>
+static cudaError_t launch_any(const LogprobArgs &a, cudaStream_t s) {
+  const int64_t pieces = (int64_t)a.vocab / Piece<T>::kN + 2;
+  const Cut deep = cut_of(a.n, pieces, true);
+  const auto paid = [&](int64_t at_once) { return (a.n * (int64_t)deep.parts + at_once - 1) / at_once * at_once; };
+  if (pieces / deep.parts >= 3 * deep.threads * kLoads && paid(152 * per_sm(true)) * 20 <= paid(152 * per_sm(false)) * 23)
+    return launch<T, kTop, true>(a, deep, s);
+  return launch<T, kTop, false>(a, cut_of(a.n, pieces, false), s);
 }
 
 cudaError_t launch_token_logprobs(int dtype, const LogprobArgs &a, cudaStream_t s) {
   if (a.n == 0) return cudaSuccess;
   g_used = true;
-  if (dtype == COPES_BF16) return a.top ? launch<__nv_bfloat16, true>(a, s) : launch<__nv_bfloat16, false>(a, s);
-  return a.top ? launch<float, true>(a, s) : launch<float, false>(a, s);
+  if (dtype == COPES_BF16) return a.top ? launch_any<__nv_bfloat16, true>(a, s) : launch_any<__nv_bfloat16, false>(a, s);
+  return a.top ? launch_any<float, true>(a, s) : launch_any<float, false>(a, s);
 }
 
 unsigned read_and_clear_logprob_errors() {
