@@ -547,7 +547,9 @@ int copes_cache_copy_pages(const copes_kv_cache *c, const int32_t *src, const in
  *   lse[i][h] = ln sum_t exp(s_t)        (fp32 [n][q_heads], or NULL).
  * The new token's own key and value are in the cache before the call (grow, append).  A slot
  * without tokens gives 0 and -inf, and so does an id outside the cache (bit 32).
- * Scores, softmax and sums are fp32, with every product of bf16 values exact.
+ * Scores, softmax and sums are fp32, with every product of bf16 values exact and fp32 values as
+ * two terms of 11 bits.  An infinity or NaN among a slot's keys and values makes what it
+ * reaches infinite or NaN; what lies past the slot's length is not read.
  * workspace: copes_paged_attention_workspace_bytes(c, n, q_heads) bytes, 16-byte aligned; its
  * contents need not be kept or cleared, and calls may share it in one stream's order. */
 size_t copes_paged_attention_workspace_bytes(const copes_kv_cache *c, int n, int q_heads);

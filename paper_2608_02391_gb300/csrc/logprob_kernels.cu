@@ -266,17 +266,28 @@ __device__ __forceinline__ void visit_piece(const Row<T> &row, int v, int least,
 // listed.  Where most of them equal it (masked tokens, with fewer than k others): those that surpass
 // it and, in the order of the indices, the first that equal it.  Else one after the other.
 template <typename T>
-__device__ __noinline__ void find_top_slowly(LogprobShared &sh, const Row<T> &row, int v0, int n, int bound, int k) {
+__device__ __noinline__ void find_top_slowly(LogprobShared &sh, const float *cell, const Row<T> &row, int v0, int n,
+                                             int merge, int bound, int k) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  // visits the thread's own logits of order `least` and above, by its cells' maxima
+  const auto each = [&](int least, auto visit) {
+    const int steps = (n + kStep * warps - 1) / (kStep * warps);
+    for (int step = 0; step < steps; ++step) {
+      if (order_of(cell[(step >> merge) * blockDim.x + tid]) < least) continue;
+      for (int u = 0; u < kLoads; ++u) {
+        const int v = ((step * warps + warp) * kLoads + u) * 32 + lane;
+        if (v < n) visit_piece(row, v0 + v, least, visit);
+      }
+    }
+  };
   __syncthreads();
   if (tid == 0) sh.n_candidates = 0;
   __syncthreads();
   if (bound != 0x7FFFFFFF)
-    for (int v = tid; v < n; v += blockDim.x)
-      visit_piece(row, v0 + v, bound + 1, [&](int order, uint32_t index) {
-        const int at = atomicAdd(&sh.n_candidates, 1);
-        if (at < kCandidates) sh.candidate[at] = ranked(order, index);
-      });
+    each(bound + 1, [&](int order, uint32_t index) {
+      const int at = atomicAdd(&sh.n_candidates, 1);
+      if (at < kCandidates) sh.candidate[at] = ranked(order, index);
+    });
   __syncthreads();
   const int above = sh.n_candidates;
   if (above <= kCandidates - COPES_MAX_TOP) {
@@ -308,11 +319,10 @@ __device__ __noinline__ void find_top_slowly(LogprobShared &sh, const Row<T> &ro
   uint64_t last = ~0ull;
   for (int r = 0; r < k; ++r) {
     uint64_t next = 0;
-    for (int v = tid; v < n; v += blockDim.x)
-      visit_piece(row, v0 + v, bound, [&](int order, uint32_t index) {
-        const uint64_t key = ranked(order, index);
-        if (key < last && key > next) next = key;
-      });
+    each(bound, [&](int order, uint32_t index) {
+      const uint64_t key = ranked(order, index);
+      if (key < last && key > next) next = key;
+    });
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
       const uint64_t y = __shfl_xor_sync(kAll, next, d);
@@ -424,7 +434,7 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
       __syncthreads();
     }
   }
-  if (!listed) find_top_slowly(sh, row, v0, n, bound, k);
+  if (!listed) find_top_slowly(sh, cell, row, v0, n, merge, bound, k);
 }
 
 // A block, or a cluster of `parts` blocks, per row; a cell is 2^merge steps of a thread.  Before it
