@@ -10,6 +10,12 @@
 
 namespace copes {
 
+// Further device error bits (the first five are in copes_internal.h).
+enum : unsigned {
+  kErrCacheId = 32u,   // a slot, page, token or target id outside its range, or named twice
+  kErrCacheFull = 64u  // more pages asked for than are free
+};
+
 // A copes_kv_cache as the kernels take it.
 struct Cache {
   char *pool;
@@ -73,5 +79,11 @@ struct LogprobArgs {
   float *top_logprobs;
 };
 cudaError_t launch_token_logprobs(int dtype, const LogprobArgs &a, cudaStream_t s);
+
+// Device error words of each translation unit: read and clear (synchronous); 0 without a copy
+// where none of its kernels was launched.
+unsigned read_and_clear_cache_errors();
+unsigned read_and_clear_attend_errors();
+unsigned read_and_clear_logprob_errors();
 
 }  // namespace copes

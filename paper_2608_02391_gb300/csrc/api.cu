@@ -12,6 +12,7 @@
 #include <utility>
 #include <vector>
 
+#include "answer.h"
 #include "copes_internal.h"
 
 using copes::ElemArgs;

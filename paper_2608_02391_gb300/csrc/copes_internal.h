@@ -201,9 +201,7 @@ enum : unsigned {
   kErrIndexRange = 2u,  // a gather index outside [0, n_alloc)
   kErrPartition = 4u,   // a partition kernel met an inconsistent workspace
   kErrStageTimeout = 8u, // a bulk-copy wait ran past its iteration limit
-  kErrPartnerRange = 16u, // an element outside the partner buffer's range
-  kErrCacheId = 32u,     // a slot, page, token or target id outside its range, or named twice
-  kErrCacheFull = 64u    // more pages asked for than are free
+  kErrPartnerRange = 16u // an element outside the partner buffer's range
 };
 
 // ---------------------------------------------------------------- launch arguments
@@ -394,8 +392,5 @@ unsigned read_and_clear_ragged_errors();
 unsigned read_and_clear_partition_errors();
 unsigned read_and_clear_replay_errors();
 unsigned read_and_clear_backup_errors();
-unsigned read_and_clear_cache_errors();
-unsigned read_and_clear_attend_errors();
-unsigned read_and_clear_logprob_errors();
 
 }  // namespace copes
