@@ -29,6 +29,13 @@ bool overlaps(const void *a, uint64_t na, const void *b, uint64_t nb) {
   return a && b && na && nb && x < y + nb && y < x + na;
 }
 
+// Bytes from the first to past the last element of rows of heads of `count` elements; 0 (never an
+// overlap) where a stride is negative.
+uint64_t extent(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t count, int elem) {
+  if (rows < 1 || heads < 1 || row < 0 || head < 0) return 0;
+  return ((uint64_t)(rows - 1) * row + (uint64_t)(heads - 1) * head + count) * elem;
+}
+
 int elem_size(int dtype) { return dtype == COPES_BF16 ? 2 : 4; }
 
 uint64_t pool_bytes(const copes::Cache &c) { return (uint64_t)c.n_pages * c.page_bytes; }
@@ -135,6 +142,10 @@ int copes_cache_append(const copes_kv_cache *p, int layer, const int32_t *slots,
   if (n && (!k || !v)) return fail(COPES_ERR_INVALID_ARG, "%s: k or v is NULL", who);
   if (!aligned(k, c.elem) || !aligned(v, c.elem))
     return fail(COPES_ERR_ALIGNMENT, "%s: k and v must be aligned to their type", who);
+  if ((int64_t)n * c.n_kv_heads > 0x7FFFFFFF) return fail(COPES_ERR_SIZE, "%s: more than 2^31-1 rows of heads", who);
+  if (overlaps(k, extent(n, k_row, c.n_kv_heads, k_head, c.head_dim, c.elem), c.pool, pool_bytes(c)) ||
+      overlaps(v, extent(n, v_row, c.n_kv_heads, v_head, c.head_dim, c.elem), c.pool, pool_bytes(c)))
+    return fail(COPES_ERR_INVALID_ARG, "%s: k, v and the pool must be disjoint", who);
   return launch_status(copes::launch_cache_append(c, layer, slots, position, n, k, k_row, k_head, v, v_row, v_head,
                                                   stream), who);
 }
@@ -216,8 +227,10 @@ int copes_paged_attention(const copes_kv_cache *p, int layer, const int32_t *slo
     return fail(COPES_ERR_ALIGNMENT, "%s: out must be 16-byte aligned, q and lse to their type", who);
   const uint64_t rows = (uint64_t)n * q_heads, out_bytes = rows * c.head_dim * c.elem;
   if (overlaps(out, out_bytes, c.pool, pool_bytes(c)) || overlaps(lse, rows * 4, c.pool, pool_bytes(c)) ||
-      overlaps(out, out_bytes, lse, rows * 4))
-    return fail(COPES_ERR_INVALID_ARG, "%s: out, lse and the cache must be disjoint", who);
+      overlaps(out, out_bytes, lse, rows * 4) ||
+      overlaps(out, out_bytes, q, extent(n, q_row, q_heads, q_head, c.head_dim, c.elem)) ||
+      overlaps(lse, rows * 4, q, extent(n, q_row, q_heads, q_head, c.head_dim, c.elem)))
+    return fail(COPES_ERR_INVALID_ARG, "%s: q, out, lse and the pool must be disjoint", who);
   if ((rc = check_workspace(workspace, workspace_bytes, copes::attend_workspace_bytes(c, n, q_heads), who))) return rc;
   a.layer = layer;
   a.n = n;
@@ -250,6 +263,10 @@ int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_
   if (!aligned(logits, elem_size(dtype)) || !aligned(target, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
       !aligned(top_ids, 8) || !aligned(top_logprobs, 4))
     return fail(COPES_ERR_ALIGNMENT, "%s: an array is not aligned to its type", who);
+  const uint64_t read = extent(n, row, 1, 0, vocab, elem_size(dtype)), written = (uint64_t)n * top;
+  if (overlaps(logits, read, logprob, 4ull * n) || overlaps(logits, read, entropy, 4ull * n) ||
+      overlaps(logits, read, top_ids, 8 * written) || overlaps(logits, read, top_logprobs, 4 * written))
+    return fail(COPES_ERR_INVALID_ARG, "%s: logits overlap an output", who);
   copes::LogprobArgs a{};
   a.logits = logits;
   a.row = row;

@@ -94,7 +94,8 @@ def test_arguments_that_are_refused(copes):
         return L.copes_cache_append(c, layer, slots, position, n, k, 64, 64, v, 64, 64, None)
 
     for kw, code in [(dict(layer=2), -1), (dict(layer=-1), -1), (dict(slots=None, n=5), -3), (dict(position=0x102), -2),
-                     (dict(k=None), -1), (dict(v=None), -1), (dict(k=0x101), -2), (dict(n=-1), -1)]:
+                     (dict(k=None), -1), (dict(v=None), -1), (dict(k=0x101), -2), (dict(n=-1), -1), (dict(k=0x1000010), -1),
+                     (dict(v=0x1000010), -1)]:
         refused(copes, append(**kw), code, "copes_cache_append")
 
     need = L.copes_paged_attention_workspace_bytes(c, 4, 8)
@@ -108,17 +109,18 @@ def test_arguments_that_are_refused(copes):
                      (dict(heads=7), -1), (dict(heads=0), -1), (dict(heads=70000), -3), (dict(scale=float("nan")), -1),
                      (dict(scale=float("inf")), -1), (dict(q=0x101), -2), (dict(out=0xD000008), -2), (dict(lse=0xE000002), -2),
                      (dict(out=0x1000010), -1), (dict(lse=0x1000010), -1), (dict(lse=0xD000010), -1), (dict(slots=0x102), -2),
+                     (dict(q=0xD000004), -1), (dict(lse=0x200), -1),
                      (dict(work=None), -4), (dict(size=need - 1), -4), (dict(work=WS + 8), -2)]:
         refused(copes, attend(**kw), code, "copes_paged_attention")
 
-    def logprobs(logits=0x100, dtype=0, n=1, vocab=100, target=0x1000, scale=1.0, top=2, lp=0x2000, ent=None, ids=0x3000,
+    def logprobs(logits=0x100000, dtype=0, n=1, vocab=100, target=0x1000, scale=1.0, top=2, lp=0x2000, ent=None, ids=0x3000,
                  tlp=0x4000):
         return L.copes_token_logprobs(logits, dtype, n, vocab, 100, target, scale, top, lp, ent, ids, tlp, None)
 
     for kw, code in [(dict(dtype=2), -1), (dict(n=-1), -1), (dict(vocab=0), -1), (dict(vocab=(1 << 30) + 1), -3), (dict(scale=0.0), -1),
                      (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(top=-1), -3),
                      (dict(top=33), -3), (dict(vocab=1), -3), (dict(logits=None), -1), (dict(target=None), -1), (dict(lp=None), -1),
-                     (dict(ids=None), -1), (dict(tlp=None), -1), (dict(logits=0x101), -2), (dict(target=0x1004), -2),
+                     (dict(lp=0x100004), -1), (dict(ent=0x100004), -1), (dict(ids=0x100008), -1), (dict(tlp=0x1000C4), -1), (dict(ids=None), -1), (dict(tlp=None), -1), (dict(logits=0x101), -2), (dict(target=0x1004), -2),
                      (dict(ids=0x3004), -2), (dict(lp=0x2002), -2), (dict(ent=0x5001), -2)]:
         refused(copes, logprobs(**kw), code, "copes_token_logprobs")
 

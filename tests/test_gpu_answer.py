@@ -124,6 +124,25 @@ def test_pages_follow_the_model_through_random_calls(copes, page_size, layers, k
     assert len(seen) >= 6
 
 
+def test_grow_and_fork_change_all_or_nothing(copes):
+    cache = copes.KVCache.empty(6, 1, 1, 4, 8, 5, 3)
+    m = model.CacheModel(6, 4, 5, 3)
+    cache.pool.normal_()
+    pool = cache.pool.clone()
+    for slots, add in [([0, 1], [5, 3]), ([1, 2], [9, 1]), ([2], [-1]), ([0, 0], [1, 1]), ([3, 5], [1, 1]), ([3, -1], [1, 1]),
+                       ([2, 3], [8, 5]), ([0], [2**31 - 1]), ([2], [0])]:
+        copes.cache_grow(cache, ids(slots), ids(add))
+        assert error_bits(copes) == m.grow(slots, add)
+        same(cache, m, pool)
+    for parents, children in [([0], [0]), ([0, 2], [2, 3]), ([0, 0], [3, 3]), ([0], [1]), ([7], [2]), ([0], [5]), ([0, 1, 0], [2, 3, 4]),
+                              ([0, 1], [2, 3])]:
+        copes.cache_fork(cache, ids(parents), ids(children))
+        assert error_bits(copes) == m.fork(parents, children)
+        for a, b in m.copies:
+            pool[b] = pool[a]
+        same(cache, m, pool)
+
+
 def test_a_long_prompt_and_many_children(copes):
     """Page lists longer than a block of the plan, refs raised from many blocks at once."""
     cache = copes.KVCache.empty(6000, 1, 1, 2, 8, 300, 2600)
