@@ -34,7 +34,7 @@ constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMostThreads = 256, kMostWarps = kMostThreads / 32;
 // blocks of an SM: with a thread's next step on its way (shallow), or the next two (deep)
 constexpr int per_sm(bool deep) { return deep ? 3 : 4; }
-constexpr int kCells = 8192;       // of a block, at most
+constexpr int kThreadCells = 32;   // of a thread, at most
 constexpr int kReached = 1024;     // cells read again by the fast way, at most
 constexpr int kCandidates = 512;   // logits ranked by counting, at most
 constexpr int kClusterMost = 8;
@@ -382,7 +382,7 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
   __syncthreads();
   const int bound = sh.bound;
   {
-    unsigned mine = 0;  // which of the thread's cells: at most kCells / kMostThreads = 32 (fewer threads have fewer)
+    unsigned mine = 0;  // which of the thread's cells, at most kThreadCells
     if (order_of(max_nan(own[0], own[1])) >= bound) {
       const int steps = (n + kStep * warps - 1) / (kStep * warps), cells = (steps + (1 << merge) - 1) >> merge;
 #pragma unroll 4
@@ -438,8 +438,8 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
 }
 
 // A block, or a cluster of `parts` blocks, per row; a cell is 2^merge steps of a thread.  Before it
-// looks for a row's alternatives a block asks for the first kAhead bytes of what a block `apart`
-// rows on reads, whose turn is near, into L2, so that HBM is not idle meanwhile.
+// looks for a row's alternatives a block asks for the first kAhead bytes (a quarter at most) of what a
+// block `apart` rows on reads, whose turn is near, into L2, so that HBM is not idle meanwhile.
 constexpr int kAhead = 48 << 10;
 
 template <typename T, bool kTop, bool kDeep>
@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   if (tid == 0 && i + apart < a.n) {
     const Row<T> later((const T *)a.logits + (i + apart) * a.row, a.vocab);
     const int v = max((int)((int64_t)later.pieces() * part / parts), later.first_full());
-    const int bytes = min(min(n, later.end_full() - v), kAhead / 16) * 16;
+    const int bytes = min(min(n, later.end_full() - v), min(kAhead / 16, n / 4)) * 16;
     if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(later.at(v)), "r"(bytes) : "memory");
   }
   if (kTop) {  // a thread's steps past its last hold nothing
@@ -600,33 +600,59 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   }
 }
 
-// How a call is cut: blocks of a row, threads of a block, steps that share a cell.
+// How a call is cut: blocks of a row, threads of a block, one step ahead or two, steps that share a cell.
 struct Cut {
   int parts, threads, merge, apart;
+  bool deep;
   uint32_t cell_bytes;
 };
 
-// Parts of a row: as many as leave at most 400 blocks, two or three of an SM, and each 256 pieces.
-// us for rows of 151,936 bf16 logits with 5 alternatives in 1, 2, 4 and 8 parts: 38 rows 15.1, 12.1,
-// 10.7, 10.3; 120 rows 18.4, 15.8, 20.6, 26.1; 300 rows 23.5, 32.1, 35.2, 53.2.
-// Threads: a step for each at least.
-static Cut cut_of(int64_t n, int64_t pieces, bool deep) {
-  Cut c{1, 32, 0, 0, 0};
-  while (c.parts < kClusterMost && n * c.parts * 2 <= 400 && pieces / (c.parts * 2) >= 256) c.parts *= 2;
-  const int64_t mine = pieces / c.parts + 1;
-  while (c.threads < kMostThreads && mine > c.threads * 2 * kLoads) c.threads *= 2;
-  const int64_t steps = (mine + c.threads * kLoads - 1) / (c.threads * kLoads);
-  while (((steps + (1 << c.merge) - 1) >> c.merge) * c.threads > kCells) ++c.merge;
-  c.cell_bytes = (uint32_t)((steps + (1 << c.merge) - 1) >> c.merge) * c.threads * 4;
-  c.apart = 152 * per_sm(deep) * kMostThreads / c.threads / c.parts;  // rows at a time
-  return c;
+// The cut that costs least by this count: waves of blocks over the GPU, times the blocks that run at
+// once (a block's share of HBM), times a block's pieces and what its beginning and end cost it,
+// 24 pieces' time a thread with alternatives and 16 without.  A block has a step for each thread at
+// least, and 256 pieces where it is one of several of a row; with one step ahead instead of two a
+// long row takes 5% longer, 15% with 64 threads.  One warp alone is for rows too short for two: the
+// end of a row is a chain of loads that more warps shorten.  What it decides, in us with 5 alternatives (bf16 where nothing is said):
+//   rows x logits     parts 1, 2, 4, 8             threads 32, 64, 128, 256 (two steps ahead)
+//   38 x 151,936      15.1, 12.1, 10.7, 10.3
+//   120 x 151,936     18.4, 15.8, 20.6, 26.1
+//   300 x 151,936     23.5, 32.1, 35.2, 53.2
+//   4,096 x 151,936                                -, -, 211, 220
+//   4,096 x 32,003                                 68, 60, 65, 84
+//   20,000 x 32,003                                296, 252, 292, 396
+//   500 x 7,500                                    9.3, 8.0, 7.4, 7.6
+// and steps ahead, 500 x 151,936 (one wave or two): 38 with one, 45 with two; 734 x 151,936: 58, 47.
+static Cut cut_of(int64_t n, int64_t pieces, bool top) {
+  Cut best{1, 32, 0, 0, false, 0};
+  double least = 0.0;
+  for (int parts = 1; parts <= kClusterMost && (parts == 1 || pieces / parts >= 256); parts *= 2) {
+    const int64_t mine = pieces / parts + 1;
+    for (int threads = mine >= 64 * kLoads ? 64 : 32; threads <= kMostThreads && (threads <= 64 || mine >= threads * kLoads);
+         threads *= 2)
+      for (int deep = 0; deep < 2; ++deep) {
+        const int64_t at_once = (int64_t)152 * per_sm(deep) * (kMostThreads / threads);
+        const bool longer = mine >= 3 * threads * kLoads;
+        if (deep && !longer) continue;
+        const int64_t waves = (n * parts + at_once - 1) / at_once;
+        const double cost = (double)(waves * at_once) * (double)(mine + (top ? 24 : 16) * threads) *
+                            (deep || !longer ? 1.0 : threads <= 64 ? 1.15 : 1.05);
+        if (least == 0.0 || cost < least) {
+          least = cost;
+          best = Cut{parts, threads, 0, (int)(at_once / parts), deep != 0, 0};
+        }
+      }
+  }
+  const int64_t mine = pieces / best.parts + 1, steps = (mine + best.threads * kLoads - 1) / (best.threads * kLoads);
+  while ((steps + (1 << best.merge) - 1) >> best.merge > kThreadCells) ++best.merge;
+  best.cell_bytes = (uint32_t)((steps + (1 << best.merge) - 1) >> best.merge) * best.threads * 4;
+  return best;
 }
 
 template <typename T, bool kTop, bool kDeep>
 static cudaError_t launch(const LogprobArgs &a, const Cut &c, cudaStream_t s) {
   const auto kernel = logprob_kernel<T, kTop, kDeep>;
   const uint32_t bytes = kTop ? c.cell_bytes : 0, fixed = sizeof(LogprobShared);
-  const cudaError_t e = allow_smem((const void *)kernel, bytes + fixed, kCells * 4);
+  const cudaError_t e = allow_smem((const void *)kernel, bytes + fixed, kThreadCells * kMostThreads * 4);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)a.n * c.parts);
@@ -642,18 +668,10 @@ static cudaError_t launch(const LogprobArgs &a, const Cut &c, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kernel, a, c.parts, c.merge, c.apart);
 }
 
-// Three blocks of an SM with two steps on their way where a thread has three steps or more, else
-// four blocks with one: 301 rows of 32,003 fp32 logits take 12.3 us deep and 13.2 shallow, 4,096 rows
-// of 7,500 bf16 logits (two steps) 37 and 32.  Four blocks, too, where their last wave is so much
-// fuller: 500 rows of 151,936 in one wave 38 us, in two of three blocks 45 (734 rows: 58 and 47).
 template <typename T, bool kTop>
 static cudaError_t launch_any(const LogprobArgs &a, cudaStream_t s) {
-  const int64_t pieces = (int64_t)a.vocab / Piece<T>::kN + 2;
-  const Cut deep = cut_of(a.n, pieces, true);
-  const auto paid = [&](int64_t at_once) { return (a.n * (int64_t)deep.parts + at_once - 1) / at_once * at_once; };
-  if (pieces / deep.parts >= 3 * deep.threads * kLoads && paid(152 * per_sm(true)) * 20 <= paid(152 * per_sm(false)) * 23)
-    return launch<T, kTop, true>(a, deep, s);
-  return launch<T, kTop, false>(a, cut_of(a.n, pieces, false), s);
+  const Cut c = cut_of(a.n, (int64_t)a.vocab / Piece<T>::kN + 2, kTop);
+  return c.deep ? launch<T, kTop, true>(a, c, s) : launch<T, kTop, false>(a, c, s);
 }
 
 cudaError_t launch_token_logprobs(int dtype, const LogprobArgs &a, cudaStream_t s) {
