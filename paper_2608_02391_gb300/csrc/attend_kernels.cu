@@ -71,8 +71,8 @@ struct Shape {
 // Where a block is in the line of tiles: row by row, key-value head by head, group of query heads
 // by group, tile by tile.
 struct Cursor {
-  int row, slot, tokens, tiles;  // of the row
-  int kv, sub, tile;  // tile == tiles: the step that stands for the end
+  int row, tokens, tiles;  // of the row
+  int kv, sub, tile;       // tile == tiles: the step that stands for the end
 };
 
 __device__ __forceinline__ int row_slot(const AttendArgs &a, int row) { return a.slots ? a.slots[row] : row; }
@@ -81,24 +81,33 @@ __device__ __forceinline__ int row_tokens(const AttendArgs &a, int slot) {
   return (unsigned)slot < (unsigned)a.c.n_slots ? slot_tokens(a.c, slot) : 0;
 }
 
+// The rows after the one that a warp looks tiles up in: their slots and lengths are asked for two and
+// one rows before they are used, since a load behind the tiles' copies takes microseconds.
+struct RowsAhead {
+  int slot, slot1, slot2, length1;  // the row's slot, the next two, the next one's length entry
+  __device__ __forceinline__ static int length_of(const AttendArgs &a, int slot) {
+    return (unsigned)slot < (unsigned)a.c.n_slots ? a.c.length[slot] : 0;
+  }
+  __device__ __forceinline__ void begin(const AttendArgs &a, int row) {
+    slot = row_slot(a, row);
+    slot1 = row + 1 < a.n ? row_slot(a, row + 1) : -1;
+    slot2 = row + 2 < a.n ? row_slot(a, row + 2) : -1;
+    length1 = length_of(a, slot1);
+  }
+  __device__ __forceinline__ int next(const AttendArgs &a, int row) {  // moves on to `row`; its tokens
+    const int most = a.c.table_width * a.c.page_size, tokens = max(0, min(length1, most));
+    slot = slot1;
+    slot1 = slot2;
+    length1 = length_of(a, slot1);
+    slot2 = row + 2 < a.n ? row_slot(a, row + 2) : -1;
+    return tokens;
+  }
+};
+
 // An empty row has one tile, of no tokens, so that somebody writes its output.
 template <int kTile>
 __device__ __forceinline__ int row_tiles(int tokens) {
   return tokens ? (tokens - 1) / kTile + 1 : 1;
-}
-
-template <int kTile>
-__device__ __forceinline__ void advance(const AttendArgs &a, int groups, int ends, Cursor &c) {
-  if (++c.tile < c.tiles + ends) return;
-  c.tile = 0;
-  if (++c.sub < groups) return;
-  c.sub = 0;
-  if (++c.kv < a.c.n_kv_heads) return;
-  c.kv = 0;
-  if (++c.row >= a.n) return;
-  c.slot = row_slot(a, c.row);
-  c.tokens = row_tokens(a, c.slot);
-  c.tiles = row_tiles<kTile>(c.tokens);
 }
 
 // The line shared out: each block has `each` steps, the first `more` of them one more.
@@ -222,8 +231,10 @@ struct Queries {
   uint32_t b[S::DP / 16][S::NT][S::kFp32 ? 4 : 2];
 };
 
+// `wide`: rows of q are aligned to what a lane loads at a time, 4 bytes of bf16 and 16 of fp32.
 template <typename T, typename S>
-__device__ __forceinline__ void load_queries(const AttendArgs &a, int row, int first_head, int heads, Queries<S> &q) {
+__device__ __forceinline__ void load_queries(const AttendArgs &a, bool wide, int row, int first_head, int heads,
+                                             Queries<S> &q) {
   const int lane = threadIdx.x & 31, D = a.c.head_dim;
 #pragma unroll
   for (int j = 0; j < S::NT; ++j) {
@@ -234,8 +245,15 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, int row, int f
       if constexpr (S::kFp32) {
         // one 16-byte piece of a key's row is the four k of two products: a lane's are d .. d + 3
         const int d = k * 16 + (lane & 3) * 4;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q.b[k][j][e] = h < heads && d < D ? __float_as_uint(from[d + e]) : 0u;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (h < heads && d < D) {
+          const uint32_t *u = reinterpret_cast<const uint32_t *>(from + d);
+          x = wide ? *reinterpret_cast<const uint4 *>(u) : make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        q.b[k][j][0] = x.x;
+        q.b[k][j][1] = x.y;
+        q.b[k][j][2] = x.z;
+        q.b[k][j][3] = x.w;
       } else {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -243,7 +261,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, int row, int f
           uint32_t x = 0;
           if (h < heads && d < D) {
             const uint16_t *u = reinterpret_cast<const uint16_t *>(from + d);
-            x = u[0] | (uint32_t)u[1] << 16;
+            x = wide ? *reinterpret_cast<const uint32_t *>(u) : u[0] | (uint32_t)u[1] << 16;
           }
           q.b[k][j][e] = x;
         }
@@ -489,8 +507,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     Cursor at;
     at.row = r0;
     for (;; ++at.row) {
-      at.slot = row_slot(a, at.row);
-      at.tokens = row_tokens(a, at.slot);
+      at.tokens = row_tokens(a, row_slot(a, at.row));
       at.tiles = row_tiles<TILE>(at.tokens);
       if (at.row + 1 >= r1 || lo < (before + at.tiles + ends) * units) break;
       before += at.tiles + ends;
@@ -503,6 +520,35 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   }
   __syncthreads();
   Cursor at = s_at, ahead = at;
+  RowsAhead rows_ahead;
+  rows_ahead.begin(a, at.row);
+  if (tid == 0 && (unsigned)rows_ahead.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
+  // The tokens of the rows between `at` and `ahead`, by row % 8: the cursors are at most kStages + 1
+  // steps, and so rows, apart.
+  static_assert(S::kStages + 1 < 8, "a lane for each row between the cursors");
+  int tokens_of_row = 0;
+  // the next (row, head group); true where that is another row
+  const auto next_unit = [&](Cursor &x) {
+    x.tile = 0;
+    if (++x.sub < groups) return false;
+    x.sub = 0;
+    if (++x.kv < c.n_kv_heads) return false;
+    x.kv = 0;
+    ++x.row;
+    return true;
+  };
+  const auto advance_ahead = [&]() {
+    if (++ahead.tile < ahead.tiles + ends || !next_unit(ahead) || ahead.row >= a.n) return;
+    ahead.tokens = rows_ahead.next(a, ahead.row);
+    ahead.tiles = row_tiles<TILE>(ahead.tokens);
+    if (tid == 0 && (unsigned)rows_ahead.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
+    if (lane == (ahead.row & 7)) tokens_of_row = ahead.tokens;
+  };
+  const auto advance_at = [&]() {
+    if (++at.tile < at.tiles + ends || !next_unit(at) || at.row >= a.n) return;
+    at.tokens = __shfl_sync(kAll, tokens_of_row, at.row & 7);
+    at.tiles = row_tiles<TILE>(at.tokens);
+  };
 
   float *s_o = reinterpret_cast<float *>(smem + S::kStages * S::kStage);  // [warp][8][kRow]
   float *s_m = s_o + S::kWarps * 8 * S::kRow, *s_l = s_m + S::kWarps * 8;
@@ -524,10 +570,10 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if (ahead.tile < ahead.tiles && t < ahead.tokens) {
       const int at_page = by_page.quotient(t);
       p.place = t - at_page * c.page_size;
-      p.page = c.table[(int64_t)ahead.slot * c.table_width + at_page];
+      p.page = c.table[(int64_t)rows_ahead.slot * c.table_width + at_page];
       if ((unsigned)p.page >= (unsigned)c.n_pages) p.page = -2;
     }
-    if (++looked < count) advance<TILE>(a, groups, ends, ahead);
+    if (++looked < count) advance_ahead();
     return p;
   };
   const auto ask = [&](int stage, const Place &p) {
@@ -548,15 +594,23 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     }
   };
   Place next = look_up();
-  Queries<S> q;
-  const auto queries_of = [&](Cursor x, int steps) {  // of the first tile of the next `steps` steps, from x on
-    if (x.tile == x.tiles) {
-      if (steps < 2) return;
-      advance<TILE>(a, groups, ends, x);
-    }
-    load_queries<T, S>(a, x.row, x.kv * group + x.sub * S::kHeads, min(S::kHeads, group - x.sub * S::kHeads), q);
+  // The queries of a (row, head group), and, registers permitting, of the next one, asked for a
+  // (row, head group) before they are used.
+  constexpr bool kNextToo = S::NT == 1 && (S::kFp32 ? S::DP <= 64 : S::DP <= 128);
+  const int64_t q_bytes = sizeof(T), q_wide = S::kFp32 ? 16 : 4;
+  const bool wide = (uintptr_t)a.q % q_wide == 0 && a.q_row * q_bytes % q_wide == 0 && a.q_head * q_bytes % q_wide == 0;
+  Queries<S> q, q_next;
+  const auto queries_of = [&](const Cursor &x, Queries<S> &to) {
+    if (x.row < a.n)
+      load_queries<T, S>(a, wide, x.row, x.kv * group + x.sub * S::kHeads, min(S::kHeads, group - x.sub * S::kHeads), to);
   };
-  queries_of(at, count);
+  Cursor asking = at;  // whose queries were asked for last
+  if (at.tile == at.tiles) next_unit(asking);
+  queries_of(asking, q);
+  if constexpr (kNextToo) {
+    next_unit(asking);
+    if (count > at.tiles - at.tile) queries_of(asking, q_next);
+  }
   Place after = look_up();
 
   int asked = 0;
@@ -593,9 +647,13 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     __syncwarp();
 
     const Cursor was = at;
-    if (j + 1 < count) advance<TILE>(a, groups, ends, at);
+    if (j + 1 < count) advance_at();
     if (was.tile == was.tiles || (was.tile + 1 < was.tiles && j + 1 < count)) continue;
-    if (j + 1 < count) queries_of(at, count - j - 1);  // on their way during what follows
+    if (j + 1 + ends < count) {
+      if constexpr (kNextToo) q = q_next;
+      next_unit(asking);
+      queries_of(asking, kNextToo ? q_next : q);
+    }
 
     // the warps' states together
     const int x0 = lo + j - was.tile, w0 = shares.owner(x0), w1 = shares.owner(x0 + was.tiles - 1);
@@ -603,7 +661,6 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     const bool whole = w0 == w1;
     float *mine_part = part + (int64_t)(2 * (int)blockIdx.x + (lo > x0 ? 0 : 1)) * slot_floats;
     const int64_t first = (int64_t)was.row * a.q_heads + first_head;
-    if (tid == 0 && (unsigned)was.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
 #pragma unroll
     for (int nt = 0; nt < S::NT; ++nt) {
       __syncthreads();  // s_o may still be read
@@ -657,7 +714,8 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
 }
 
 // Joins the parts of what begins in one block and goes on in others: `per` blocks for each block of
-// attend_kernel, one for a head (of the kheads that a part has room for).  Warps (pairs of them for more than 128 components) take the parts by turns.
+// attend_kernel, one for a head (of the kheads that a part has room for).  Warps (pairs of them for
+// more than 128 components) take the parts by turns.
 constexpr int kJoinThreads = 256;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttendArgs a, const Split *split, const float *part,
