@@ -372,12 +372,15 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
         p[j][e][1] = __byte_perm(lo, hi, 0x7632);
       }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int row = e * 8 + (lane & 3) * 2;
-      const uint32_t at = values + row * kPitch;
+    for (int g = 0; g < S::DP / 32; ++g) {
+      // The matrix unit cuts its sums where an addition rounds them: a tile's go into a sum of
+      // their own, and that by an addition to the row's, lest thousands of tokens' cuts add up.
+      float sum[2][NT][4] = {};
+      const int piece = g * 8 + (lane >> 2);  // d = 32 g + 4 (lane / 4) + 0 .. 3
 #pragma unroll
-      for (int g = 0; g < S::DP / 32; ++g) {
-        const int piece = g * 8 + (lane >> 2);  // d = 32 g + 4 (lane / 4) + 0 .. 3
+      for (int e = 0; e < 2; ++e) {
+        const int row = e * 8 + (lane & 3) * 2;
+        const uint32_t at = values + row * kPitch;
         uint32_t u[4], v[4];
         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
                      : "r"(at + (uint32_t)((piece ^ swizzle<S>(row)) * 16)) : "memory");
@@ -386,10 +389,17 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
         const uint32_t a0[4] = {u[0], u[1], v[0], v[1]}, a1[4] = {u[2], u[3], v[2], v[3]};
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          mma_split(r.o[2 * g][j], a0, p[j][e][0], p[j][e][1]);
-          mma_split(r.o[2 * g + 1][j], a1, p[j][e][0], p[j][e][1]);
+          mma_split(sum[0][j], a0, p[j][e][0], p[j][e][1]);
+          mma_split(sum[1][j], a1, p[j][e][0], p[j][e][1]);
         }
       }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          r.o[2 * g][j][e] += sum[0][j][e];
+          r.o[2 * g + 1][j][e] += sum[1][j][e];
+        }
     }
   } else {
     uint32_t p[NT][2], rest[NT][2];  // tokens 0 .. 7 and 8 .. 15, in two bf16 terms
