@@ -566,10 +566,17 @@ def update(arena: Arena, sub: SubspaceHandle, noise_id: np.ndarray, sign: np.nda
 _DTYPE_CODES = {torch.bfloat16: BF16, torch.float32: FP32}
 
 
+@functools.lru_cache(maxsize=256)
+def _template(shape, dtype, device) -> torch.Tensor:
+    """A tensor of this shape in one element of memory, for empty_like: that call takes about 2 us
+    less than empty() with its keywords, which a call of a few microseconds notices."""
+    return torch.empty((), dtype=dtype, device=device).expand(shape)
+
+
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
-    """An output of a call on `stream`, allocated in that stream's order."""
+    """A contiguous output of a call on `stream`, allocated in that stream's order."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty_like(_template(shape, dtype, device), memory_format=torch.contiguous_format)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
@@ -722,7 +729,8 @@ def token_logprobs(logits: torch.Tensor, target: torch.Tensor, top: int = 0, sca
     assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
     assert target.shape == (n,) and target.dtype == torch.int64 and target.device == device and target.is_contiguous()
     dtype = _DTYPE_CODES[logits.dtype]
-    logprob, entropy = _empty((2, n), torch.float32, device, stream).unbind(0)
+    logprob = _empty((n,), torch.float32, device, stream)
+    entropy = _empty((n,), torch.float32, device, stream)
     ids = _empty((n, top), torch.int64, device, stream)
     top_logprobs = _empty((n, top), torch.float32, device, stream)
     _check(load().copes_token_logprobs(logits.data_ptr(), dtype, n, vocab, logits.stride(0), target.data_ptr(), scale,
