@@ -190,13 +190,13 @@ int copes_cache_copy_pages(const copes_kv_cache *p, const int32_t *src, const in
   return launch_status(copes::launch_cache_copy(c, src, dst, n, stream), who);
 }
 
-// Query heads come in whole groups of the cache's heads.  The kernel counts tiles of at least 32
-// tokens of up to 8 heads, and one more for each row, in 32 bits.
+// Query heads come in whole groups of the cache's heads.  The kernel counts tiles of at least 16
+// tokens of up to 8 heads, and two more for each row, in 32 bits.
 static int check_q_heads(const copes::Cache &c, int n, int q_heads, const char *who) {
   if (q_heads < 1 || q_heads % c.n_kv_heads)
     return fail(COPES_ERR_INVALID_ARG, "%s: %d query heads on %d key-value heads", who, q_heads, c.n_kv_heads);
   const int64_t units = (int64_t)c.n_kv_heads * ((q_heads / c.n_kv_heads + 7) / 8);
-  const int64_t tiles = ((int64_t)c.table_width * c.page_size + 31) / 32 + 1;
+  const int64_t tiles = ((int64_t)c.table_width * c.page_size + 15) / 16 + 2;
   if (q_heads > 65535 || (int64_t)n * q_heads > 0x7FFFFFFF || (int64_t)n * units > 0x7FFFFFFF / tiles)
     return fail(COPES_ERR_SIZE, "%s: too many query heads, or tokens that the tables have room for", who);
   return COPES_OK;

@@ -20,7 +20,10 @@
 //
 // A tile.  Each warp keeps 16 of a tile's tokens to itself, from the copy into shared memory to
 // its own running maximum, sum and output, so that the warps need each other only at the end of
-// a row.  Keys are the rows of the first product and the query heads its columns,
+// a row.  Where there are rows enough, they do not need each other at all: each warp has a key-value
+// head to itself, of as many heads side by side as a block has warps, with tiles of 16 tokens (1,024
+// rows of up to 100 tokens: TODO us with the warps on one head, TODO us so; fewer, longer rows would be cut
+// into four times the parts).  Keys are the rows of the first product and the query heads its columns,
 // S^T[token][head] = K Q^T, and in the second O^T[d][head] = V^T P^T: 8 heads fill a tile of the
 // matrix unit, where heads as rows would fill half of 16.  P^T is S^T's registers transposed in
 // 8 x 8 blocks (movmatrix).
@@ -42,8 +45,9 @@ __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_attend_er
 constexpr int kSMs = 152;
 constexpr unsigned kAll = 0xffffffffu;
 
-// What a kernel variant is made of: T of the cache, head_dim padded to DP, NT x 8 query heads.
-template <typename T, int DP_, int NT_>
+// What a kernel variant is made of: T of the cache, head_dim padded to DP, NT x 8 query heads, and
+// whether the warps of a block have heads side by side or share one.
+template <typename T, int DP_, int NT_, bool kBeside>
 struct Shape {
   static constexpr bool kFp32 = sizeof(T) == 4;
   static constexpr int DP = DP_, NT = NT_;
@@ -53,7 +57,8 @@ struct Shape {
   static constexpr int kWarps = !kFp32 ? 4 : DP <= 128 ? 2 : DP <= 192 ? 4 : 3;
   static constexpr int kStages = kFp32 ? 2 : DP <= 96 ? 4 : 3;
   static constexpr int kThreads = kWarps * 32;
-  static constexpr int kTile = kWarps * 16;               // tokens
+  static constexpr int kTeam = kBeside ? 1 : kWarps, kSides = kWarps / kTeam;  // warps on a head, heads
+  static constexpr int kTile = kTeam * 16;                // tokens
   static constexpr int kChunks = DP * (int)sizeof(T) / 16;  // 16-byte pieces of a token's row
   static constexpr int kPart = 16 * kChunks * 16;         // a warp's keys (or values) of a tile, bytes
   static constexpr int kStage = 2 * kPart * kWarps;
@@ -72,7 +77,7 @@ struct Shape {
 // by group, tile by tile.
 struct Cursor {
   int row, tokens, tiles;  // of the row
-  int kv, sub, tile;       // tile == tiles: the step that stands for the end
+  int kv, sub, tile;       // kv in kSides; tile >= tiles: a step that stands for the end
 };
 
 __device__ __forceinline__ int row_slot(const AttendArgs &a, int row) { return a.slots ? a.slots[row] : row; }
@@ -446,8 +451,8 @@ __device__ __forceinline__ void fma4(float4 &o, float f, const float4 &x) {
 }
 // o / L, 0 of an empty row.
 __device__ __forceinline__ float4 normalised(const float4 &o, float L) {
-  if (L == 0.0f) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  return make_float4(o.x / L, o.y / L, o.z / L, o.w / L);
+  const float f = L == 0.0f ? 0.0f : 1.0f / L;
+  return make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
 }
 __device__ __forceinline__ float log_sum(float M, float L) {
   return L == 0.0f ? -INFINITY : fmaf(0.6931471805599453094f, M, logf(L));
@@ -466,9 +471,9 @@ struct Divisor {
 };
 
 // The workspace: a Split for every block, then the parts: block w's at 2 w (of a row that begins
-// before the block's share) and 2 w + 1 (of one that ends after it), each kHeads maxima, kHeads sums
-// and kHeads x head_dim values.
-struct Split {  // what begins in block w and goes on to block `last`; row -1: nothing
+// before the block's share) and 2 w + 1 (of one that ends after it), each for kSides heads kHeads
+// maxima, kHeads sums and kHeads x head_dim values.
+struct alignas(16) Split {  // what begins in block w's share and goes on to that of block `last`; row -1: nothing
   int row, kv, sub, last;
 };
 
@@ -478,16 +483,30 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   extern __shared__ __align__(128) char smem[];
   __shared__ Cursor s_at;
   __shared__ int s_sum[S::kWarps];
-  constexpr int TILE = S::kTile;
+  constexpr int TILE = S::kTile, kTeamThreads = S::kTeam * 32;
   const Cache &c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = c.head_dim;
-  const int group = a.q_heads / c.n_kv_heads, units = c.n_kv_heads * groups;
+  // this warp's head beside the others', its place among the warps on that head, and this thread's
+  const int side = warp / S::kTeam, member = warp % S::kTeam, rank = tid % kTeamThreads;
+  const int group = a.q_heads / c.n_kv_heads, beside = c.n_kv_heads / S::kSides, units = beside * groups;
+  const auto team_sync = [] {
+    if constexpr (S::kTeam == 1) __syncwarp();
+    else __syncthreads();
+  };
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  // the line's length and this block's share [lo, hi) of it
+  // The line's length and this block's share [lo, hi) of it: a thread adds up a few rows in order.
+  // Their tiles wait where the keys and values will be, if there is room, or are counted twice.
+  int *s_tiles = reinterpret_cast<int *>(smem);
+  const bool kept = a.n <= S::kStages * S::kStage / 4;
+  const auto tiles_of = [&](int i) { return kept ? s_tiles[i] : row_tiles<TILE>(row_tokens(a, row_slot(a, i))); };
+  if (kept) {
+    for (int i = tid; i < a.n; i += S::kThreads) s_tiles[i] = row_tiles<TILE>(row_tokens(a, row_slot(a, i)));
+    __syncthreads();
+  }
   const int rows = (a.n + S::kThreads - 1) / S::kThreads, r0 = min(a.n, tid * rows), r1 = min(a.n, r0 + rows);
   int mine = 0;
-  for (int i = r0; i < r1; ++i) mine += row_tiles<TILE>(row_tokens(a, row_slot(a, i)));
+  for (int i = r0; i < r1; ++i) mine += tiles_of(i);
   int before = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -502,7 +521,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if (w < warp) before += s_sum[w];
     total += s_sum[w];
   }
-  const int ends = total * units > (int)gridDim.x;  // 1: an end is a step
+  const int ends = total * units > (int)gridDim.x ? S::NT : 0;  // steps that an end counts for
   before += r0 * ends - mine;
   mine += (r1 - r0) * ends;
   total = (total + a.n * ends) * units;
@@ -517,11 +536,11 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     Cursor at;
     at.row = r0;
     for (;; ++at.row) {
-      at.tokens = row_tokens(a, row_slot(a, at.row));
-      at.tiles = row_tiles<TILE>(at.tokens);
+      at.tiles = tiles_of(at.row);
       if (at.row + 1 >= r1 || lo < (before + at.tiles + ends) * units) break;
       before += at.tiles + ends;
     }
+    at.tokens = row_tokens(a, row_slot(a, at.row));
     const int unit = (lo - before * units) / (at.tiles + ends);
     at.tile = (lo - before * units) % (at.tiles + ends);
     at.kv = unit / groups;
@@ -542,7 +561,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     x.tile = 0;
     if (++x.sub < groups) return false;
     x.sub = 0;
-    if (++x.kv < c.n_kv_heads) return false;
+    if (++x.kv < beside) return false;
     x.kv = 0;
     ++x.row;
     return true;
@@ -561,12 +580,13 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   };
 
   float *s_o = reinterpret_cast<float *>(smem + S::kStages * S::kStage);  // [warp][8][kRow]
-  float *s_m = s_o + S::kWarps * 8 * S::kRow, *s_l = s_m + S::kWarps * 8;
+  float *s_m = s_o + S::kWarps * 8 * S::kRow + side * S::kTeam * 8, *s_l = s_m + S::kWarps * 8;
+  s_o += side * S::kTeam * 8 * S::kRow;  // of the warps on this head, like s_m and s_l
   const uint32_t stages = smem_addr(smem) + warp * 2 * S::kPart;
-  const char *pool = c.pool + (uint64_t)a.layer * c.layer_elems * sizeof(T);
   const uint64_t head_bytes = (uint64_t)c.head_elems * sizeof(T), to_values = c.n_kv_heads * head_bytes;
+  const char *pool = c.pool + (uint64_t)a.layer * c.layer_elems * sizeof(T) + side * head_bytes;
 
-  // Where token (16 warp + lane % 16) of a tile is: its page (-1 for none, -2 for one outside the
+  // Where token (16 member + lane % 16) of a tile is: its page (-1 for none, -2 for one outside the
   // pool), its place there and the tile's key-value head.  Tables are read two tiles ahead of the
   // tile that is asked for, so that nothing waits for them.
   struct Place {
@@ -576,7 +596,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   const auto look_up = [&]() {
     Place p{-1, 0, ahead.kv};
     if (looked == count) return p;
-    const int t = ahead.tile * TILE + warp * 16 + (lane & 15);
+    const int t = ahead.tile * TILE + member * 16 + (lane & 15);
     if (ahead.tile < ahead.tiles && t < ahead.tokens) {
       const int at_page = by_page.quotient(t);
       p.place = t - at_page * c.page_size;
@@ -589,7 +609,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   const auto ask = [&](int stage, const Place &p) {
     if (!__any_sync(kAll, p.page != -1)) return;  // nothing of this warp's is read
     const char *from = nullptr;
-    if (p.page >= 0) from = pool + (uint64_t)p.page * c.page_bytes + p.kv * head_bytes + (uint64_t)p.place * D * sizeof(T);
+    if (p.page >= 0) from = pool + (uint64_t)p.page * c.page_bytes + p.kv * S::kSides * head_bytes + (uint64_t)p.place * D * sizeof(T);
     else if (p.page == -2) flag_error(kErrCacheId);
     const uint32_t to = stages + stage * S::kStage;
 #pragma unroll
@@ -612,10 +632,11 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   Queries<S> q, q_next;
   const auto queries_of = [&](const Cursor &x, Queries<S> &to) {
     if (x.row < a.n)
-      load_queries<T, S>(a, wide, x.row, x.kv * group + x.sub * S::kHeads, min(S::kHeads, group - x.sub * S::kHeads), to);
+      load_queries<T, S>(a, wide, x.row, (x.kv * S::kSides + side) * group + x.sub * S::kHeads,
+                         min(S::kHeads, group - x.sub * S::kHeads), to);
   };
   Cursor asking = at;  // whose queries were asked for last
-  if (at.tile == at.tiles) next_unit(asking);
+  if (at.tile >= at.tiles) next_unit(asking);
   queries_of(asking, q);
   if constexpr (kNextToo) {
     next_unit(asking);
@@ -651,14 +672,14 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     asm volatile("cp.async.commit_group;" ::: "memory");
     asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
     __syncwarp();
-    const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - warp * 16 : 0;
+    const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - member * 16 : 0;
     const uint32_t tile = stages + j % S::kStages * S::kStage;
     if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
     __syncwarp();
 
     const Cursor was = at;
     if (j + 1 < count) advance_at();
-    if (was.tile == was.tiles || (was.tile + 1 < was.tiles && j + 1 < count)) continue;
+    if (was.tile >= was.tiles || (was.tile + 1 < was.tiles && j + 1 < count)) continue;
     if (j + 1 + ends < count) {
       if constexpr (kNextToo) q = q_next;
       next_unit(asking);
@@ -666,70 +687,94 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     }
 
     // the warps' states together
-    const int x0 = lo + j - was.tile, w0 = shares.owner(x0), w1 = shares.owner(x0 + was.tiles - 1);
-    const int first_head = was.kv * group + was.sub * S::kHeads, heads = min(S::kHeads, group - was.sub * S::kHeads);
-    const bool whole = w0 == w1;
-    float *mine_part = part + (int64_t)(2 * (int)blockIdx.x + (lo > x0 ? 0 : 1)) * slot_floats;
+    const int x0 = lo + j - was.tile, x1 = x0 + was.tiles - 1;
+    const bool whole = lo <= x0 && x1 < lo + count;
+    const int first_head = (was.kv * S::kSides + side) * group + was.sub * S::kHeads;
+    const int heads = min(S::kHeads, group - was.sub * S::kHeads);
+    float *mine_part = part + ((int64_t)(2 * (int)blockIdx.x + (lo > x0 ? 0 : 1)) * S::kSides + side) * slot_floats;
     const int64_t first = (int64_t)was.row * a.q_heads + first_head;
 #pragma unroll
     for (int nt = 0; nt < S::NT; ++nt) {
-      __syncthreads();  // s_o may still be read
+      team_sync();  // s_o may still be read
+      float factor[2] = {1.0f, 1.0f};  // a warp alone normalises its values on their way to s_o
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float l = r.l[nt][e];
         l += __shfl_xor_sync(kAll, l, 4);
         l += __shfl_xor_sync(kAll, l, 8);
         l += __shfl_xor_sync(kAll, l, 16);
-        if (lane < 4) {
-          s_m[warp * 8 + lane * 2 + e] = r.m[nt][e];
-          s_l[warp * 8 + lane * 2 + e] = l;
+        const int h = lane * 2 + e;
+        if constexpr (S::kTeam > 1) {
+          if (lane < 4) {
+            s_m[member * 8 + h] = r.m[nt][e];
+            s_l[member * 8 + h] = l;
+          }
+        } else {
+          if (whole) factor[e] = l == 0.0f ? 0.0f : 1.0f / l;
+          if (lane < 4 && nt * 8 + h < heads) {
+            if (!whole) {
+              mine_part[nt * 8 + h] = r.m[nt][e];
+              mine_part[S::kHeads + nt * 8 + h] = l;
+            } else if (a.lse) {
+              a.lse[first + nt * 8 + h] = log_sum(r.m[nt][e], l);
+            }
+          }
         }
       }
 #pragma unroll
       for (int i = 0; i < S::DP / 16; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          s_o[(warp * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e];
-      __syncthreads();
-      for (int v = tid; v < 8 * kD4; v += S::kThreads) {
+          s_o[(member * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e] * factor[e & 1];
+      team_sync();
+      for (int v = rank; v < 8 * kD4; v += kTeamThreads) {
         const int h = v / kD4, d = v % kD4 * 4;
         if (nt * 8 + h >= heads || d >= D) continue;
-        float M = -INFINITY, L = 0.0f;
+        float4 o;
+        if constexpr (S::kTeam > 1) {
+          float M = -INFINITY, L = 0.0f;
 #pragma unroll
-        for (int w = 0; w < S::kWarps; ++w) M = fmaxf(M, s_m[w * 8 + h]);
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int w = 0; w < S::kTeam; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+          o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < S::kWarps; ++w) {
-          const float weight = part_weight(s_m[w * 8 + h], M);
-          L = fmaf(weight, s_l[w * 8 + h], L);
-          fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + d));
-        }
-        if (whole) {
-          store(normalised(o, L), (T *)a.out + (first + nt * 8 + h) * D + d);
-          if (d == 0 && a.lse) a.lse[first + nt * 8 + h] = log_sum(M, L);
-        } else {
-          *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
-          if (d == 0) {
+          for (int w = 0; w < S::kTeam; ++w) {
+            const float weight = part_weight(s_m[w * 8 + h], M);
+            L = fmaf(weight, s_l[w * 8 + h], L);
+            fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + d));
+          }
+          if (whole) o = normalised(o, L);
+          if (d == 0 && !whole) {
             mine_part[nt * 8 + h] = M;
             mine_part[S::kHeads + nt * 8 + h] = L;
+          } else if (d == 0 && a.lse) {
+            a.lse[first + nt * 8 + h] = log_sum(M, L);
           }
+        } else {
+          o = *reinterpret_cast<const float4 *>(s_o + h * S::kRow + d);
         }
+        if (whole) store(o, (T *)a.out + (first + nt * 8 + h) * D + d);
+        else *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
       }
     }
-    if (!whole && lo <= x0) begun = Split{was.row, was.kv, was.sub, w1};
+    if (!whole && lo <= x0) begun = Split{was.row, was.kv, was.sub, shares.owner(x1)};
     r.clear();
   }
 
   if (tid == 0) split[blockIdx.x] = begun;
 }
 
-// Joins the parts of what begins in one block and goes on in others: `per` blocks for each block of
-// attend_kernel, one for a head (of the kheads that a part has room for).  Warps (pairs of them for
-// more than 128 components) take the parts by turns.
+// Joins the parts of what begins in one block's share and goes on in others: `per` blocks for each
+// block of attend_kernel, one for a query head (of the kheads that a part has room for) of all `sides`
+// heads beside one another.  Warps (pairs of them for more than 128 components) take the sides and
+// the parts by turns, kBatch of them on their way at once.
+// Most blocks find nothing to join, and all that the SMs hold wait there for attend_kernel's end, so
+// there are to be many of them on an SM: 1,216 blocks took 9 us with the 80 registers of a batch of
+// 8, which only few rows in many parts want.
 constexpr int kJoinThreads = 256;
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(AttendArgs a, const Split *split, const float *part,
-                                                            int kheads, int per) {
+template <typename T, int kBatch>
+__global__ void __launch_bounds__(kJoinThreads, kBatch > 4 ? 3 : 6) join_kernel(AttendArgs a, const Split *split,
+                                                                              const float *part, int kheads, int per,
+                                                                              int sides) {
   __shared__ float4 s_o[kJoinThreads];
   __shared__ float s_m[kJoinThreads / 32], s_l[kJoinThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -737,22 +782,21 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttendArgs a, const 
   const Split x = split[w0];
   const int group = a.q_heads / a.c.n_kv_heads;
   if (x.row < 0 || h >= min(kheads, group - x.sub * kheads)) return;
-  const int wide = D > 128 ? 64 : 32, groups = kJoinThreads / wide, mine = threadIdx.x / wide;
+  const int wide = D > 128 ? 64 : 32, mine = threadIdx.x / wide, turns = kJoinThreads / wide / sides;
   const int d = threadIdx.x % wide * 4, slot_floats = kheads * (D + 2);
   float M = -INFINITY, L = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  constexpr int kBatch = 8;  // parts on their way at once
-  for (int w = w0 + mine; w <= x.last; w += groups * kBatch) {
+  for (int w = w0 + mine / sides; w <= x.last; w += turns * kBatch) {
     float m[kBatch], l[kBatch];
     float4 y[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const int from = w + u * groups;
+      const int from = w + u * turns;
       m[u] = -INFINITY;
       l[u] = 0.0f;
       y[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       if (from <= x.last) {
-        const float *p = part + (int64_t)(2 * from + (from == w0 ? 1 : 0)) * slot_floats;
+        const float *p = part + ((int64_t)(2 * from + (from == w0 ? 1 : 0)) * sides + mine % sides) * slot_floats;
         m[u] = p[h];
         l[u] = p[kheads + h];
         if (d < D) y[u] = *reinterpret_cast<const float4 *>(p + 2 * kheads + h * D + d);
@@ -778,39 +822,33 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttendArgs a, const 
     s_l[mine] = L;
   }
   __syncthreads();
-  if (threadIdx.x >= wide || d >= D) return;
+  if (mine >= sides || d >= D) return;  // the first turns of the sides go on
   M = -INFINITY;
   L = 0.0f;
   o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int g = 0; g < groups; ++g) M = fmaxf(M, s_m[g]);
-  for (int g = 0; g < groups; ++g) {
-    const float weight = part_weight(s_m[g], M);
-    L = fmaf(weight, s_l[g], L);
-    fma4(o, weight, s_o[g * wide + threadIdx.x]);
+  for (int t = 0; t < turns; ++t) M = fmaxf(M, s_m[t * sides + mine]);
+  for (int t = 0; t < turns; ++t) {
+    const float weight = part_weight(s_m[t * sides + mine], M);
+    L = fmaf(weight, s_l[t * sides + mine], L);
+    fma4(o, weight, s_o[t * sides * wide + threadIdx.x]);
   }
-  const int64_t head = (int64_t)x.row * a.q_heads + x.kv * group + x.sub * kheads + h;
+  const int64_t head = (int64_t)x.row * a.q_heads + (x.kv * sides + mine) * group + x.sub * kheads + h;
   store(normalised(o, L), (T *)a.out + head * D + d);
   if (d == 0 && a.lse) a.lse[head] = log_sum(M, L);
 }
 
 namespace {
 
-// Blocks that the GPU runs at once, and how many of them the tiles that the tables have room for
-// can feed.
-template <typename S>
-unsigned attend_blocks(const Cache &c, int n, int units) {
-  const int64_t room = (int64_t)c.table_width * c.page_size, tiles = (room + S::kTile - 1) / S::kTile;
-  const int64_t most = (int64_t)n * units * tiles, run = (int64_t)kSMs * S::kPerSm;
-  return (unsigned)(most < run ? most : run);
-}
-
-template <typename T, int DP, int NT>
+template <typename T, int DP, int NT, bool kBeside>
 cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
-  using S = Shape<T, DP, NT>;
+  using S = Shape<T, DP, NT, kBeside>;
   const int group = a.q_heads / a.c.n_kv_heads, groups = (group + S::kHeads - 1) / S::kHeads;
-  const unsigned blocks = attend_blocks<S>(a.c, a.n, a.c.n_kv_heads * groups);
+  // blocks that the GPU runs at once, or fewer where the tables have no room for so many tiles
+  const int64_t room = (int64_t)a.c.table_width * a.c.page_size, tiles = (room + S::kTile - 1) / S::kTile;
+  const int64_t most = (int64_t)a.n * (a.c.n_kv_heads / S::kSides) * groups * tiles;
+  const unsigned blocks = (unsigned)(most < kSMs * S::kPerSm ? most : kSMs * S::kPerSm);
   if (bytes) {
-    *bytes = blocks * sizeof(Split) + (size_t)2 * blocks * S::kHeads * (a.c.head_dim + 2) * 4;
+    *bytes = blocks * sizeof(Split) + (size_t)2 * blocks * S::kSides * S::kHeads * (a.c.head_dim + 2) * 4;
     return cudaSuccess;
   }
   cudaError_t e = allow_smem((const void *)attend_kernel<T, S>, S::kSmem, S::kSmem);
@@ -819,7 +857,7 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
   float *part = (float *)(split + blocks);
   attend_kernel<T, S><<<blocks, S::kThreads, S::kSmem, s>>>(a, split, part, groups, Divisor(a.c.page_size));
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  if ((int64_t)a.c.table_width * a.c.page_size <= S::kTile) return cudaSuccess;  // a row is one tile
+  if (tiles <= 1) return cudaSuccess;  // nothing is split
   cudaLaunchConfig_t cfg{};
   const int per = S::kHeads < group ? S::kHeads : group;
   cfg.gridDim = dim3(blocks * per);
@@ -830,7 +868,17 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, join_kernel<T>, a, (const Split *)split, (const float *)part, S::kHeads, per);
+  const auto join = blocks >= 16 * (int64_t)a.n * a.c.n_kv_heads * groups ? join_kernel<T, 8> : join_kernel<T, 4>;
+  return cudaLaunchKernelEx(&cfg, join, a, (const Split *)split, (const float *)part, S::kHeads, per, S::kSides);
+}
+
+// Heads side by side where each block that runs at once has a row's to itself.
+template <typename T, int DP>
+cudaError_t one_group(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
+  using S = Shape<T, DP, 1, true>;
+  if (a.c.n_kv_heads % S::kSides == 0 && (int64_t)a.n * (a.c.n_kv_heads / S::kSides) >= kSMs * S::kPerSm)
+    return launch<T, DP, 1, true>(a, ws, s, bytes);
+  return launch<T, DP, 1, false>(a, ws, s, bytes);
 }
 
 // Up to 8 query heads of a key-value head at a time, or 16 where it has more (each further group
@@ -839,11 +887,11 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
 template <typename T>
 cudaError_t by_shape(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   const bool many = a.q_heads / a.c.n_kv_heads > 8;
-  if (a.c.head_dim <= 64) return many ? launch<T, 64, 2>(a, ws, s, bytes) : launch<T, 64, 1>(a, ws, s, bytes);
-  if (a.c.head_dim <= 96) return many ? launch<T, 96, 2>(a, ws, s, bytes) : launch<T, 96, 1>(a, ws, s, bytes);
-  if (a.c.head_dim <= 128) return many ? launch<T, 128, 2>(a, ws, s, bytes) : launch<T, 128, 1>(a, ws, s, bytes);
-  if (a.c.head_dim <= 192) return launch<T, 192, 1>(a, ws, s, bytes);
-  return launch<T, 256, 1>(a, ws, s, bytes);
+  if (a.c.head_dim <= 64) return many ? launch<T, 64, 2, false>(a, ws, s, bytes) : one_group<T, 64>(a, ws, s, bytes);
+  if (a.c.head_dim <= 96) return many ? launch<T, 96, 2, false>(a, ws, s, bytes) : one_group<T, 96>(a, ws, s, bytes);
+  if (a.c.head_dim <= 128) return many ? launch<T, 128, 2, false>(a, ws, s, bytes) : one_group<T, 128>(a, ws, s, bytes);
+  if (a.c.head_dim <= 192) return launch<T, 192, 1, false>(a, ws, s, bytes);
+  return launch<T, 256, 1, false>(a, ws, s, bytes);
 }
 
 cudaError_t dispatch(int dtype, const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {

@@ -270,10 +270,12 @@ def test_attention_matches_64_bits(copes, heads, kv, d, ps, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,longest,heads,kv,d,ps", [(1, 20011, 32, 8, 128, 16), (1, 9001, 2, 1, 64, 16), (3, 7013, 14, 2, 64, 7),
-                                                     (200, 90, 4, 2, 64, 16), (2, 4099, 12, 4, 256, 48)])
+                                                     (200, 90, 4, 2, 64, 16), (2, 4099, 12, 4, 256, 48),
+                                                     (1000, 60, 4, 2, 64, 16), (420, 150, 12, 4, 128, 16), (500, 3000, 12, 4, 80, 16),
+                                                     (470, 2000, 24, 8, 64, 7)])
 def test_attention_split_over_long_and_many_sequences(copes, n, longest, heads, kv, d, ps, dtype):
     rng = np.random.default_rng(n)
-    lens = rng.integers(0, longest + 1, n)
+    lens = rng.integers(0, min(longest, 200) + 1 if n > 100 else longest + 1, n)
     lens[-1] = longest
     cache = filled(copes, lens, 1, kv, ps, d, dtype, seed=n)
     q = (torch.randn(n, heads, d, device="cuda") * 3).to(DT[dtype])
