@@ -22,7 +22,7 @@
 // its own running maximum, sum and output, so that the warps need each other only at the end of
 // a row.  Where there are rows enough, they do not need each other at all: each warp has a key-value
 // head to itself, of as many heads side by side as a block has warps, with tiles of 16 tokens (1,024
-// rows of up to 100 tokens: TODO us with the warps on one head, TODO us so; fewer, longer rows would be cut
+// rows of up to 100 tokens: 90 us with the warps on one head, 55 us so; fewer, longer rows would be cut
 // into four times the parts).  Keys are the rows of the first product and the query heads its columns,
 // S^T[token][head] = K Q^T, and in the second O^T[d][head] = V^T P^T: 8 heads fill a tile of the
 // matrix unit, where heads as rows would fill half of 16.  P^T is S^T's registers transposed in
@@ -872,11 +872,13 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
   return cudaLaunchKernelEx(&cfg, join, a, (const Split *)split, (const float *)part, S::kHeads, per, S::kSides);
 }
 
-// Heads side by side where each block that runs at once has a row's to itself.
+// Heads side by side where there are three rows' for four of the blocks that run at once (32/8 heads
+// of 128, us on one head and side by side: 80 rows of up to 300 tokens 18.7, 20.4; 128 of them 25.7,
+// 25.2; 512 72.7, 64.2; 128 of up to 8,000 321.8, 318.8; 1,024 of up to 100 90, 55).
 template <typename T, int DP>
 cudaError_t one_group(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   using S = Shape<T, DP, 1, true>;
-  if (a.c.n_kv_heads % S::kSides == 0 && (int64_t)a.n * (a.c.n_kv_heads / S::kSides) >= kSMs * S::kPerSm)
+  if (a.c.n_kv_heads % S::kSides == 0 && (int64_t)a.n * (a.c.n_kv_heads / S::kSides) * 4 >= 3 * kSMs * S::kPerSm)
     return launch<T, DP, 1, true>(a, ws, s, bytes);
   return launch<T, DP, 1, false>(a, ws, s, bytes);
 }
