@@ -3,10 +3,10 @@
 // For a row's query heads h of one key-value head, over its tokens t:
 //   s_t = scale q.k_t,  out = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),  m = max_t s_t.
 // Every key and value is read once, for up to 8 or 16 query heads together: 2 flops per value
-// and head, 32 flops a byte at 8 heads of bf16.  That is past the fp32 units at the rate of HBM
-// (54 TFLOP/s at 6.8 TB/s), and 3% of the tensor cores': the bound is HBM, and mma.sync on
-// registers filled from shared memory is enough (tcgen05 takes 64 rows or more of one operand;
-// a group of query heads has 1 to 16).
+// and head, 8 flops a byte at 8 heads of bf16.  At the rate of HBM, 6.8 TB/s, that is two thirds of
+// the fp32 units' whole rate before a single conversion, and 3% of the tensor cores': the bound is
+// HBM, and mma.sync on registers filled from shared memory is enough (tcgen05 takes 64 rows or more
+// of one operand; a group of query heads has 1 to 16, and a block of these has no room to wait in).
 //
 // Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
 // are shared out evenly among as many blocks as the GPU runs at once, whatever the lengths are.
@@ -14,7 +14,7 @@
 // (not where every tile has a block of its own): 32 rows of up to 4,096 tokens took 61 us without
 // it, a block with many short rows 67 us where the others took 39.
 // A (row, head group) whose tiles lie in several blocks is joined, over the parts in order, by a
-// second kernel, which is on the GPU by the time the first ends (a dependent launch).  (Joined by
+// second kernel, whose blocks move in as the first's end (a dependent launch).  (Joined by
 // the last of its blocks, counted by an atomic, 60 parts of 16 heads took that block 25 us, and
 // few parts 3 us.)
 //
