@@ -7,6 +7,8 @@
 // the fp32 units' whole rate before a single conversion, and 3% of the tensor cores': the bound is
 // HBM, and mma.sync on registers filled from shared memory is enough (tcgen05 takes 64 rows or more
 // of one operand; a group of query heads has 1 to 16, and a block of these has no room to wait in).
+// Measured: 128 rows of up to 16,384 tokens, 32/8 heads of 128, bf16: 4.24 GB in 628 us, 6.75 TB/s;
+// fp32, 32 rows of up to 34,629, heads of 80: 97% of the rate of a copy; heads of 256: 53%.
 //
 // Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
 // are shared out evenly among as many blocks as the GPU runs at once, whatever the lengths are.
