@@ -7,8 +7,8 @@
 // g = scale (m' - m) log2 e (h' = 2^-g (h - g s)), so each logit is read once.  y is held at
 // kLeast or above, where 2^y is 0: a masked token adds 0 to both sums.  A logit costs
 // one exponential and about six more instructions, and HBM bounds it: 4,096 rows of 151,936 in bf16
-// take 189 us, 6.6 TB/s (a plain copy: 6.8), and 221 us, 5.6 TB/s, with 20 alternatives, with 62%
-// of the issue slots and 26% of the special-function units busy.
+// take 180 us, 6.9 TB/s (a plain copy: 6.8), and 215 us, 5.8 TB/s, with 20 alternatives: the ends
+// of the rows, chains of loads and barriers, are partly hidden by the other blocks of an SM.
 //
 // The alternatives need no second pass over the row: while it is read, the maximum of every cell
 // (a thread's pieces of one step, or of a few) is kept in shared memory, and each thread's over
@@ -35,11 +35,15 @@ constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMostThreads = 256, kMostWarps = kMostThreads / 32;
 // blocks of an SM: with a thread's next step on its way (shallow), or the next two (deep)
 constexpr int per_sm(bool deep) { return deep ? 3 : 4; }
-constexpr int kThreadCells = 32;   // of a thread, at most
-constexpr int kReached = 1024;     // cells read again by the fast way, at most
-constexpr int kCandidates = 512;   // logits ranked by counting, at most
+constexpr int kThreadCells = 48;   // of a thread, at most
+constexpr int kReached = 512;      // cells read again by the fast way, at most
+constexpr int kCandidates = 320;   // logits ranked by counting, at most
 constexpr int kClusterMost = 8;
 constexpr int kLoads = 4;          // 16-byte pieces of a lane in one step
+// Shared memory of an SM that its blocks' cells may fill.  The rest of the 228 KB holds what loads
+// have on their way: 1,216 rows of 151,936 with 20 alternatives take 67.5 us with 132 KB for the
+// cells, 74.7 with 227, and 68.6 with 100, where cells of twice the size are read again.
+constexpr int kShared = 132 << 10;
 constexpr int kStep = kLoads * 32;  // pieces of a warp in one step
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -127,6 +131,20 @@ __device__ __forceinline__ float max_of(const Piece<T> &p) {
   }
 }
 
+// A logit as it is kept in shared memory: in the logits' own bits.
+template <typename T>
+struct Kept {
+  using Bits = uint32_t;
+  __device__ static Bits from(float x) { return __float_as_uint(x); }
+  __device__ static float to(Bits b) { return __uint_as_float(b); }
+};
+template <>
+struct Kept<__nv_bfloat16> {
+  using Bits = uint16_t;
+  __device__ static Bits from(float x) { return (uint16_t)(__float_as_uint(x) >> 16); }
+  __device__ static float to(Bits b) { return __uint_as_float((uint32_t)b << 16); }
+};
+
 template <typename T>
 __device__ __forceinline__ Piece<T> load_piece(const void *at) {
   Piece<T> p;
@@ -150,18 +168,23 @@ struct Row {
   __device__ int first(int v) const { return v * Piece<T>::kN - shift; }
   // what lies outside the row reads as -inf
   __device__ __forceinline__ Piece<T> load(int v) const {
-    Piece<T> p;
+    Piece<T> p{};
     const int j = first(v);
     if (j >= 0 && j + Piece<T>::kN <= vocab) return load_piece<T>(x + j);
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 2) {
+      for (int i = 0; i < 4; ++i)
+        p.r[i] = j + i >= 0 && j + i < vocab ? reinterpret_cast<const uint32_t *>(x)[j + i] : 0xFF800000u;
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {  // few pieces of a row: short code
         uint32_t u = 0xFF80u, w = 0xFF80u;
         if (j + 2 * i >= 0 && j + 2 * i < vocab) u = reinterpret_cast<const uint16_t *>(x)[j + 2 * i];
         if (j + 2 * i + 1 >= 0 && j + 2 * i + 1 < vocab) w = reinterpret_cast<const uint16_t *>(x)[j + 2 * i + 1];
-        p.r[i] = u | w << 16;
-      } else {
-        p.r[i] = j + i >= 0 && j + i < vocab ? reinterpret_cast<const uint32_t *>(x)[j + i] : 0xFF800000u;
+        p.r[0] = p.r[1];
+        p.r[1] = p.r[2];
+        p.r[2] = p.r[3];
+        p.r[3] = u | w << 16;
       }
     }
     return p;
@@ -206,12 +229,13 @@ __device__ __forceinline__ Sums warp_join(const Sums *from, int n, float c) {
 static_assert(kMostWarps <= 8 && kClusterMost <= 8, "warp_join adds up 8 lanes");
 
 struct LogprobShared {
-  alignas(16) uint64_t candidate[kCandidates];
-  alignas(16) uint64_t theirs[kClusterMost * COPES_MAX_TOP];  // of the cluster's blocks, in the first
+  union {
+    alignas(16) uint64_t candidate[kCandidates];
+    int group[2][kMostThreads];  // read before there are candidates
+  };
   uint64_t top[COPES_MAX_TOP];
   uint16_t reached[kReached];  // cells that reach the bound
   Sums sums[kClusterMost];
-  int group[2][kMostThreads];
   int bound;
   Sums warp[kMostWarps];
   uint64_t best[kMostWarps];
@@ -267,14 +291,14 @@ __device__ __forceinline__ void visit_piece(const Row<T> &row, int v, int least,
 // listed.  Where most of them equal it (masked tokens, with fewer than k others): those that surpass
 // it and, in the order of the indices, the first that equal it.  Else one after the other.
 template <typename T>
-__device__ __noinline__ void find_top_slowly(LogprobShared &sh, const float *cell, const Row<T> &row, int v0, int n,
+__device__ __noinline__ void find_top_slowly(LogprobShared &sh, const typename Kept<T>::Bits *cell, const Row<T> &row, int v0, int n,
                                              int merge, int bound, int k) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   // visits the thread's own logits of order `least` and above, by its cells' maxima
   const auto each = [&](int least, auto visit) {
     const int steps = (n + kStep * warps - 1) / (kStep * warps);
     for (int step = 0; step < steps; ++step) {
-      if (order_of(cell[(step >> merge) * blockDim.x + tid]) < least) continue;
+      if (order_of(Kept<T>::to(cell[(step >> merge) * blockDim.x + tid])) < least) continue;
       for (int u = 0; u < kLoads; ++u) {
         const int v = ((step * warps + warp) * kLoads + u) * 32 + lane;
         if (v < n) visit_piece(row, v0 + v, least, visit);
@@ -364,7 +388,7 @@ __device__ __forceinline__ int kth_of_64(int a, int b, int k) {
 // The block's alternatives into sh.top, from the cells' maxima of pieces [v0, v0 + n) and `own`,
 // this thread's over all, in two halves.  cell[j blockDim + tid]: steps j 2^merge and on of the thread.
 template <typename T>
-__device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, const Row<T> &row, int v0, int n, int merge,
+__device__ __forceinline__ void find_top(LogprobShared &sh, const typename Kept<T>::Bits *cell, const Row<T> &row, int v0, int n, int merge,
                                          const float (&own)[2], int k) {
   constexpr int N = Piece<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
@@ -383,15 +407,15 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
   __syncthreads();
   const int bound = sh.bound;
   {
-    unsigned mine = 0;  // which of the thread's cells, at most kThreadCells
+    uint64_t mine = 0;  // which of the thread's cells, at most kThreadCells
     if (order_of(max_nan(own[0], own[1])) >= bound) {
       const int steps = (n + kStep * warps - 1) / (kStep * warps), cells = (steps + (1 << merge) - 1) >> merge;
 #pragma unroll 4
-      for (int j = 0; j < cells; ++j) mine |= (unsigned)(order_of(cell[j * threads + tid]) >= bound) << j;
+      for (int j = 0; j < cells; ++j) mine |= (uint64_t)(order_of(Kept<T>::to(cell[j * threads + tid])) >= bound) << j;
     }
-    int at = warp_reserve(__popc(mine), &sh.n_reached);
+    int at = warp_reserve(__popcll(mine), &sh.n_reached);
     for (; mine; mine &= mine - 1, ++at)
-      if (at < kReached) sh.reached[at] = (uint16_t)((__ffs(mine) - 1) * threads + tid);
+      if (at < kReached) sh.reached[at] = (uint16_t)((__ffsll(mine) - 1) * threads + tid);
   }
   __syncthreads();
   const int reached = sh.n_reached;
@@ -444,8 +468,9 @@ __device__ __forceinline__ void find_top(LogprobShared &sh, const float *cell, c
 constexpr int kAhead = 48 << 10;
 
 template <typename T, bool kTop, bool kDeep>
-__global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(LogprobArgs a, int parts, int merge, int apart) {
-  extern __shared__ float cell[];
+__global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(LogprobArgs a, int parts, int merge, int apart, int cell_bytes) {
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  auto *const cell = reinterpret_cast<typename Kept<T>::Bits *>(dynamic);
   __shared__ LogprobShared sh;
   constexpr int N = Piece<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, stride = warps * kStep;
@@ -464,7 +489,7 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   Sums t{-FLT_MAX, 0.0f, 0.0f};
   float own[2] = {-INFINITY, -INFINITY};
   uint64_t s2 = 0, h2 = 0;
-  Piece<T> now[kLoads], next[kLoads], then[kDeep ? kLoads : 1];
+  Piece<T> now[kLoads], next[kLoads], then[kLoads];
   const auto fetch = [&](int base, Piece<T>(&to)[kLoads]) {
     if (base >= full0 && base + kStep <= full1) {
 #pragma unroll
@@ -490,19 +515,14 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
     if (tid == 0) sh.n_reached = sh.n_candidates = 0;
   }
   int step = 0;
-  for (int base = warp * kStep; base < n; base += stride, ++step) {
-    if constexpr (kDeep) {
-      if (base + 2 * stride < n) fetch(base + 2 * stride, then);
-    } else {
-      if (base + stride < n) fetch(base + stride, next);
-    }
-    const float half[2] = {max_nan(max_of(now[0]), max_of(now[1])), max_nan(max_of(now[2]), max_of(now[3]))};
+  const auto take = [&](const Piece<T>(&p)[kLoads]) {
+    const float half[2] = {max_nan(max_of(p[0]), max_of(p[1])), max_nan(max_of(p[2]), max_of(p[3]))};
     const float most = max_nan(half[0], half[1]);
     if (kTop) {
       own[0] = max_nan(own[0], half[0]);
       own[1] = max_nan(own[1], half[1]);
-      float *to = cell + (step >> merge) * blockDim.x + tid;
-      *to = step & ((1 << merge) - 1) ? max_nan(*to, most) : most;
+      auto *to = cell + (step >> merge) * blockDim.x + tid;
+      *to = Kept<T>::from(step & ((1 << merge) - 1) ? max_nan(Kept<T>::to(*to), most) : most);
     }
     const float M = max_nan(t.m, warp_max_nan(most));
     if (!(M == t.m)) {  // the same for the whole warp
@@ -522,18 +542,39 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
 #pragma unroll
       for (int e = 0; e < N / 2; ++e) {
         float x, y;
-        pair_of(now[u], e, x, y);
+        pair_of(p[u], e, x, y);
         unpack2(mul2(add2(pack2(x, y), minus_m), c2), x, y);
         x = max_nan(x, kLeast);
         y = max_nan(y, kLeast);
-        const uint64_t p = pack2(exp2_fast(x), exp2_fast(y));
-        s2 = add2(s2, p);
-        h2 = fma2(p, pack2(x, y), h2);
+        const uint64_t q = pack2(exp2_fast(x), exp2_fast(y));
+        s2 = add2(s2, q);
+        h2 = fma2(q, pack2(x, y), h2);
       }
+    ++step;
+  };
+  // The buffers take turns (4,096 rows: 180 us, where each moves on 188; 1,216 with 20 alternatives 69
+  // and 73).  With two steps ahead and alternatives each moves on: three copies of that loop beside
+  // the end of a row are too much code (225 us in turns, 215 so).
+  for (int base = warp * kStep; base < n;) {
+    const auto turn = [&](const Piece<T>(&p)[kLoads], Piece<T>(&later)[kLoads]) {
+      if (base + (kDeep ? 2 : 1) * stride < n) fetch(base + (kDeep ? 2 : 1) * stride, later);
+      take(p);
+      base += stride;
+      return base < n;
+    };
+    if constexpr (kDeep && kTop) {
+      if (!turn(now, then)) break;
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      now[u] = next[u];
-      if constexpr (kDeep) next[u] = then[u];
+      for (int u = 0; u < kLoads; ++u) {
+        now[u] = next[u];
+        next[u] = then[u];
+      }
+    } else if constexpr (kDeep) {
+      if (!turn(now, then) || !turn(next, now)) break;
+      turn(then, next);
+    } else {
+      if (!turn(now, next)) break;
+      turn(next, now);
     }
   }
   if (tid == 0 && i + apart < a.n) {
@@ -544,7 +585,7 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   }
   if (kTop) {  // a thread's steps past its last hold nothing
     const int steps = (n + stride - 1) / stride, cells = (steps + (1 << merge) - 1) >> merge;
-    for (int j = (step + (1 << merge) - 1) >> merge; j < cells; ++j) cell[j * blockDim.x + tid] = -INFINITY;
+    for (int j = (step + (1 << merge) - 1) >> merge; j < cells; ++j) cell[j * blockDim.x + tid] = Kept<T>::from(-INFINITY);
   }
   float odd_s, odd_h;
   unpack2(s2, t.s, odd_s);
@@ -562,20 +603,21 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   if (kTop) find_top(sh, cell, row, v0, n, merge, own, a.top);
 
   if (parts > 1) {
+    uint64_t *const theirs = reinterpret_cast<uint64_t *>(dynamic + cell_bytes);  // of the cluster's blocks, in the first
     cluster_wait();  // the first block has begun
     const uint32_t to = in_first(&sh.sums[part]);
     if (tid < 3)
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * tid), "f"(tid == 0 ? t.m : tid == 1 ? t.s : t.h)
                    : "memory");
     if (kTop && tid < a.top)
-      asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(in_first(&sh.theirs[part * a.top + tid])), "l"(sh.top[tid])
+      asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(in_first(theirs + part * a.top + tid)), "l"(sh.top[tid])
                    : "memory");
     cluster_arrive();
     cluster_wait();
     if (part) return;
     t = warp_join(sh.sums, parts, c);
     if (kTop) {
-      rank_by_counting(sh.theirs, parts * a.top, a.top, sh.top);  // sh.top was read before the barrier
+      rank_by_counting(theirs, parts * a.top, a.top, sh.top);  // sh.top was read before the barrier
       __syncthreads();
     }
   }
@@ -601,9 +643,10 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   }
 }
 
-// How a call is cut: blocks of a row, threads of a block, one step ahead or two, steps that share a cell.
+// How a call is cut: blocks of a row, threads of a block, 2^merge steps that share a cell, blocks the
+// GPU runs at once, one step ahead or two.
 struct Cut {
-  int parts, threads, merge, apart;
+  int parts, threads, merge, at_once;
   bool deep;
   uint32_t cell_bytes;
 };
@@ -623,8 +666,8 @@ struct Cut {
 //   20,000 x 32,003                                296, 252, 292, 396
 //   500 x 7,500                                    9.3, 8.0, 7.4, 7.6
 // and steps ahead, 500 x 151,936 (one wave or two): 38 with one, 45 with two; 734 x 151,936: 58, 47.
-static Cut cut_of(int64_t n, int64_t pieces, bool top) {
-  Cut best{1, 32, 0, 0, false, 0};
+static Cut cut_of(int64_t n, int64_t pieces, bool top, int size) {
+  Cut best{1, 32, 0, 152, false, 0};
   double least = 0.0;
   for (int parts = 1; parts <= kClusterMost && (parts == 1 || pieces / parts >= 256); parts *= 2) {
     const int64_t mine = pieces / parts + 1;
@@ -639,21 +682,24 @@ static Cut cut_of(int64_t n, int64_t pieces, bool top) {
                             (deep || !longer ? 1.0 : threads <= 64 ? 1.15 : 1.05);
         if (least == 0.0 || cost < least) {
           least = cost;
-          best = Cut{parts, threads, 0, (int)(at_once / parts), deep != 0, 0};
+          best = Cut{parts, threads, 0, (int)at_once, deep != 0, 0};
         }
       }
   }
   const int64_t mine = pieces / best.parts + 1, steps = (mine + best.threads * kLoads - 1) / (best.threads * kLoads);
-  while ((steps + (1 << best.merge) - 1) >> best.merge > kThreadCells) ++best.merge;
-  best.cell_bytes = (uint32_t)((steps + (1 << best.merge) - 1) >> best.merge) * best.threads * 4;
+  const int64_t room = kShared / (best.at_once / 152) - 1024 - (int64_t)sizeof(LogprobShared);
+  // few cells are not worth merging: what they save is less than an SM has
+  const auto cells = [&] { return (steps + (1 << best.merge) - 1) >> best.merge; };
+  while (cells() > kThreadCells || (cells() > 8 && cells() * best.threads * size > room)) ++best.merge;
+  best.cell_bytes = top ? (uint32_t)cells() * best.threads * size : 0;
   return best;
 }
 
 template <typename T, bool kTop, bool kDeep>
 static cudaError_t launch(const LogprobArgs &a, const Cut &c, cudaStream_t s) {
   const auto kernel = logprob_kernel<T, kTop, kDeep>;
-  const uint32_t bytes = kTop ? c.cell_bytes : 0, fixed = sizeof(LogprobShared);
-  const cudaError_t e = allow_smem((const void *)kernel, bytes + fixed, kThreadCells * kMostThreads * 4);
+  const uint32_t bytes = c.cell_bytes + (kTop && c.parts > 1 ? c.parts * a.top * 8 : 0), fixed = sizeof(LogprobShared);
+  const cudaError_t e = allow_smem((const void *)kernel, bytes + fixed, kThreadCells * kMostThreads * 4 + kClusterMost * COPES_MAX_TOP * 8);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)a.n * c.parts);
@@ -666,12 +712,12 @@ static cudaError_t launch(const LogprobArgs &a, const Cut &c, cudaStream_t s) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = c.parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, a, c.parts, c.merge, c.apart);
+  return cudaLaunchKernelEx(&cfg, kernel, a, c.parts, c.merge, c.at_once / c.parts, (int)c.cell_bytes);
 }
 
 template <typename T, bool kTop>
 static cudaError_t launch_any(const LogprobArgs &a, cudaStream_t s) {
-  const Cut c = cut_of(a.n, (int64_t)a.vocab / Piece<T>::kN + 2, kTop);
+  const Cut c = cut_of(a.n, (int64_t)a.vocab / Piece<T>::kN + 2, kTop, sizeof(T));
   return c.deep ? launch<T, kTop, true>(a, c, s) : launch<T, kTop, false>(a, c, s);
 }
 
