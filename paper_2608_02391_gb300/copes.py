@@ -566,19 +566,21 @@ def update(arena: Arena, sub: SubspaceHandle, noise_id: np.ndarray, sign: np.nda
 _DTYPE_CODES = {torch.bfloat16: BF16, torch.float32: FP32}
 
 
-@functools.lru_cache(maxsize=256)
 def _template(shape, dtype, device) -> torch.Tensor:
     """A tensor of this shape in one element of memory, for empty_like: that call takes about 2 us
     less than empty() with its keywords, which a call of a few microseconds notices."""
     return torch.empty((), dtype=dtype, device=device).expand(shape)
 
 
-def _empty(shape, dtype, device, stream) -> torch.Tensor:
+_empty_like, _contiguous = torch.empty_like, torch.contiguous_format
+
+
+def _empty(template: torch.Tensor, stream) -> torch.Tensor:
     """A contiguous output of a call on `stream`, allocated in that stream's order."""
     if stream is None:
-        return torch.empty_like(_template(shape, dtype, device), memory_format=torch.contiguous_format)
+        return _empty_like(template, memory_format=_contiguous)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty_like(template, memory_format=_contiguous)
 
 
 class KVCache:
@@ -605,7 +607,8 @@ class KVCache:
             raise CopesError(ERR_INVALID_ARG, last_error())
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=pool.device)
         self.attend_workspace = None  # paged_attention's
-        self._attend_bytes = {}       # (rows, query heads) -> bytes of it
+        self._attend_room = 0         # its bytes
+        self._attend_kept = {}        # (rows, query heads) -> bytes of it, templates of out and lse
 
     @classmethod
     def empty(cls, n_pages: int, n_layers: int, n_kv_heads: int, page_size: int, head_dim: int, n_slots: int,
@@ -623,20 +626,30 @@ class KVCache:
         assert n is None or t.numel() == n
         return t.data_ptr()
 
-    def attend_space(self, n: int, q_heads: int, stream=None) -> Tuple[int, int]:
-        """paged_attention's workspace (address, bytes), allocated where it has to grow."""
-        need = self._attend_bytes.get((n, q_heads))
-        if need is None:
+    def _attend_shapes(self, n: int, q_heads: int) -> Tuple[int, torch.Tensor, torch.Tensor]:
+        """What a call of these sizes needs: bytes of the workspace, templates of out and lse."""
+        kept = self._attend_kept.get((n, q_heads))
+        if kept is None:
             need = load().copes_paged_attention_workspace_bytes(self.ref, n, q_heads)
             if need == 0:
                 raise CopesError(ERR_INVALID_ARG, last_error())
-            self._attend_bytes[n, q_heads] = need
+            if len(self._attend_kept) >= 256:
+                self._attend_kept.clear()
+            kept = self._attend_kept[n, q_heads] = (
+                need, _template((n, q_heads, self.desc.head_dim), self.pool.dtype, self.pool.device),
+                _template((n, q_heads), torch.float32, self.pool.device))
+        return kept
+
+    def attend_space(self, n: int, q_heads: int, stream=None) -> Tuple[int, int]:
+        """paged_attention's workspace (address, bytes), allocated where it has to grow."""
+        need = self._attend_shapes(n, q_heads)[0]
         ws = self.attend_workspace
-        if ws is None or ws.numel() < need:
+        if self._attend_room < need:
             if ws is not None and stream is not None:
                 ws.record_stream(stream)
-            ws = self.attend_workspace = _empty((need,), torch.uint8, self.pool.device, stream)
-        return ws.data_ptr(), ws.numel()
+            ws = self.attend_workspace = _empty(_template((need,), torch.uint8, self.pool.device), stream)
+            self._attend_room = need
+        return ws.data_ptr(), self._attend_room
 
 
 def cache_grow(cache: KVCache, slots: torch.Tensor, add, stream=None) -> None:
@@ -694,12 +707,13 @@ def paged_attention(cache: KVCache, layer: int, q: torch.Tensor, slots: Optional
     n, heads, d = q.shape
     assert d == cache.desc.head_dim and q.dtype == cache.pool.dtype and q.device == cache.pool.device
     assert q.stride(2) == 1
+    _, like_out, like_lse = cache._attend_shapes(n, heads)
     if out is None:
-        out = _empty((n, heads, d), q.dtype, q.device, stream)
+        out = _empty(like_out, stream)
     else:
         assert out.shape == q.shape and out.dtype == q.dtype and out.device == q.device and out.is_contiguous()
     if lse is None:
-        lse = _empty((n, heads), torch.float32, q.device, stream)
+        lse = _empty(like_lse, stream)
     else:
         assert lse.shape == (n, heads) and lse.dtype == torch.float32 and lse.device == q.device and lse.is_contiguous()
     ws, nbytes = cache.attend_space(n, heads, stream)
@@ -719,6 +733,12 @@ class TokenLogprobs:
     top_logprobs: torch.Tensor
 
 
+@functools.lru_cache(maxsize=256)
+def _logprob_templates(n: int, top: int, device) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    return (_template((n,), torch.float32, device), _template((n, top), torch.int64, device),
+            _template((n, top), torch.float32, device))
+
+
 def token_logprobs(logits: torch.Tensor, target: torch.Tensor, top: int = 0, scale: float = 1.0,
                    stream=None) -> TokenLogprobs:
     """copes_token_logprobs: log probability of target[i] (int64, negative: padding) and entropy
@@ -729,10 +749,9 @@ def token_logprobs(logits: torch.Tensor, target: torch.Tensor, top: int = 0, sca
     assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
     assert target.shape == (n,) and target.dtype == torch.int64 and target.device == device and target.is_contiguous()
     dtype = _DTYPE_CODES[logits.dtype]
-    logprob = _empty((n,), torch.float32, device, stream)
-    entropy = _empty((n,), torch.float32, device, stream)
-    ids = _empty((n, top), torch.int64, device, stream)
-    top_logprobs = _empty((n, top), torch.float32, device, stream)
+    like_row, like_ids, like_top = _logprob_templates(n, top, device)
+    logprob, entropy = _empty(like_row, stream), _empty(like_row, stream)
+    ids, top_logprobs = _empty(like_ids, stream), _empty(like_top, stream)
     _check(load().copes_token_logprobs(logits.data_ptr(), dtype, n, vocab, logits.stride(0), target.data_ptr(), scale,
                                        top, logprob.data_ptr(), entropy.data_ptr(), ids.data_ptr(),
                                        top_logprobs.data_ptr(), _stream(stream)))
