@@ -35,7 +35,7 @@ __device__ __forceinline__ int slot_tokens(const Cache &c, int slot) {
 
 // Workspace of the page plans, in int32: a header (kPlan...), by listed slot the rank of its first new
 // page, by slot its place in the list, and two lists of pages.
-enum { kPlanDone = 0, kPlanTotal = 1, kPlanHeader = 4 };
+enum { kPlanDone = 0, kPlanTotal = 1, kPlanJob = 2, kPlanHeader = 4 };
 inline size_t cache_workspace_ints(int n_pages, int n_slots) {
   return (size_t)kPlanHeader + 2 * (size_t)n_slots + 2 * (size_t)n_pages;
 }

@@ -87,14 +87,16 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(Cache c, const
   int total = 0;
   for (int base = 0; base < n; base += kPlanThreads) {
     const int i = base + tid;
-    int need = 0;
+    int need = 0, source = -1;
     if (i < n) {
       const int slot = slots[i];
       bool ok = (unsigned)slot < (unsigned)c.n_slots && atomicCAS(&mark[slot], -1, i) == -1;
       if (kFork) {
         const int parent = parents[i];
         ok = ok && (unsigned)parent < (unsigned)c.n_slots && slot_tokens(c, slot) == 0;
-        if (ok) need = slot_tokens(c, parent) % c.page_size != 0;
+        const int tokens = ok ? slot_tokens(c, parent) : 0;
+        need = tokens % c.page_size != 0;
+        if (need) source = c.table[(int64_t)parent * c.table_width + tokens / c.page_size];
       } else if (ok) {
         const int more = add ? add[i] : add_all;
         const int64_t now = (int64_t)slot_tokens(c, slot) + more;
@@ -106,6 +108,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(Cache c, const
     int sum;
     const int at = block_scan(need, s_scan, &sum);
     if (i < n) first[i] = total + at;
+    if (kFork && need && total + at < c.n_pages) fresh[c.n_pages + total + at] = source;  // the page to copy
     total += sum;
   }
   __syncthreads();
@@ -145,53 +148,92 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(Cache c, const
   __syncthreads();  // lengths are read above
   for (int i = tid; i < n; i += kPlanThreads)
     c.length[slots[i]] = kFork ? slot_tokens(c, parents[i]) : slot_tokens(c, slots[i]) + (add ? add[i] : add_all);
-  if (tid == 0) ws[kPlanDone] = 1;
-}
-
-// Copies 16-byte pieces [begin, end) of a page, several of a thread's on their way at once.
-__device__ __forceinline__ void copy_pieces(const Cache &c, int to, int from, uint64_t begin, uint64_t end) {
-  const int4 *a = reinterpret_cast<const int4 *>(c.pool + (uint64_t)from * c.page_bytes);
-  int4 *b = reinterpret_cast<int4 *>(c.pool + (uint64_t)to * c.page_bytes);
-  constexpr int kBatch = 8;
-  uint64_t i = begin + threadIdx.x;
-  for (; i + (kBatch - 1) * blockDim.x < end; i += kBatch * blockDim.x) {
-    int4 v[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u] = a[i + u * blockDim.x];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) b[i + u * blockDim.x] = v[u];
+  if (tid == 0) {
+    ws[kPlanDone] = 1;
+    ws[kPlanTotal] = total;
+    ws[kPlanJob] = 0;
   }
-  for (; i < end; i += blockDim.x) b[i] = a[i];
 }
 
-// Children's tables, the shared pages' refs and the copies of partly filled pages: `parts`
-// blocks work on each child.  The pages are read from L2 after the first child, so stores bound it:
-// 240 copies of 2.4 MB pages in 98 us, 5.8 TB/s (torch's fill of a large tensor: 4.1 TB/s).  A
-// block that kept its piece and stored it for every child took 94, and 2 us longer for 8 children.
-__global__ void __launch_bounds__(256) fork_copy_kernel(Cache c, const int32_t *parents, const int32_t *children,
-                                                        int parts, const int32_t *ws) {
+// A job is 32 KB of a page's copy: 8 pieces of 16 bytes of each thread, all on their way at once.
+constexpr int kCopyThreads = 256, kJobPieces = 8 * kCopyThreads;
+struct Job {
+  int4 v[8];
+  __device__ __forceinline__ void load(const Cache &c, int page, int64_t begin) {
+    const int4 *at = reinterpret_cast<const int4 *>(c.pool + (uint64_t)page * c.page_bytes);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i = begin + u * kCopyThreads + threadIdx.x;
+      if (i < (int64_t)(c.page_bytes / 16)) v[u] = at[i];
+    }
+  }
+  __device__ __forceinline__ void store(const Cache &c, int page, int64_t begin) const {
+    int4 *at = reinterpret_cast<int4 *>(c.pool + (uint64_t)page * c.page_bytes);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i = begin + u * kCopyThreads + threadIdx.x;
+      if (i < (int64_t)(c.page_bytes / 16)) at[i] = v[u];
+    }
+  }
+};
+__host__ __device__ inline int64_t jobs_of(const Cache &c) { return (int64_t)(c.page_bytes / 16 + kJobPieces - 1) / kJobPieces; }
+
+// Copies page from[r] to page to[r], r < n, in jobs that the blocks take one after the other: a block's
+// first has its own number, the later ones are counted by *taken and asked for while a job is loaded.
+// SMs differ by a tenth in the rate at which they reach HBM, so equal shares wait for the slowest: a
+// fork with 256 copies of 2.4 MB pages to as many others took 203 us in shares, 185 so.  (A block of its own
+// for each job: 186, and a fork without copies 22 us instead of 9.)
+__device__ __forceinline__ void copy_pages(const Cache &c, const int32_t *to, const int32_t *from, int n, int32_t *taken) {
+  __shared__ int64_t s_next[2];
+  const int64_t parts = jobs_of(c), jobs = parts * n;
+  int64_t job = blockIdx.x;
+  if (job >= jobs) return;
+  int64_t begin = job % parts * kJobPieces;
+  int source = from[job / parts], target = to[job / parts];
+  for (int turn = 0;; turn ^= 1) {
+    Job data;
+    const bool ok = (unsigned)source < (unsigned)c.n_pages;
+    if (ok) data.load(c, source, begin);
+    else if (threadIdx.x == 0) flag_error(kErrCacheId);
+    const int target_now = target;
+    const int64_t begin_now = begin;
+    job = jobs;
+    if (jobs > gridDim.x) {
+      if (threadIdx.x == 0) s_next[turn] = (int64_t)gridDim.x + atomicAdd(reinterpret_cast<unsigned *>(taken), 1u);
+      __syncthreads();
+      job = s_next[turn];
+      if (job < jobs) {
+        begin = job % parts * kJobPieces;
+        source = from[job / parts];
+        target = to[job / parts];
+      }
+    }
+    if (ok) data.store(c, target_now, begin_now);
+    if (job >= jobs) return;
+  }
+}
+
+// Children's tables and the shared pages' refs, then the copies of partly filled pages, which are read
+// from L2 after a parent's first child, so that stores bound it: 240 copies of 2.4 MB pages in 88 us,
+// 6.4 TB/s.
+__global__ void __launch_bounds__(kCopyThreads, 4) fork_copy_kernel(Cache c, const int32_t *parents, const int32_t *children, int n,
+                                                        int32_t *ws) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!ws[kPlanDone]) return;
-  const int i = blockIdx.x / parts, part = blockIdx.x % parts;
-  const int32_t *first = ws + kPlanHeader, *fresh = plan_pages(c, ws);
-  const int32_t *from = c.table + (int64_t)parents[i] * c.table_width;
-  int32_t *to = c.table + (int64_t)children[i] * c.table_width;
-  const int tokens = slot_tokens(c, parents[i]), full = tokens / c.page_size;
-  for (int j = part * blockDim.x + threadIdx.x; j < full; j += parts * blockDim.x) {
-    const int page = from[j];
-    to[j] = page;
+  const int32_t *first = ws + kPlanHeader, *to = plan_pages(c, ws);
+  const int spans = (c.table_width - 1) / blockDim.x + 1;  // of a table, an entry for each thread
+  for (int64_t u = blockIdx.x; u < (int64_t)n * spans; u += gridDim.x) {
+    const int i = (int)(u / spans), j = (int)(u % spans) * blockDim.x + threadIdx.x;
+    const int tokens = slot_tokens(c, parents[i]), full = tokens / c.page_size;
+    int32_t *entry = c.table + (int64_t)children[i] * c.table_width + j;
+    if (j == full && tokens % c.page_size) *entry = to[first[i]];
+    if (j >= full) continue;
+    const int page = c.table[(int64_t)parents[i] * c.table_width + j];
+    *entry = page;
     if ((unsigned)page < (unsigned)c.n_pages) atomicAdd(&c.refs[page], 1);
     else flag_error(kErrCacheId);
   }
-  if (tokens % c.page_size == 0) return;
-  const int page = from[full], copy = fresh[first[i]];
-  if (part == 0 && threadIdx.x == 0) to[full] = copy;
-  if ((unsigned)page >= (unsigned)c.n_pages) {
-    if (threadIdx.x == 0) flag_error(kErrCacheId);
-    return;
-  }
-  const uint64_t pieces = c.page_bytes / 16;
-  copy_pieces(c, copy, page, pieces * part / parts, pieces * (part + 1) / parts);
+  copy_pages(c, to, to + c.n_pages, ws[kPlanTotal], ws + kPlanJob);
 }
 
 // One block per slot.  The exchange of the length makes one of a slot's blocks the one that frees it.
@@ -235,6 +277,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(Cache c, int
   }
   if (tid == 0) {
     ws[kPlanTotal] = movers;
+    ws[kPlanJob] = 0;
     if (counts) {
       counts[0] = used;
       counts[1] = movers;
@@ -242,9 +285,9 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(Cache c, int
   }
 }
 
-// The moves' copies, in pieces of 16 bytes over the whole grid, and the tables' new ids.  Bound by
-// HBM: 360 pages of 2.4 MB, 1.70 GB read and written, in 253 us, 6.7 TB/s (a plain copy: 6.8).
-__global__ void __launch_bounds__(256) compact_move_kernel(Cache c, const int32_t *ws) {
+// The tables' new ids and the moves' copies.  Bound by
+// HBM: 369 pages of 2.4 MB, 1.74 GB read and written, in 253 us, 6.9 TB/s (a plain copy: 6.8).
+__global__ void __launch_bounds__(kCopyThreads, 4) compact_move_kernel(Cache c, int32_t *ws) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int moves = ws[kPlanTotal];
   if (moves == 0) return;
@@ -265,21 +308,20 @@ __global__ void __launch_bounds__(256) compact_move_kernel(Cache c, const int32_
       if (from[lo] == page) row[j] = to[lo];
     }
   }
-  const uint64_t pieces = c.page_bytes / 16, share = 2048, parts = (pieces + share - 1) / share;
-  for (uint64_t job = blockIdx.x; job < parts * moves; job += gridDim.x) {
-    const uint64_t r = job / parts, begin = job % parts * share;
-    copy_pieces(c, to[r], from[r], begin, begin + share < pieces ? begin + share : pieces);
-  }
+  copy_pages(c, to, from, moves, ws + kPlanJob);
 }
 
-__global__ void __launch_bounds__(256) copy_pages_kernel(Cache c, const int32_t *src, const int32_t *dst, int parts) {
-  const int i = blockIdx.x / parts, part = blockIdx.x % parts, from = src[i], to = dst[i];
+// A block for each job: 255 copies of one page of 2.4 MB in 82 us, 7.4 TB/s of stores.
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(Cache c, const int32_t *src, const int32_t *dst) {
+  const int64_t parts = jobs_of(c), i = blockIdx.x / parts, begin = blockIdx.x % parts * kJobPieces;
+  const int from = src[i], to = dst[i];
   if ((unsigned)from >= (unsigned)c.n_pages || (unsigned)to >= (unsigned)c.n_pages) {
     if (threadIdx.x == 0) flag_error(kErrCacheId);
     return;
   }
-  const uint64_t pieces = c.page_bytes / 16;
-  copy_pieces(c, to, from, pieces * part / parts, pieces * (part + 1) / parts);
+  Job data;
+  data.load(c, from, begin);
+  data.store(c, to, begin);
 }
 
 // A warp per (row, key-value head, key or value).
@@ -334,11 +376,8 @@ cudaError_t launch_cache_grow(const Cache &c, const int32_t *slots, int n, const
   return cudaGetLastError();
 }
 
-// Blocks a page's copy is cut into: enough for the GPU over `pages` of them, none under 32 KB.
-static int copy_parts(const Cache &c, int pages) {
-  const uint64_t most = (c.page_bytes + (32 << 10) - 1) / (32 << 10), want = (152 * 8 + pages - 1) / pages;
-  return (int)(want < most ? want : most);
-}
+// What the GPU runs at once with 64 registers a thread.  (Five blocks an SM: 131 us where four take 97.)
+constexpr int kCopyBlocks = 152 * 4;
 
 cudaError_t launch_cache_fork(const Cache &c, const int32_t *parents, const int32_t *children, int n, int32_t *ws,
                               cudaStream_t s) {
@@ -347,8 +386,10 @@ cudaError_t launch_cache_fork(const Cache &c, const int32_t *parents, const int3
   cache_plan_kernel<true><<<1, kPlanThreads, 0, s>>>(c, children, parents, nullptr, 0, n, ws);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int parts = copy_parts(c, n);
-  return launch_after((unsigned)n * parts, 256, s, fork_copy_kernel, c, parents, children, parts, (const int32_t *)ws);
+  const int64_t parts = jobs_of(c), spans = (c.table_width - 1) / kCopyThreads + 1;
+  const int64_t jobs = (parts > spans ? parts : spans) * n;
+  return launch_after((unsigned)(jobs < kCopyBlocks ? jobs : kCopyBlocks), kCopyThreads, s, fork_copy_kernel, c, parents, children, n,
+                      ws);
 }
 
 cudaError_t launch_cache_free(const Cache &c, const int32_t *slots, int n, cudaStream_t s) {
@@ -363,14 +404,13 @@ cudaError_t launch_cache_compact(const Cache &c, int32_t *counts, int32_t *ws, c
   compact_plan_kernel<<<1, kPlanThreads, 0, s>>>(c, counts, ws);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_after(152 * 8, 256, s, compact_move_kernel, c, (const int32_t *)ws);
+  return launch_after(kCopyBlocks, kCopyThreads, s, compact_move_kernel, c, ws);
 }
 
 cudaError_t launch_cache_copy(const Cache &c, const int32_t *src, const int32_t *dst, int n, cudaStream_t s) {
   if (n == 0) return cudaSuccess;
   g_used = true;
-  const int parts = copy_parts(c, n);
-  copy_pages_kernel<<<(unsigned)n * parts, 256, 0, s>>>(c, src, dst, parts);
+  copy_pages_kernel<<<(unsigned)(n * jobs_of(c)), kCopyThreads, 0, s>>>(c, src, dst);
   return cudaGetLastError();
 }
 
