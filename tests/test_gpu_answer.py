@@ -168,6 +168,51 @@ def test_a_long_prompt_and_many_children(copes):
     same(cache, m, pool)
 
 
+def test_large_pages_are_copied_whole(copes):
+    """Pages of several jobs, the last of them partly filled, and more jobs than blocks."""
+    cache = copes.KVCache.empty(420, 30, 2, 5, 256, 210, 4)
+    m = model.CacheModel(420, 5, 210, 4)
+    cache.pool.normal_()
+    pool = cache.pool.clone()
+
+    def follow():
+        for a, b in m.copies:
+            pool[b] = pool[a]
+        assert error_bits(copes) == 0
+        same(cache, m, pool)
+
+    parents = [0, 1, 2]
+    copes.cache_grow(cache, ids(parents), ids([7, 5, 19]))
+    assert m.grow(parents, [7, 5, 19]) == 0
+    children = list(range(3, 210))
+    of = [parents[i * 3 // len(children)] for i in range(len(children))]
+    copes.cache_fork(cache, ids(of), ids(children))
+    assert m.fork(of, children) == 0
+    follow()
+    copes.cache_free(cache, ids(children[:100]))
+    m.free(children[:100])
+    copes.cache_compact(cache)
+    m.compact()
+    follow()
+    src, dst = list(range(0, 100)), list(range(300, 400))
+    copes.cache_copy_pages(cache, ids(src), ids(dst))
+    pool[300:400] = pool[0:100]
+    assert error_bits(copes) == 0
+    assert torch.equal(cache.pool.view(torch.int16), pool.view(torch.int16))
+
+
+def test_a_fork_of_a_page_outside_the_pool_is_reported(copes):
+    cache = copes.KVCache.empty(8, 1, 1, 4, 8, 3, 3)
+    cache.pool.normal_()
+    copes.cache_grow(cache, ids([0]), 6)
+    cache.table[0, 1] = 77
+    before = cache.pool.clone()
+    copes.cache_fork(cache, ids([0, 0]), ids([1, 2]))
+    assert error_bits(copes) == 32
+    assert torch.equal(cache.pool, before)
+    assert cache.table[1:, 0].tolist() == [0, 0] and cache.refs[0].item() == 3
+
+
 def test_ids_outside_the_cache_are_skipped(copes):
     cache = copes.KVCache.empty(4, 1, 1, 4, 8, 2, 3)
     cache.pool.zero_()
