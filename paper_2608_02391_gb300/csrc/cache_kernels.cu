@@ -14,6 +14,14 @@ __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_cache_err
 
 constexpr int kPlanThreads = 1024;
 
+// The kernels are launched while the one before them on the stream ends, and wait here for all it
+// wrote, so that a launch's own time is hidden (fork, grow, append and free of 256 rollouts among three
+// copies of the tables: 107 us, 114 without); the next may come as soon as all blocks are here.
+__device__ __forceinline__ void after_the_last() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Exclusive prefix sum of v over the block and the block's total.  `s` holds 33 ints.
 __device__ __forceinline__ int block_scan(int v, int *s, int *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -71,7 +79,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(Cache c, const
                                                                   const int32_t *add, int add_all, int n, int32_t *ws) {
   __shared__ int s_scan[32];
   __shared__ unsigned s_bad;
-  if (kFork) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  after_the_last();
   const int tid = threadIdx.x;
   int32_t *first = ws + kPlanHeader;       // rank of slot i's first new page
   int32_t *mark = first + c.n_slots;       // by slot: its place in the list
@@ -218,7 +226,7 @@ __device__ __forceinline__ void copy_pages(const Cache &c, const int32_t *to, co
 // 6.4 TB/s.
 __global__ void __launch_bounds__(kCopyThreads, 4) fork_copy_kernel(Cache c, const int32_t *parents, const int32_t *children, int n,
                                                         int32_t *ws) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_the_last();
   if (!ws[kPlanDone]) return;
   const int32_t *first = ws + kPlanHeader, *to = plan_pages(c, ws);
   const int spans = (c.table_width - 1) / blockDim.x + 1;  // of a table, an entry for each thread
@@ -239,6 +247,7 @@ __global__ void __launch_bounds__(kCopyThreads, 4) fork_copy_kernel(Cache c, con
 // One block per slot.  The exchange of the length makes one of a slot's blocks the one that frees it.
 __global__ void __launch_bounds__(256) cache_free_kernel(Cache c, const int32_t *slots) {
   __shared__ int s_tokens;
+  after_the_last();
   const int slot = slots[blockIdx.x];
   if ((unsigned)slot >= (unsigned)c.n_slots) {
     if (threadIdx.x == 0) flag_error(kErrCacheId);
@@ -261,8 +270,8 @@ __global__ void __launch_bounds__(256) cache_free_kernel(Cache c, const int32_t 
 // Compact: counts the pages in use (U) and pairs those at U and above with the free ids below.
 // ws: to[r] and from[r] of move r (the list of fresh pages' place and the one after it).
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(Cache c, int32_t *counts, int32_t *ws) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ int s_scan[32];
+  after_the_last();
   const int tid = threadIdx.x;
   int32_t *to = plan_pages(c, ws), *from = to + c.n_pages;
   int mine = 0, used;
@@ -288,7 +297,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(Cache c, int
 // The tables' new ids and the moves' copies.  Bound by
 // HBM: 369 pages of 2.4 MB, 1.74 GB read and written, in 253 us, 6.9 TB/s (a plain copy: 6.8).
 __global__ void __launch_bounds__(kCopyThreads, 4) compact_move_kernel(Cache c, int32_t *ws) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_the_last();
   const int moves = ws[kPlanTotal];
   if (moves == 0) return;
   const int32_t *to = plan_pages(c, ws), *from = to + c.n_pages;
@@ -314,6 +323,7 @@ __global__ void __launch_bounds__(kCopyThreads, 4) compact_move_kernel(Cache c, 
 // A block for each job, as far as a grid goes: 255 copies of one page of 2.4 MB in 82 us, 7.4 TB/s of
 // stores.
 __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(Cache c, const int32_t *src, const int32_t *dst, int n) {
+  after_the_last();
   const int64_t parts = jobs_of(c);
   for (int64_t job = blockIdx.x; job < parts * n; job += gridDim.x) {
     const int64_t i = job / parts, begin = job % parts * kJobPieces;
@@ -333,6 +343,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) append_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position,
                                                      int n, const T *k, int64_t k_row, int64_t k_head, const T *v,
                                                      int64_t v_row, int64_t v_head) {
+  after_the_last();
   const int64_t job = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (job >= (int64_t)n * c.n_kv_heads * 2) return;
@@ -357,7 +368,7 @@ __global__ void __launch_bounds__(256) append_kernel(Cache c, int layer, const i
   for (int d = lane; d < c.head_dim; d += 32) to[d] = from[d];
 }
 
-// Launches a kernel that begins with griddepcontrol.wait on the one launched before it.
+// Launches a kernel that begins with after_the_last().
 template <typename... Params, typename... Args>
 static cudaError_t launch_after(unsigned blocks, unsigned threads, cudaStream_t s, void (*kernel)(Params...), Args... args) {
   cudaLaunchConfig_t cfg{};
@@ -376,8 +387,7 @@ cudaError_t launch_cache_grow(const Cache &c, const int32_t *slots, int n, const
                               cudaStream_t s) {
   if (n == 0) return cudaSuccess;
   g_used = true;
-  cache_plan_kernel<false><<<1, kPlanThreads, 0, s>>>(c, slots, nullptr, add, add_all, n, ws);
-  return cudaGetLastError();
+  return launch_after(1, kPlanThreads, s, cache_plan_kernel<false>, c, slots, nullptr, add, add_all, n, ws);
 }
 
 // What the GPU runs at once with 64 registers a thread.  (Five blocks an SM: 131 us where four take 97.)
@@ -387,8 +397,7 @@ cudaError_t launch_cache_fork(const Cache &c, const int32_t *parents, const int3
                               cudaStream_t s) {
   if (n == 0) return cudaSuccess;
   g_used = true;
-  cache_plan_kernel<true><<<1, kPlanThreads, 0, s>>>(c, children, parents, nullptr, 0, n, ws);
-  cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_after(1, kPlanThreads, s, cache_plan_kernel<true>, c, children, parents, nullptr, 0, n, ws);
   if (e != cudaSuccess) return e;
   const int64_t parts = jobs_of(c), spans = (c.table_width - 1) / kCopyThreads + 1;
   const int64_t jobs = (parts > spans ? parts : spans) * n;
@@ -399,14 +408,12 @@ cudaError_t launch_cache_fork(const Cache &c, const int32_t *parents, const int3
 cudaError_t launch_cache_free(const Cache &c, const int32_t *slots, int n, cudaStream_t s) {
   if (n == 0) return cudaSuccess;
   g_used = true;
-  cache_free_kernel<<<n, 256, 0, s>>>(c, slots);
-  return cudaGetLastError();
+  return launch_after(n, 256, s, cache_free_kernel, c, slots);
 }
 
 cudaError_t launch_cache_compact(const Cache &c, int32_t *counts, int32_t *ws, cudaStream_t s) {
   g_used = true;
-  compact_plan_kernel<<<1, kPlanThreads, 0, s>>>(c, counts, ws);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_after(1, kPlanThreads, s, compact_plan_kernel, c, counts, ws);
   if (e != cudaSuccess) return e;
   return launch_after(kCopyBlocks, kCopyThreads, s, compact_move_kernel, c, ws);
 }
@@ -415,8 +422,7 @@ cudaError_t launch_cache_copy(const Cache &c, const int32_t *src, const int32_t 
   if (n == 0) return cudaSuccess;
   g_used = true;
   const int64_t jobs = jobs_of(c) * n;
-  copy_pages_kernel<<<(unsigned)(jobs < 1 << 30 ? jobs : 1 << 30), kCopyThreads, 0, s>>>(c, src, dst, n);
-  return cudaGetLastError();
+  return launch_after((unsigned)(jobs < 1 << 30 ? jobs : 1 << 30), kCopyThreads, s, copy_pages_kernel, c, src, dst, n);
 }
 
 cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n,
@@ -426,12 +432,10 @@ cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots,
   g_used = true;
   const unsigned blocks = (unsigned)(((int64_t)n * c.n_kv_heads * 2 + 7) / 8);
   if (c.elem == 2)
-    append_kernel<uint16_t><<<blocks, 256, 0, s>>>(c, layer, slots, position, n, (const uint16_t *)k, k_row, k_head,
-                                                   (const uint16_t *)v, v_row, v_head);
-  else
-    append_kernel<uint32_t><<<blocks, 256, 0, s>>>(c, layer, slots, position, n, (const uint32_t *)k, k_row, k_head,
-                                                   (const uint32_t *)v, v_row, v_head);
-  return cudaGetLastError();
+    return launch_after(blocks, 256, s, append_kernel<uint16_t>, c, layer, slots, position, n, (const uint16_t *)k, k_row,
+                        k_head, (const uint16_t *)v, v_row, v_head);
+  return launch_after(blocks, 256, s, append_kernel<uint32_t>, c, layer, slots, position, n, (const uint32_t *)k, k_row,
+                      k_head, (const uint32_t *)v, v_row, v_head);
 }
 
 // Read only once a kernel of this file was launched: copes_check of a program without a cache

@@ -476,6 +476,9 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, stride = warps * kStep;
   const int part = blockIdx.x % parts;
   const int64_t i = blockIdx.x / parts;
+  // launched while the kernel before it on the stream ends, whose results are waited for here
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const float c = a.scale * 1.44269504088896340736f;
   const uint64_t c2 = pack2(c, c);
   if (parts > 1) cluster_arrive();
@@ -706,12 +709,14 @@ static cudaError_t launch(const LogprobArgs &a, const Cut &c, cudaStream_t s) {
   cfg.blockDim = dim3(c.threads);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = c.parts;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = c.parts > 1 ? 1 : 0;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = c.parts;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = c.parts > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, a, c.parts, c.merge, c.at_once / c.parts, (int)c.cell_bytes);
 }
 
