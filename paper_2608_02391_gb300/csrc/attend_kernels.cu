@@ -7,7 +7,7 @@
 // the fp32 units' whole rate before a single conversion, and 3% of the tensor cores': the bound is
 // HBM, and mma.sync on registers filled from shared memory is enough (tcgen05 takes 64 rows or more
 // of one operand; a group of query heads has 1 to 16, and a block of these has no room to wait in).
-// Measured: 128 rows of up to 16,384 tokens, 32/8 heads of 128, bf16: 4.24 GB in 628 us, 6.75 TB/s;
+// Measured: 128 rows of up to 16,384 tokens, 32/8 heads of 128, bf16: 4.24 GB in 605 us, 7.0 TB/s;
 // fp32, 32 rows of up to 34,629, heads of 80: 97% of the rate of a copy; heads of 256: 53%.
 //
 // Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
@@ -53,11 +53,12 @@ template <typename T, int DP_, int NT_, bool kBeside>
 struct Shape {
   static constexpr bool kFp32 = sizeof(T) == 4;
   static constexpr int DP = DP_, NT = NT_;
-  // Warps of a block and tiles in shared memory, two or more of them on their way: what lets the
-  // most warps run on an SM.  (fp32 takes twice the room and three times the products, and wants
-  // warps more than tiles ahead.)
+  // Warps of a block: what lets the most of them run on an SM.  (fp32 takes twice the room and three
+  // times the products.)  Tiles in shared memory: one is worked on while the next is on its way.  With
+  // two on their way there is more asked for than HBM can give, and the SMs far from it come to be the
+  // last: 128 rows of up to 16,384 tokens took 633 us, 605 so.
   static constexpr int kWarps = !kFp32 ? 4 : DP <= 128 ? 2 : DP <= 192 ? 4 : 3;
-  static constexpr int kStages = kFp32 ? 2 : DP <= 96 ? 4 : 3;
+  static constexpr int kStages = 2;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kTeam = kBeside ? 1 : kWarps, kSides = kWarps / kTeam;  // warps on a head, heads
   static constexpr int kTile = kTeam * 16;                // tokens
@@ -783,7 +784,6 @@ __global__ void __launch_bounds__(kJoinThreads, kBatch > 4 ? 3 : 6) join_kernel(
   __shared__ float4 s_o[kJoinThreads];
   __shared__ float s_m[kJoinThreads / 32], s_l[kJoinThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int w0 = blockIdx.x / per, h = blockIdx.x % per, D = a.c.head_dim;
   const Split x = split[w0];
   const int group = a.q_heads / a.c.n_kv_heads;

@@ -332,6 +332,16 @@ def test_attention_split_over_long_and_many_sequences(copes, n, longest, heads, 
     assert error_bits(copes) == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_of_more_rows_than_a_block_keeps_lengths_of(copes, dtype):
+    lens = np.random.default_rng(6).integers(0, 7, 9000)
+    cache = filled(copes, lens, 1, 1, 4, 8, dtype, seed=6)
+    q = torch.randn(9000, 2, 8, device="cuda").to(DT[dtype])
+    out, lse = copes.paged_attention(cache, 0, q)
+    check_attention(cache, 0, q, range(9000), 8 ** -0.5, out, lse)
+    assert error_bits(copes) == 0
+
+
 def test_attention_of_extreme_scores(copes):
     """One token outweighs all others by far, first or last; scores of +-1e4; equal scores."""
     for dtype in ("bf16", "fp32"):
