@@ -556,8 +556,9 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
     ++step;
   };
   // The buffers take turns (4,096 rows: 180 us, where each moves on 188; 1,216 with 20 alternatives 69
-  // and 73).  With two steps ahead and alternatives each moves on: three copies of that loop beside
-  // the end of a row are too much code (225 us in turns, 215 so).
+  // and 73; 2,000 rows of fp32 with 20 190 and 203).  Of bf16 with two steps ahead and alternatives
+  // each moves on: three copies of that loop, of twice the logits, beside the end of a row are too
+  // much code (225 us in turns, 215 so).
   for (int base = warp * kStep; base < n;) {
     const auto turn = [&](const Piece<T>(&p)[kLoads], Piece<T>(&later)[kLoads]) {
       if (base + (kDeep ? 2 : 1) * stride < n) fetch(base + (kDeep ? 2 : 1) * stride, later);
@@ -565,7 +566,7 @@ __global__ void __launch_bounds__(kMostThreads, per_sm(kDeep)) logprob_kernel(Lo
       base += stride;
       return base < n;
     };
-    if constexpr (kDeep && kTop) {
+    if constexpr (kDeep && kTop && sizeof(T) == 2) {
       if (!turn(now, then)) break;
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
