@@ -588,7 +588,8 @@ class KVCache:
     page_size, head_dim] (bf16 or fp32), table [n_slots, table_width], length [n_slots] and
     refs [n_pages] (int32).  The tensors are the caller's and may be read at any time; the
     cache_* calls change them in stream order.  KVCache.empty allocates an empty cache.  The
-    handle keeps the calls' workspaces: its calls run in one stream's order."""
+    handle keeps the calls' workspaces: its calls run in one stream's order, and it outlives the
+    graphs that captured them."""
 
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, refs: torch.Tensor):
         assert pool.dim() == 6 and pool.shape[2] == 2 and table.dim() == 2
@@ -608,6 +609,7 @@ class KVCache:
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=pool.device)
         self.attend_workspace = None  # paged_attention's
         self._attend_room = 0         # its bytes
+        self._attend_before = []      # the smaller ones that calls were given before it
         self._attend_kept = {}        # (rows, query heads) -> bytes of it, templates of out and lse
 
     @classmethod
@@ -641,15 +643,16 @@ class KVCache:
         return kept
 
     def attend_space(self, n: int, q_heads: int, stream=None) -> Tuple[int, int]:
-        """paged_attention's workspace (address, bytes), allocated where it has to grow."""
+        """paged_attention's workspace (address, bytes), allocated where it has to grow.  The one before
+        stays allocated with the handle, since a captured graph goes on writing to it; each is twice
+        as large as the one before at least, so all together take less than twice the last."""
         need = self._attend_shapes(n, q_heads)[0]
-        ws = self.attend_workspace
         if self._attend_room < need:
-            if ws is not None and stream is not None:
-                ws.record_stream(stream)
-            ws = self.attend_workspace = _empty(_template((need,), torch.uint8, self.pool.device), stream)
-            self._attend_room = need
-        return ws.data_ptr(), self._attend_room
+            if self.attend_workspace is not None:
+                self._attend_before.append(self.attend_workspace)
+            self._attend_room = max(need, 2 * self._attend_room)
+            self.attend_workspace = _empty(_template((self._attend_room,), torch.uint8, self.pool.device), stream)
+        return self.attend_workspace.data_ptr(), self._attend_room
 
 
 def cache_grow(cache: KVCache, slots: torch.Tensor, add, stream=None) -> None:

@@ -2,9 +2,12 @@
 call, with a message that names the entry; the fake addresses are never read."""
 import copy
 import ctypes
+import gc
 import os
+import weakref
 
 import pytest
+import torch
 
 import answer_model as model
 
@@ -123,6 +126,19 @@ def test_arguments_that_are_refused(copes):
                      (dict(lp=0x100004), -1), (dict(ent=0x100004), -1), (dict(ids=0x100008), -1), (dict(tlp=0x1000C4), -1), (dict(ids=None), -1), (dict(tlp=None), -1), (dict(logits=0x101), -2), (dict(target=0x1004), -2),
                      (dict(ids=0x3004), -2), (dict(lp=0x2002), -2), (dict(ent=0x5001), -2)]:
         refused(copes, logprobs(**kw), code, "copes_token_logprobs")
+
+
+def test_workspaces_that_calls_were_given_stay_with_the_handle(copes):
+    """A captured call goes on writing to the address that it was given.  (On a handle without its
+    constructor, which wants a GPU's tensors.)"""
+    c = object.__new__(copes.KVCache)
+    c.pool, c.attend_workspace, c._attend_room, c._attend_before = torch.empty(0), None, 0, []
+    c._attend_shapes = lambda n, q_heads: (1000 * n, None, None)
+    given = [(c.attend_space(n, 1), weakref.ref(c.attend_workspace)) for n in (1, 3, 2, 4, 300)]
+    gc.collect()
+    for (at, size), ws in given:
+        assert ws() is not None and ws().data_ptr() == at and ws().numel() == size
+    assert [size for (_, size), _ in given] == [1000, 3000, 3000, 6000, 300000]
 
 
 def test_the_model_of_the_pages():

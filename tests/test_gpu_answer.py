@@ -428,6 +428,29 @@ def test_calls_run_on_the_stream_they_are_given_and_in_a_graph(copes):
     assert error_bits(copes) == 0
 
 
+def test_a_graph_keeps_the_workspace_it_was_captured_with(copes):
+    """A larger call between capture and replay: the graph's workspace is nobody else's then."""
+    lens = [3000] + [40] * 299
+    cache = filled(copes, lens, 1, 2, 16, 64, "bf16", seed=11)
+    q = torch.randn(300, 14, 64, device="cuda").bfloat16()
+    want = copes.paged_attention(cache, 0, q[:1])
+    captured = cache.attend_workspace.data_ptr(), cache.attend_workspace.numel()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = copes.paged_attention(cache, 0, q[:1])
+    copes.paged_attention(cache, 0, q)
+    assert cache.attend_workspace.data_ptr() != captured[0]  # the call was large enough to need more
+    others = [torch.full((captured[1],), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    assert all(x.data_ptr() != captured[0] for x in others)
+    for x in held:
+        x.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(held[0], want[0]) and torch.equal(held[1], want[1])
+    assert all((x == 7).all() for x in others)
+    assert error_bits(copes) == 0
+
+
 # ---------------------------------------------------------------- token log probabilities
 def check_logprobs(copes, logits, target, top, scale=1.0):
     """ids exactly.  Numbers: the subtraction from the maximum, the product with the scale and the
