@@ -132,10 +132,39 @@ class Decoder:
                 last[i] = logits[rows.index(i)]
         return torch.stack(last)
 
+    def _check_room(self, cache: copes.KVCache, lengths: Sequence[int], pages: int) -> None:
+        """Raises where sequences of these lengths, in `pages` pages that are not there yet, have no room in the
+        first slots of the cache.  The cache's calls refuse on the device, and what is computed after that
+        would be a reward like any other."""
+        d = cache.desc
+        if len(lengths) > d.n_slots:
+            raise ValueError(f"{len(lengths)} sequences in a cache of {d.n_slots} slots")
+        if max(lengths) > d.table_width * d.page_size:
+            raise ValueError(f"a sequence of {max(lengths)} tokens in a cache of up to {d.table_width * d.page_size}")
+        begun, used = torch.stack((cache.length[:len(lengths)].count_nonzero(), cache.refs.count_nonzero())).tolist()
+        if begun:
+            raise ValueError(f"{begun} of the cache's first {len(lengths)} slots are not empty")
+        if used + pages > d.n_pages:
+            raise ValueError(f"{pages} pages are needed, and {d.n_pages - used} of the cache's {d.n_pages} are free")
+
+    def _check_score(self, cache: copes.KVCache, prompts: Sequence[Sequence[int]],
+                     answers: Sequence[Sequence[Sequence[int]]]) -> None:
+        size, prompt = cache.desc.page_size, [len(p) for p in prompts]
+        pages = sum(-(-p // size) for p in prompt)
+        lengths = list(prompt)
+        for p, group in zip(prompt, answers):
+            for a in group:  # its last token is not written; the prompt's full pages are shared
+                lengths.append(p + len(a) - 1)
+                pages += -(-lengths[-1] // size) - p // size
+        self._check_room(cache, lengths, pages)
+
     def score(self, w: torch.Tensor, cache: copes.KVCache, prompts: Sequence[Sequence[int]],
               answers: Sequence[Sequence[Sequence[int]]]) -> torch.Tensor:
         """Mean log probability of every answer under the weights w: fp32, the answers of prompt 0,
-        then those of prompt 1, ...  The cache is empty before and after."""
+        then those of prompt 1, ...  The cache's first slots, one for each prompt and each answer, are
+        empty before and after.  What it has no room for raises ValueError before any work; what a kernel
+        reports (copes.check), CopesError."""
+        self._check_score(cache, prompts, answers)
         weights, device = self.weights(w), cache.pool.device
         flat = [(i, a) for i, group in enumerate(answers) for a in group]
         n, first = len(flat), len(prompts)
@@ -156,11 +185,14 @@ class Decoder:
             logits = self.step(weights, cache, children[rows], table[t - 1, rows])
             total[rows] += copes.token_logprobs(logits, table[t, rows]).logprob
         copes.cache_free(cache, torch.arange(first + n, dtype=torch.int32, device=device))
+        copes.check()
         return total / lengths.to(device)
 
     def greedy(self, w: torch.Tensor, cache: copes.KVCache, prompts: Sequence[Sequence[int]], n_tokens: int) -> torch.Tensor:
         """The n_tokens likeliest next tokens of each prompt, one after the other: int64 [prompts,
-        n_tokens].  The cache is empty before and after."""
+        n_tokens].  The cache's first slots, one for each prompt, are empty before and after; errors as score's."""
+        lengths = [len(p) + n_tokens - 1 for p in prompts]  # the last token is not written
+        self._check_room(cache, lengths, sum(-(-k // cache.desc.page_size) for k in lengths))
         weights, device = self.weights(w), cache.pool.device
         slots = torch.arange(len(prompts), dtype=torch.int32, device=device)
         none = torch.full((len(prompts),), -1, dtype=torch.int64, device=device)
@@ -170,4 +202,5 @@ class Decoder:
             if t + 1 < n_tokens:
                 logits = self.step(weights, cache, slots, out[-1])
         copes.cache_free(cache, slots)
+        copes.check()
         return torch.stack(out, 1)

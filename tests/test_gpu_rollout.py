@@ -114,3 +114,27 @@ def test_greedy_continuations_and_bf16():
     got = decoder.score(half, cache, prompts, answers).double().cpu().numpy()
     assert np.abs(got - plain_score(decoder.shape, half, prompts, answers)).max() <= 2.0**-4
     copes.check()
+
+
+def test_scores_need_the_pages_they_take_and_no_more(monkeypatch):
+    """Exactly enough pages give the scores that plenty of them give; one less is refused, before any work or,
+    where that check is left out, by the report of the page that a kernel did not find."""
+    copes, rollout, decoder, layout, arena, prompts, answers = setup(torch.float32, q_heads=6, kv_heads=2, head_dim=16)
+    plenty = decoder.cache(n_slots=13, max_tokens=48, dtype=torch.float32)
+    want = decoder.score(arena.w, plenty, prompts, answers)
+    # pages of 16: prompts of 5, 1, 16, 23 take 1 + 1 + 1 + 2; answers 1 + 1 + 1; 1; 1 + 1; 1 + 1
+    for spare in (0, 1):  # a page of another sequence
+        cache = decoder.cache(n_slots=13, max_tokens=48, n_pages=13 + spare, dtype=torch.float32)
+        last = torch.tensor([12], dtype=torch.int32, device="cuda")
+        copes.cache_grow(cache, last, spare)
+        assert torch.equal(decoder.score(arena.w, cache, prompts, answers), want)
+        assert cache.refs.sum().item() == spare
+        short = decoder.cache(n_slots=13, max_tokens=48, n_pages=12 + spare, dtype=torch.float32)
+        copes.cache_grow(short, last, spare)
+        with pytest.raises(ValueError, match="pages"):
+            decoder.score(arena.w, short, prompts, answers)
+        assert short.refs.sum().item() == spare
+    monkeypatch.setattr(rollout.Decoder, "_check_room", lambda *a: None)
+    with pytest.raises(copes.CopesError, match="bits 0x40:"):
+        decoder.score(arena.w, short, prompts, answers)
+    copes.check()

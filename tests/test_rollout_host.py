@@ -1,0 +1,69 @@
+"""What a decoder refuses before any work: every case is decided by the host, on a cache that has a
+cache's sizes and counts and nothing else."""
+import random
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+import answer_model as model
+from paper_2608_02391_gb300 import copes, rollout
+
+SHAPE = rollout.Shape(2, 48, 80, 301, q_heads=6, kv_heads=2, head_dim=16)
+
+
+def cache_of(n_pages, page_size, n_slots, width):
+    return SimpleNamespace(desc=copes.KVCacheDesc(1, 0, n_pages, 2, 2, page_size, 16, 1, n_slots, width, 1, 1),
+                           length=torch.zeros(n_slots, dtype=torch.int32), refs=torch.zeros(n_pages, dtype=torch.int32))
+
+
+def refused(match, cache, prompts, answers, n_tokens=4):
+    """By score and by greedy; None for the one that is not asked."""
+    d = rollout.Decoder(SHAPE, device="cpu")
+    if answers is not None:
+        with pytest.raises(ValueError, match=match):
+            d.score(None, cache, prompts, answers)
+    if n_tokens is not None:
+        with pytest.raises(ValueError, match=match):
+            d.greedy(None, cache, prompts, n_tokens)
+
+
+def test_work_that_the_cache_has_no_room_for_is_refused():
+    prompts, answers = [[1] * 5, [2] * 16], [[[3] * 4, [4]], [[5] * 17]]
+    refused("slots", cache_of(100, 16, 4, 9), prompts, answers, None)
+    refused("slots", cache_of(100, 16, 1, 9), prompts, None)
+    refused("slots", cache_of(100, 16, 64, 9), [[1]] * 40, [[[1]]] * 40, None)
+    refused("tokens", cache_of(100, 4, 5, 7), prompts, answers, None)  # 32 tokens
+    refused("tokens", cache_of(100, 3, 5, 6), prompts, None)           # 19 tokens
+    refused("tokens", cache_of(100, 5, 5, 3), [[1] * 16], [[[1]]], 1)
+    busy = cache_of(100, 16, 5, 9)
+    busy.length[1] = 1
+    refused("not empty", busy, prompts, answers)
+    full = cache_of(5, 16, 5, 9)
+    full.refs[3] = 1  # of the 5 that are needed: two for the prompts, and one for each answer's own tokens
+    refused("pages", full, prompts, answers, None)
+    refused("pages", cache_of(2, 16, 5, 9), prompts, None)  # 8 and 19 tokens
+
+
+def test_pages_that_a_score_needs_are_those_it_takes():
+    """Against the pages in use when every answer is written, by the model of the bookkeeping."""
+    rng = random.Random(7)
+    for _ in range(200):
+        size = rng.choice([1, 3, 7, 16])
+        prompts = [[1] * rng.randint(1, 40) for _ in range(rng.randint(1, 4))]
+        answers = [[[2] * rng.randint(1, 20) for _ in range(rng.randint(0, 3))] for _ in prompts]
+        n = len(prompts) + sum(map(len, answers))
+        m = model.CacheModel(4000, size, n, 100)
+        assert m.grow(range(len(prompts)), [len(p) for p in prompts]) == 0
+        parents = [i for i, group in enumerate(answers) for _ in group]
+        children = list(range(len(prompts), n))
+        assert m.fork(parents, children) == 0
+        assert m.grow(children, [len(a) - 1 for group in answers for a in group]) == 0
+        need, longest = sum(r != 0 for r in m.refs), max(m.length)
+        d = rollout.Decoder(SHAPE, device="cpu")
+        d._check_score(cache_of(need, size, n, -(-longest // size)), prompts, answers)
+        for few in (cache_of(need - 1, size, n, 100), cache_of(need, size, n - 1, 100),
+                    cache_of(need, 1, n, longest - 1)):
+            if few.desc.n_pages and few.desc.n_slots and few.desc.table_width:
+                with pytest.raises(ValueError):
+                    d._check_score(few, prompts, answers)
