@@ -97,10 +97,11 @@ class Decoder:
     def step(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: torch.Tensor, tokens: torch.Tensor,
              logits: bool = True):
         """The next token of each of `slots` (distinct, int32) is tokens (int64): their logits [n, vocab],
-        or None where they are not asked for."""
+        or None where they are not asked for.  Slots past the cache, and tokens that it has no room for, are
+        reported by copes.check()."""
         s, n = self.shape, slots.numel()
         copes.cache_grow(cache, slots, 1)
-        place = cache.length[slots.long()] - 1
+        place = cache.length[slots.long().clamp_(0, cache.desc.n_slots - 1)] - 1  # a slot past the cache is the calls' to report
         angles = place.double()[:, None] * self.frequencies
         x = weights["embed"][tokens]
         for l in range(s.layers):

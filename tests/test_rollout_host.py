@@ -45,6 +45,19 @@ def test_work_that_the_cache_has_no_room_for_is_refused():
     refused("pages", cache_of(2, 16, 5, 9), prompts, None)  # 8 and 19 tokens
 
 
+def test_a_step_reads_no_length_past_the_cache(monkeypatch):
+    """A slot past the cache is skipped and reported by the cache's calls; torch's indexing would end the
+    GPU's context.  (Here with the cache's calls left out, on the CPU, where such an index raises.)"""
+    for name in ("cache_grow", "cache_append"):
+        monkeypatch.setattr(copes, name, lambda *a, **kw: None)
+    monkeypatch.setattr(copes, "paged_attention", lambda cache, l, q, **kw: (torch.zeros_like(q), None))
+    d = rollout.Decoder(SHAPE, device="cpu")
+    w = torch.zeros(d.offsets[-1] + d.tensors[-1].numel)
+    slots = torch.tensor([0, 4, -1, 2**31 - 1, -2**31], dtype=torch.int32)
+    logits = d.step(d.weights(w), cache_of(8, 4, 4, 2), slots, torch.zeros(5, dtype=torch.int64))
+    assert logits.shape == (5, 301) and slots.tolist() == [0, 4, -1, 2**31 - 1, -2**31]
+
+
 def test_pages_that_a_score_needs_are_those_it_takes():
     """Against the pages in use when every answer is written, by the model of the bookkeeping."""
     rng = random.Random(7)
