@@ -119,9 +119,17 @@ class Decoder:
             return None
         return _rms_norm(x, weights["final_norm"], s.eps) @ weights["embed" if s.tied else "lm_head"].T
 
+    def _check_tokens(self, what: str, sequences: Sequence[Sequence[int]]) -> None:
+        """Raises for no sequences, or one without tokens: its reward would be 0 / 0."""
+        if len(sequences) == 0:
+            raise ValueError(f"no {what}s")
+        if min(map(len, sequences)) == 0:
+            raise ValueError(f"an empty {what}")
+
     def read(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: Sequence[int],
              prompts: Sequence[Sequence[int]]) -> torch.Tensor:
         """Writes prompts (one token at least each) into empty slots and returns the logits after each."""
+        self._check_tokens("prompt", prompts)
         device = cache.pool.device
         last = [None] * len(prompts)
         for t in range(max(map(len, prompts))):
@@ -150,6 +158,8 @@ class Decoder:
 
     def _check_score(self, cache: copes.KVCache, prompts: Sequence[Sequence[int]],
                      answers: Sequence[Sequence[Sequence[int]]]) -> None:
+        self._check_tokens("prompt", prompts)
+        self._check_tokens("answer", [a for group in answers for a in group])
         size, prompt = cache.desc.page_size, [len(p) for p in prompts]
         pages = sum(-(-p // size) for p in prompt)
         lengths = list(prompt)
@@ -163,8 +173,8 @@ class Decoder:
               answers: Sequence[Sequence[Sequence[int]]]) -> torch.Tensor:
         """Mean log probability of every answer under the weights w: fp32, the answers of prompt 0,
         then those of prompt 1, ...  The cache's first slots, one for each prompt and each answer, are
-        empty before and after.  What it has no room for raises ValueError before any work; what a kernel
-        reports (copes.check), CopesError."""
+        empty before and after.  Prompts or answers without tokens, and what the cache has no room for, raise
+        ValueError before any work; what a kernel reports (copes.check), CopesError."""
         self._check_score(cache, prompts, answers)
         weights, device = self.weights(w), cache.pool.device
         flat = [(i, a) for i, group in enumerate(answers) for a in group]
@@ -192,6 +202,9 @@ class Decoder:
     def greedy(self, w: torch.Tensor, cache: copes.KVCache, prompts: Sequence[Sequence[int]], n_tokens: int) -> torch.Tensor:
         """The n_tokens likeliest next tokens of each prompt, one after the other: int64 [prompts,
         n_tokens].  The cache's first slots, one for each prompt, are empty before and after; errors as score's."""
+        self._check_tokens("prompt", prompts)
+        if n_tokens < 1:
+            raise ValueError(f"a continuation of {n_tokens} tokens")
         lengths = [len(p) + n_tokens - 1 for p in prompts]  # the last token is not written
         self._check_room(cache, lengths, sum(-(-k // cache.desc.page_size) for k in lengths))
         weights, device = self.weights(w), cache.pool.device

@@ -45,6 +45,21 @@ def test_work_that_the_cache_has_no_room_for_is_refused():
     refused("pages", cache_of(2, 16, 5, 9), prompts, None)  # 8 and 19 tokens
 
 
+def test_sequences_without_tokens_are_refused():
+    cache = cache_of(100, 16, 9, 9)
+    refused("empty answer", cache, [[1], [2]], [[[3], []], [[4]]], None)
+    refused("empty prompt", cache, [[1], []], [[[3]], [[4]]])
+    refused("no answers", cache, [[1], [2]], [[], []], None)
+    refused("no answers", cache, [[1], [2]], [], None)
+    refused("no prompts", cache, [], [])
+    for n_tokens in (0, -1):
+        refused("continuation", cache, [[1]], None, n_tokens)
+    d = rollout.Decoder(SHAPE, device="cpu")
+    for prompts in ([], [[1], []]):
+        with pytest.raises(ValueError):
+            d.read({}, cache, [0, 1], prompts)
+
+
 def test_a_step_reads_no_length_past_the_cache(monkeypatch):
     """A slot past the cache is skipped and reported by the cache's calls; torch's indexing would end the
     GPU's context.  (Here with the cache's calls left out, on the CPU, where such an index raises.)"""
@@ -65,6 +80,7 @@ def test_pages_that_a_score_needs_are_those_it_takes():
         size = rng.choice([1, 3, 7, 16])
         prompts = [[1] * rng.randint(1, 40) for _ in range(rng.randint(1, 4))]
         answers = [[[2] * rng.randint(1, 20) for _ in range(rng.randint(0, 3))] for _ in prompts]
+        answers[0].append([2])
         n = len(prompts) + sum(map(len, answers))
         m = model.CacheModel(4000, size, n, 100)
         assert m.grow(range(len(prompts)), [len(p) for p in prompts]) == 0
