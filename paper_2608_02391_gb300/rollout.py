@@ -96,7 +96,7 @@ class Decoder:
 
     def step(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: torch.Tensor, tokens: torch.Tensor,
              logits: bool = True):
-        """The next token of each of `slots` (distinct, int32) is tokens (int64): their logits [n, vocab],
+        """The next token of each of `slots` (distinct, int32) is tokens (int64, in the vocabulary): their logits [n, vocab],
         or None where they are not asked for.  Slots past the cache, and tokens that it has no room for, are
         reported by copes.check()."""
         s, n = self.shape, slots.numel()
@@ -120,11 +120,14 @@ class Decoder:
         return _rms_norm(x, weights["final_norm"], s.eps) @ weights["embed" if s.tied else "lm_head"].T
 
     def _check_tokens(self, what: str, sequences: Sequence[Sequence[int]]) -> None:
-        """Raises for no sequences, or one without tokens: its reward would be 0 / 0."""
+        """Raises for no sequences, for one without tokens, whose reward would be 0 / 0, and for an id outside the
+        vocabulary: a negative one would be read as another token, one past it end the GPU's context."""
         if len(sequences) == 0:
             raise ValueError(f"no {what}s")
         if min(map(len, sequences)) == 0:
             raise ValueError(f"an empty {what}")
+        if min(map(min, sequences)) < 0 or max(map(max, sequences)) >= self.shape.vocab:
+            raise ValueError(f"a token outside the vocabulary of {self.shape.vocab} in the {what}s")
 
     def read(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: Sequence[int],
              prompts: Sequence[Sequence[int]]) -> torch.Tensor:
@@ -159,6 +162,8 @@ class Decoder:
     def _check_score(self, cache: copes.KVCache, prompts: Sequence[Sequence[int]],
                      answers: Sequence[Sequence[Sequence[int]]]) -> None:
         self._check_tokens("prompt", prompts)
+        if len(answers) > len(prompts):
+            raise ValueError(f"answers for {len(answers)} prompts, and {len(prompts)} prompts")
         self._check_tokens("answer", [a for group in answers for a in group])
         size, prompt = cache.desc.page_size, [len(p) for p in prompts]
         pages = sum(-(-p // size) for p in prompt)
@@ -173,8 +178,9 @@ class Decoder:
               answers: Sequence[Sequence[Sequence[int]]]) -> torch.Tensor:
         """Mean log probability of every answer under the weights w: fp32, the answers of prompt 0,
         then those of prompt 1, ...  The cache's first slots, one for each prompt and each answer, are
-        empty before and after.  Prompts or answers without tokens, and what the cache has no room for, raise
-        ValueError before any work; what a kernel reports (copes.check), CopesError."""
+        empty before and after.  Prompts or answers without tokens, ids outside the vocabulary, answers without
+        a prompt and what the cache has no room for raise ValueError before any work; what a kernel reports
+        (copes.check), CopesError."""
         self._check_score(cache, prompts, answers)
         weights, device = self.weights(w), cache.pool.device
         flat = [(i, a) for i, group in enumerate(answers) for a in group]

@@ -60,6 +60,17 @@ def test_sequences_without_tokens_are_refused():
             d.read({}, cache, [0, 1], prompts)
 
 
+def test_tokens_outside_the_vocabulary_and_answers_without_a_prompt_are_refused():
+    cache = cache_of(100, 16, 9, 9)
+    for bad in (301, -1, 2**40, -301):
+        refused("vocabulary", cache, [[1], [2, bad]], [[[3]], [[4]]])
+        refused("vocabulary", cache, [[1], [2]], [[[3]], [[4, 0], [0, bad]]], None)
+        with pytest.raises(ValueError):
+            rollout.Decoder(SHAPE, device="cpu").read({}, cache, [0, 1], [[1], [bad]])
+    refused("answers for 3 prompts", cache, [[1], [2]], [[[3]], [[4]], [[5]]], None)
+    rollout.Decoder(SHAPE, device="cpu")._check_score(cache, [[0, 300], [2]], [[[300]]])
+
+
 def test_a_step_reads_no_length_past_the_cache(monkeypatch):
     """A slot past the cache is skipped and reported by the cache's calls; torch's indexing would end the
     GPU's context.  (Here with the cache's calls left out, on the CPU, where such an index raises.)"""
