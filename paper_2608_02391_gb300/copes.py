@@ -610,6 +610,7 @@ class KVCache:
         self.attend_workspace = None  # paged_attention's
         self._attend_room = 0         # its bytes
         self._attend_before = []      # the smaller ones that calls were given before it
+        self._streams = {}            # raw handles of the streams that calls ran on -> the streams
         self._attend_kept = {}        # (rows, query heads) -> bytes of it, templates of out and lse
 
     @classmethod
@@ -619,6 +620,18 @@ class KVCache:
         return cls(torch.empty((n_pages, n_layers, 2, n_kv_heads, page_size, head_dim), dtype=dtype, device=device),
                    torch.full((n_slots, table_width), -1, **i32), torch.zeros(n_slots, **i32),
                    torch.zeros(n_pages, **i32))
+
+    def _stream(self, stream) -> int:
+        """The stream of a call, noted for the cache's arrays and workspaces: where the handle is dropped before
+        that stream is through, their memory is nobody else's until it is."""
+        raw = _stream(stream)
+        if raw not in self._streams:
+            stream = self._streams[raw] = torch.cuda.current_stream() if stream is None else stream
+            for t in (self.pool, self.table, self.length, self.refs, self.workspace, self.attend_workspace,
+                      *self._attend_before):
+                if t is not None:
+                    t.record_stream(stream)
+        return raw
 
     def _ids(self, t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
         """The address of a list of int32 ids on the cache's device."""
@@ -652,6 +665,8 @@ class KVCache:
                 self._attend_before.append(self.attend_workspace)
             self._attend_room = max(need, 2 * self._attend_room)
             self.attend_workspace = _empty(_template((self._attend_room,), torch.uint8, self.pool.device), stream)
+            for used in self._streams.values():
+                self.attend_workspace.record_stream(used)
         return self.attend_workspace.data_ptr(), self._attend_room
 
 
@@ -660,7 +675,7 @@ def cache_grow(cache: KVCache, slots: torch.Tensor, add, stream=None) -> None:
     n = slots.numel()
     each, every = (cache._ids(add, n), 0) if isinstance(add, torch.Tensor) else (None, add)
     _check(load().copes_cache_grow(cache.ref, cache._ids(slots), n, each, every, cache.workspace.data_ptr(),
-                                   cache.workspace_bytes, _stream(stream)))
+                                   cache.workspace_bytes, cache._stream(stream)))
 
 
 def cache_append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None,
@@ -673,32 +688,32 @@ def cache_append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, s
         assert t.stride(2) == 1
     _check(load().copes_cache_append(cache.ref, layer, cache._ids(slots, n), cache._ids(position, n), n, k.data_ptr(),
                                      k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                     _stream(stream)))
+                                     cache._stream(stream)))
 
 
 def cache_fork(cache: KVCache, parents: torch.Tensor, children: torch.Tensor, stream=None) -> None:
     """copes_cache_fork: the empty slot children[i] becomes a copy of parents[i]."""
     n = parents.numel()
     _check(load().copes_cache_fork(cache.ref, cache._ids(parents), cache._ids(children, n), n,
-                                   cache.workspace.data_ptr(), cache.workspace_bytes, _stream(stream)))
+                                   cache.workspace.data_ptr(), cache.workspace_bytes, cache._stream(stream)))
 
 
 def cache_free(cache: KVCache, slots: torch.Tensor, stream=None) -> None:
     """copes_cache_free: empties `slots`."""
-    _check(load().copes_cache_free(cache.ref, cache._ids(slots), slots.numel(), _stream(stream)))
+    _check(load().copes_cache_free(cache.ref, cache._ids(slots), slots.numel(), cache._stream(stream)))
 
 
 def cache_compact(cache: KVCache, counts: Optional[torch.Tensor] = None, stream=None) -> None:
     """copes_cache_compact: the pages in use move to the lowest ids; `counts` (int32 [2], device)
     gets their number and how many moved."""
     _check(load().copes_cache_compact(cache.ref, cache._ids(counts, 2), cache.workspace.data_ptr(),
-                                      cache.workspace_bytes, _stream(stream)))
+                                      cache.workspace_bytes, cache._stream(stream)))
 
 
 def cache_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
     """copes_cache_copy_pages: pool[dst[i]] = pool[src[i]]."""
     n = src.numel()
-    _check(load().copes_cache_copy_pages(cache.ref, cache._ids(src), cache._ids(dst, n), n, _stream(stream)))
+    _check(load().copes_cache_copy_pages(cache.ref, cache._ids(src), cache._ids(dst, n), n, cache._stream(stream)))
 
 
 def paged_attention(cache: KVCache, layer: int, q: torch.Tensor, slots: Optional[torch.Tensor] = None,
@@ -722,7 +737,7 @@ def paged_attention(cache: KVCache, layer: int, q: torch.Tensor, slots: Optional
     ws, nbytes = cache.attend_space(n, heads, stream)
     _check(load().copes_paged_attention(cache.ref, layer, cache._ids(slots, n), n, q.data_ptr(), q.stride(0),
                                         q.stride(1), heads, d ** -0.5 if scale is None else scale, out.data_ptr(),
-                                        lse.data_ptr(), ws, nbytes, _stream(stream)))
+                                        lse.data_ptr(), ws, nbytes, cache._stream(stream)))
     return out, lse
 
 

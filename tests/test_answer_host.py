@@ -5,6 +5,7 @@ import ctypes
 import gc
 import os
 import weakref
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -132,13 +133,41 @@ def test_workspaces_that_calls_were_given_stay_with_the_handle(copes):
     """A captured call goes on writing to the address that it was given.  (On a handle without its
     constructor, which wants a GPU's tensors.)"""
     c = object.__new__(copes.KVCache)
-    c.pool, c.attend_workspace, c._attend_room, c._attend_before = torch.empty(0), None, 0, []
+    c.pool, c.attend_workspace, c._attend_room, c._attend_before, c._streams = torch.empty(0), None, 0, [], {}
     c._attend_shapes = lambda n, q_heads: (1000 * n, None, None)
     given = [(c.attend_space(n, 1), weakref.ref(c.attend_workspace)) for n in (1, 3, 2, 4, 300)]
     gc.collect()
     for (at, size), ws in given:
         assert ws() is not None and ws().data_ptr() == at and ws().numel() == size
     assert [size for (_, size), _ in given] == [1000, 3000, 3000, 6000, 300000]
+
+
+def test_every_array_of_a_handle_is_noted_on_every_stream_of_its_calls(copes, monkeypatch):
+    """On stand-ins for tensors and streams: what is freed later waits for these streams."""
+    class Tensor:
+        def __init__(self):
+            self.on = []
+
+        def record_stream(self, stream):
+            self.on.append(stream.cuda_stream)
+
+        def data_ptr(self):
+            return 256
+
+    monkeypatch.setattr(copes, "_empty", lambda template, stream: Tensor())
+    c = object.__new__(copes.KVCache)
+    arrays = [Tensor() for _ in range(5)]
+    c.pool, c.table, c.length, c.refs, c.workspace = arrays
+    c.pool.device = "cpu"
+    c.attend_workspace, c._attend_room, c._attend_before, c._streams = None, 0, [], {}
+    c._attend_shapes = lambda n, q_heads: (n, None, None)
+    streams = [SimpleNamespace(cuda_stream=i) for i in (5, 9)]
+    for n in (1, 10):
+        for s in streams:
+            c.attend_space(n, 1, s)
+            assert c._stream(s) == s.cuda_stream
+    for t in arrays + c._attend_before + [c.attend_workspace]:
+        assert t.on == [5, 9]
 
 
 def test_the_model_of_the_pages():

@@ -451,6 +451,28 @@ def test_a_graph_keeps_the_workspace_it_was_captured_with(copes):
     assert error_bits(copes) == 0
 
 
+def test_a_dropped_handle_keeps_its_memory_until_its_streams_are_through(copes):
+    cache = filled(copes, [2000, 33, 700], 1, 2, 16, 64, "bf16", seed=12)
+    q = torch.randn(3, 14, 64, device="cuda").bfloat16()
+    want = copes.paged_attention(cache, 0, q)
+    arrays = (cache.pool, cache.table, cache.length, cache.refs, cache.workspace, cache.attend_workspace)
+    held = [(t.data_ptr(), t.numel() * t.element_size()) for t in arrays]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)  # cycles: some 50 ms
+    out, lse = copes.paged_attention(cache, 0, q, stream=side)
+    del cache, arrays
+    others = [torch.full((size,), 0x7F, dtype=torch.uint8, device="cuda") for _, size in held for _ in range(3)]
+    busy = not side.query()
+    for x in others:
+        assert all(x.data_ptr() + x.numel() <= at or at + size <= x.data_ptr() for at, size in held)
+    assert busy  # else the check above says nothing
+    side.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert error_bits(copes) == 0
+
+
 # ---------------------------------------------------------------- token log probabilities
 def check_logprobs(copes, logits, target, top, scale=1.0):
     """ids exactly.  Numbers: the subtraction from the maximum, the product with the scale and the
