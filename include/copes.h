@@ -470,7 +470,8 @@ int copes_backup_update(const copes_backup_params *p, const copes_subspace *S, i
  *  length: device int32 [n_slots]: the tokens of each sequence, 0 for an empty slot.
  *  refs:   device int32 [n_pages]: how many table entries name the page; 0: free.
  * The caller owns the four arrays, which must be disjoint, and an all-zero length and refs
- * are an empty cache.  The calls below keep them consistent: a page is free, or held by one
+ * are an empty cache.  What a call writes (the workspace among it) is disjoint from its other
+ * arguments: a call whose arguments overlap so is refused.  The calls below keep them consistent: a page is free, or held by one
  * slot, or full and shared by several (copes_cache_fork).  Only pages of tokens below a
  * slot's length are ever read.  An id in table outside [0, n_pages) is not followed (its tokens
  * read as zeros) and is reported by copes_check (bit 32).

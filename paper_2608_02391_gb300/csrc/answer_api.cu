@@ -104,6 +104,30 @@ int check_workspace(const void *ws, size_t have, size_t need, const char *who) {
   return COPES_OK;
 }
 
+// Arrays that a call reads or writes besides the cache's.
+struct Array {
+  const void *at;
+  uint64_t bytes;
+};
+bool overlaps(const Array &a, const Array &b) { return overlaps(a.at, a.bytes, b.at, b.bytes); }
+Array pool_of(const copes::Cache &c) { return {c.pool, pool_bytes(c)}; }
+Array list_of(const int32_t *ids, int n) { return {ids, 4ull * n}; }
+
+// Refuses arrays of which one lies in the cache's books (table, length, refs) or in another; `reading`:
+// the last `reading` of them are only read, and may share memory with one another.
+template <int N>
+int check_disjoint(const copes::Cache &c, const Array (&a)[N], int reading, const char *who) {
+  const Array books[3] = {{c.table, 4ull * c.n_slots * c.table_width}, {c.length, 4ull * c.n_slots}, {c.refs, 4ull * c.n_pages}};
+  for (int i = 0; i < N; ++i) {
+    for (const Array &b : books)
+      if (overlaps(a[i], b))
+        return fail(COPES_ERR_INVALID_ARG, "%s: an argument lies in the cache's table, length or refs", who);
+    for (int j = 0; j < i && j < N - reading; ++j)
+      if (overlaps(a[i], a[j])) return fail(COPES_ERR_INVALID_ARG, "%s: an output or the workspace lies in another argument", who);
+  }
+  return COPES_OK;
+}
+
 size_t cache_workspace(const copes::Cache &c) { return 4 * copes::cache_workspace_ints(c.n_pages, c.n_slots); }
 
 }  // namespace
@@ -125,6 +149,8 @@ int copes_cache_grow(const copes_kv_cache *p, const int32_t *slots, int n, const
   if (!aligned(add, 4)) return fail(COPES_ERR_ALIGNMENT, "%s: add must be 4-byte aligned", who);
   if (!add && add_all < 0) return fail(COPES_ERR_INVALID_ARG, "%s: add_all is negative", who);
   if ((rc = check_workspace(workspace, workspace_bytes, cache_workspace(c), who))) return rc;
+  const Array arrays[] = {{workspace, cache_workspace(c)}, pool_of(c), list_of(slots, n), list_of(add, n)};
+  if ((rc = check_disjoint(c, arrays, 2, who))) return rc;
   return launch_status(copes::launch_cache_grow(c, slots, n, add, add_all, (int32_t *)workspace, stream), who);
 }
 
@@ -146,6 +172,8 @@ int copes_cache_append(const copes_kv_cache *p, int layer, const int32_t *slots,
   if (overlaps(k, extent(n, k_row, c.n_kv_heads, k_head, c.head_dim, c.elem), c.pool, pool_bytes(c)) ||
       overlaps(v, extent(n, v_row, c.n_kv_heads, v_head, c.head_dim, c.elem), c.pool, pool_bytes(c)))
     return fail(COPES_ERR_INVALID_ARG, "%s: k, v and the pool must be disjoint", who);
+  if (overlaps(list_of(slots, n), pool_of(c)) || overlaps(list_of(position, n), pool_of(c)))
+    return fail(COPES_ERR_INVALID_ARG, "%s: a list of ids lies in the pool", who);
   return launch_status(copes::launch_cache_append(c, layer, slots, position, n, k, k_row, k_head, v, v_row, v_head,
                                                   stream), who);
 }
@@ -158,6 +186,8 @@ int copes_cache_fork(const copes_kv_cache *p, const int32_t *parents, const int3
   if (rc) return rc;
   if ((rc = check_list(c, parents, n, true, who)) || (rc = check_list(c, children, n, true, who))) return rc;
   if ((rc = check_workspace(workspace, workspace_bytes, cache_workspace(c), who))) return rc;
+  const Array arrays[] = {{workspace, cache_workspace(c)}, pool_of(c), list_of(parents, n), list_of(children, n)};
+  if ((rc = check_disjoint(c, arrays, 2, who))) return rc;
   return launch_status(copes::launch_cache_fork(c, parents, children, n, (int32_t *)workspace, stream), who);
 }
 
@@ -167,6 +197,8 @@ int copes_cache_free(const copes_kv_cache *p, const int32_t *slots, int n, cudaS
   int rc = check_cache(p, &c, who);
   if (rc) return rc;
   if ((rc = check_list(c, slots, n, false, who))) return rc;
+  const Array arrays[] = {list_of(slots, n)};
+  if ((rc = check_disjoint(c, arrays, 1, who))) return rc;
   return launch_status(copes::launch_cache_free(c, slots, n, stream), who);
 }
 
@@ -178,6 +210,8 @@ int copes_cache_compact(const copes_kv_cache *p, int32_t *counts, void *workspac
   if (rc) return rc;
   if (!aligned(counts, 4)) return fail(COPES_ERR_ALIGNMENT, "%s: counts must be 4-byte aligned", who);
   if ((rc = check_workspace(workspace, workspace_bytes, cache_workspace(c), who))) return rc;
+  const Array arrays[] = {{workspace, cache_workspace(c)}, pool_of(c), {counts, 8}};
+  if ((rc = check_disjoint(c, arrays, 0, who))) return rc;
   return launch_status(copes::launch_cache_compact(c, counts, (int32_t *)workspace, stream), who);
 }
 
@@ -187,6 +221,8 @@ int copes_cache_copy_pages(const copes_kv_cache *p, const int32_t *src, const in
   int rc = check_cache(p, &c, who);
   if (rc) return rc;
   if ((rc = check_list(c, src, n, false, who)) || (rc = check_list(c, dst, n, false, who))) return rc;
+  if (overlaps(list_of(src, n), pool_of(c)) || overlaps(list_of(dst, n), pool_of(c)))
+    return fail(COPES_ERR_INVALID_ARG, "%s: a list of ids lies in the pool", who);
   return launch_status(copes::launch_cache_copy(c, src, dst, n, stream), who);
 }
 
@@ -225,13 +261,16 @@ int copes_paged_attention(const copes_kv_cache *p, int layer, const int32_t *slo
   if (!isfinite(scale)) return fail(COPES_ERR_INVALID_ARG, "%s: scale is not finite", who);
   if (!aligned(q, c.elem) || !aligned(out, 16) || !aligned(lse, 4))
     return fail(COPES_ERR_ALIGNMENT, "%s: out must be 16-byte aligned, q and lse to their type", who);
-  const uint64_t rows = (uint64_t)n * q_heads, out_bytes = rows * c.head_dim * c.elem;
-  if (overlaps(out, out_bytes, c.pool, pool_bytes(c)) || overlaps(lse, rows * 4, c.pool, pool_bytes(c)) ||
-      overlaps(out, out_bytes, lse, rows * 4) ||
-      overlaps(out, out_bytes, q, extent(n, q_row, q_heads, q_head, c.head_dim, c.elem)) ||
-      overlaps(lse, rows * 4, q, extent(n, q_row, q_heads, q_head, c.head_dim, c.elem)))
-    return fail(COPES_ERR_INVALID_ARG, "%s: q, out, lse and the pool must be disjoint", who);
-  if ((rc = check_workspace(workspace, workspace_bytes, copes::attend_workspace_bytes(c, n, q_heads), who))) return rc;
+  const size_t need = copes::attend_workspace_bytes(c, n, q_heads);
+  if ((rc = check_workspace(workspace, workspace_bytes, need, who))) return rc;
+  const uint64_t rows = (uint64_t)n * q_heads;
+  const Array written[] = {{out, rows * c.head_dim * c.elem}, {lse, rows * 4}, {workspace, need}},
+              read[] = {pool_of(c), {q, extent(n, q_row, q_heads, q_head, c.head_dim, c.elem)}, list_of(slots, n)};
+  if ((rc = check_disjoint(c, written, 0, who))) return rc;
+  for (const Array &w : written)
+    for (const Array &r : read)
+      if (overlaps(w, r))
+        return fail(COPES_ERR_INVALID_ARG, "%s: out, lse and the workspace must be disjoint from q, slots and the pool", who);
   a.layer = layer;
   a.n = n;
   a.q_heads = q_heads;

@@ -129,6 +129,46 @@ def test_arguments_that_are_refused(copes):
         refused(copes, logprobs(**kw), code, "copes_token_logprobs")
 
 
+def test_arguments_in_the_cache_or_in_one_another_are_refused(copes):
+    """Each in the last byte of what it must not share, and read-only lists where they may lie."""
+    L, c = copes.load(), cache(copes)
+    ws, pool, table, length, refs = L.copes_cache_workspace_bytes(c), GOOD["pool"], GOOD["table"], GOOD["length"], GOOD["refs"]
+    pool_end, books = pool + 8 * 2 * 2 * 2 * 16 * 64 * 2, (table + 4 * 19, length + 4 * 3, refs + 4 * 7)
+
+    def check(name, call, fine, bad):
+        """`bad`: by the number of an argument what makes the call overlap; `fine` does not."""
+        for at, values in bad.items():
+            for v in values:
+                args = list(fine)
+                args[at] = v
+                refused(copes, call(*args), -1, name)
+
+    check("copes_cache_grow", lambda slots, add, work: L.copes_cache_grow(c, slots, 2, add, 0, work, BIG, None), (0x100, 0x200, WS),
+          {0: (*books, table - 4, WS, WS + ws - 4, pool), 1: (*books, length, WS - 4, pool_end - 4),
+           2: (pool, pool_end - 16, pool - 16, table, table - 16, 0xA000000, 0xB000010, 0xB000000 - 16)})
+    check("copes_cache_fork", lambda a, b, work: L.copes_cache_fork(c, a, b, 2, work, BIG, None), (0x100, 0x200, WS),
+          {0: (*books, WS, pool), 1: (*books, WS + ws - 4, pool_end - 4), 2: (pool, pool_end - 16, table, length - 16, refs)})
+    check("copes_cache_free", lambda slots: L.copes_cache_free(c, slots, 2, None), (0x100,), {0: (*books, table - 4)})
+    check("copes_cache_compact", lambda counts, work: L.copes_cache_compact(c, counts, work, BIG, None), (0x100, WS),
+          {0: (*books, pool, pool_end - 4, WS, WS + ws - 4, WS - 4), 1: (pool, pool_end - 16, table, length, refs)})
+    check("copes_cache_copy_pages", lambda a, b: L.copes_cache_copy_pages(c, a, b, 2, None), (0x100, 0x200),
+          {0: (pool, pool_end - 4, pool - 4), 1: (pool, pool_end - 4)})
+    check("copes_cache_append", lambda s, p: L.copes_cache_append(c, 0, s, p, 2, 0x100, 128, 64, 0x100, 128, 64, None),
+          (0x100, None), {0: (pool, pool_end - 4), 1: (pool - 4, pool_end - 4)})
+    need, out, lse, q = L.copes_paged_attention_workspace_bytes(c, 2, 8), 0xE0000000, 0xE1000000, 0xE2000000
+
+    def attend(slots, q, out, lse, work):
+        return L.copes_paged_attention(c, 0, slots, 2, q, 512, 64, 8, 0.1, out, lse, work, 1 << 20, None)
+
+    assert need < 1 << 20
+    check("copes_paged_attention", attend, (0x100, q, out, lse, WS),
+          {0: (out, out + 2044, lse, lse - 4, WS, WS + need - 4), 1: (WS, WS + need - 2, WS - 2046),
+           2: (table, table + 64, length, refs, refs - 16, WS, WS + (need - 1) // 16 * 16, pool),
+           3: (*books, WS, WS + need - 4, WS - 60, pool), 4: (pool, pool_end - 16, table, length, refs, out, lse, q)})
+    # what is only read may lie anywhere among what is only read: no refusal before the workspace's
+    assert L.copes_paged_attention(c, 0, table, 2, q, 512, 64, 8, 0.1, out, lse, None, 0, None) == -4
+
+
 def test_workspaces_that_calls_were_given_stay_with_the_handle(copes):
     """A captured call goes on writing to the address that it was given.  (On a handle without its
     constructor, which wants a GPU's tensors.)"""
