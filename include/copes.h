@@ -569,7 +569,8 @@ int copes_paged_attention(const copes_kv_cache *c, int layer, const int32_t *slo
  * gives NaN and is reported by copes_check (bit 32).  A logit of -inf is a masked token: no
  * probability, and nothing in the entropy.  A row of nothing else has logprob -inf, entropy
  * 0 and the lowest ids as alternatives, at -inf.  A NaN or +inf in a row makes its
- * outputs NaN, but for top_ids, which order NaN above +inf, and logprob 0 of padding. */
+ * outputs NaN, but for top_ids, which order NaN above +inf, and logprob 0 of padding.
+ * The outputs are disjoint from one another, from logits and from target. */
 int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_t row, const int64_t *target,
                          float scale, int top, float *logprob, float *entropy, int64_t *top_ids,
                          float *top_logprobs, cudaStream_t stream);

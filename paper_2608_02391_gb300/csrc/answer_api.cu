@@ -302,10 +302,13 @@ int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_
   if (!aligned(logits, elem_size(dtype)) || !aligned(target, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
       !aligned(top_ids, 8) || !aligned(top_logprobs, 4))
     return fail(COPES_ERR_ALIGNMENT, "%s: an array is not aligned to its type", who);
-  const uint64_t read = extent(n, row, 1, 0, vocab, elem_size(dtype)), written = (uint64_t)n * top;
-  if (overlaps(logits, read, logprob, 4ull * n) || overlaps(logits, read, entropy, 4ull * n) ||
-      overlaps(logits, read, top_ids, 8 * written) || overlaps(logits, read, top_logprobs, 4 * written))
-    return fail(COPES_ERR_INVALID_ARG, "%s: logits overlap an output", who);
+  const uint64_t rows = n, alternatives = (uint64_t)n * top;
+  const Array arrays[] = {{logprob, 4 * rows}, {entropy, 4 * rows}, {top_ids, 8 * alternatives}, {top_logprobs, 4 * alternatives},
+                          {logits, extent(n, row, 1, 0, vocab, elem_size(dtype))}, {target, 8 * rows}};
+  for (int i = 0; i < 6; ++i)
+    for (int j = 0; j < i && j < 4; ++j)
+      if (overlaps(arrays[i], arrays[j]))
+        return fail(COPES_ERR_INVALID_ARG, "%s: an output overlaps the logits, target or another output", who);
   copes::LogprobArgs a{};
   a.logits = logits;
   a.row = row;

@@ -169,6 +169,21 @@ def test_arguments_in_the_cache_or_in_one_another_are_refused(copes):
     assert L.copes_paged_attention(c, 0, table, 2, q, 512, 64, 8, 0.1, out, lse, None, 0, None) == -4
 
 
+def test_log_probabilities_into_one_another_or_the_targets_are_refused(copes):
+    L = copes.load()
+    fine = dict(logits=0x100000, target=0x1000, lp=0x2000, ent=0x3000, ids=0x4000, tlp=0x5000)
+
+    def call(logits, target, lp, ent, ids, tlp):
+        return L.copes_token_logprobs(logits, 0, 3, 100, 200, target, 1.0, 5, lp, ent, ids, tlp, None)
+
+    size = dict(logits=1000, target=24, lp=12, ent=12, ids=120, tlp=60)
+    for out in ("lp", "ent", "ids", "tlp"):
+        for other in set(fine) - {out}:
+            step = 8 if out == "ids" else 4
+            for at in (fine[other], fine[other] + size[other] - step, fine[other] - size[out] + step):
+                refused(copes, call(**{**fine, out: at // step * step}), -1, "copes_token_logprobs")
+
+
 def test_workspaces_that_calls_were_given_stay_with_the_handle(copes):
     """A captured call goes on writing to the address that it was given.  (On a handle without its
     constructor, which wants a GPU's tensors.)"""
