@@ -549,8 +549,10 @@ int copes_cache_copy_pages(const copes_kv_cache *c, const int32_t *src, const in
  * The new token's own key and value are in the cache before the call (grow, append).  A slot
  * without tokens gives 0 and -inf, and so does an id outside the cache (bit 32).
  * Scores, softmax and sums are fp32, with every product of bf16 values exact and fp32 values as
- * two terms of 11 bits.  An infinity or NaN among a slot's keys and values makes what it
- * reaches infinite or NaN; what lies past the slot's length is not read.
+ * two terms of 11 bits (2^-21 of a product lost at most).  An infinity or NaN among a slot's
+ * keys and values makes what it reaches infinite or NaN, and so do fp32 values of 2^128 - 2^116
+ * (3.40199e38) and more in q, keys or values, and sums of e^(s_t - max s) |v_t| past fp32; what lies past
+ * the slot's length is not read.
  * workspace: copes_paged_attention_workspace_bytes(c, n, q_heads) bytes, 16-byte aligned; its
  * contents need not be kept or cleared, and calls may share it in one stream's order. */
 size_t copes_paged_attention_workspace_bytes(const copes_kv_cache *c, int n, int q_heads);

@@ -33,7 +33,8 @@
 // Precision.  Scores, maxima, sums and outputs are fp32.  bf16: products are exact, and a weight
 // p goes into the second product as two bf16 terms (2^-16 of it lost; one term would lose 2^-8
 // where the tensor cores have room for both).  fp32: every factor is split into two tf32 terms
-// and three of the four products are taken (2^-22 lost at most: the product of the small terms).
+// and three of the four products are taken (2^-21 of a product lost at most: that of the small terms,
+// 2^-22, and what the splits lose).
 #include <math.h>
 
 #include "answer.h"
@@ -176,9 +177,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// x in two tf32 terms: hi rounded to nearest, so that x - hi is exact, of either sign and at most 2^-12
-// of x's power of two; of it the upper bits (2^-22 of x lost at most, either way).  The conversion
-// instruction does this, too, and slowly: 32 fp32 rows of up to 34,629 tokens took 329 us with it, 257 so.
+// x in two tf32 terms: hi rounded to nearest, so that x - hi is exact, of either sign and at most 2^-11
+// of x's power of two; of it the upper bits (2^-23 of x lost at most, either way).  From 2^128 - 2^116 on
+// x would round to infinity, and such values are the caller's not to give: to keep hi finite by
+// one more instruction takes 5% longer with heads of 64 to 128 and 16% with 256 (32 rows of up to 3,000: 106 us
+// and 123).  The conversion instruction rounds, too, and slowly: 32 fp32 rows of up to 34,629 tokens took
+// 329 us with it, 257 so.
 __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t &hi, uint32_t &lo) {
   hi = (x + 0x1000u) & 0xFFFFE000u;
   lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) & 0xFFFFE000u;

@@ -359,6 +359,24 @@ def test_attention_of_extreme_scores(copes):
         check_attention(cache, 0, q, range(4), 1.0, out, lse)
 
 
+def test_attention_of_the_largest_values(copes):
+    """The largest fp32 values that a split leaves finite, as value, key and query, where the results are finite."""
+    largest = [3.4019927e38, 3.4011621e38, 3.40039e38, 3.4e38]
+    for d in (8, 72, 128, 256):
+        cache = filled(copes, [1, 2, 1, 3], 1, 1, 4, d, "fp32", seed=d)
+        cache.pool.nan_to_num_(0.0)
+        page = lambda i: cache.pool[cache.table[i, 0].item(), 0, :, 0]  # [key or value][token][d]
+        q = torch.zeros(4, 4, d, device="cuda")
+        page(0)[1, 0] = torch.tensor([s * x for x in largest for s in (1, -1)], device="cuda").repeat(d // 8)
+        page(1)[1, 0], page(1)[1, 1] = largest[0], -largest[0]
+        page(2)[0, 0, 0] = -largest[0]  # a score of -2.6 by a tiny query and this scale
+        q[2, :, 0] = 2.0**-120
+        page(3)[0, :3, 1] = torch.tensor([2.0**-124, -2.0**-123, 2.0**-122], device="cuda")
+        q[3, :, 1] = torch.tensor(largest, device="cuda")
+        out, lse = copes.paged_attention(cache, 0, q, scale=0.01)
+        check_attention(cache, 0, q, range(4), 0.01, out, lse)
+
+
 def test_attention_reports_ids_outside_the_cache(copes):
     cache = filled(copes, [20, 40], 1, 2, 16, 64, "bf16", seed=3)
     q = torch.randn(3, 4, 64, device="cuda").bfloat16()
