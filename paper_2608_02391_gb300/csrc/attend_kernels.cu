@@ -32,7 +32,10 @@
 //
 // Precision.  Scores, maxima, sums and outputs are fp32.  bf16: products are exact, and a weight
 // p goes into the second product as two bf16 terms (2^-16 of it lost; one term would lose 2^-8
-// where the tensor cores have room for both).  fp32: every factor is split into two tf32 terms
+// where the tensor cores have room for both).  The matrix unit cuts its sums where an addition rounds
+// them, so a tile's go into a sum of their own, and that by an addition to the row's: continued in the
+// matrix unit a row of 131,071 tokens came out 2^-10 of itself too small (the additions cost 6% with heads of
+// 192, 4% with 256, 3% with 16 heads on one of the cache's, and nothing else measurable).  fp32: every factor is split into two tf32 terms
 // and three of the four products are taken (2^-21 of a product lost at most: that of the small terms,
 // 2^-22, and what the splits lose).
 #include <math.h>
@@ -390,9 +393,7 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
       }
 #pragma unroll
     for (int g = 0; g < S::DP / 32; ++g) {
-      // The matrix unit cuts its sums where an addition rounds them: a tile's go into a sum of
-      // their own, and that by an addition to the row's, lest thousands of tokens' cuts add up.
-      float sum[2][NT][4] = {};
+      float sum[2][NT][4] = {};  // of the tile
       const int piece = g * 8 + (lane >> 2);  // d = 32 g + 4 (lane / 4) + 0 .. 3
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -437,8 +438,11 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
       ldmatrix_trans(a, at + (uint32_t)(((i * 2 + ((lane >> 3) & 1)) ^ x) * 16));
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        mma_bf16(r.o[i][j], a, rest[j][0], rest[j][1]);
-        mma_bf16(r.o[i][j], a, p[j][0], p[j][1]);
+        float sum[4] = {};  // of the tile
+        mma_bf16(sum, a, rest[j][0], rest[j][1]);
+        mma_bf16(sum, a, p[j][0], p[j][1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.o[i][j][e] += sum[e];
       }
     }
   }

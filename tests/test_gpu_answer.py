@@ -359,6 +359,30 @@ def test_attention_of_extreme_scores(copes):
         check_attention(cache, 0, q, range(4), 1.0, out, lse)
 
 
+@pytest.mark.parametrize("heads,kv,d,n", [(32, 8, 128, 128), (14, 2, 64, 700), (8, 4, 256, 16), (32, 2, 96, 32)])
+def test_attention_of_long_rows_is_not_drawn_to_zero(copes, heads, kv, d, n):
+    """Weighted means of 131,071 positive values, by rows on the same pages.  Rounding to bf16 is off by 2^-8 at
+    most, either way, 2^-8 / sqrt(3) in the root mean square at most, independently for the kv d values: their mean
+    error lies within six of its deviations.  (Sums that are cut 16,000 times by up to 2^-23 of them lose 2^-10.)"""
+    tokens, pages = 131071, 8192
+    generator = torch.Generator("cuda").manual_seed(d)
+    pool = torch.rand(pages, 1, 2, kv, 16, d, device="cuda", generator=generator) + 0.5
+    pool *= 2 ** torch.rand(kv, 1, d, device="cuda", generator=generator)
+    pool = pool.bfloat16()
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").expand(n, pages).contiguous()
+    cache = copes.KVCache(pool, table, ids([tokens] * n), ids([n] * pages))
+    q = (torch.randn(d, device="cuda", generator=generator) * 0.3).bfloat16()
+    out, lse = copes.paged_attention(cache, 0, q.expand(n, heads, d))
+    keys, values = (pool[:, 0, i].transpose(0, 1).reshape(kv, -1, d)[:, :tokens].double() for i in (0, 1))
+    scores = keys @ q.double() * d ** -0.5
+    want = torch.einsum("gt,gtd->gd", torch.softmax(scores, -1), values)
+    off = out.double().view(n, kv, heads // kv, d) / want[None, :, None] - 1
+    assert off.abs().max() <= 1.01 * 2.0**-8
+    assert off.mean().abs() <= 6 * 2.0**-8 / (3 * kv * d) ** 0.5
+    assert (lse.double().view(n, kv, -1) - torch.logsumexp(scores, -1)[:, None]).abs().max() <= 2.0**-18
+    assert error_bits(copes) == 0
+
+
 def test_attention_of_the_largest_values(copes):
     """The largest fp32 values that a split leaves finite, as value, key and query, where the results are finite."""
     largest = [3.4019927e38, 3.4011621e38, 3.40039e38, 3.4e38]
