@@ -542,8 +542,8 @@ int copes_cache_copy_pages(const copes_kv_cache *c, const int32_t *src, const in
 
 /* Attention of one new token per row over its slot's pages of one layer.  Row i reads slot
  * slots[i] (device int32 [n]; NULL: slot i); query head h (q + i q_row + h q_head, elements)
- * reads key-value head h / (q_heads / n_kv_heads), and with s_t = scale q . k_t over the
- * slot's tokens t < length:
+ * reads key-value head h / (q_heads / n_kv_heads), and with s_t = scale q . k_t (scale log2 e
+ * finite in fp32) over the slot's tokens t < length:
  *   out[i][h] = sum_t softmax(s)_t v_t   ([n][q_heads][head_dim] of dtype),
  *   lse[i][h] = ln sum_t exp(s_t)        (fp32 [n][q_heads], or NULL).
  * The new token's own key and value are in the cache before the call (grow, append).  A slot

@@ -258,7 +258,8 @@ int copes_paged_attention(const copes_kv_cache *p, int layer, const int32_t *slo
   if (!slots && n > c.n_slots) return fail(COPES_ERR_SIZE, "%s: %d rows without slots, and %d slots", who, n, c.n_slots);
   if ((rc = check_q_heads(c, n, q_heads, who))) return rc;
   if (n && (!q || !out)) return fail(COPES_ERR_INVALID_ARG, "%s: q or out is NULL", who);
-  if (!isfinite(scale)) return fail(COPES_ERR_INVALID_ARG, "%s: scale is not finite", who);
+  if (!isfinite(scale * 1.44269504088896340736f))  // the kernel's, of log2
+    return fail(COPES_ERR_INVALID_ARG, "%s: scale log2 e is not finite in fp32", who);
   if (!aligned(q, c.elem) || !aligned(out, 16) || !aligned(lse, 4))
     return fail(COPES_ERR_ALIGNMENT, "%s: out must be 16-byte aligned, q and lse to their type", who);
   const size_t need = copes::attend_workspace_bytes(c, n, q_heads);

@@ -184,6 +184,14 @@ def test_log_probabilities_into_one_another_or_the_targets_are_refused(copes):
                 refused(copes, call(**{**fine, out: at // step * step}), -1, "copes_token_logprobs")
 
 
+def test_an_attention_scale_past_fp32_in_log2_is_refused(copes):
+    """A score of 0 would be 0 times infinity."""
+    L, c = copes.load(), cache(copes)
+    for scale, code in [(2.4e38, -1), (-3.4e38, -1), (2.3e38, -4), (-2.3e38, -4)]:  # -4: past this check, no workspace
+        refused(copes, L.copes_paged_attention(c, 0, None, 1, 0x100, 256, 64, 4, scale, 0xD000000, None, None, 0, None),
+                code, "copes_paged_attention")
+
+
 def test_workspaces_that_calls_were_given_stay_with_the_handle(copes):
     """A captured call goes on writing to the address that it was given.  (On a handle without its
     constructor, which wants a GPU's tensors.)"""
