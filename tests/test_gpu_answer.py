@@ -470,6 +470,46 @@ def test_calls_run_on_the_stream_they_are_given_and_in_a_graph(copes):
     assert error_bits(copes) == 0
 
 
+def test_cache_calls_in_a_graph(copes):
+    """Replays of a captured step do what the calls do one after the other: every page, count and value."""
+    d, kv, layers, ps = 64, 2, 3, 4
+    k, v = torch.randn(2, 3, kv, d, device="cuda").bfloat16()
+    rows, child, counts = ids([0, 1, 2]), ids([3, 4]), ids([0, 0])
+    src, dst = ids([2, 5]), ids([38, 39])
+
+    def fresh():
+        cache = copes.KVCache.empty(40, layers, kv, ps, d, 5, 6)
+        cache.pool.copy_(torch.arange(cache.pool.numel(), device="cuda").view(cache.pool.shape) % 251)
+        copes.cache_grow(cache, rows, ids([3, 9, 0]))
+        copes.cache_append(cache, 1, k, v, slots=ids([0, 1, 1]), position=ids([1, 8, 0]))
+        copes.cache_free(cache, ids([0]))
+        copes.cache_grow(cache, ids([0]), 2)
+        return cache
+
+    def step(cache):
+        copes.cache_grow(cache, rows, 1)
+        copes.cache_append(cache, 2, k, v, slots=rows)
+        copes.cache_fork(cache, rows[1:], child)
+        copes.cache_copy_pages(cache, src, dst)
+        copes.cache_free(cache, rows[1:2])
+        copes.cache_compact(cache, counts)
+        copes.cache_free(cache, child)
+        copes.cache_grow(cache, rows[1:2], 5)
+
+    cache, want = fresh(), fresh()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cache)
+    for _ in range(8):
+        graph.replay()
+        got = counts.clone()
+        step(want)
+        assert error_bits(copes) == 0
+        assert torch.equal(got, counts) and torch.equal(cache.pool, want.pool)
+        for name in ("table", "length", "refs"):
+            assert torch.equal(getattr(cache, name), getattr(want, name)), name
+
+
 def test_a_graph_keeps_the_workspace_it_was_captured_with(copes):
     """A larger call between capture and replay: the graph's workspace is nobody else's then."""
     lens = [3000] + [40] * 299
@@ -592,6 +632,22 @@ def test_logprobs_of_ties_masks_and_orders(copes, vocab, dtype):
             check_logprobs(copes, logits, target, top)
     check_logprobs(copes, logits[:1], target[:1] * 0, min(vocab, 5), scale=0.01)
     check_logprobs(copes, logits, target * 0, min(vocab, 5), scale=3.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,vocab", [(1, 151936), (400, 20011), (1, 700001)])
+def test_logprobs_whose_largest_recur(copes, n, vocab, dtype):
+    """The largest logits in one 16-byte piece of every 32: most threads see none of them, so hundreds surpass what
+    is known of the alternatives when the row has been read."""
+    piece = 8 if dtype == "bf16" else 4
+    g = torch.Generator("cuda").manual_seed(vocab)
+    logits = torch.randn(n, vocab, device="cuda", generator=g).to(DT[dtype])
+    place = torch.arange(vocab, device="cuda")
+    large = place // piece % 32 == 7
+    logits[:, large] = (torch.randn(n, int(large.sum()), device="cuda", generator=g) + 20).to(DT[dtype])
+    target = torch.randint(0, vocab, (n,), device="cuda", generator=g)
+    for top in (5, 32):
+        check_logprobs(copes, logits, target, top)
 
 
 def test_logprobs_rows_past_32_bits(copes):
