@@ -610,7 +610,8 @@ class KVCache:
         self.attend_workspace = None  # paged_attention's
         self._attend_room = 0         # its bytes
         self._attend_before = []      # the smaller ones that calls were given before it
-        self._streams = {}            # raw handles of the streams that calls ran on -> the streams
+        here = torch.cuda.current_stream()
+        self._streams = {here.cuda_stream: here}  # the allocation's, and those that calls ran on
         self._attend_kept = {}        # (rows, query heads) -> bytes of it, templates of out and lse
 
     @classmethod
@@ -622,8 +623,8 @@ class KVCache:
                    torch.zeros(n_pages, **i32))
 
     def _stream(self, stream) -> int:
-        """The stream of a call, noted for the cache's arrays and workspaces: where the handle is dropped before
-        that stream is through, their memory is nobody else's until it is."""
+        """The stream of a call, noted for the cache's arrays and workspaces where it is not the one that the
+        handle was made on: dropped before that stream is through, their memory is nobody else's until it is."""
         raw = _stream(stream)
         if raw not in self._streams:
             stream = self._streams[raw] = torch.cuda.current_stream() if stream is None else stream
@@ -665,8 +666,9 @@ class KVCache:
                 self._attend_before.append(self.attend_workspace)
             self._attend_room = max(need, 2 * self._attend_room)
             self.attend_workspace = _empty(_template((self._attend_room,), torch.uint8, self.pool.device), stream)
-            for used in self._streams.values():
-                self.attend_workspace.record_stream(used)
+            for raw, used in self._streams.items():
+                if raw != _stream(stream):
+                    self.attend_workspace.record_stream(used)
         return self.attend_workspace.data_ptr(), self._attend_room
 
 

@@ -208,8 +208,8 @@ def test_workspaces_that_calls_were_given_stay_with_the_handle(copes):
 def test_every_array_of_a_handle_is_noted_on_every_stream_of_its_calls(copes, monkeypatch):
     """On stand-ins for tensors and streams: what is freed later waits for these streams."""
     class Tensor:
-        def __init__(self):
-            self.on = []
+        def __init__(self, *streams):
+            self.on = [s.cuda_stream for s in streams]
 
         def record_stream(self, stream):
             self.on.append(stream.cuda_stream)
@@ -217,7 +217,7 @@ def test_every_array_of_a_handle_is_noted_on_every_stream_of_its_calls(copes, mo
         def data_ptr(self):
             return 256
 
-    monkeypatch.setattr(copes, "_empty", lambda template, stream: Tensor())
+    monkeypatch.setattr(copes, "_empty", lambda template, stream: Tensor(stream))
     c = object.__new__(copes.KVCache)
     arrays = [Tensor() for _ in range(5)]
     c.pool, c.table, c.length, c.refs, c.workspace = arrays
@@ -230,7 +230,7 @@ def test_every_array_of_a_handle_is_noted_on_every_stream_of_its_calls(copes, mo
             c.attend_space(n, 1, s)
             assert c._stream(s) == s.cuda_stream
     for t in arrays + c._attend_before + [c.attend_workspace]:
-        assert t.on == [5, 9]
+        assert sorted(set(t.on)) == [5, 9]  # allocated there or noted
 
 
 def test_the_model_of_the_pages():
