@@ -7,8 +7,9 @@
 // the fp32 units' whole rate before a single conversion, and 3% of the tensor cores': the bound is
 // HBM, and mma.sync on registers filled from shared memory is enough (tcgen05 takes 64 rows or more
 // of one operand; a group of query heads has 1 to 16, and a block of these has no room to wait in).
-// Measured: 128 rows of up to 16,384 tokens, 32/8 heads of 128, bf16: 4.24 GB in 605 us, 7.0 TB/s;
-// fp32, 32 rows of up to 34,629, heads of 80: 97% of the rate of a copy; heads of 256: 53%.
+// Measured: 128 rows of up to 16,384 tokens, 32/8 heads of 128, bf16: 4.24 GB in 605 us, 7.0 TB/s.  Of the
+// rate of a copy, 32 rows: bf16 of up to 8,000, 12/4 heads of 192 76%, of 256 86%; fp32 of up to 34,629,
+// heads of 80, 94%, of up to 8,000, heads of 192, 75%, of up to 3,000, heads of 256, 51%.
 //
 // Work.  A row's tokens are cut into tiles; the tiles of all rows and head groups, in one line,
 // are shared out evenly among as many blocks as the GPU runs at once, whatever the lengths are.
@@ -75,6 +76,8 @@ struct Shape {
   static constexpr int kSmem = kStages * kStage + kFixed;
   // blocks of an SM by its 228 KB, 1 KB of them taken for each block, and by its registers
   static constexpr int kFit = 228 * 1024 / (kSmem + 1280);
+  // (Three variants spill all the same: fp32 heads of 256 20 bytes of a thread, of 128 with two column
+  // tiles 40, of 64 side by side 16.)
   static constexpr int kByRegs = 65536 / (kThreads * (DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
   static constexpr int kPerSm = kFit < kByRegs ? kFit : kByRegs;
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
@@ -571,9 +574,9 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   RowsAhead rows_ahead;
   rows_ahead.begin(a, at.row);
   if (tid == 0 && (unsigned)rows_ahead.slot >= (unsigned)c.n_slots) flag_error(kErrCacheId);
-  // The tokens of the rows between `at` and `ahead`, by row % 8: the cursors are at most kStages + 1
-  // steps, and so rows, apart.
-  static_assert(S::kStages + 1 < 8, "a lane for each row between the cursors");
+  // The tokens of the rows between `at` and `ahead`, by row % 8: the cursors are at most kStages + 2
+  // steps, and so rows, apart (two look-ups before the first tile is asked for, one with each).
+  static_assert(S::kStages + 2 < 8, "a lane for each row between the cursors");
   int tokens_of_row = 0;
   // the next (row, head group); true where that is another row
   const auto next_unit = [&](Cursor &x) {
@@ -788,7 +791,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
 // the parts by turns, kBatch of them on their way at once.
 // Most blocks find nothing to join, and all that the SMs hold wait there for attend_kernel's end, so
 // there are to be many of them on an SM: 1,216 blocks took 9 us with the 80 registers of a batch of
-// 8, which only few rows in many parts want.
+// 8, which only few rows in many parts want.  (In the 40 of a batch of 4 28 bytes are spilled.)
 constexpr int kJoinThreads = 256;
 template <typename T, int kBatch>
 __global__ void __launch_bounds__(kJoinThreads, kBatch > 4 ? 3 : 6) join_kernel(AttendArgs a, const Split *split,
@@ -890,13 +893,23 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
   cfg.gridDim = dim3(blocks * per);
   cfg.blockDim = dim3(kJoinThreads);
   cfg.dynamicSmemBytes = 0;
+  // Batches of 8 parts where a row has many (us with 8 and with 4; 16/1 heads of 128, bf16: 1 row of 20,000 tokens 20.9,
+  // 37.3, 32 of up to 4,000 19.9, 17.7; 14/2 heads of 64: 1 row of 20,000 15.3, 19.0, 16 of up to 8,000 15.5, 14.2).  Near the
+  // bound it takes 8 where 4 suits better: 8 rows of up to 4,000 of the former 14.4, 13.1, of up to 8,000 of the latter 13.1, 12.4.
   const auto join = blocks >= 16 * (int64_t)a.n * a.c.n_kv_heads * groups ? join_kernel<T, 8> : join_kernel<T, 4>;
   return cudaLaunchKernelEx(&cfg, join, a, (const Split *)split, (const float *)part, S::kHeads, per, S::kSides);
 }
 
-// Heads side by side where there are three rows' for four of the blocks that run at once (32/8 heads
-// of 128, us on one head and side by side: 80 rows of up to 300 tokens 18.7, 20.4; 128 of them 25.7,
-// 25.2; 512 72.7, 64.2; 128 of up to 8,000 321.8, 318.8; 1,024 of up to 100 90, 55).
+// Heads side by side where there are three rows' for four of the blocks that run at once.  32/8 heads, us
+// on one head and side by side (* what the rule takes), rows of up to 300 tokens, and of up to 3,000:
+//                40 rows       120           160           480           960             120 (3,000)
+//   bf16  64     10.8* 11.8    16.7* 16.5    20.6* 19.9    42.3 37.2*    74.8 59.0*      65.0* 62.1
+//         96     12.0* 13.2    21.4 22.0*    27.0 25.8*    61.2 50.6*    113.7 83.1*     93.4 88.5*
+//         128    12.7* 14.1    23.1 22.9*    29.2 27.1*    67.3 56.6*    126.3 97.6*     114.4 114.3*
+//   fp32  64     14.7* 15.0    25.9* 26.0    31.8 31.2*    70.7 67.1*    130.1 120.0*    130.0* 126.7
+//         96     16.8* 16.2    29.8 28.9*    36.2 35.0*    83.1 78.2*    155.1 142.7*    166.7 171.1*
+//         128    19.8* 18.5    38.3 36.0*    47.6 44.6*    119.0 107.3*   225.3 203.1*   231.8 228.0*
+// and 1,024 rows of up to 100 (bf16, 128) 90, 52.
 template <typename T, int DP>
 cudaError_t one_group(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   using S = Shape<T, DP, 1, true>;

@@ -22,7 +22,8 @@ __device__ __forceinline__ void after_the_last() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// Exclusive prefix sum of v over the block and the block's total.  `s` holds 33 ints.
+// Exclusive prefix sum of v over the block of kPlanThreads and the block's total.  `s` holds 32 ints, one
+// for each warp.
 __device__ __forceinline__ int block_scan(int v, int *s, int *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = v;

@@ -33,7 +33,8 @@ __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_logprob_e
 
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMostThreads = 256, kMostWarps = kMostThreads / 32;
-// blocks of an SM: with a thread's next step on its way (shallow), or the next two (deep)
+// blocks of an SM: with a thread's next step on its way (shallow), or the next two (deep).  (With alternatives
+// three of the four variants spill 4 or 8 bytes of a thread in the registers that this leaves.)
 constexpr int per_sm(bool deep) { return deep ? 3 : 4; }
 constexpr int kThreadCells = 48;   // of a thread, at most
 constexpr int kReached = 512;      // cells read again by the fast way, at most
