@@ -60,6 +60,8 @@ enum {
 };
 
 enum { COPES_BF16 = 0, COPES_FP32 = 1 };
+/* Of a key-value cache alone: 8 bits a value (2 is no type). */
+enum { COPES_E4M3 = 3 };
 
 /* Stream tags: independent Philox streams under the same seed. */
 enum { COPES_TAG_NOISE = 0, COPES_TAG_INIT = 1, COPES_TAG_PARTITION = 2, COPES_TAG_SEED = 3,
@@ -475,12 +477,21 @@ int copes_backup_update(const copes_backup_params *p, const copes_subspace *S, i
  * slot, or full and shared by several (copes_cache_fork).  Only pages of tokens below a
  * slot's length are ever read.  An id in table outside [0, n_pages) is not followed (its tokens
  * read as zeros) and is reported by copes_check (bit 32).
- * head_dim is a multiple of 8 and at most COPES_MAX_HEAD_DIM; n_pages is at most
- * COPES_MAX_PAGES; table_width * page_size and n_slots * table_width are below 2^31. */
+ * head_dim is a multiple of 8 (of 16 for COPES_E4M3) and at most COPES_MAX_HEAD_DIM; n_pages is at most
+ * COPES_MAX_PAGES; table_width * page_size and n_slots * table_width are below 2^31.
+ *
+ * COPES_E4M3: a cache in 8 bits for a model in bf16, which is the type of k, v, q and out beside it.  The
+ * head_dim values of a token's key, or value, of one head are codes, floats of 4 exponent and 3 mantissa
+ * bits (up to 448, no infinity, 0x7F and 0xFF NaN), and share one byte b of 1 to 254: value = code * 2^(b - 127).
+ * A layer's part of a page is [2][n_kv_heads][page_size][head_dim] codes, then [2][n_kv_heads][page_size] such
+ * bytes, then zero to 15 bytes that make it a multiple of 16; pool is [n_pages][n_layers] of these.
+ * copes_cache_append writes with the power of two that brings the largest finite value into (224, 448] (at
+ * least 2^-126: rows of zeros and of less than 448 of those), rounded to nearest, ties to even: 2^-4 of
+ * a value lost at most, or 2^-17 of the row's largest where that is more.  An infinity or NaN becomes NaN. */
 enum { COPES_MAX_HEAD_DIM = 256, COPES_MAX_PAGES = 1 << 22, COPES_MAX_TOP = 32 };
 typedef struct {
   void *pool;
-  int dtype;        /* COPES_BF16 or COPES_FP32 */
+  int dtype;        /* COPES_BF16, COPES_FP32 or COPES_E4M3 */
   int n_pages;
   int n_layers;
   int n_kv_heads;
@@ -516,6 +527,14 @@ int copes_cache_append(const copes_kv_cache *c, int layer, const int32_t *slots,
                        const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
                        int64_t v_head, cudaStream_t stream);
 
+/* Reads back what the cache holds: keys and values of one layer, of token position[i] of slots[i] (slots and
+ * position as for copes_cache_append), to row i of k and v (strides as there, not negative, rows and heads
+ * disjoint).  Of COPES_E4M3, code * 2^(b - 127) rounded to bf16, which is exact from 2^-133 on.
+ * A row that is not a token of its slot becomes zeros and is reported (bit 32). */
+int copes_cache_read(const copes_kv_cache *c, int layer, const int32_t *slots, const int32_t *position, int n,
+                     void *k, int64_t k_row, int64_t k_head, void *v, int64_t v_row, int64_t v_head,
+                     cudaStream_t stream);
+
 /* Fork: the empty slot children[i] becomes a copy of parents[i] (device int32 [n], children
  * distinct and none of them a parent, parents may repeat).  Full pages are shared (refs grows by one); a partly filled
  * last page is copied whole, in all layers, to the free page with the lowest id, in the order
@@ -549,7 +568,8 @@ int copes_cache_copy_pages(const copes_kv_cache *c, const int32_t *src, const in
  * The new token's own key and value are in the cache before the call (grow, append).  A slot
  * without tokens gives 0 and -inf, and so does an id outside the cache (bit 32).
  * Scores, softmax and sums are fp32, with every product of bf16 values exact and fp32 values as
- * two terms of 11 bits (2^-21 of a product lost at most).  An infinity or NaN among a slot's
+ * two terms of 11 bits (2^-21 of a product lost at most).  Of COPES_E4M3, products are exact but for what of q is
+ * below 2^-32 of its row's largest (2^-39 of that lost at most).  An infinity or NaN among a slot's
  * keys and values makes what it reaches infinite or NaN, and so do fp32 values of 2^128 - 2^116
  * (3.40199e38) and more in q, keys or values, and sums of e^(s_t - max s) |v_t| past fp32; what lies past
  * the slot's length is not read.
@@ -576,6 +596,51 @@ int copes_paged_attention(const copes_kv_cache *c, int layer, const int32_t *slo
 int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_t row, const int64_t *target,
                          float scale, int top, float *logprob, float *entropy, int64_t *top_ids,
                          float *top_logprobs, cudaStream_t stream);
+
+/* The next token of each row of logits (as copes_token_logprobs takes them) from given random numbers u
+ * (fp32 [n], each in [0, 1)), under softmax(scale * logits), 1e-30 <= scale <= 1e38, cut to
+ *  - the top_k largest logits, equal ones by ascending id (0: all);
+ *  - of these the fewest, from the largest down, that hold top_p of their probability
+ *    (0 < top_p <= 1; 1: all);
+ *  - of these the ones with at least min_p of the largest's probability (0 <= min_p <= 1).
+ * The same numbers give the same token on every machine and in every batch: probabilities are counted
+ * in whole numbers.  With m the row's largest logit, t = (m - x)(scale log2 e) by fp32 operations,
+ * n = floor(t) and f = t - n, a token's weight is floor(P(f) 2^(40 - n)), P(f) in [1/2, 1] the polynomial of
+ * the fp32 coefficients -0.00089964044, 0.0090985559, -0.055210155, 0.24015228, -0.69314098, 1 by
+ * Horner's fused steps, which is 2^-f within 2^-21.  A token less likely than 2^-40 of the largest has
+ * weight 0 and is never drawn, nor is one whose m - x is past fp32.  top_p keeps what begins below
+ * ceil((double)top_p * (double)sum), and the token drawn is the first, by ascending id, at which the
+ * sum of the weights kept passes floor(floor(u 2^31) * sum / 2^31).
+ *   ids[i]:     the token (int64 [n]),
+ *   logprob[i]: its log probability among the tokens kept (fp32 [n]),
+ *   kept[i]:    how many these are (int32 [n]).
+ * A logit of -inf is a masked token.  A row of nothing else has id -1, logprob NaN and kept 0; so has one
+ * with a NaN or +inf among its logits or a u outside [0, 1), which copes_check reports (bit 32).
+ * vocab is at most COPES_MAX_SAMPLE_VOCAB.  The outputs are disjoint from one another, from logits and
+ * from u. */
+enum { COPES_MAX_SAMPLE_VOCAB = 4000000 };
+int copes_sample_tokens(const void *logits, int dtype, int n, int vocab, int64_t row, const float *u, float scale,
+                        int top_k, float top_p, float min_p, int64_t *ids, float *logprob, int32_t *kept,
+                        cudaStream_t stream);
+
+/* The residual sum after a block with the norms before and after it, for n rows of hidden values of dtype
+ * (row i of x at x + i x_row elements, and so on).  With rms(a) = sqrt(mean a^2 + eps):
+ *   z = y / rms(y) * out_weight     (y where out_weight is NULL),
+ *   s = x + scale * gate * z        (without gate where that is NULL),
+ *   sum = round(s),  normed = round(s / rms(s) * weight).
+ * s itself, not its rounding, is what is normed; everything between is fp32 (a square past it counts as it
+ * should).  y NULL: s is x, and out_weight, gate and sum are NULL.  Otherwise one of sum and normed may be
+ * NULL, and weight is NULL exactly where normed is.  out_weight and weight are [hidden] of dtype; gate is
+ * one for every channel (gate_row 0) or one for every value (rows gate_row apart).
+ * 1e-30 <= eps <= 1e30, so that a row of zeros gives zeros; scale is finite.  An infinity in s makes its
+ * normed value NaN and the others of its row 0; a NaN, all of the row.
+ * Row strides are not negative, and those of the outputs at least hidden where n > 1.  sum may be x, and normed
+ * may be y, in place (the same address and stride); otherwise what is written is disjoint from all else.
+ * hidden is at most COPES_MAX_HIDDEN. */
+enum { COPES_MAX_HIDDEN = 1 << 24 };
+int copes_residual_norm(int dtype, int n, int hidden, const void *x, int64_t x_row, const void *y, int64_t y_row,
+                        const void *out_weight, const void *gate, int64_t gate_row, float scale, const void *weight,
+                        float eps, void *sum, int64_t sum_row, void *normed, int64_t normed_row, cudaStream_t stream);
 
 /* ------------------------------------------------------------------- debug exports */
 

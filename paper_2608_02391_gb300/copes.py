@@ -21,10 +21,10 @@ LIB_PATH = os.path.join(HERE, "libcopes.so")
 OK = 0
 ERR_INVALID_ARG, ERR_ALIGNMENT, ERR_SIZE, ERR_WORKSPACE, ERR_CUDA, ERR_DEVICE_CHECK, ERR_UNSUPPORTED = \
     -1, -2, -3, -4, -5, -6, -7
-BF16, FP32 = 0, 1
+BF16, FP32, E4M3 = 0, 1, 3
 TAG_NOISE, TAG_INIT, TAG_PARTITION, TAG_SEED, TAG_CHUNK = 0, 1, 2, 3, 4
 MAX_MEMBERS, MAX_NOISE, MAX_K, TILE_MAX = 256, 256, 64, 1 << 20
-MAX_HEAD_DIM, MAX_PAGES, MAX_TOP = 256, 1 << 22, 32
+MAX_HEAD_DIM, MAX_PAGES, MAX_TOP, MAX_SAMPLE_VOCAB, MAX_HIDDEN = 256, 1 << 22, 32, 4_000_000, 1 << 24
 SUBSPACE_TILES, SUBSPACE_INDICES, SUBSPACE_HASH_REPLAY = 0, 1, 2
 PART_CONTIGUOUS, PART_TENSOR_GROUPS, PART_HASH, PART_RANDOM_CHUNKS = 0, 1, 2, 3
 SHAPE_NONE, SHAPE_ZSCORE, SHAPE_ZSCORE_GROUPED, SHAPE_CENTERED_RANK = 0, 1, 2, 3
@@ -123,6 +123,7 @@ SIGNATURES = {
     "copes_cache_workspace_bytes": (_SZ, [_VP]),
     "copes_cache_grow": (_I32, [_VP, _VP, _I32, _VP, _I32, _VP, _SZ, _VP]),
     "copes_cache_append": (_I32, [_VP, _I32, _VP, _VP, _I32, _VP, _I64, _I64, _VP, _I64, _I64, _VP]),
+    "copes_cache_read": (_I32, [_VP, _I32, _VP, _VP, _I32, _VP, _I64, _I64, _VP, _I64, _I64, _VP]),
     "copes_cache_fork": (_I32, [_VP, _VP, _VP, _I32, _VP, _SZ, _VP]),
     "copes_cache_free": (_I32, [_VP, _VP, _I32, _VP]),
     "copes_cache_compact": (_I32, [_VP, _VP, _VP, _SZ, _VP]),
@@ -130,6 +131,9 @@ SIGNATURES = {
     "copes_paged_attention_workspace_bytes": (_SZ, [_VP, _I32, _I32]),
     "copes_paged_attention": (_I32, [_VP, _I32, _VP, _I32, _VP, _I64, _I64, _I32, _F32, _VP, _VP, _VP, _SZ, _VP]),
     "copes_token_logprobs": (_I32, [_VP, _I32, _I32, _I32, _I64, _VP, _F32, _I32, _VP, _VP, _VP, _VP, _VP]),
+    "copes_sample_tokens": (_I32, [_VP, _I32, _I32, _I32, _I64, _VP, _F32, _I32, _F32, _F32, _VP, _VP, _VP, _VP]),
+    "copes_residual_norm": (_I32, [_I32, _I32, _I32, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _F32, _VP, _F32, _VP, _I64, _VP,
+                                   _I64, _VP]),
     "copes_debug_philox": (_I32, [_U64, _U64, _U64, _U32, _U32, _VP, _VP]),
     "copes_debug_normals": (_I32, [_U64, _U32, _U64, _U64, _VP, _VP]),
     "copes_debug_transform": (_I32, [_VP, _U64, _VP, _VP]),
@@ -583,23 +587,38 @@ def _empty(template: torch.Tensor, stream) -> torch.Tensor:
         return _empty_like(template, memory_format=_contiguous)
 
 
+@functools.lru_cache(maxsize=256)
+def _kv_template(n: int, kv: int, d: int, dtype, device) -> torch.Tensor:
+    return _template((n, kv, d), dtype, device)
+
+
 class KVCache:
     """A paged key-value cache (copes_kv_cache): pool [n_pages, n_layers, 2, n_kv_heads,
     page_size, head_dim] (bf16 or fp32), table [n_slots, table_width], length [n_slots] and
     refs [n_pages] (int32).  The tensors are the caller's and may be read at any time; the
     cache_* calls change them in stream order.  KVCache.empty allocates an empty cache.  The
     handle keeps the calls' workspaces: its calls run in one stream's order, and it outlives the
-    graphs that captured them."""
+    graphs that captured them.
+    An 8-bit cache (COPES_E4M3) of a bf16 model: pool is uint8 [n_pages, n_layers, KVCache.layer_bytes(*heads)],
+    heads = (n_kv_heads, page_size, head_dim); KVCache.empty takes dtype=torch.float8_e4m3fn."""
 
-    def __init__(self, pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, refs: torch.Tensor):
-        assert pool.dim() == 6 and pool.shape[2] == 2 and table.dim() == 2
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor, refs: torch.Tensor,
+                 heads: Optional[Tuple[int, int, int]] = None):
+        if heads is None:
+            assert pool.dim() == 6 and pool.shape[2] == 2
+            heads = tuple(pool.shape[3:])
+        else:
+            assert pool.dim() == 3 and pool.dtype == torch.uint8 and pool.shape[2] == self.layer_bytes(*heads)
+        assert table.dim() == 2
         assert length.shape == (table.shape[0],) and refs.shape == (pool.shape[0],)
         for t in (pool, table, length, refs):
             assert t.is_cuda and t.is_contiguous() and t.device == pool.device
         assert all(t.dtype == torch.int32 for t in (table, length, refs))
         self.pool, self.table, self.length, self.refs = pool, table, length, refs
-        self.dtype = _DTYPE_CODES[pool.dtype]
-        n_pages, n_layers, _, kv, ps, d = pool.shape
+        self.dtype = E4M3 if pool.dtype == torch.uint8 else _DTYPE_CODES[pool.dtype]
+        self.io_dtype = torch.bfloat16 if self.dtype == E4M3 else pool.dtype  # of q, k, v and out
+        n_pages, n_layers = pool.shape[:2]
+        self.heads = kv, ps, d = heads
         self.desc = KVCacheDesc(pool.data_ptr(), self.dtype, n_pages, n_layers, kv, ps, d, table.data_ptr(),
                                 table.shape[0], table.shape[1], length.data_ptr(), refs.data_ptr())
         self.ref = ctypes.byref(self.desc)
@@ -618,9 +637,16 @@ class KVCache:
     def empty(cls, n_pages: int, n_layers: int, n_kv_heads: int, page_size: int, head_dim: int, n_slots: int,
               table_width: int, dtype=torch.bfloat16, device="cuda") -> "KVCache":
         i32 = dict(dtype=torch.int32, device=device)
-        return cls(torch.empty((n_pages, n_layers, 2, n_kv_heads, page_size, head_dim), dtype=dtype, device=device),
-                   torch.full((n_slots, table_width), -1, **i32), torch.zeros(n_slots, **i32),
-                   torch.zeros(n_pages, **i32))
+        heads = (n_kv_heads, page_size, head_dim)
+        books = (torch.full((n_slots, table_width), -1, **i32), torch.zeros(n_slots, **i32), torch.zeros(n_pages, **i32))
+        if dtype == torch.float8_e4m3fn:
+            return cls(torch.empty((n_pages, n_layers, cls.layer_bytes(*heads)), dtype=torch.uint8, device=device), *books, heads=heads)
+        return cls(torch.empty((n_pages, n_layers, 2, *heads), dtype=dtype, device=device), *books)
+
+    @staticmethod
+    def layer_bytes(n_kv_heads: int, page_size: int, head_dim: int) -> int:
+        """Bytes of a layer's part of a page of an 8-bit cache: codes, then a byte for each key and value of a head."""
+        return -(-2 * n_kv_heads * page_size * (head_dim + 1) // 16) * 16
 
     def _stream(self, stream) -> int:
         """The stream of a call, noted for the cache's arrays and workspaces where it is not the one that the
@@ -652,7 +678,7 @@ class KVCache:
             if len(self._attend_kept) >= 256:
                 self._attend_kept.clear()
             kept = self._attend_kept[n, q_heads] = (
-                need, _template((n, q_heads, self.desc.head_dim), self.pool.dtype, self.pool.device),
+                need, _template((n, q_heads, self.desc.head_dim), self.io_dtype, self.pool.device),
                 _template((n, q_heads), torch.float32, self.pool.device))
         return kept
 
@@ -684,13 +710,26 @@ def cache_append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, s
                  position: Optional[torch.Tensor] = None, stream=None) -> None:
     """copes_cache_append: rows of k and v [n, n_kv_heads, head_dim] (any strides over rows and
     heads) into tokens `position` (default: the last ones) of `slots` (default: 0 .. n-1)."""
-    n, want = k.shape[0], cache.pool.shape
+    n, (kv, _, d) = k.shape[0], cache.heads
     for t in (k, v):
-        assert t.shape == (n, want[3], want[5]) and t.dtype == cache.pool.dtype and t.device == cache.pool.device
+        assert t.shape == (n, kv, d) and t.dtype == cache.io_dtype and t.device == cache.pool.device
         assert t.stride(2) == 1
     _check(load().copes_cache_append(cache.ref, layer, cache._ids(slots, n), cache._ids(position, n), n, k.data_ptr(),
                                      k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                                      cache._stream(stream)))
+
+
+def cache_read(cache: KVCache, layer: int, slots: Optional[torch.Tensor] = None, position: Optional[torch.Tensor] = None,
+               stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """copes_cache_read: keys and values [n, n_kv_heads, head_dim] of tokens `position` (default: the last ones) of
+    `slots` (default: all, in order)."""
+    n = cache.desc.n_slots if slots is None else slots.numel()
+    kv, _, d = cache.heads
+    like = _kv_template(n, kv, d, cache.io_dtype, cache.pool.device)
+    k, v = _empty(like, stream), _empty(like, stream)
+    _check(load().copes_cache_read(cache.ref, layer, cache._ids(slots, n), cache._ids(position, n), n, k.data_ptr(), kv * d, d,
+                                   v.data_ptr(), kv * d, d, cache._stream(stream)))
+    return k, v
 
 
 def cache_fork(cache: KVCache, parents: torch.Tensor, children: torch.Tensor, stream=None) -> None:
@@ -725,7 +764,7 @@ def paged_attention(cache: KVCache, layer: int, q: torch.Tensor, slots: Optional
     over slot slots[i] (default: i), scale 1 / sqrt(head_dim) by default.  Returns (out, lse):
     [n, q_heads, head_dim] and fp32 [n, q_heads]."""
     n, heads, d = q.shape
-    assert d == cache.desc.head_dim and q.dtype == cache.pool.dtype and q.device == cache.pool.device
+    assert d == cache.desc.head_dim and q.dtype == cache.io_dtype and q.device == cache.pool.device
     assert q.stride(2) == 1
     _, like_out, like_lse = cache._attend_shapes(n, heads)
     if out is None:
@@ -776,6 +815,71 @@ def token_logprobs(logits: torch.Tensor, target: torch.Tensor, top: int = 0, sca
                                        top, logprob.data_ptr(), entropy.data_ptr(), ids.data_ptr(),
                                        top_logprobs.data_ptr(), _stream(stream)))
     return TokenLogprobs(logprob, entropy, ids, top_logprobs)
+
+
+@dataclass
+class SampledTokens:
+    """sample_tokens' result: int64 ids [n], fp32 logprob [n] among the tokens kept, int32 kept [n]."""
+    ids: torch.Tensor
+    logprob: torch.Tensor
+    kept: torch.Tensor
+
+
+@functools.lru_cache(maxsize=256)
+def _sample_templates(n: int, device) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    return tuple(_template((n,), dtype, device) for dtype in (torch.int64, torch.float32, torch.int32))
+
+
+def sample_tokens(logits: torch.Tensor, u: torch.Tensor, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+                  scale: float = 1.0, stream=None) -> SampledTokens:
+    """copes_sample_tokens: a token of each row of logits [n, vocab] (bf16 or fp32, any stride over rows) under
+    softmax(scale * logits) cut by top_k, top_p and min_p, by the random numbers u (fp32 [n], in [0, 1))."""
+    n, vocab = logits.shape
+    device = logits.device
+    assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
+    assert u.shape == (n,) and u.dtype == torch.float32 and u.device == device and u.is_contiguous()
+    dtype = _DTYPE_CODES[logits.dtype]
+    ids, logprob, kept = (_empty(like, stream) for like in _sample_templates(n, device))
+    _check(load().copes_sample_tokens(logits.data_ptr(), dtype, n, vocab, logits.stride(0), u.data_ptr(), scale, top_k, top_p,
+                                      min_p, ids.data_ptr(), logprob.data_ptr(), kept.data_ptr(), _stream(stream)))
+    return SampledTokens(ids, logprob, kept)
+
+
+@functools.lru_cache(maxsize=256)
+def _rows_template(n: int, hidden: int, dtype, device) -> torch.Tensor:
+    return _template((n, hidden), dtype, device)
+
+
+def residual_norm(x: torch.Tensor, weight: Optional[torch.Tensor], y: Optional[torch.Tensor] = None,
+                  out_weight: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, scale: float = 1.0,
+                  eps: float = 1e-6, out: Optional[torch.Tensor] = None, normed: Optional[torch.Tensor] = None,
+                  stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """copes_residual_norm: s = x + scale * gate * (y / rms(y) * out_weight) and s / rms(s) * weight, rows x and y
+    [n, hidden] (any stride over rows), weights [hidden], gate [hidden] or [n, hidden], all of one type.  Without y, s is x;
+    without out_weight y is not normed; without weight there is no second result.  Returns (s, normed): new
+    tensors, or `out` (which may be x) and `normed` (which may be y)."""
+    n, hidden = x.shape
+    dtype, device = x.dtype, x.device
+    assert x.is_cuda
+    for t in (x, y, out, normed):
+        assert t is None or (t.shape == (n, hidden) and t.dtype == dtype and t.device == device and (t.stride(1) == 1 or hidden == 1))
+    for t in (weight, out_weight):
+        assert t is None or (t.shape == (hidden,) and t.dtype == dtype and t.device == device and t.is_contiguous())
+    gate_row = 0
+    if gate is not None:
+        assert gate.shape in ((hidden,), (n, hidden)) and gate.dtype == dtype and gate.device == device
+        assert gate.stride(-1) == 1 or hidden == 1
+        gate_row = gate.stride(0) if gate.dim() == 2 else 0
+    like = _rows_template(n, hidden, dtype, device)
+    if y is not None and out is None:
+        out = _empty(like, stream)
+    if weight is not None and normed is None:
+        normed = _empty(like, stream)
+    row = lambda t: 0 if t is None else t.stride(0)
+    _check(load().copes_residual_norm(_DTYPE_CODES[dtype], n, hidden, x.data_ptr(), row(x), _ptr(y), row(y), _ptr(out_weight),
+                                      _ptr(gate), gate_row, scale, _ptr(weight), eps, _ptr(out), row(out), _ptr(normed),
+                                      row(normed), _stream(stream)))
+    return x if y is None else out, normed
 
 
 # ----------------------------------------------------------------------------- debug

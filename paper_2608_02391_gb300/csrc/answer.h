@@ -22,8 +22,9 @@ struct Cache {
   int32_t *table, *length, *refs;
   uint64_t page_bytes;   // of all layers
   uint64_t layer_elems;  // 2 * n_kv_heads * page_size * head_dim
+  uint64_t layer_bytes;  // of one layer's part of a page
   uint32_t head_elems;   // page_size * head_dim (below 2^31: page_size is)
-  int elem;              // bytes of an element
+  int elem;              // bytes of an element; 1: codes, whose exponents follow a layer's elements
   int n_pages, n_layers, n_kv_heads, page_size, head_dim, n_slots, table_width;
 };
 
@@ -49,6 +50,8 @@ cudaError_t launch_cache_grow(const Cache &c, const int32_t *slots, int n, const
 cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n,
                                 const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
                                 int64_t v_head, cudaStream_t s);
+cudaError_t launch_cache_read(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n, void *k,
+                              int64_t k_row, int64_t k_head, void *v, int64_t v_row, int64_t v_head, cudaStream_t s);
 cudaError_t launch_cache_fork(const Cache &c, const int32_t *parents, const int32_t *children, int n, int32_t *ws,
                               cudaStream_t s);
 cudaError_t launch_cache_free(const Cache &c, const int32_t *slots, int n, cudaStream_t s);
@@ -80,10 +83,33 @@ struct LogprobArgs {
 };
 cudaError_t launch_token_logprobs(int dtype, const LogprobArgs &a, cudaStream_t s);
 
+struct NormArgs {
+  int n, hidden;
+  const void *x, *y, *out_weight, *gate, *weight;  // y, out_weight, gate and weight may be NULL
+  int64_t x_row, y_row, gate_row;
+  float scale, eps;
+  void *sum, *normed;  // either may be NULL
+  int64_t sum_row, normed_row;
+};
+cudaError_t launch_residual_norm(int dtype, const NormArgs &a, cudaStream_t s);
+
+struct SampleArgs {
+  const void *logits;
+  int64_t row;
+  const float *u;
+  int n, vocab, top_k;
+  float scale, top_p, min_p;
+  int64_t *ids;
+  float *logprob;
+  int32_t *kept;
+};
+cudaError_t launch_sample_tokens(int dtype, const SampleArgs &a, cudaStream_t s);
+
 // Device error words of each translation unit: read and clear (synchronous); 0 without a copy
 // where none of its kernels was launched.
 unsigned read_and_clear_cache_errors();
 unsigned read_and_clear_attend_errors();
 unsigned read_and_clear_logprob_errors();
+unsigned read_and_clear_sample_errors();
 
 }  // namespace copes

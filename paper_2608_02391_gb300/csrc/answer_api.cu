@@ -38,6 +38,9 @@ uint64_t extent(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t 
 
 int elem_size(int dtype) { return dtype == COPES_BF16 ? 2 : 4; }
 
+// Of q, k, v and outputs beside a cache.
+int io_size(const copes::Cache &c) { return c.elem == 4 ? 4 : 2; }
+
 uint64_t pool_bytes(const copes::Cache &c) { return (uint64_t)c.n_pages * c.page_bytes; }
 
 // Checks a cache and fills in what the kernels take.
@@ -45,13 +48,15 @@ int check_cache(const copes_kv_cache *p, copes::Cache *c, const char *who) {
   if (!p) return fail(COPES_ERR_INVALID_ARG, "%s: cache is NULL", who);
   if (!p->pool || !p->table || !p->length || !p->refs)
     return fail(COPES_ERR_INVALID_ARG, "%s: pool, table, length or refs is NULL", who);
-  if (p->dtype != COPES_BF16 && p->dtype != COPES_FP32)
-    return fail(COPES_ERR_INVALID_ARG, "%s: dtype %d is neither COPES_BF16 nor COPES_FP32", who, p->dtype);
+  if (p->dtype != COPES_BF16 && p->dtype != COPES_FP32 && p->dtype != COPES_E4M3)
+    return fail(COPES_ERR_INVALID_ARG, "%s: dtype %d is neither COPES_BF16, COPES_FP32 nor COPES_E4M3", who, p->dtype);
   if (p->n_pages < 1 || p->n_layers < 1 || p->n_kv_heads < 1 || p->page_size < 1 || p->n_slots < 1 || p->table_width < 1)
     return fail(COPES_ERR_INVALID_ARG, "%s: every size of the cache must be at least 1", who);
   if (p->head_dim < 8 || p->head_dim > COPES_MAX_HEAD_DIM || p->head_dim % 8)
     return fail(COPES_ERR_SIZE, "%s: head_dim %d is not a multiple of 8 of at most %d", who, p->head_dim,
                 COPES_MAX_HEAD_DIM);
+  if (p->dtype == COPES_E4M3 && p->head_dim % 16)
+    return fail(COPES_ERR_SIZE, "%s: head_dim %d of an 8-bit cache is not a multiple of 16", who, p->head_dim);
   if (p->n_pages > COPES_MAX_PAGES)
     return fail(COPES_ERR_SIZE, "%s: more than %d pages", who, COPES_MAX_PAGES);
   const int64_t most = 0x7FFFFFFF;
@@ -64,12 +69,14 @@ int check_cache(const copes_kv_cache *p, copes::Cache *c, const char *who) {
   c->table = p->table;
   c->length = p->length;
   c->refs = p->refs;
-  c->elem = elem_size(p->dtype);
+  c->elem = p->dtype == COPES_E4M3 ? 1 : elem_size(p->dtype);
   c->head_elems = (uint32_t)(p->page_size * p->head_dim);
   c->layer_elems = 2ull * p->n_kv_heads * c->head_elems;
   if (c->layer_elems > (1ull << 44) / p->n_layers)
     return fail(COPES_ERR_SIZE, "%s: a page of more than 2^44 elements", who);
-  c->page_bytes = c->layer_elems * p->n_layers * c->elem;
+  c->layer_bytes = c->layer_elems * c->elem;
+  if (c->elem == 1) c->layer_bytes = (c->layer_bytes + 2ull * p->n_kv_heads * p->page_size + 15) / 16 * 16;
+  c->page_bytes = c->layer_bytes * p->n_layers;
   if (c->page_bytes > (1ull << 48) / p->n_pages) return fail(COPES_ERR_SIZE, "%s: a pool of more than 2^48 bytes", who);
   c->n_pages = p->n_pages;
   c->n_layers = p->n_layers;
@@ -166,16 +173,53 @@ int copes_cache_append(const copes_kv_cache *p, int layer, const int32_t *slots,
   if (!slots && n > c.n_slots) return fail(COPES_ERR_SIZE, "%s: %d rows without slots, and %d slots", who, n, c.n_slots);
   if (!aligned(position, 4)) return fail(COPES_ERR_ALIGNMENT, "%s: position must be 4-byte aligned", who);
   if (n && (!k || !v)) return fail(COPES_ERR_INVALID_ARG, "%s: k or v is NULL", who);
-  if (!aligned(k, c.elem) || !aligned(v, c.elem))
+  if (!aligned(k, io_size(c)) || !aligned(v, io_size(c)))
     return fail(COPES_ERR_ALIGNMENT, "%s: k and v must be aligned to their type", who);
   if ((int64_t)n * c.n_kv_heads > 0x7FFFFFFF) return fail(COPES_ERR_SIZE, "%s: more than 2^31-1 rows of heads", who);
-  if (overlaps(k, extent(n, k_row, c.n_kv_heads, k_head, c.head_dim, c.elem), c.pool, pool_bytes(c)) ||
-      overlaps(v, extent(n, v_row, c.n_kv_heads, v_head, c.head_dim, c.elem), c.pool, pool_bytes(c)))
+  if (overlaps(k, extent(n, k_row, c.n_kv_heads, k_head, c.head_dim, io_size(c)), c.pool, pool_bytes(c)) ||
+      overlaps(v, extent(n, v_row, c.n_kv_heads, v_head, c.head_dim, io_size(c)), c.pool, pool_bytes(c)))
     return fail(COPES_ERR_INVALID_ARG, "%s: k, v and the pool must be disjoint", who);
   if (overlaps(list_of(slots, n), pool_of(c)) || overlaps(list_of(position, n), pool_of(c)))
     return fail(COPES_ERR_INVALID_ARG, "%s: a list of ids lies in the pool", who);
   return launch_status(copes::launch_cache_append(c, layer, slots, position, n, k, k_row, k_head, v, v_row, v_head,
                                                   stream), who);
+}
+
+int copes_cache_read(const copes_kv_cache *p, int layer, const int32_t *slots, const int32_t *position, int n, void *k,
+                     int64_t k_row, int64_t k_head, void *v, int64_t v_row, int64_t v_head, cudaStream_t stream) {
+  const char *who = "copes_cache_read";
+  copes::Cache c;
+  int rc = check_cache(p, &c, who);
+  if (rc) return rc;
+  if (layer < 0 || layer >= c.n_layers) return fail(COPES_ERR_INVALID_ARG, "%s: layer %d of %d", who, layer, c.n_layers);
+  if ((rc = check_list(c, slots ? slots : p->length, n, false, who))) return rc;
+  if (!slots && n > c.n_slots) return fail(COPES_ERR_SIZE, "%s: %d rows without slots, and %d slots", who, n, c.n_slots);
+  if (!aligned(position, 4)) return fail(COPES_ERR_ALIGNMENT, "%s: position must be 4-byte aligned", who);
+  if (n && (!k || !v)) return fail(COPES_ERR_INVALID_ARG, "%s: k or v is NULL", who);
+  const int size = io_size(c);
+  if (!aligned(k, size) || !aligned(v, size))
+    return fail(COPES_ERR_ALIGNMENT, "%s: k and v must be aligned to their type", who);
+  if ((int64_t)n * c.n_kv_heads > 0x7FFFFFFF) return fail(COPES_ERR_SIZE, "%s: more than 2^31-1 rows of heads", who);
+  // Heads and rows of an output follow one another, in either order.
+  const int64_t strides[2][2] = {{k_row, k_head}, {v_row, v_head}}, most = 1ll << 40;
+  for (const auto &s : strides) {
+    if (s[0] < 0 || s[1] < 0 || s[0] > most || s[1] > most)
+      return fail(COPES_ERR_INVALID_ARG, "%s: a stride of k or v is negative or above 2^40", who);
+    const bool heads_inside = (c.n_kv_heads == 1 || s[1] >= c.head_dim) && (n <= 1 || s[0] >= (c.n_kv_heads - 1) * s[1] + c.head_dim);
+    const bool rows_inside = (n <= 1 || s[0] >= c.head_dim) && (c.n_kv_heads == 1 || s[1] >= (n - 1) * s[0] + c.head_dim);
+    if (!heads_inside && !rows_inside) return fail(COPES_ERR_INVALID_ARG, "%s: rows or heads of k or v overlap", who);
+  }
+  const Array arrays[] = {{k, extent(n, k_row, c.n_kv_heads, k_head, c.head_dim, size)},
+                          {v, extent(n, v_row, c.n_kv_heads, v_head, c.head_dim, size)}, pool_of(c), list_of(slots, n), list_of(position, n)};
+  if (overlaps(arrays[0], arrays[1])) return fail(COPES_ERR_INVALID_ARG, "%s: k and v overlap", who);
+  for (int i = 0; i < 2; ++i) {
+    for (int j = 2; j < 5; ++j)
+      if (overlaps(arrays[i], arrays[j]))
+        return fail(COPES_ERR_INVALID_ARG, "%s: k and v must be disjoint from slots, position and the pool", who);
+    const Array alone[] = {arrays[i]};
+    if ((rc = check_disjoint(c, alone, 0, who))) return rc;
+  }
+  return launch_status(copes::launch_cache_read(c, layer, slots, position, n, k, k_row, k_head, v, v_row, v_head, stream), who);
 }
 
 int copes_cache_fork(const copes_kv_cache *p, const int32_t *parents, const int32_t *children, int n, void *workspace,
@@ -260,13 +304,13 @@ int copes_paged_attention(const copes_kv_cache *p, int layer, const int32_t *slo
   if (n && (!q || !out)) return fail(COPES_ERR_INVALID_ARG, "%s: q or out is NULL", who);
   if (!isfinite(scale * 1.44269504088896340736f))  // the kernel's, of log2
     return fail(COPES_ERR_INVALID_ARG, "%s: scale log2 e is not finite in fp32", who);
-  if (!aligned(q, c.elem) || !aligned(out, 16) || !aligned(lse, 4))
+  if (!aligned(q, io_size(c)) || !aligned(out, 16) || !aligned(lse, 4))
     return fail(COPES_ERR_ALIGNMENT, "%s: out must be 16-byte aligned, q and lse to their type", who);
   const size_t need = copes::attend_workspace_bytes(c, n, q_heads);
   if ((rc = check_workspace(workspace, workspace_bytes, need, who))) return rc;
   const uint64_t rows = (uint64_t)n * q_heads;
-  const Array written[] = {{out, rows * c.head_dim * c.elem}, {lse, rows * 4}, {workspace, need}},
-              read[] = {pool_of(c), {q, extent(n, q_row, q_heads, q_head, c.head_dim, c.elem)}, list_of(slots, n)};
+  const Array written[] = {{out, rows * c.head_dim * io_size(c)}, {lse, rows * 4}, {workspace, need}},
+              read[] = {pool_of(c), {q, extent(n, q_row, q_heads, q_head, c.head_dim, io_size(c))}, list_of(slots, n)};
   if ((rc = check_disjoint(c, written, 0, who))) return rc;
   for (const Array &w : written)
     for (const Array &r : read)
@@ -323,6 +367,104 @@ int copes_token_logprobs(const void *logits, int dtype, int n, int vocab, int64_
   a.top_ids = top_ids;
   a.top_logprobs = top_logprobs;
   return launch_status(copes::launch_token_logprobs(dtype, a, stream), who);
+}
+
+int copes_sample_tokens(const void *logits, int dtype, int n, int vocab, int64_t row, const float *u, float scale,
+                        int top_k, float top_p, float min_p, int64_t *ids, float *logprob, int32_t *kept,
+                        cudaStream_t stream) {
+  const char *who = "copes_sample_tokens";
+  if (dtype != COPES_BF16 && dtype != COPES_FP32)
+    return fail(COPES_ERR_INVALID_ARG, "%s: dtype %d is neither COPES_BF16 nor COPES_FP32", who, dtype);
+  if (n < 0 || vocab < 1) return fail(COPES_ERR_INVALID_ARG, "%s: n is negative or vocab below 1", who);
+  if (vocab > COPES_MAX_SAMPLE_VOCAB)
+    return fail(COPES_ERR_SIZE, "%s: a vocabulary of more than %d", who, COPES_MAX_SAMPLE_VOCAB);
+  if (n > (1 << 27)) return fail(COPES_ERR_SIZE, "%s: more than 2^27 rows", who);
+  if (!(scale >= 1e-30f) || !(scale <= 1e38f))
+    return fail(COPES_ERR_INVALID_ARG, "%s: scale must be at least 1e-30 and at most 1e38", who);
+  if (top_k < 0) return fail(COPES_ERR_INVALID_ARG, "%s: top_k is negative", who);
+  if (!(top_p > 0.0f) || !(top_p <= 1.0f))
+    return fail(COPES_ERR_INVALID_ARG, "%s: top_p must be above 0 and at most 1", who);
+  if (!(min_p >= 0.0f) || !(min_p <= 1.0f))
+    return fail(COPES_ERR_INVALID_ARG, "%s: min_p must be at least 0 and at most 1", who);
+  if (n && (!logits || !u || !ids || !logprob || !kept))
+    return fail(COPES_ERR_INVALID_ARG, "%s: logits, u, ids, logprob or kept is NULL", who);
+  if (!aligned(logits, elem_size(dtype)) || !aligned(u, 4) || !aligned(ids, 8) || !aligned(logprob, 4) || !aligned(kept, 4))
+    return fail(COPES_ERR_ALIGNMENT, "%s: an array is not aligned to its type", who);
+  const uint64_t rows = n;
+  const Array arrays[] = {{ids, 8 * rows}, {logprob, 4 * rows}, {kept, 4 * rows}, {logits, extent(n, row, 1, 0, vocab, elem_size(dtype))},
+                          {u, 4 * rows}};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i && j < 3; ++j)
+      if (overlaps(arrays[i], arrays[j]))
+        return fail(COPES_ERR_INVALID_ARG, "%s: an output overlaps the logits, u or another output", who);
+  copes::SampleArgs a{};
+  a.logits = logits;
+  a.row = row;
+  a.u = u;
+  a.n = n;
+  a.vocab = vocab;
+  a.top_k = top_k < vocab ? top_k : 0;
+  a.scale = scale;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.ids = ids;
+  a.logprob = logprob;
+  a.kept = kept;
+  return launch_status(copes::launch_sample_tokens(dtype, a, stream), who);
+}
+
+int copes_residual_norm(int dtype, int n, int hidden, const void *x, int64_t x_row, const void *y, int64_t y_row,
+                        const void *out_weight, const void *gate, int64_t gate_row, float scale, const void *weight,
+                        float eps, void *sum, int64_t sum_row, void *normed, int64_t normed_row, cudaStream_t stream) {
+  const char *who = "copes_residual_norm";
+  if (dtype != COPES_BF16 && dtype != COPES_FP32)
+    return fail(COPES_ERR_INVALID_ARG, "%s: dtype %d is neither COPES_BF16 nor COPES_FP32", who, dtype);
+  if (n < 0 || hidden < 1) return fail(COPES_ERR_INVALID_ARG, "%s: n is negative or hidden below 1", who);
+  if (hidden > COPES_MAX_HIDDEN) return fail(COPES_ERR_SIZE, "%s: rows of more than %d values", who, COPES_MAX_HIDDEN);
+  if (n && !x) return fail(COPES_ERR_INVALID_ARG, "%s: x is NULL", who);
+  if (n && !y && (out_weight || gate || sum))
+    return fail(COPES_ERR_INVALID_ARG, "%s: out_weight, gate and sum go with y", who);
+  if (n && !sum && !normed) return fail(COPES_ERR_INVALID_ARG, "%s: neither sum nor normed is asked for", who);
+  if (n && !weight != !normed) return fail(COPES_ERR_INVALID_ARG, "%s: weight and normed go together", who);
+  if (!(eps >= 1e-30f) || !(eps <= 1e30f) || !isfinite(scale))
+    return fail(COPES_ERR_INVALID_ARG, "%s: eps must be at least 1e-30 and at most 1e30, and scale finite", who);
+  const int64_t most = 1ll << 40, strides[] = {x_row, y_row, gate_row, sum_row, normed_row};
+  for (const int64_t r : strides)
+    if (r < 0 || r > most) return fail(COPES_ERR_INVALID_ARG, "%s: a row stride is negative or above 2^40", who);
+  if (n > 1 && ((sum && sum_row < hidden) || (normed && normed_row < hidden)))
+    return fail(COPES_ERR_INVALID_ARG, "%s: rows of sum or normed overlap", who);
+  const int size = elem_size(dtype);
+  const void *all[] = {x, y, out_weight, gate, weight, sum, normed};
+  for (const void *p : all)
+    if (!aligned(p, size)) return fail(COPES_ERR_ALIGNMENT, "%s: an array is not aligned to its type", who);
+  const auto rows = [&](const void *p, int64_t r) { return Array{p, extent(n, r, 1, 0, hidden, size)}; };
+  const Array to[] = {rows(sum, sum_row), rows(normed, normed_row)};
+  const Array from[] = {rows(x, x_row), rows(y, y_row), rows(gate, gate_row), {out_weight, (uint64_t)hidden * size},
+                        {weight, (uint64_t)hidden * size}};
+  const bool in_place[] = {sum == x && sum_row == x_row, normed == y && normed_row == y_row};
+  if (overlaps(to[0], to[1])) return fail(COPES_ERR_INVALID_ARG, "%s: sum and normed overlap", who);
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 5; ++j)
+      if (overlaps(to[i], from[j]) && !(i == j && in_place[i]))
+        return fail(COPES_ERR_INVALID_ARG, "%s: an output overlaps an input, and not in place", who);
+  copes::NormArgs a{};
+  a.n = n;
+  a.hidden = hidden;
+  a.x = x;
+  a.y = y;
+  a.out_weight = out_weight;
+  a.gate = gate;
+  a.weight = weight;
+  a.x_row = x_row;
+  a.y_row = y_row;
+  a.gate_row = gate_row;
+  a.scale = scale;
+  a.eps = eps;
+  a.sum = sum;
+  a.normed = normed;
+  a.sum_row = sum_row;
+  a.normed_row = normed_row;
+  return launch_status(copes::launch_residual_norm(dtype, a, stream), who);
 }
 
 }  // extern "C"

@@ -293,7 +293,7 @@ int copes_check(cudaStream_t stream) {
                         copes::read_and_clear_partition_errors() |
                         copes::read_and_clear_replay_errors() | copes::read_and_clear_backup_errors() |
                         copes::read_and_clear_cache_errors() | copes::read_and_clear_attend_errors() |
-                        copes::read_and_clear_logprob_errors();
+                        copes::read_and_clear_logprob_errors() | copes::read_and_clear_sample_errors();
   if ((e = cudaGetLastError()) != cudaSuccess) return cuda_fail(e, "copes_check");
   if (bits)
     return fail(COPES_ERR_DEVICE_CHECK,
@@ -301,7 +301,7 @@ int copes_check(cudaStream_t stream) {
                 "outside the arena, 2 = gather index outside the arena, 4 = inconsistent partition "
                 "workspace or replay table, 8 = a bulk-copy wait ran out, 16 = an element outside "
                 "the partner buffer, 32 = a slot, page, token or target id outside its range or named "
-                "twice, 64 = too few free pages)",
+                "twice, or a row of logits that nothing can be drawn from, 64 = too few free pages)",
                 bits);
   return COPES_OK;
 }

@@ -52,11 +52,24 @@ __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_attend_er
 constexpr int kSMs = 152;
 constexpr unsigned kAll = 0xffffffffu;
 
+// An element of an 8-bit cache, and what queries and outputs are beside a cache of T.
+struct E4m3 {
+  uint8_t bits;
+};
+template <typename T>
+struct Beside {
+  using type = T;
+};
+template <>
+struct Beside<E4m3> {
+  using type = __nv_bfloat16;
+};
+
 // What a kernel variant is made of: T of the cache, head_dim padded to DP, NT x 8 query heads, and
 // whether the warps of a block have heads side by side or share one.
 template <typename T, int DP_, int NT_, bool kBeside>
 struct Shape {
-  static constexpr bool kFp32 = sizeof(T) == 4;
+  static constexpr bool kFp32 = sizeof(T) == 4, kFp8 = sizeof(T) == 1;
   static constexpr int DP = DP_, NT = NT_;
   // Warps of a block: what lets the most of them run on an SM.  (fp32 takes twice the room and three
   // times the products.)  Tiles in shared memory: one is worked on while the next is on its way.  With
@@ -183,6 +196,27 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t x) {
+  float2 r;
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.f32.f16 %0, l; cvt.f32.f16 %1, h;}" : "=f"(r.x), "=f"(r.y) : "r"(x));
+  return r;
+}
+// Codes 2i and 2i + 1 of four as fp16, exactly.
+__device__ __forceinline__ void codes_to_f16(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}"
+      : "=r"(lo), "=r"(hi) : "r"(codes));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
 // x in two tf32 terms: hi rounded to nearest, so that x - hi is exact, of either sign and at most 2^-11
 // of x's power of two; of it the upper bits (2^-23 of x lost at most, either way).  From 2^128 - 2^116 on
 // x would round to infinity, and such values are the caller's not to give: to keep hi finite by
@@ -220,10 +254,17 @@ __device__ __forceinline__ void mma_split3(float (&c)[3][4], const uint32_t (&a)
 
 // A 16-byte piece's place in a row of a tile is its number xor this, so that what one load
 // instruction reads lies in different banks.  (Rows of 4 pieces more than a multiple of 8 begin at
-// one of two places in the banks, by turns.)
+// one of two places in the banks, by turns.)  8 bits: a load takes two rows' 64 bytes of keys, or 32 of four
+// even or odd rows of values; of rows of 64 bytes these are made to begin in different halves of the banks.
 template <typename S>
 __device__ __forceinline__ int swizzle(int row) {
-  return S::kFp32 ? (row & 6) ^ ((row & 1) << 2) : S::kChunks % 8 ? (row >> 1) & 3 : row & 7;
+  if (S::kFp8 && S::kChunks == 4) return (row >> 1) & 2;
+  return S::kFp32 || S::kFp8 ? (row & 6) ^ ((row & 1) << 2) : S::kChunks % 8 ? (row >> 1) & 3 : row & 7;
+}
+
+template <typename S>
+__device__ __forceinline__ int row_at(int row) {  // where a tile's row is
+  return S::kFp8 && S::kChunks == 4 ? row ^ ((row >> 1) & 1) : row;
 }
 
 // Factor of a part with maximum m (of log2) in a whole with maximum M.  A part without weight has
@@ -248,10 +289,12 @@ struct Running {
   }
 };
 
-// Query heads as the columns of the first product's second factor.
+// Query heads as the columns of the first product's second factor.  8 bits: in fp16, each head divided by a power of
+// two, and of heads 8 nt + 2 (lane % 4) + {0, 1} that power.
 template <typename S>
 struct Queries {
   uint32_t b[S::DP / 16][S::NT][S::kFp32 ? 4 : 2];
+  float unit[S::NT][2];
 };
 
 // `wide`: rows of q are aligned to what a lane loads at a time, 4 bytes of bf16 and 16 of fp32.
@@ -262,10 +305,22 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, bool wide, int
 #pragma unroll
   for (int j = 0; j < S::NT; ++j) {
     const int h = j * 8 + (lane >> 2);
-    const T *from = (const T *)a.q + row * a.q_row + (first_head + h) * a.q_head;
+    const auto *from = (const typename Beside<T>::type *)a.q + row * a.q_row + (first_head + h) * a.q_head;
 #pragma unroll
     for (int k = 0; k < S::DP / 16; ++k) {
-      if constexpr (S::kFp32) {
+      if constexpr (S::kFp8) {
+        // one 16-byte piece of a key's row is the k of four products, 4 values of each
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int d = k / 4 * 64 + (lane & 3) * 16 + k % 4 * 4 + e * 2;
+          uint32_t x = 0;
+          if (h < heads && d < D) {
+            const uint16_t *u = reinterpret_cast<const uint16_t *>(from + d);
+            x = wide ? *reinterpret_cast<const uint32_t *>(u) : u[0] | (uint32_t)u[1] << 16;
+          }
+          q.b[k][j][e] = x;
+        }
+      } else if constexpr (S::kFp32) {
         // one 16-byte piece of a key's row is the four k of two products: a lane's are d .. d + 3
         const int d = k * 16 + (lane & 3) * 4;
         uint4 x = make_uint4(0, 0, 0, 0);
@@ -293,15 +348,75 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, bool wide, int
   }
 }
 
+// Queries for codes: the largest of a head comes to lie in [2^14, 2^15), so that fp16 holds all of a value of 8 bits
+// down to 2^-32 of it, and 2^-39 of it is lost at most of a smaller one.
+template <typename S>
+__device__ __forceinline__ void to_units(Queries<S> &q) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int j = 0; j < S::NT; ++j) {
+    uint32_t most = 0;  // of the finite ones
+#pragma unroll
+    for (int k = 0; k < S::DP / 16; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t lo = q.b[k][j][e] & 0x7FFFu, hi = q.b[k][j][e] >> 16 & 0x7FFFu;
+        most = max(most, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+      }
+    most = max(most, __shfl_xor_sync(kAll, most, 1));
+    most = max(most, __shfl_xor_sync(kAll, most, 2));
+    const uint32_t power = max(most >> 7, 27u) - 14;  // 127 more than the unit's
+    const float over = __uint_as_float((254 - power) << 23);
+#pragma unroll
+    for (int k = 0; k < S::DP / 16; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t x = q.b[k][j][e];
+        q.b[k][j][e] = pack_f16(__uint_as_float(x << 16) * over, __uint_as_float(x & 0xFFFF0000u) * over);
+      }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) q.unit[j][e] = __uint_as_float(__shfl_sync(kAll, power, ((lane & 3) * 2 + e) * 4) << 23);
+  }
+}
+
 // One warp's 16 tokens: scores, the running maximum and sum, and the weighted values.
-// `left`: how many of the 16 are tokens.
+// `left`: how many of the 16 are tokens.  8 bits: `power` is 127 more than the exponent of the key, or in the upper
+// half of the warp of the value, of token lane % 16.
 template <typename S>
 __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int left, float scale, const Queries<S> &q,
-                                          Running<S> &r) {
+                                          Running<S> &r, uint32_t power) {
   constexpr int NT = S::NT, KS = S::DP / 16, kPitch = S::kChunks * 16;
   const int lane = threadIdx.x & 31;
   float s[NT][4];
-  if constexpr (S::kFp32) {
+  if constexpr (S::kFp8) {
+    float part[NT][2][4] = {};
+    const int row = lane >> 2;
+    const uint32_t at = keys + row_at<S>(row) * kPitch;
+    const int x = swizzle<S>(row);
+#pragma unroll
+    for (int g = 0; g < KS / 4; ++g) {
+      const uint32_t off = (uint32_t)(((g * 4 + (lane & 3)) ^ x) * 16);
+      uint32_t u[4], v[4];
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(at + off) : "memory");
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                   : "r"(at + off + 8 * kPitch) : "memory");
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t a[4];
+        codes_to_f16(u[w], a[0], a[2]);
+        codes_to_f16(v[w], a[1], a[3]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mma_f16(part[j][w & 1], a, q.b[g * 4 + w][j][0], q.b[g * 4 + w][j][1]);
+      }
+    }
+    const float first = __uint_as_float(__shfl_sync(kAll, power, row) << 23);
+    const float second = __uint_as_float(__shfl_sync(kAll, power, row + 8) << 23);
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s[j][e] = (part[j][0][e] + part[j][1][e]) * q.unit[j][e & 1] * (e < 2 ? first : second);
+  } else if constexpr (S::kFp32) {
     constexpr int kSums = NT == 1 ? 2 : 1;  // one for each of the two products of a piece, registers permitting
     float part[NT][kSums][3][4] = {};
     const int row = lane >> 2;
@@ -381,7 +496,70 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
         for (int e = 0; e < 4; ++e) r.o[i][j][e] *= keep[j][e & 1];
   }
 
-  if constexpr (S::kFp32) {
+  if constexpr (S::kFp8) {
+    // The weights times their values' powers of two, in units that bring the tile's largest of a head into
+    // [2^14, 2^15), in two fp16 terms: 2^-22 of one, or 2^-39 of the largest, lost.
+    const float first = __uint_as_float(__shfl_sync(kAll, power, 16 + (lane >> 2)) << 23);
+    const float second = __uint_as_float(__shfl_sync(kAll, power, 24 + (lane >> 2)) << 23);
+    uint32_t p[NT][2], rest[NT][2];
+    float unit[NT][2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      uint32_t most = 0;  // two exponents
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        s[j][e] *= first;
+        s[j][2 + e] *= second;
+        most |= max(__float_as_uint(s[j][e]) >> 23, __float_as_uint(s[j][2 + e]) >> 23) << 16 * e;
+      }
+      most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 4));
+      most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 8));
+      most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 16));
+      float over[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t up = min(268u - (most >> 16 * e & 0xFFu), 253u);
+        over[e] = __uint_as_float(up << 23);
+        unit[j][e] = __uint_as_float((254u - up) << 23);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float u = s[j][2 * e] * over[0], v = s[j][2 * e + 1] * over[1];
+        const uint32_t hi = pack_f16(u, v);
+        const float2 held = unpack_f16(hi);
+        p[j][e] = transpose8(hi);
+        rest[j][e] = transpose8(pack_f16(u - held.x, v - held.y));
+      }
+    }
+    const int row = (lane & 3) * 2, x = swizzle<S>(row), y = swizzle<S>(row + 1);
+#pragma unroll
+    for (int g = 0; g < KS / 4; ++g) {
+      const int piece = g * 4 + (lane >> 3), half = (lane >> 2 & 1) * 8;  // d = 64 g + 8 (lane / 4) + 0 .. 7
+      const uint32_t at = values + row_at<S>(row) * kPitch + (piece ^ x) * 16 + half;
+      const uint32_t next = values + row_at<S>(row + 1) * kPitch + (piece ^ y) * 16 + half;
+      uint32_t u[2][2], v[2][2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[e][0]), "=r"(u[e][1]) : "r"(at + e * 8 * kPitch) : "memory");
+        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v[e][0]), "=r"(v[e][1]) : "r"(next + e * 8 * kPitch) : "memory");
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // d + 2 i and d + 2 i + 1
+        const unsigned pick = i & 1 ? 0x7362 : 0x5140;
+        uint32_t a[4];
+        codes_to_f16(__byte_perm(u[0][i / 2], v[0][i / 2], pick), a[0], a[1]);
+        codes_to_f16(__byte_perm(u[1][i / 2], v[1][i / 2], pick), a[2], a[3]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          float sum[4] = {};  // of the tile
+          mma_f16(sum, a, rest[j][0], rest[j][1]);
+          mma_f16(sum, a, p[j][0], p[j][1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r.o[g * 4 + i][j][e] = fmaf(unit[j][e & 1], sum[e], r.o[g * 4 + i][j][e]);
+        }
+      }
+    }
+  } else if constexpr (S::kFp32) {
     // P^T: 8 tokens x 8 heads at a time, in 16-bit halves.  A lane then has tokens 2j and 2j + 1
     // (j = lane % 4) as the k of one product: its values are read from those rows.
     uint32_t p[NT][2][2];
@@ -455,6 +633,7 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
 template <typename S>
 __device__ __forceinline__ int output_d(int i, int half) {
   const int lane = threadIdx.x & 31;
+  if (S::kFp8) return (i >> 2) * 64 + (lane >> 2) * 8 + (i & 3) * 2 + half;
   return S::kFp32 ? (i >> 1) * 32 + (lane >> 2) * 4 + (i & 1) * 2 + half : i * 16 + (lane >> 2) + half * 8;
 }
 
@@ -606,7 +785,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   s_o += side * S::kTeam * 8 * S::kRow;  // of the warps on this head, like s_m and s_l
   const uint32_t stages = smem_addr(smem) + warp * 2 * S::kPart;
   const uint64_t head_bytes = (uint64_t)c.head_elems * sizeof(T), to_values = c.n_kv_heads * head_bytes;
-  const char *pool = c.pool + (uint64_t)a.layer * c.layer_elems * sizeof(T) + side * head_bytes;
+  const char *pool = c.pool + a.layer * c.layer_bytes + side * head_bytes;
 
   // Where token (16 member + lane % 16) of a tile is: its page (-1 for none, -2 for one outside the
   // pool), its place there and the tile's key-value head.  Tables are read two tiles ahead of the
@@ -628,11 +807,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if (++looked < count) advance_ahead();
     return p;
   };
+  uint32_t powers[S::kStages] = {};  // of the tiles from the one that is worked on, 8 bits
   const auto ask = [&](int stage, const Place &p) {
-    if (!__any_sync(kAll, p.page != -1)) return;  // nothing of this warp's is read
+    if (!__any_sync(kAll, p.page != -1)) return 0u;  // nothing of this warp's is read
     const char *from = nullptr;
     if (p.page >= 0) from = pool + (uint64_t)p.page * c.page_bytes + p.kv * S::kSides * head_bytes + (uint64_t)p.place * D * sizeof(T);
     else if (p.page == -2) flag_error(kErrCacheId);
+    uint32_t power = 127;
+    if constexpr (S::kFp8)
+      if (from)
+        power = *reinterpret_cast<const uint8_t *>(c.pool + (uint64_t)p.page * c.page_bytes + a.layer * c.layer_bytes + c.layer_elems +
+                                                   (uint64_t)(((lane >> 4) * c.n_kv_heads + p.kv * S::kSides + side) * c.page_size + p.place));
     const uint32_t to = stages + stage * S::kStage;
 #pragma unroll
     for (int i = 0; i < S::kChunks / 2; ++i) {
@@ -640,16 +825,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       const char *src = reinterpret_cast<const char *>(__shfl_sync(kAll, (unsigned long long)from, row));
       const int bytes = src && piece * 16 < D * (int)sizeof(T) ? 16 : 0;  // 0: zeros
       src = bytes ? src + piece * 16 : c.pool;
-      const uint32_t dst = to + (row * S::kChunks + (piece ^ swizzle<S>(row))) * 16;
+      const uint32_t dst = to + (row_at<S>(row) * S::kChunks + (piece ^ swizzle<S>(row))) * 16;
       copy_async(dst, src, bytes);
       copy_async(dst + S::kPart, bytes ? src + to_values : src, bytes);
     }
+    return power;
   };
   Place next = look_up();
   // The queries of a (row, head group), and, registers permitting, of the next one, asked for a
   // (row, head group) before they are used.
   constexpr bool kNextToo = S::NT == 1 && (S::kFp32 ? S::DP <= 64 : S::DP <= 128);
-  const int64_t q_bytes = sizeof(T), q_wide = S::kFp32 ? 16 : 4;
+  const int64_t q_bytes = sizeof(typename Beside<T>::type), q_wide = S::kFp32 ? 16 : 4;
   const bool wide = (uintptr_t)a.q % q_wide == 0 && a.q_row * q_bytes % q_wide == 0 && a.q_head * q_bytes % q_wide == 0;
   Queries<S> q, q_next;
   const auto queries_of = [&](const Cursor &x, Queries<S> &to) {
@@ -660,6 +846,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   Cursor asking = at;  // whose queries were asked for last
   if (at.tile >= at.tiles) next_unit(asking);
   queries_of(asking, q);
+  if constexpr (S::kFp8) to_units(q);
   if constexpr (kNextToo) {
     next_unit(asking);
     if (count > at.tiles - at.tile) queries_of(asking, q_next);
@@ -670,7 +857,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s) {
     if (asked < count) {
-      ask(s, next);
+      powers[s] = ask(s, next);
       ++asked;
       next = after;
       after = look_up();
@@ -686,7 +873,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   Split begun{-1, 0, 0, 0};
   for (int j = 0; j < count; ++j) {
     if (asked < count) {
-      ask(asked % S::kStages, next);
+      powers[S::kStages - 1] = ask(asked % S::kStages, next);
       ++asked;
       next = after;
       after = look_up();
@@ -696,7 +883,9 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     __syncwarp();
     const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - member * 16 : 0;
     const uint32_t tile = stages + j % S::kStages * S::kStage;
-    if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
+    if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r, powers[0]);
+#pragma unroll
+    for (int s = 0; s + 1 < S::kStages; ++s) powers[s] = powers[s + 1];
     __syncwarp();
 
     const Cursor was = at;
@@ -706,6 +895,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       if constexpr (kNextToo) q = q_next;
       next_unit(asking);
       queries_of(asking, kNextToo ? q_next : q);
+      if constexpr (S::kFp8) to_units(q);
     }
 
     // the warps' states together
@@ -774,7 +964,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
         } else {
           o = *reinterpret_cast<const float4 *>(s_o + h * S::kRow + d);
         }
-        if (whole) store(o, (T *)a.out + (first + nt * 8 + h) * D + d);
+        if (whole) store(o, (typename Beside<T>::type *)a.out + (first + nt * 8 + h) * D + d);
         else *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
       }
     }
@@ -896,7 +1086,8 @@ cudaError_t launch(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes)
   // Batches of 8 parts where a row has many (us with 8 and with 4; 16/1 heads of 128, bf16: 1 row of 20,000 tokens 20.9,
   // 37.3, 32 of up to 4,000 19.9, 17.7; 14/2 heads of 64: 1 row of 20,000 15.3, 19.0, 16 of up to 8,000 15.5, 14.2).  Near the
   // bound it takes 8 where 4 suits better: 8 rows of up to 4,000 of the former 14.4, 13.1, of up to 8,000 of the latter 13.1, 12.4.
-  const auto join = blocks >= 16 * (int64_t)a.n * a.c.n_kv_heads * groups ? join_kernel<T, 8> : join_kernel<T, 4>;
+  using Out = typename Beside<T>::type;
+  const auto join = blocks >= 16 * (int64_t)a.n * a.c.n_kv_heads * groups ? join_kernel<Out, 8> : join_kernel<Out, 4>;
   return cudaLaunchKernelEx(&cfg, join, a, (const Split *)split, (const float *)part, S::kHeads, per, S::kSides);
 }
 
@@ -924,14 +1115,21 @@ cudaError_t one_group(const AttendArgs &a, void *ws, cudaStream_t s, size_t *byt
 template <typename T>
 cudaError_t by_shape(const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
   const bool many = a.q_heads / a.c.n_kv_heads > 8;
-  if (a.c.head_dim <= 64) return many ? launch<T, 64, 2, false>(a, ws, s, bytes) : one_group<T, 64>(a, ws, s, bytes);
-  if (a.c.head_dim <= 96) return many ? launch<T, 96, 2, false>(a, ws, s, bytes) : one_group<T, 96>(a, ws, s, bytes);
-  if (a.c.head_dim <= 128) return many ? launch<T, 128, 2, false>(a, ws, s, bytes) : one_group<T, 128>(a, ws, s, bytes);
-  if (a.c.head_dim <= 192) return launch<T, 192, 1, false>(a, ws, s, bytes);
-  return launch<T, 256, 1, false>(a, ws, s, bytes);
+  if constexpr (sizeof(T) == 1) {  // whole 64 components at a time
+    if (a.c.head_dim <= 64) return many ? launch<T, 64, 2, false>(a, ws, s, bytes) : one_group<T, 64>(a, ws, s, bytes);
+    if (a.c.head_dim <= 128) return many ? launch<T, 128, 2, false>(a, ws, s, bytes) : one_group<T, 128>(a, ws, s, bytes);
+    return launch<T, 256, 1, false>(a, ws, s, bytes);
+  } else {
+    if (a.c.head_dim <= 64) return many ? launch<T, 64, 2, false>(a, ws, s, bytes) : one_group<T, 64>(a, ws, s, bytes);
+    if (a.c.head_dim <= 96) return many ? launch<T, 96, 2, false>(a, ws, s, bytes) : one_group<T, 96>(a, ws, s, bytes);
+    if (a.c.head_dim <= 128) return many ? launch<T, 128, 2, false>(a, ws, s, bytes) : one_group<T, 128>(a, ws, s, bytes);
+    if (a.c.head_dim <= 192) return launch<T, 192, 1, false>(a, ws, s, bytes);
+    return launch<T, 256, 1, false>(a, ws, s, bytes);
+  }
 }
 
 cudaError_t dispatch(int dtype, const AttendArgs &a, void *ws, cudaStream_t s, size_t *bytes) {
+  if (dtype == COPES_E4M3) return by_shape<E4m3>(a, ws, s, bytes);
   return dtype == COPES_BF16 ? by_shape<__nv_bfloat16>(a, ws, s, bytes) : by_shape<float>(a, ws, s, bytes);
 }
 
@@ -943,7 +1141,7 @@ size_t attend_workspace_bytes(const Cache &c, int n, int q_heads) {
   a.n = n;
   a.q_heads = q_heads;
   size_t bytes = 0;
-  dispatch(c.elem == 2 ? COPES_BF16 : COPES_FP32, a, nullptr, 0, &bytes);
+  dispatch(c.elem == 1 ? COPES_E4M3 : c.elem == 2 ? COPES_BF16 : COPES_FP32, a, nullptr, 0, &bytes);
   return bytes ? bytes : 16;
 }
 

@@ -4,6 +4,8 @@
 // list's needs, by prefix sums), so that the same calls give the same pages; what has to be
 // copied then is copied by as many blocks as fill the GPU.  The plan is bound by latency (2 us a
 // launch in a graph), the copies by HBM.
+#include <cuda_fp16.h>
+
 #include "answer.h"
 
 namespace copes {
@@ -339,6 +341,17 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(Cache c, const
   }
 }
 
+// Where the token of a row of append or read is: its page and place there, false (and reported) where there is none.
+__device__ __forceinline__ bool find_token(const Cache &c, const int32_t *slots, const int32_t *position, int i, int &page, int &place) {
+  const int slot = slots ? slots[i] : i;
+  if ((unsigned)slot >= (unsigned)c.n_slots) return false;
+  const int tokens = slot_tokens(c, slot), t = position ? position[i] : tokens - 1;
+  if (t < 0 || t >= tokens) return false;
+  page = c.table[(int64_t)slot * c.table_width + t / c.page_size];
+  place = t % c.page_size;
+  return (unsigned)page < (unsigned)c.n_pages;
+}
+
 // A warp per (row, key-value head, key or value).
 template <typename T>
 __global__ void __launch_bounds__(256) append_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position,
@@ -349,23 +362,120 @@ __global__ void __launch_bounds__(256) append_kernel(Cache c, int layer, const i
   const int lane = threadIdx.x & 31;
   if (job >= (int64_t)n * c.n_kv_heads * 2) return;
   const int which = (int)(job & 1), h = (int)((job >> 1) % c.n_kv_heads), i = (int)((job >> 1) / c.n_kv_heads);
-  const int slot = slots ? slots[i] : i;
-  bool ok = (unsigned)slot < (unsigned)c.n_slots;
-  int page = 0, t = 0;
-  if (ok) {
-    const int tokens = slot_tokens(c, slot);
-    t = position ? position[i] : tokens - 1;
-    ok = t >= 0 && t < tokens;
-    if (ok) page = c.table[(int64_t)slot * c.table_width + t / c.page_size];
-    ok = ok && (unsigned)page < (unsigned)c.n_pages;
-  }
-  if (!ok) {
+  int page, place;
+  if (!find_token(c, slots, position, i, page, place)) {
     if (lane == 0) flag_error(kErrCacheId);
     return;
   }
   const T *from = which ? v + i * v_row + h * v_head : k + i * k_row + h * k_head;
   T *to = reinterpret_cast<T *>(c.pool + (uint64_t)page * c.page_bytes) + (uint64_t)layer * c.layer_elems +
-          (uint64_t)(which * c.n_kv_heads + h) * c.head_elems + (uint64_t)(t % c.page_size) * c.head_dim;
+          (uint64_t)(which * c.n_kv_heads + h) * c.head_elems + (uint64_t)place * c.head_dim;
+  for (int d = lane; d < c.head_dim; d += 32) to[d] = from[d];
+}
+
+// A token's key or value in memory of the caller's.
+struct Rows {
+  uint16_t *at;
+  int64_t row, head;
+};
+
+// 8 bits: a team of lanes, a power of two of at least head_dim / 8, per (row, key-value head, key or value), 8 values
+// each.  The row's unit is the power of two that brings its largest finite value into (224, 448]; as codes are
+// floats, a power of two costs no precision that a finer factor would keep.  `wide`: all rows are 16-byte aligned.
+template <bool kWrite>
+__global__ void __launch_bounds__(256) codes_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position, int n,
+                                                    Rows k, Rows v, int team, bool wide) {
+  after_the_last();
+  const int64_t job = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / team;
+  const int d = (int)(threadIdx.x & (team - 1)) * 8;
+  const bool there = job < (int64_t)n * c.n_kv_heads * 2;
+  const int h = (int)(job % c.n_kv_heads), which = (int)(job / c.n_kv_heads & 1), i = (int)(job / c.n_kv_heads / 2);
+  int page = 0, place = 0;
+  bool token = there && find_token(c, slots, position, i, page, place);
+  if (there && !token && d == 0) flag_error(kErrCacheId);
+  const bool mine = there && d < c.head_dim;
+  const Rows &rows = which ? v : k;
+  uint16_t *outside = mine ? rows.at + i * rows.row + h * rows.head + d : nullptr;
+  char *base = c.pool + (uint64_t)page * c.page_bytes + layer * c.layer_bytes;
+  const int head = which * c.n_kv_heads + h;
+  uint2 *codes = reinterpret_cast<uint2 *>(base + (uint64_t)head * c.head_elems + (uint64_t)place * c.head_dim + d);
+  uint8_t *power = reinterpret_cast<uint8_t *>(base + c.layer_elems + (uint64_t)head * c.page_size + place);
+  uint32_t w[4] = {};  // 8 values of bf16
+  if constexpr (kWrite) {
+    if (mine && token) {
+      if (wide) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(outside);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = outside[2 * e] | (uint32_t)outside[2 * e + 1] << 16;
+      }
+    }
+    uint32_t most = 0;  // as bits of bf16
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t x = w[e / 2] >> 16 * (e & 1) & 0x7FFFu;
+      if (x < 0x7F80u) most = max(most, x);
+    }
+    for (int s = team >> 1; s; s >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
+    // 127 more than the exponent e: 448 is 1.75 2^8
+    const int biased = max((int)(most >> 7) - 8 + ((most & 0x7Fu) > 0x60u), 1);
+    const float over = __uint_as_float((uint32_t)(254 - biased) << 23);
+    if (!mine || !token) return;
+    uint32_t pair[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float lo = __uint_as_float(w[e] << 16) * over, hi = __uint_as_float(w[e] & 0xFFFF0000u) * over;
+      if (isinf(lo)) lo = NAN;  // the type has no infinity
+      if (isinf(hi)) hi = NAN;
+      uint16_t two;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
+      pair[e] = two;
+    }
+    *codes = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
+    if (d == 0) *power = (uint8_t)biased;
+  } else {
+    if (!mine) return;
+    if (token) {
+      const uint2 x = *codes;
+      const float unit = __uint_as_float((uint32_t)*power << 23);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint16_t two = (uint16_t)((e < 2 ? x.x : x.y) >> 16 * (e & 1));
+        uint32_t both;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(both) : "h"(two));
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&both));
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * unit, f.y * unit);
+        w[e] = *reinterpret_cast<const uint32_t *>(&b);
+      }
+    }
+    if (wide) {
+      *reinterpret_cast<uint4 *>(outside) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) outside[e] = (uint16_t)(w[e / 2] >> 16 * (e & 1));
+    }
+  }
+}
+
+// A warp per (row, key-value head, key or value), as append_kernel.
+template <typename T>
+__global__ void __launch_bounds__(256) read_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position, int n, T *k,
+                                                   int64_t k_row, int64_t k_head, T *v, int64_t v_row, int64_t v_head) {
+  after_the_last();
+  const int64_t job = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (job >= (int64_t)n * c.n_kv_heads * 2) return;
+  const int which = (int)(job & 1), h = (int)((job >> 1) % c.n_kv_heads), i = (int)((job >> 1) / c.n_kv_heads);
+  T *to = which ? v + i * v_row + h * v_head : k + i * k_row + h * k_head;
+  int page, place;
+  if (!find_token(c, slots, position, i, page, place)) {
+    if (lane == 0) flag_error(kErrCacheId);
+    for (int d = lane; d < c.head_dim; d += 32) to[d] = 0;
+    return;
+  }
+  const T *from = reinterpret_cast<const T *>(c.pool + (uint64_t)page * c.page_bytes) + (uint64_t)layer * c.layer_elems +
+                  (uint64_t)(which * c.n_kv_heads + h) * c.head_elems + (uint64_t)place * c.head_dim;
   for (int d = lane; d < c.head_dim; d += 32) to[d] = from[d];
 }
 
@@ -426,17 +536,44 @@ cudaError_t launch_cache_copy(const Cache &c, const int32_t *src, const int32_t 
   return launch_after((unsigned)(jobs < 1 << 30 ? jobs : 1 << 30), kCopyThreads, s, copy_pages_kernel, c, src, dst, n);
 }
 
+template <bool kWrite>
+static cudaError_t launch_codes(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n, Rows k, Rows v,
+                                cudaStream_t s) {
+  int team = 2;
+  while (team * 8 < c.head_dim) team *= 2;
+  uintptr_t all = 0;
+  for (const Rows &r : {k, v}) all |= (uintptr_t)r.at | (uintptr_t)r.row * 2 | (uintptr_t)r.head * 2;
+  const unsigned blocks = (unsigned)(((int64_t)n * c.n_kv_heads * 2 * team + 255) / 256);
+  return launch_after(blocks, 256, s, codes_kernel<kWrite>, c, layer, slots, position, n, k, v, team, all % 16 == 0);
+}
+
 cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n,
                                 const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
                                 int64_t v_head, cudaStream_t s) {
   if (n == 0) return cudaSuccess;
   g_used = true;
+  if (c.elem == 1)
+    return launch_codes<true>(c, layer, slots, position, n, {(uint16_t *)k, k_row, k_head}, {(uint16_t *)v, v_row, v_head}, s);
   const unsigned blocks = (unsigned)(((int64_t)n * c.n_kv_heads * 2 + 7) / 8);
   if (c.elem == 2)
     return launch_after(blocks, 256, s, append_kernel<uint16_t>, c, layer, slots, position, n, (const uint16_t *)k, k_row,
                         k_head, (const uint16_t *)v, v_row, v_head);
   return launch_after(blocks, 256, s, append_kernel<uint32_t>, c, layer, slots, position, n, (const uint32_t *)k, k_row,
                       k_head, (const uint32_t *)v, v_row, v_head);
+}
+
+cudaError_t launch_cache_read(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n, void *k,
+                              int64_t k_row, int64_t k_head, void *v, int64_t v_row, int64_t v_head, cudaStream_t s) {
+  if (n == 0) return cudaSuccess;
+  g_used = true;
+  if (c.elem == 1)
+    return launch_codes<false>(c, layer, slots, position, n, {(uint16_t *)k, k_row, k_head}, {(uint16_t *)v, v_row, v_head}, s);
+  const unsigned blocks = (unsigned)(((int64_t)n * c.n_kv_heads * 2 + 7) / 8);
+  if (c.elem == 2)
+    return launch_after(blocks, 256, s, read_kernel<uint16_t>, c, layer, slots, position, n, (uint16_t *)k, k_row, k_head,
+                        (uint16_t *)v, v_row, v_head);
+  return launch_after(blocks, 256, s, read_kernel<uint32_t>, c, layer, slots, position, n, (uint32_t *)k, k_row, k_head,
+                      (uint32_t *)v, v_row, v_head);
 }
 
 // Read only once a kernel of this file was launched: copes_check of a program without a cache

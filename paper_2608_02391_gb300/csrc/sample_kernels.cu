@@ -1,0 +1,729 @@
+// The next token of each row of logits from a given random number, with the usual cuts.
+//
+// Every token has a weight that is a whole number, so that sums are exact in any order and a row's token
+// does not depend on how the row was shared out: with m the row's largest logit,
+//   t = (m - x) * (scale log2 e),  n = floor(t),  f = t - n   (each step rounded to fp32),
+//   weight = floor(P(f) 2^(40 - n)),   P(f) = 2^-f within 2^-21 (kPoly, Horner's steps fused).
+// The tokens in order of falling logit, equal ones by ascending id, are cut to the first top_k, to the
+// shortest beginning that holds top_p of their weight, and to t <= -log2 min_p.  Of the tokens kept, in
+// ascending id, the one drawn is the first at which the sum of the weights passes
+// floor(floor(u 2^31) total / 2^31).
+//
+// A row is read by a block, or by a cluster of up to 8 where rows alone would leave SMs without work.  It
+// comes from HBM once, for its maximum; what follows reads it again from L2.  About 16 instructions a
+// logit for its weight, against 2 bytes from HBM, make the weights' passes as dear as the first one.
+//
+// Cuts.  While the maximum is sought, each thread keeps the maxima of four cells of the row: the k-th
+// largest of the 2,048 cells is a bound that k logits at least reach.  Those that do are collected
+// (a few more than k, as a rule), sorted, cut, and drawn from, in shared memory.  Where the cut lies
+// behind what can be collected (a flat row, thousands of equal logits), it is bracketed by passes that
+// measure three bounds each, until what lies between can be collected.
+#include <float.h>
+#include <math.h>
+
+#include "answer.h"
+
+namespace copes {
+
+__device__ unsigned g_sample_error;
+static std::atomic<bool> g_used{false};
+__device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_sample_error, bit); }
+
+namespace {
+
+constexpr unsigned kAll = 0xffffffffu;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kEach = 4;                   // pieces of 16 bytes of a lane in a chunk, and cells of a thread
+constexpr int kChunkPieces = 32 * kEach;
+constexpr int kList = 4096;                // logits that can be collected
+constexpr int kMaxCluster = 8;
+using u64 = unsigned long long;
+
+// P(f) = 1 + f Q(f): Q of degree 4 that makes the largest |P 2^f - 1| on [0, 1] least (1.6e-7 before rounding),
+// with P at most 1 and at least 1/2.
+__device__ __forceinline__ float power(float f) {
+  float p = -0.0008996404358185828f;
+  p = fmaf(p, f, 0.009098555892705917f);
+  p = fmaf(p, f, -0.05521015450358391f);
+  p = fmaf(p, f, 0.2401522845029831f);
+  p = fmaf(p, f, -0.693140983581543f);
+  return fmaf(p, f, 1.0f);
+}
+
+__device__ __forceinline__ float distance(float x, float m, float c) { return fminf(__fmul_rn(__fsub_rn(m, x), c), 63.0f); }
+
+// The weight of a token at distance t: P lies in [1/2, 1], so its bits less those of 1/4 are P 2^24.
+__device__ __forceinline__ u64 weight_of(float t) {
+  const float z = __fadd_rd(t, 8388608.0f);  // 2^23 + n
+  const uint32_t p = __float_as_uint(power(t - (z - 8388608.0f))) - 0x3E800000u;
+  return ((u64)p << 16) >> (__float_as_uint(z) & 63u);
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float c;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+  return c;
+}
+
+// A row in pieces of 16 aligned bytes; what lies outside the row is -infinity.
+template <typename T>
+struct Row {
+  static constexpr int kN = 16 / (int)sizeof(T);
+  const uint4 *base;
+  const T *first;
+  int shift, vocab, pieces;  // elements of the first piece before the row
+  __device__ Row(const void *logits, int64_t row, int64_t i, int n) : first((const T *)logits + i * row), vocab(n) {
+    shift = (int)(((uintptr_t)first & 15) / sizeof(T));
+    base = reinterpret_cast<const uint4 *>((uintptr_t)first & ~(uintptr_t)15);
+    pieces = (shift + n - 1) / kN + 1;
+  }
+  __device__ __forceinline__ int id(int piece) const { return piece * kN - shift; }
+  __device__ __forceinline__ uint4 load(int piece) const {
+    const int at = id(piece);
+    if (at >= 0 && at + kN <= vocab) return base[piece];
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+      if (at + e < 0 || at + e >= vocab) continue;
+      if constexpr (sizeof(T) == 4) {
+        w[e] = reinterpret_cast<const uint32_t *>(first)[at + e];
+      } else {
+        const uint32_t x = reinterpret_cast<const uint16_t *>(first)[at + e];
+        w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | x << 16 : (w[e / 2] & 0xFFFF0000u) | x;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ static float element(const uint4 &p, int e) {
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+  }
+  __device__ __forceinline__ float at(int id) const {
+    if constexpr (sizeof(T) == 4) return first[id];
+    else return __bfloat162float(first[id]);
+  }
+  // An order of the elements (but NaN) as whole numbers of the type's size, +0 and -0 the same, and back.
+  static constexpr int kBits = 8 * (int)sizeof(T);
+  static constexpr uint32_t kInfinity = sizeof(T) == 4 ? 0xFF800000u : 0xFF80u, kNothing = sizeof(T) == 4 ? 0x007FFFFFu : 0x7Fu;
+  __device__ __forceinline__ static uint32_t key(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return (u ^ (uint32_t)((int32_t)u >> 31 | 0x80000000)) >> (32 - kBits);
+  }
+  __device__ __forceinline__ static float value_of(uint32_t key) {
+    const uint32_t u = key << (32 - kBits);
+    return __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u & ~((1ull << (32 - kBits)) - 1));
+  }
+  // The largest element of a piece and of what `before` holds (as `none` at first), in the elements' own type.
+  static constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+  __device__ __forceinline__ static uint32_t largest(uint32_t before, const uint4 &p) {
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 4) before = __float_as_uint(max_nan(__uint_as_float(before), __uint_as_float(w[e])));
+      else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(before) : "r"(before), "r"(w[e]));
+    }
+    return before;
+  }
+  __device__ __forceinline__ static float value(uint32_t largest) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(largest);
+    else return max_nan(__uint_as_float(largest << 16), __uint_as_float(largest & 0xFFFF0000u));
+  }
+};
+
+// What is in shared memory beside the list.
+struct Shared {
+  u64 sums[2][kWarps][4];        // of warps, by turns
+  u64 peers[2][kMaxCluster][4];  // of the blocks of a cluster
+  u64 scan[kWarps];
+  uint32_t counts[2][kWarps];
+  int collected;
+  int outcome;
+  u64 total;
+  int chunk;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ uint32_t remote(uint32_t at, int rank) {
+  uint32_t to;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(rank));
+  return to;
+}
+
+// The blocks that share a row: one, or a cluster.
+struct Group {
+  int size, rank, turn;
+  Shared *s;
+  __device__ __forceinline__ void sync() const {
+    if (size == 1) {
+      __syncthreads();
+    } else {
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+  }
+  // v[j] over all threads, by adding or, kMax, as the largest; the same in every thread.
+  template <int kM, bool kMax = false>
+  __device__ __forceinline__ void all(u64 (&v)[kM]) {
+    const auto join = [](u64 a, u64 b) { return kMax ? (a > b ? a : b) : a + b; };
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    turn ^= 1;
+#pragma unroll
+    for (int j = 0; j < kM; ++j) {
+#pragma unroll
+      for (int d = 16; d; d >>= 1) v[j] = join(v[j], __shfl_xor_sync(kAll, v[j], d));
+      if (lane == 0) s->sums[turn][warp][j] = v[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kM; ++j) {
+      v[j] = s->sums[turn][lane % kWarps][j];
+#pragma unroll
+      for (int d = kWarps / 2; d; d >>= 1) v[j] = join(v[j], __shfl_xor_sync(kAll, v[j], d));
+    }
+    if (size == 1) return;
+    if (warp == 0 && lane < size)
+#pragma unroll
+      for (int j = 0; j < kM; ++j)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(smem_addr(&s->peers[turn][rank][j]), lane)), "l"(v[j]) : "memory");
+    sync();
+#pragma unroll
+    for (int j = 0; j < kM; ++j) {
+      v[j] = s->peers[turn][0][j];
+      for (int r = 1; r < size; ++r) v[j] = join(v[j], s->peers[turn][r][j]);
+    }
+  }
+};
+
+// Runs f(piece number, piece) over this block's share of the row: chunk c is its where c % size == rank.
+// after(c) follows the pieces of chunk c, in all lanes of the warp that has it.
+template <typename T, typename F, typename After>
+__device__ __forceinline__ void for_row(const Row<T> &row, const Group &g, const F &f, const After &after) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int chunks = (row.pieces - 1) / kChunkPieces + 1;
+  for (int c = g.rank + g.size * warp; c < chunks; c += g.size * kWarps) {
+    uint4 p[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) p[j] = row.load(c * kChunkPieces + j * 32 + lane);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) f(c * kChunkPieces + j * 32 + lane, p[j], j);
+    after(c);
+  }
+}
+
+// Exclusive sums of v over the block's threads, and the total.
+__device__ __forceinline__ u64 block_scan(u64 v, Shared *s, u64 *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u64 x = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const u64 y = __shfl_up_sync(kAll, x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();  // scan may still be read
+  if (lane == 31) s->scan[warp] = x;
+  __syncthreads();
+  u64 before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += s->scan[w];
+    sum += s->scan[w];
+  }
+  *total = sum;
+  return before + x - v;
+}
+
+// Sorts list[0 .. n), n a power of two, ascending.
+__device__ void sort_list(u64 *list, int n) {
+  for (int k = 2; k <= n; k <<= 1)
+    for (int j = k >> 1; j; j >>= 1) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+        const int a = 2 * i - (i & (j - 1)), b = a + j;
+        const u64 x = list[a], y = list[b];
+        if ((x > y) == ((a & k) == 0)) {
+          list[a] = y;
+          list[b] = x;
+        }
+      }
+    }
+  __syncthreads();
+}
+
+// The largest b <= 65535 that at least k of the block's cells reach (0: fewer are that many), of the upper 16
+// bits of their keys.
+__device__ __forceinline__ uint32_t cell_bound(const uint32_t (&upper)[kEach], int k, Shared *s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t found = 0;
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t mid = found | 1u << bit;
+    unsigned mine = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) mine += upper[j] >= mid;
+    mine = __reduce_add_sync(kAll, mine);
+    if (lane == 0) s->counts[bit & 1][warp] = mine;
+    __syncthreads();
+    const unsigned all = __reduce_add_sync(kAll, lane < kWarps ? s->counts[bit & 1][lane] : 0u);
+    if ((int)all >= k) found = mid;
+  }
+  return found;
+}
+
+struct Cut {  // tokens are kept from the largest down to this one: key, and id among equal ones
+  uint32_t key;
+  int id;
+  __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= id); }
+};
+
+// floor(floor(u 2^31) total / 2^31), total < 2^62.
+__device__ __forceinline__ u64 place_of(float u, u64 total) {
+  const u64 r = (u64)(u * 2147483648.0f);
+  return (total >> 31) * r + (((total & 0x7FFFFFFFull) * r) >> 31);
+}
+
+__device__ __forceinline__ int power_of_two(int n) { return n <= 2 ? 2 : 1 << (32 - __clz(n - 1)); }
+
+// A row's problem and its steps; every step is called by all threads of the group.
+template <typename T>
+struct Sampler {
+  using R = Row<T>;
+  const SampleArgs &a;
+  const R &row;
+  Group &g;
+  Shared *s;
+  u64 *list, *weights;  // kList each; together the chunks' sums
+  float m, c, farthest;
+  int index;
+
+  __device__ __forceinline__ float t_of(float x) const { return distance(x, m, c); }
+  __device__ __forceinline__ float t_of(u64 entry) const { return t_of(R::value_of(~(uint32_t)(entry >> 32))); }
+
+  __device__ void write(int id, float logprob, int kept) const {
+    a.ids[index] = id;
+    a.logprob[index] = logprob;
+    a.kept[index] = kept;
+  }
+  // The token at distance t of tokens of `total` together.  The largest one's weight is 2^40, so no part is
+  // below 0.
+  __device__ void write_token(int id, float t, u64 total, int kept) const {
+    write(id, 0.0f - (t * 0.69314718055994531f + log1pf((float)(total - (1ull << 40)) * 0x1p-40f)), kept);
+  }
+
+  // Tokens with keys in [lo, hi) into the first block's list; how many there were.  Of what f returns for each
+  // token's x the group's sum goes to *sum.
+  template <typename F>
+  __device__ int collect(uint32_t lo, uint32_t hi, u64 *sum, const F &f) {
+    if (threadIdx.x == 0) s->collected = 0;
+    g.sync();
+    const uint32_t counter = remote(smem_addr(&s->collected), 0), to = remote(smem_addr(list), 0);
+    const float least = R::value_of(lo);
+    u64 v[1] = {0};
+    for_row(row, g, [&](int piece, const uint4 &p, int) {
+      v[0] += f(p);
+      if (!(R::value(R::largest(R::none, p)) >= least)) return;
+#pragma unroll
+      for (int e = 0; e < R::kN; ++e) {
+        const uint32_t key = R::key(R::element(p, e));
+        if (key < lo || key >= hi) continue;
+        int at;
+        asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(counter) : "memory");
+        const u64 entry = (u64)~key << 32 | (uint32_t)(row.id(piece) + e);
+        if (at < kList) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to + 8u * (uint32_t)at), "l"(entry) : "memory");
+      }
+    }, [](int) {});
+    if (sum) {
+      g.template all<1>(v);
+      *sum = v[0];
+    }
+    g.sync();
+    int count;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(count) : "r"(counter) : "memory");
+    return count;
+  }
+
+  // The first block: the list in order, and weights of its tokens.
+  __device__ void order(int count) {
+    const int n = power_of_two(count);
+    for (int i = count + threadIdx.x; i < n; i += kThreads) list[i] = ~0ull;
+    sort_list(list, n);
+    for (int i = threadIdx.x; i < count; i += kThreads) weights[i] = weight_of(t_of(list[i]));
+    __syncthreads();
+  }
+
+  // The first block: cuts the ordered list, which begins with the row's largest, and draws from it.  False where
+  // it does not hold top_p of `total` (0: of its first top_k).
+  __device__ bool draw_from_list(int count, u64 total) {
+    const int each = (count - 1) / kThreads + 1, first = min(count, (int)threadIdx.x * each), last = min(count, first + each);
+    const int most = a.top_k ? min(a.top_k, count) : count;
+    u64 mine = 0, all;
+    for (int i = first; i < min(last, most); ++i) mine += weights[i];
+    u64 before = block_scan(mine, s, &all);
+    if (a.top_k) total = all;
+    const u64 need = a.top_p < 1.0f ? (u64)ceil((double)total * (double)a.top_p) : ~0ull;
+    if (!a.top_k && all < need) return false;
+    u64 kept = 0, held = 0, kept_all, held_all;
+    for (int i = first; i < min(last, most) && before < need; ++i) {
+      if (weights[i] == 0 || t_of(list[i]) > farthest) break;
+      ++kept;
+      held += weights[i];
+      before += weights[i];
+    }
+    block_scan(kept, s, &kept_all);
+    block_scan(held, s, &held_all);
+    // by id, with the place of the weight
+    const int n = power_of_two((int)kept_all);
+    for (int i = threadIdx.x; i < n; i += kThreads)
+      list[i] = i < (int)kept_all ? list[i] << 32 | (uint32_t)i : ~0ull;
+    sort_list(list, n);
+    const u64 place = place_of(a.u[index], held_all);
+    const int per = (n - 1) / kThreads + 1, from = min((int)kept_all, (int)threadIdx.x * per), to = min((int)kept_all, from + per);
+    mine = 0;
+    for (int i = from; i < to; ++i) mine += weights[(uint32_t)list[i]];
+    before = block_scan(mine, s, &all);
+    for (int i = from; i < to; ++i) {
+      const u64 w = weights[(uint32_t)list[i]];
+      if (before <= place && place < before + w) {
+        const int id = (int)(list[i] >> 32);
+        write_token(id, t_of(row.at(id)), held_all, (int)kept_all);
+      }
+      before += w;
+    }
+    return true;
+  }
+
+  // The cut at the token at which the sum (of weights, or of ones) from the largest down reaches `need`.  Below
+  // `lo` it is not sought, and the sum from there up reaches it; `above` is the sum from hi up.
+  template <bool kWeights>
+  __device__ Cut find_cut(uint32_t lo, uint32_t hi, u64 above, u64 need) {
+    u64 between = ~0ull;
+    for (int turn = 0; hi - lo > 1 && between > kList; ++turn) {
+      // three bounds, of distance and of the key by turns: the first come near fast, the others come to an end
+      uint32_t bound[3];
+      const float t0 = t_of(R::value_of(hi - 1)), t1 = fminf(t_of(R::value_of(lo)), 48.0f);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        uint32_t b = hi - (uint32_t)(((u64)(hi - lo) * (j + 1)) >> 2);
+        if (!(turn & 1)) b = R::key(m - (t0 + (t1 - t0) * (0.25f * (j + 1))) / c);
+        bound[j] = min(max(b, lo + 1), hi - 1);
+      }
+      u64 v[4] = {0, 0, 0, 0}, n[3] = {0, 0, 0};
+      for_row(row, g, [&](int, const uint4 &p, int) {
+#pragma unroll
+        for (int e = 0; e < R::kN; ++e) {
+          const float x = R::element(p, e);
+          const uint32_t key = R::key(x);
+          const u64 w = kWeights ? weight_of(t_of(x)) : 1;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) {
+            if (key >= bound[j]) v[j] += w;
+            n[j] += key >= bound[j] && key < hi;
+          }
+          v[3] += key >= lo && key < hi;
+        }
+      }, [](int) {});
+      g.template all<4>(v);
+      g.template all<3>(n);
+      // the bounds fall: the last that does not reach `need` becomes hi, the first that does lo
+      u64 outside = 0, inside = v[3];
+      uint32_t new_lo = lo, new_hi = hi;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        if (v[j] < need) {
+          if (bound[j] < new_hi) {
+            new_hi = bound[j];
+            above = v[j];
+            outside = n[j];
+          }
+        } else if (bound[j] > new_lo) {
+          new_lo = bound[j];
+          inside = n[j];
+        }
+      }
+      between = inside - outside;
+      lo = new_lo;
+      hi = new_hi;
+    }
+    if (between <= kList) {
+      const int count = collect(lo, hi, nullptr, [](const uint4 &) { return 0ull; });
+      if (g.rank == 0) {
+        order(count);
+        const int each = (count - 1) / kThreads + 1, first = min(count, (int)threadIdx.x * each), last = min(count, first + each);
+        u64 mine = 0, all;
+        for (int i = first; i < last; ++i) mine += kWeights ? weights[i] : 1;
+        u64 before = above + block_scan(mine, s, &all);
+        for (int i = first; i < last; ++i) {
+          const u64 w = kWeights ? weights[i] : 1;
+          if (before < need && need <= before + w) s->total = list[i];
+          before += w;
+        }
+        __syncthreads();
+      }
+    } else {  // equal logits, too many to collect: the one of them by its rank among their ids
+      const u64 w = kWeights ? weight_of(t_of(R::value_of(lo))) : 1;
+      const u64 rank = (need - above - 1) / w;
+      id_of_rank(lo, rank);
+    }
+    g.sync();
+    u64 entry;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(entry) : "r"(remote(smem_addr(&s->total), 0)) : "memory");
+    g.sync();
+    return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
+  }
+
+  // Sums of chunks into the first block's shared memory.
+  __device__ __forceinline__ void put_chunk(int chunk, u64 sum) const {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kAll, sum, d);
+    if ((threadIdx.x & 31) == 0)
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(smem_addr(list), 0) + 8u * (uint32_t)chunk), "l"(sum) : "memory");
+  }
+  // The first block: the chunk in which the sum passes `place`, and the sum before it, in s->chunk and s->total.
+  __device__ void find_chunk(u64 place) const {
+    const int chunks = (row.pieces - 1) / kChunkPieces + 1, per = (chunks - 1) / kThreads + 1;
+    const int from = min(chunks, (int)threadIdx.x * per), to = min(chunks, from + per);
+    u64 mine = 0, all;
+    for (int i = from; i < to; ++i) mine += list[i];
+    u64 before = block_scan(mine, s, &all);
+    for (int i = from; i < to; ++i) {
+      if (before <= place && place < before + list[i]) {
+        s->chunk = i;
+        s->total = before;
+      }
+      before += list[i];
+    }
+    __syncthreads();
+  }
+  // One warp: the first token of s->chunk at which the sum of f(x, id) passes `place`: then(id, x).
+  template <typename F, typename Then>
+  __device__ void find_token(u64 place, const F &f, const Then &then) const {
+    const int lane = threadIdx.x & 31;
+    u64 before = s->total;
+    for (int j = 0; j < kEach; ++j) {
+      const int piece = s->chunk * kChunkPieces + j * 32 + lane;
+      const uint4 p = row.load(piece);
+      u64 mine = 0;
+#pragma unroll
+      for (int e = 0; e < R::kN; ++e) mine += f(R::element(p, e), row.id(piece) + e);
+      u64 x = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const u64 y = __shfl_up_sync(kAll, x, d);
+        if (lane >= d) x += y;
+      }
+      u64 at = before + x - mine;
+      if (at <= place && place < at + mine) {
+#pragma unroll
+        for (int e = 0; e < R::kN; ++e) {
+          const u64 w = f(R::element(p, e), row.id(piece) + e);
+          if (at <= place && place < at + w) then(row.id(piece) + e, R::element(p, e));
+          at += w;
+        }
+      }
+      before += __shfl_sync(kAll, x, 31);
+    }
+  }
+
+  // The token of this key with so many of lower ids before it, as an entry in the first block's s->total.
+  __device__ void id_of_rank(uint32_t key, u64 rank) {
+    const auto equal = [&](float x, int) -> u64 { return R::key(x) == key; };
+    g.sync();
+    u64 mine = 0;
+    for_row(row, g, [&](int piece, const uint4 &p, int) {
+#pragma unroll
+      for (int e = 0; e < R::kN; ++e) mine += equal(R::element(p, e), 0);
+    }, [&](int chunk) {
+      put_chunk(chunk, mine);
+      mine = 0;
+    });
+    g.sync();
+    if (g.rank != 0) return;
+    find_chunk(rank);
+    u64 entry = 0;
+    if (threadIdx.x < 32) {
+      bool mine_too = false;
+      find_token(rank, equal, [&](int id, float) {
+        entry = (u64)~key << 32 | (uint32_t)id;
+        mine_too = true;
+      });
+      __syncwarp();
+      if (mine_too) s->total = entry;
+    }
+    __syncthreads();
+  }
+
+  // Draws from all tokens that the cut and min_p keep.
+  __device__ void draw_from_row(bool cuts, const Cut &cut) {
+    const auto kept = [&](float x, int id) -> u64 {
+      const float t = t_of(x);
+      return t <= farthest && (!cuts || cut.keeps(R::key(x), id)) ? weight_of(t) : 0;
+    };
+    g.sync();  // the list was read
+    u64 sum = 0, v[2] = {0, 0};
+    for_row(row, g, [&](int piece, const uint4 &p, int) {
+#pragma unroll
+      for (int e = 0; e < R::kN; ++e) {
+        const u64 w = kept(R::element(p, e), row.id(piece) + e);
+        sum += w;
+        v[1] += w != 0;
+      }
+    }, [&](int chunk) {
+      v[0] += sum;
+      put_chunk(chunk, sum);
+      sum = 0;
+    });
+    g.template all<2>(v);
+    g.sync();
+    if (g.rank != 0) return;
+    const u64 place = place_of(a.u[index], v[0]);
+    find_chunk(place);
+    if (threadIdx.x < 32)
+      find_token(place, kept, [&](int id, float x) { write_token(id, t_of(x), v[0], (int)v[1]); });
+  }
+
+  __device__ void run() {
+    // the maximum, and those of the cells
+    uint32_t cell[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) cell[j] = R::none;
+    for_row(row, g, [&](int, const uint4 &p, int j) { cell[j] = R::largest(cell[j], p); }, [](int) {});
+    float top = -INFINITY;
+    uint32_t upper[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      top = max_nan(top, R::value(cell[j]));
+      upper[j] = R::key(R::value(cell[j])) >> (R::kBits - 16);
+    }
+    u64 v[1] = {isnan(top) ? ~0ull : (u64)R::key(top)};
+    g.template all<1, true>(v);
+    const float u = a.u[index];
+    const bool nothing = v[0] == R::kNothing, wrong = v[0] >= R::kInfinity || !(u >= 0.0f && u < 1.0f);
+    if (nothing || wrong) {
+      if (g.rank == 0 && threadIdx.x == 0) {
+        if (wrong) flag_error(kErrCacheId);
+        write(-1, nanf(""), 0);
+      }
+      return;
+    }
+    m = R::value_of((uint32_t)v[0]);
+    const uint32_t lowest = R::kNothing + 1, past = (uint32_t)v[0] + 1;
+    const bool top_k = a.top_k != 0, top_p = a.top_p < 1.0f;
+    if (!top_k && !top_p) return draw_from_row(false, Cut{0, 0});
+    u64 total = 0;
+    const auto weights_of = [&](const uint4 &p) {
+      u64 sum = 0;
+#pragma unroll
+      for (int e = 0; e < R::kN; ++e) sum += weight_of(t_of(R::element(p, e)));
+      return sum;
+    };
+    // what the cells' bound collects
+    const int want = top_k ? a.top_k : 512, share = (want - 1) / g.size + 1;
+    bool in_list = false;
+    if (share <= kThreads * kEach / 2) {
+      u64 least[1] = {0xFFFFull - cell_bound(upper, share, s)};
+      g.template all<1, true>(least);
+      const uint32_t bound = max((uint32_t)(0xFFFFull - least[0]) << (R::kBits - 16), lowest);
+      const int count = top_k ? collect(bound, past, nullptr, [](const uint4 &) { return 0ull; }) : collect(bound, past, &total, weights_of);
+      if (count <= kList) {
+        if (g.rank == 0) {
+          order(count);
+          const bool done = draw_from_list(count, total);
+          if (threadIdx.x == 0) s->outcome = done;
+        }
+        g.sync();
+        int done;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(done) : "r"(remote(smem_addr(&s->outcome), 0)) : "memory");
+        in_list = done;
+        g.sync();
+      }
+    }
+    if (in_list) return;
+    Cut cut{lowest, 0x7FFFFFFF};
+    if (top_k) {
+      u64 finite[1] = {0};
+      for_row(row, g, [&](int, const uint4 &p, int) {
+#pragma unroll
+        for (int e = 0; e < R::kN; ++e) finite[0] += R::key(R::element(p, e)) >= lowest;
+      }, [](int) {});
+      g.template all<1>(finite);
+      if (finite[0] > (u64)a.top_k) cut = find_cut<false>(lowest, past, 0, (u64)a.top_k);
+    }
+    if (top_p) {
+      u64 sum[1] = {0};
+      for_row(row, g, [&](int piece, const uint4 &p, int) {
+#pragma unroll
+        for (int e = 0; e < R::kN; ++e) {
+          const float x = R::element(p, e);
+          if (cut.keeps(R::key(x), row.id(piece) + e)) sum[0] += weight_of(t_of(x));
+        }
+      }, [](int) {});
+      g.template all<1>(sum);
+      const u64 need = (u64)ceil((double)sum[0] * (double)a.top_p);
+      cut = find_cut<true>(cut.key, past, 0, need);  // among the first top_k, whose weight is at least `need`
+    }
+    draw_from_row(true, cut);
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleArgs a, float c, float farthest, int size) {
+  extern __shared__ __align__(16) char smem[];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  u64 *list = reinterpret_cast<u64 *>(smem);
+  Shared *s = reinterpret_cast<Shared *>(list + 2 * kList);
+  Group g{size, (int)blockIdx.x % size, 0, s};
+  const int index = (int)blockIdx.x / size;
+  const Row<T> row(a.logits, a.row, index, a.vocab);
+  if (size > 1) g.sync();  // no block writes to one that has not begun
+  Sampler<T> sampler{a, row, g, s, list, list + kList, 0.0f, c, farthest, index};
+  sampler.run();
+  if (size > 1) g.sync();  // or to one that has ended
+}
+
+template <typename T>
+cudaError_t launch(const SampleArgs &a, cudaStream_t s) {
+  constexpr int kSmem = 2 * kList * 8 + (int)sizeof(Shared);
+  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two blocks of an SM");
+  cudaError_t e = allow_smem((const void *)sample_kernel<T>, kSmem, kSmem);
+  if (e != cudaSuccess) return e;
+  // as many blocks as an SM holds of a row where there are few
+  int size = 1;
+  while (size < kMaxCluster && (int64_t)a.n * size * 2 <= 152) size *= 2;
+  const float c = a.scale * 1.44269504088896340736f;
+  const float farthest = a.min_p > 0.0f ? (float)-log2((double)a.min_p) : 64.0f;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = size;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)a.n * size);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, c, farthest, size);
+}
+
+}  // namespace
+
+cudaError_t launch_sample_tokens(int dtype, const SampleArgs &a, cudaStream_t s) {
+  if (a.n == 0) return cudaSuccess;
+  g_used = true;
+  return dtype == COPES_BF16 ? launch<__nv_bfloat16>(a, s) : launch<float>(a, s);
+}
+
+unsigned read_and_clear_sample_errors() {
+  if (!g_used) return 0;
+  unsigned v = 0, zero = 0;
+  cudaMemcpyFromSymbol(&v, g_sample_error, sizeof(v));
+  if (v) cudaMemcpyToSymbol(g_sample_error, &zero, sizeof(zero));
+  return v;
+}
+
+}  // namespace copes
