@@ -37,6 +37,8 @@ constexpr int kEach = 4;                   // pieces of 16 bytes of a lane in a 
 constexpr int kChunkPieces = 32 * kEach;
 constexpr int kList = 4096;                // logits that can be collected
 constexpr int kMaxCluster = 8;
+constexpr float kFarthest = 40.0f;         // the weight is 0 past it
+constexpr int kBinsOfOne = 64, kBins = 40 * kBinsOfOne + 1;
 using u64 = unsigned long long;
 
 // P(f) = 1 + f Q(f): Q of degree 4 that makes the largest |P 2^f - 1| on [0, 1] least (1.6e-7 before rounding),
@@ -50,14 +52,36 @@ __device__ __forceinline__ float power(float f) {
   return fmaf(p, f, 1.0f);
 }
 
-__device__ __forceinline__ float distance(float x, float m, float c) { return fminf(__fmul_rn(__fsub_rn(m, x), c), 63.0f); }
-
 // The weight of a token at distance t: P lies in [1/2, 1], so its bits less those of 1/4 are P 2^24.
 __device__ __forceinline__ u64 weight_of(float t) {
+  t = fminf(t, 63.0f);
   const float z = __fadd_rd(t, 8388608.0f);  // 2^23 + n
   const uint32_t p = __float_as_uint(power(t - (z - 8388608.0f))) - 0x3E800000u;
   return ((u64)p << 16) >> (__float_as_uint(z) & 63u);
 }
+
+// The sum of the weights of at most 256 tokens, in 32-bit registers.  With y = P(f) 2^-n, whose bits are P's less n
+// in the exponent, a weight is floor(y 2^40): 2^23 floor(y 2^17), which is what adding 64 downwards leaves in the
+// last bits, and floor(rest 2^40), by 2^-17 likewise.  (A 64-bit shift and addition for each token take half as
+// long again.)
+struct Weights {
+  uint32_t hi = 0, lo = 0, n = 0;
+  __device__ __forceinline__ void add(float t, bool keep) {
+    const float z = __fadd_rd(t, 8388608.0f);
+    const float p = power(t - (z - 8388608.0f));
+    const float y = __uint_as_float(__float_as_uint(p) - (__float_as_uint(z) << 23));
+    const float top = __fadd_rd(y, 64.0f);
+    const float rest = __fadd_rd(y - (top - 64.0f), 0x1p-17f);
+    if (keep) {
+      hi += __float_as_uint(top);
+      lo += __float_as_uint(rest);
+      ++n;
+    }
+  }
+  __device__ __forceinline__ u64 sum() const {
+    return ((u64)(hi - n * 0x42800000u) << 23) + (lo - n * 0x37000000u);
+  }
+};
 
 __device__ __forceinline__ float max_nan(float a, float b) {
   float c;
@@ -140,9 +164,9 @@ struct Shared {
   u64 scan[kWarps];
   uint32_t counts[2][kWarps];
   int collected;
-  int outcome;
   u64 total;
   int chunk;
+  int bins[2];  // first and last
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -298,7 +322,7 @@ struct Sampler {
   float m, c, farthest;
   int index;
 
-  __device__ __forceinline__ float t_of(float x) const { return distance(x, m, c); }
+  __device__ __forceinline__ float t_of(float x) const { return __fmul_rn(__fsub_rn(m, x), c); }
   __device__ __forceinline__ float t_of(u64 entry) const { return t_of(R::value_of(~(uint32_t)(entry >> 32))); }
 
   __device__ void write(int id, float logprob, int kept) const {
@@ -312,29 +336,40 @@ struct Sampler {
     write(id, 0.0f - (t * 0.69314718055994531f + log1pf((float)(total - (1ull << 40)) * 0x1p-40f)), kept);
   }
 
-  // Tokens with keys in [lo, hi) into the first block's list; how many there were.  Of what f returns for each
-  // token's x the group's sum goes to *sum.
-  template <typename F>
-  __device__ int collect(uint32_t lo, uint32_t hi, u64 *sum, const F &f) {
+  // Tokens with nearest <= t < beyond into the first block's list; how many there were.  The weights of all tokens
+  // with t < near are summed over the group into *sum.
+  template <bool kSum>
+  __device__ int collect(float nearest, float beyond, float near, u64 *sum) {
     if (threadIdx.x == 0) s->collected = 0;
     g.sync();
     const uint32_t counter = remote(smem_addr(&s->collected), 0), to = remote(smem_addr(list), 0);
-    const float least = R::value_of(lo);
     u64 v[1] = {0};
+    Weights w;
     for_row(row, g, [&](int piece, const uint4 &p, int) {
-      v[0] += f(p);
-      if (!(R::value(R::largest(R::none, p)) >= least)) return;
+      const float first = t_of(R::value(R::largest(R::none, p)));
+      if (kSum && first < near) {
+#pragma unroll
+        for (int e = 0; e < R::kN; ++e) {
+          const float t = t_of(R::element(p, e));
+          w.add(t, t < near);
+        }
+      }
+      if (!(first < beyond)) return;
 #pragma unroll
       for (int e = 0; e < R::kN; ++e) {
-        const uint32_t key = R::key(R::element(p, e));
-        if (key < lo || key >= hi) continue;
+        const float x = R::element(p, e), t = t_of(x);
+        if (t < nearest || !(t < beyond)) continue;
         int at;
         asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(counter) : "memory");
-        const u64 entry = (u64)~key << 32 | (uint32_t)(row.id(piece) + e);
+        const u64 entry = (u64)~R::key(x) << 32 | (uint32_t)(row.id(piece) + e);
         if (at < kList) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to + 8u * (uint32_t)at), "l"(entry) : "memory");
       }
-    }, [](int) {});
-    if (sum) {
+    }, [&](int) {
+      if (!kSum) return;
+      v[0] += w.sum();
+      w = Weights();
+    });
+    if (kSum) {
       g.template all<1>(v);
       *sum = v[0];
     }
@@ -366,7 +401,7 @@ struct Sampler {
     if (!a.top_k && all < need) return false;
     u64 kept = 0, held = 0, kept_all, held_all;
     for (int i = first; i < min(last, most) && before < need; ++i) {
-      if (weights[i] == 0 || t_of(list[i]) > farthest) break;
+      if (t_of(list[i]) > farthest) break;
       ++kept;
       held += weights[i];
       before += weights[i];
@@ -394,82 +429,142 @@ struct Sampler {
     return true;
   }
 
-  // The cut at the token at which the sum (of weights, or of ones) from the largest down reaches `need`.  Below
-  // `lo` it is not sought, and the sum from there up reaches it; `above` is the sum from hi up.
+  // What the first block put in s->total, in all blocks.
+  __device__ __forceinline__ u64 told() {
+    g.sync();
+    u64 v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(smem_addr(&s->total), 0)) : "memory");
+    g.sync();
+    return v;
+  }
+
+  // The first block: of the collected tokens, in order, the one at which the sum (of weights, or of ones) from `above`
+  // reaches `need`, into s->total as an entry; all ones where none does.
   template <bool kWeights>
-  __device__ Cut find_cut(uint32_t lo, uint32_t hi, u64 above, u64 need) {
-    u64 between = ~0ull;
-    for (int turn = 0; hi - lo > 1 && between > kList; ++turn) {
-      // three bounds, of distance and of the key by turns: the first come near fast, the others come to an end
-      uint32_t bound[3];
-      const float t0 = t_of(R::value_of(hi - 1)), t1 = fminf(t_of(R::value_of(lo)), 48.0f);
+  __device__ void find_in_list(int count, u64 above, u64 need) {
+    if (count > 0) order(count);
+    if (threadIdx.x == 0) s->total = ~0ull;
+    const int each = count / kThreads + 1, first = min(count, (int)threadIdx.x * each), last = min(count, first + each);
+    u64 mine = 0, all;
+    for (int i = first; i < last; ++i) mine += kWeights ? weights[i] : 1;
+    u64 before = above + block_scan(mine, s, &all);
+    for (int i = first; i < last; ++i) {
+      const u64 w = kWeights ? weights[i] : 1;
+      if (before < need && need <= before + w) s->total = list[i];
+      before += w;
+    }
+  }
+
+  // The cut at the token at which the sum (of weights, or of ones) from the largest down reaches `need`, where the
+  // weights, or the tokens at t <= 40, come to that.  Tokens are counted by their distance in steps of 1/64: of
+  // ones that gives the step of the cut, and of weights, which differ by 2^(1/64) in a step, one near it.  The step, or
+  // some on either side, are collected, and the rest is exact.
+  template <bool kWeights>
+  __device__ Cut find_cut(u64 need) {
+    uint32_t *bins = reinterpret_cast<uint32_t *>(weights);
+    g.sync();  // the weights were read
+    for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
+    __syncthreads();
+    for_row(row, g, [&](int, const uint4 &p, int) {
 #pragma unroll
-      for (int j = 0; j < 3; ++j) {
-        uint32_t b = hi - (uint32_t)(((u64)(hi - lo) * (j + 1)) >> 2);
-        if (!(turn & 1)) b = R::key(m - (t0 + (t1 - t0) * (0.25f * (j + 1))) / c);
-        bound[j] = min(max(b, lo + 1), hi - 1);
+      for (int e = 0; e < R::kN; ++e) {
+        const float t = t_of(R::element(p, e));
+        if (t <= kFarthest) atomicAdd(&bins[(int)(t * kBinsOfOne)], 1u);
       }
-      u64 v[4] = {0, 0, 0, 0}, n[3] = {0, 0, 0};
+    }, [](int) {});
+    g.sync();
+    u64 above = 0;
+    if (g.rank == 0) {
+      constexpr int kOf = (kBins - 1) / kThreads + 1;
+      const int first = threadIdx.x * kOf;
+      for (int r = 1; r < g.size; ++r)
+        for (int i = first; i < min(kBins, first + kOf); ++i) {
+          uint32_t more;
+          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(more) : "r"(remote(smem_addr(bins + i), r)) : "memory");
+          bins[i] += more;
+        }
+      const auto mass = [&](int i) { return kWeights ? weight_of((i + 0.5f) / kBinsOfOne) * bins[i] : (u64)bins[i]; };
+      u64 mine = 0, all;
+      for (int i = first; i < min(kBins, first + kOf); ++i) mine += mass(i);
+      if (threadIdx.x == 0) s->bins[0] = s->bins[1] = kBins - 1;
+      u64 before = block_scan(mine, s, &all);
+      for (int i = first; i < min(kBins, first + kOf); ++i) {
+        const u64 w = mass(i);
+        if (before < need && need <= before + w) {
+          s->bins[0] = s->bins[1] = i;
+          if (!kWeights) s->total = before;
+        }
+        before += w;
+      }
+      __syncthreads();
+      if (kWeights && threadIdx.x == 0) {  // as far to either side as goes in the list with room to spare
+        int lo = s->bins[0], hi = lo;
+        uint32_t held = bins[lo];
+        for (int d = 0; d < 8; ++d) {
+          const uint32_t more = (lo > 0 ? bins[lo - 1] : 0) + (hi + 1 < kBins ? bins[hi + 1] : 0);
+          if (held + more > kList) break;
+          held += more;
+          lo = max(lo - 1, 0);
+          hi = min(hi + 1, kBins - 1);
+        }
+        s->bins[0] = lo;
+        s->bins[1] = hi;
+      }
+      __syncthreads();
+    }
+    if (!kWeights) above = told();
+    else g.sync();
+    int bin[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(bin[j]) : "r"(remote(smem_addr(&s->bins[j]), 0)) : "memory");
+    const float nearest = (float)bin[0] / kBinsOfOne, beyond = (float)(bin[1] + 1) / kBinsOfOne;
+    const int count = collect<kWeights>(nearest, beyond, nearest, &above);
+    if (count <= kList && (!kWeights || above < need)) {
+      if (g.rank == 0) find_in_list<kWeights>(count, above, need);
+      const u64 entry = told();
+      if (entry != ~0ull) return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
+    }
+    return bracket_cut<kWeights>(need);
+  }
+
+  // The same by passes that measure three keys each, however many tokens are equal or nearly so.
+  template <bool kWeights>
+  __device__ Cut bracket_cut(u64 need) {
+    uint32_t lo = R::kNothing + 1, hi = R::key(m) + 1;  // the sum from lo up reaches `need`, from hi up it does not
+    u64 above = 0;
+    while (hi - lo > 1) {
+      uint32_t key[3];
+#pragma unroll
+      for (int j = 0; j < 3; ++j) key[j] = min(max(hi - (uint32_t)(((u64)(hi - lo) * (j + 1)) >> 2), lo + 1), hi - 1);
+      u64 v[3] = {0, 0, 0};
       for_row(row, g, [&](int, const uint4 &p, int) {
 #pragma unroll
         for (int e = 0; e < R::kN; ++e) {
-          const float x = R::element(p, e);
-          const uint32_t key = R::key(x);
-          const u64 w = kWeights ? weight_of(t_of(x)) : 1;
+          const float x = R::element(p, e), t = t_of(x);
+          const u64 w = kWeights ? weight_of(t) : t <= kFarthest;
 #pragma unroll
-          for (int j = 0; j < 3; ++j) {
-            if (key >= bound[j]) v[j] += w;
-            n[j] += key >= bound[j] && key < hi;
-          }
-          v[3] += key >= lo && key < hi;
+          for (int j = 0; j < 3; ++j)
+            if (R::key(x) >= key[j]) v[j] += w;
         }
       }, [](int) {});
-      g.template all<4>(v);
-      g.template all<3>(n);
-      // the bounds fall: the last that does not reach `need` becomes hi, the first that does lo
-      u64 outside = 0, inside = v[3];
+      g.template all<3>(v);
       uint32_t new_lo = lo, new_hi = hi;
 #pragma unroll
       for (int j = 0; j < 3; ++j) {
-        if (v[j] < need) {
-          if (bound[j] < new_hi) {
-            new_hi = bound[j];
-            above = v[j];
-            outside = n[j];
-          }
-        } else if (bound[j] > new_lo) {
-          new_lo = bound[j];
-          inside = n[j];
+        if (v[j] >= need) {
+          new_lo = max(new_lo, key[j]);
+        } else if (key[j] < new_hi) {
+          new_hi = key[j];
+          above = v[j];
         }
       }
-      between = inside - outside;
       lo = new_lo;
       hi = new_hi;
     }
-    if (between <= kList) {
-      const int count = collect(lo, hi, nullptr, [](const uint4 &) { return 0ull; });
-      if (g.rank == 0) {
-        order(count);
-        const int each = (count - 1) / kThreads + 1, first = min(count, (int)threadIdx.x * each), last = min(count, first + each);
-        u64 mine = 0, all;
-        for (int i = first; i < last; ++i) mine += kWeights ? weights[i] : 1;
-        u64 before = above + block_scan(mine, s, &all);
-        for (int i = first; i < last; ++i) {
-          const u64 w = kWeights ? weights[i] : 1;
-          if (before < need && need <= before + w) s->total = list[i];
-          before += w;
-        }
-        __syncthreads();
-      }
-    } else {  // equal logits, too many to collect: the one of them by its rank among their ids
-      const u64 w = kWeights ? weight_of(t_of(R::value_of(lo))) : 1;
-      const u64 rank = (need - above - 1) / w;
-      id_of_rank(lo, rank);
-    }
-    g.sync();
-    u64 entry;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(entry) : "r"(remote(smem_addr(&s->total), 0)) : "memory");
-    g.sync();
+    const u64 w = kWeights ? weight_of(t_of(R::value_of(lo))) : 1;
+    id_of_rank(lo, (need - above - 1) / w);
+    const u64 entry = told();
     return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
   }
 
@@ -555,24 +650,24 @@ struct Sampler {
   }
 
   // Draws from all tokens that the cut and min_p keep.
-  __device__ void draw_from_row(bool cuts, const Cut &cut) {
-    const auto kept = [&](float x, int id) -> u64 {
-      const float t = t_of(x);
-      return t <= farthest && (!cuts || cut.keeps(R::key(x), id)) ? weight_of(t) : 0;
-    };
+  template <bool kCut>
+  __device__ void draw_from_row(const Cut &cut) {
+    const auto keeps = [&](float x, float t, int id) { return t <= farthest && (!kCut || cut.keeps(R::key(x), id)); };
     g.sync();  // the list was read
-    u64 sum = 0, v[2] = {0, 0};
+    u64 v[2] = {0, 0};
+    Weights w;
     for_row(row, g, [&](int piece, const uint4 &p, int) {
 #pragma unroll
       for (int e = 0; e < R::kN; ++e) {
-        const u64 w = kept(R::element(p, e), row.id(piece) + e);
-        sum += w;
-        v[1] += w != 0;
+        const float x = R::element(p, e), t = t_of(x);
+        w.add(t, keeps(x, t, row.id(piece) + e));
       }
     }, [&](int chunk) {
+      const u64 sum = w.sum();
       v[0] += sum;
+      v[1] += w.n;
       put_chunk(chunk, sum);
-      sum = 0;
+      w = Weights();
     });
     g.template all<2>(v);
     g.sync();
@@ -580,7 +675,8 @@ struct Sampler {
     const u64 place = place_of(a.u[index], v[0]);
     find_chunk(place);
     if (threadIdx.x < 32)
-      find_token(place, kept, [&](int id, float x) { write_token(id, t_of(x), v[0], (int)v[1]); });
+      find_token(place, [&](float x, int id) { return keeps(x, t_of(x), id) ? weight_of(t_of(x)) : 0; },
+                 [&](int id, float x) { write_token(id, t_of(x), v[0], (int)v[1]); });
   }
 
   __device__ void run() {
@@ -608,62 +704,57 @@ struct Sampler {
       return;
     }
     m = R::value_of((uint32_t)v[0]);
-    const uint32_t lowest = R::kNothing + 1, past = (uint32_t)v[0] + 1;
     const bool top_k = a.top_k != 0, top_p = a.top_p < 1.0f;
-    if (!top_k && !top_p) return draw_from_row(false, Cut{0, 0});
-    u64 total = 0;
-    const auto weights_of = [&](const uint4 &p) {
-      u64 sum = 0;
-#pragma unroll
-      for (int e = 0; e < R::kN; ++e) sum += weight_of(t_of(R::element(p, e)));
-      return sum;
-    };
+    if (!top_k && !top_p) return draw_from_row<false>(Cut{0, 0});
     // what the cells' bound collects
+    const float past = __uint_as_float(__float_as_uint(kFarthest) + 1);
     const int want = top_k ? a.top_k : 512, share = (want - 1) / g.size + 1;
-    bool in_list = false;
+    u64 total = 0;
     if (share <= kThreads * kEach / 2) {
       u64 least[1] = {0xFFFFull - cell_bound(upper, share, s)};
       g.template all<1, true>(least);
-      const uint32_t bound = max((uint32_t)(0xFFFFull - least[0]) << (R::kBits - 16), lowest);
-      const int count = top_k ? collect(bound, past, nullptr, [](const uint4 &) { return 0ull; }) : collect(bound, past, &total, weights_of);
+      const uint32_t bound = max((uint32_t)(0xFFFFull - least[0]) << (R::kBits - 16), R::kNothing + 1);
+      const float t = t_of(R::value_of(bound)), beyond = t < kFarthest ? __uint_as_float(__float_as_uint(t) + 1) : past;
+      const int count = top_k ? collect<false>(0.0f, beyond, 0.0f, nullptr) : collect<true>(0.0f, beyond, past, &total);
       if (count <= kList) {
         if (g.rank == 0) {
           order(count);
           const bool done = draw_from_list(count, total);
-          if (threadIdx.x == 0) s->outcome = done;
+          if (threadIdx.x == 0) s->total = done;
         }
-        g.sync();
-        int done;
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(done) : "r"(remote(smem_addr(&s->outcome), 0)) : "memory");
-        in_list = done;
-        g.sync();
+        if (told()) return;
       }
     }
-    if (in_list) return;
-    Cut cut{lowest, 0x7FFFFFFF};
+    Cut cut{R::kNothing + 1, 0x7FFFFFFF};
     if (top_k) {
-      u64 finite[1] = {0};
+      u64 tokens[1] = {0};
       for_row(row, g, [&](int, const uint4 &p, int) {
 #pragma unroll
-        for (int e = 0; e < R::kN; ++e) finite[0] += R::key(R::element(p, e)) >= lowest;
+        for (int e = 0; e < R::kN; ++e) tokens[0] += t_of(R::element(p, e)) <= kFarthest;
       }, [](int) {});
-      g.template all<1>(finite);
-      if (finite[0] > (u64)a.top_k) cut = find_cut<false>(lowest, past, 0, (u64)a.top_k);
+      g.template all<1>(tokens);
+      if (tokens[0] > (u64)a.top_k) cut = find_cut<false>((u64)a.top_k);
     }
     if (top_p) {
-      u64 sum[1] = {0};
-      for_row(row, g, [&](int piece, const uint4 &p, int) {
+      u64 sum[1] = {total};
+      if (top_k) {
+        Weights w;
+        for_row(row, g, [&](int piece, const uint4 &p, int) {
 #pragma unroll
-        for (int e = 0; e < R::kN; ++e) {
-          const float x = R::element(p, e);
-          if (cut.keeps(R::key(x), row.id(piece) + e)) sum[0] += weight_of(t_of(x));
-        }
-      }, [](int) {});
-      g.template all<1>(sum);
-      const u64 need = (u64)ceil((double)sum[0] * (double)a.top_p);
-      cut = find_cut<true>(cut.key, past, 0, need);  // among the first top_k, whose weight is at least `need`
+          for (int e = 0; e < R::kN; ++e) {
+            const float x = R::element(p, e), t = t_of(x);
+            w.add(t, t <= kFarthest && cut.keeps(R::key(x), row.id(piece) + e));
+          }
+        }, [&](int) {
+          sum[0] += w.sum();
+          w = Weights();
+        });
+        g.template all<1>(sum);
+      }
+      // among the first top_k, whose weight is at least what is needed
+      cut = find_cut<true>((u64)ceil((double)sum[0] * (double)a.top_p));
     }
-    draw_from_row(true, cut);
+    draw_from_row<true>(cut);
   }
 };
 
@@ -691,9 +782,9 @@ cudaError_t launch(const SampleArgs &a, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   // as many blocks as an SM holds of a row where there are few
   int size = 1;
-  while (size < kMaxCluster && (int64_t)a.n * size * 2 <= 152) size *= 2;
+  while (size < kMaxCluster && (int64_t)a.n * size * 2 <= 152 * 2) size *= 2;
   const float c = a.scale * 1.44269504088896340736f;
-  const float farthest = a.min_p > 0.0f ? (float)-log2((double)a.min_p) : 64.0f;
+  const float farthest = a.min_p > 0.0f ? fminf((float)-log2((double)a.min_p), kFarthest) : kFarthest;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
