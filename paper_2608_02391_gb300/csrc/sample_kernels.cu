@@ -60,27 +60,84 @@ __device__ __forceinline__ u64 weight_of(float t) {
   return ((u64)p << 16) >> (__float_as_uint(z) & 63u);
 }
 
-// The sum of the weights of at most 256 tokens, in 32-bit registers.  With y = P(f) 2^-n, whose bits are P's less n
-// in the exponent, a weight is floor(y 2^40): 2^23 floor(y 2^17), which is what adding 64 downwards leaves in the
-// last bits, and floor(rest 2^40), by 2^-17 likewise.  (A 64-bit shift and addition for each token take half as
-// long again.)
+// Two floats in one register pair, and operations on both.
+using Pair = u64;
+__device__ __forceinline__ Pair pair_of(float a, float b) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ float2 floats_of(Pair p) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+  return f;
+}
+__device__ __forceinline__ Pair both(float a) { return pair_of(a, a); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair add2_down(Pair a, Pair b) {
+  Pair d;
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair add2_up(Pair a, Pair b) {
+  Pair d;
+  asm("add.rp.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+// -t of two tokens: (x - m) c, each operation rounded.
+__device__ __forceinline__ Pair minus_t(float x0, float x1, float m, float c) {
+  return mul2(add2(pair_of(x0, x1), both(-m)), both(c));
+}
+
+// The sum of the weights of at most 60 tokens, and their number, in 32-bit registers.  With y = P(f) 2^-n, whose
+// bits are P's less n in the exponent, a weight is floor(y 2^40): 2^23 floor(y 2^17), which is what adding 64
+// downwards leaves in the last bits, and floor(rest 2^40), by 2^-17 likewise.  The upper 9 bits of 64's, 133 each,
+// count the tokens.  (With 64-bit shifts and additions, and each token for itself, 2,048 rows of 151,936 took 377 us.)
 struct Weights {
-  uint32_t hi = 0, lo = 0, n = 0;
-  __device__ __forceinline__ void add(float t, bool keep) {
-    const float z = __fadd_rd(t, 8388608.0f);
-    const float p = power(t - (z - 8388608.0f));
-    const float y = __uint_as_float(__float_as_uint(p) - (__float_as_uint(z) << 23));
-    const float top = __fadd_rd(y, 64.0f);
-    const float rest = __fadd_rd(y - (top - 64.0f), 0x1p-17f);
-    if (keep) {
-      hi += __float_as_uint(top);
-      lo += __float_as_uint(rest);
-      ++n;
+  uint32_t hi = 0, lo = 0;
+  // Tokens at -minus.x and -minus.y, where keep.
+  __device__ __forceinline__ void add(Pair minus, bool keep_x, bool keep_y) {
+    const Pair z = add2_up(minus, both(12582912.0f));  // 1.5 2^23 - n
+    const Pair less = add2(z, both(-12582912.0f));     // -n
+    const Pair f = fma2(minus, both(-1.0f), less);
+    Pair p = both(-0.0008996404358185828f);
+    p = fma2(p, f, both(0.009098555892705917f));
+    p = fma2(p, f, both(-0.05521015450358391f));
+    p = fma2(p, f, both(0.2401522845029831f));
+    p = fma2(p, f, both(-0.693140983581543f));
+    p = fma2(p, f, both(1.0f));
+    const float2 zz = floats_of(z), pp = floats_of(p);
+    const Pair y = pair_of(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(zz.x) << 23)),
+                           __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(zz.y) << 23)));
+    const Pair top = add2_down(y, both(64.0f));
+    const Pair rest = add2_down(fma2(add2(top, both(-64.0f)), both(-1.0f), y), both(0x1p-17f));
+    const float2 t = floats_of(top), r = floats_of(rest);
+    if (keep_x) {
+      hi += __float_as_uint(t.x);
+      lo += __float_as_uint(r.x);
+    }
+    if (keep_y) {
+      hi += __float_as_uint(t.y);
+      lo += __float_as_uint(r.y);
     }
   }
-  __device__ __forceinline__ u64 sum() const {
-    return ((u64)(hi - n * 0x42800000u) << 23) + (lo - n * 0x37000000u);
-  }
+  __device__ __forceinline__ uint32_t tokens() const { return (hi >> 23) * 77u & 511u; }  // 77 * 133 = 1 (mod 512)
+  __device__ __forceinline__ u64 sum() const { return ((u64)(hi & 0x7FFFFFu) << 23) + (lo - tokens() * 0x37000000u); }
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -164,6 +221,7 @@ struct Shared {
   u64 scan[kWarps];
   uint32_t counts[2][kWarps];
   int collected;
+  uint32_t first;  // upper half of the list's first entry
   u64 total;
   int chunk;
   int bins[2];  // first and last
@@ -260,22 +318,86 @@ __device__ __forceinline__ u64 block_scan(u64 v, Shared *s, u64 *total) {
   return before + x - v;
 }
 
-// Sorts list[0 .. n), n a power of two, ascending.
-__device__ void sort_list(u64 *list, int n) {
-  for (int k = 2; k <= n; k <<= 1)
-    for (int j = k >> 1; j; j >>= 1) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < n / 2; i += kThreads) {
-        const int a = 2 * i - (i & (j - 1)), b = a + j;
-        const u64 x = list[a], y = list[b];
-        if ((x > y) == ((a & k) == 0)) {
-          list[a] = y;
-          list[b] = x;
-        }
-      }
-    }
-  __syncthreads();
+// Sums of v < 2^48 over a warp.
+__device__ __forceinline__ u64 warp_sum(u64 v) {
+  const uint32_t a = __reduce_add_sync(kAll, (uint32_t)v & 0xFFFFFu), b = __reduce_add_sync(kAll, (uint32_t)(v >> 20) & 0xFFFFFu);
+  return a + ((u64)b << 20) + ((u64)__reduce_add_sync(kAll, (uint32_t)(v >> 40)) << 40);
 }
+
+// Collected tokens in the registers of a team, a warp or the block: entries, which ascend in the order of the
+// tokens (keys falling, then ids rising), and weights.  Everything about them is found by searching for the bits
+// of an answer one after the other, each by a sum over the team, which sorts nothing.
+template <int kTeam>
+struct Items {
+  static constexpr int kWidth = kTeam, kEvery = kTeam == 32 ? 8 : kList / kTeam;
+  u64 entry[kEvery], weight[kEvery];
+  int count, turn = 0;
+  Shared *s;
+
+  template <typename F>
+  __device__ Items(const u64 *list, int n, Shared *shared, const F &weight_at) : count(n), s(shared) {
+#pragma unroll
+    for (int i = 0; i < kEvery; ++i) {
+      const int at = i * kTeam + (int)threadIdx.x;
+      entry[i] = at < n ? list[at] : ~0ull;
+      weight[i] = at < n ? weight_at(list[at]) : 0;
+    }
+  }
+  __device__ __forceinline__ u64 sum(u64 v) {
+    v = warp_sum(v);
+    if constexpr (kTeam > 32) {
+      const int lane = threadIdx.x & 31;
+      turn ^= 1;
+      if (lane == 0) s->sums[turn][threadIdx.x >> 5][3] = v;
+      __syncthreads();
+      v = warp_sum(lane < kWarps ? s->sums[turn][lane][3] : 0);
+    }
+    return v;
+  }
+  // Over the items i that f takes: of weights, or of ones.
+  template <bool kWeights, typename F>
+  __device__ __forceinline__ u64 sum_where(const F &f) {
+    u64 v = 0;
+#pragma unroll
+    for (int i = 0; i < kEvery; ++i)
+      if (f(i)) v += kWeights ? weight[i] : 1;
+    return sum(v);
+  }
+  // The largest x below 2^bits, of what f(item, x) asks, for which the sum over f is not more than `most`.
+  template <bool kWeights, typename F>
+  __device__ __forceinline__ uint32_t largest(int bits, uint32_t x, u64 most, const F &f) {
+    for (int bit = bits - 1; bit >= 0; --bit) {
+      const uint32_t next = x | 1u << bit;
+      if (sum_where<kWeights>([&](int i) { return f(i, next); }) <= most) x = next;
+    }
+    return x;
+  }
+  // The entry at which the sum, in order, reaches `need`; that of all items does.
+  template <bool kWeights>
+  __device__ u64 reach(u64 need, int id_bits) {
+    uint32_t differ = 0;
+    const uint32_t some = s->first;
+#pragma unroll
+    for (int i = 0; i < kEvery; ++i)
+      if (i * kTeam + (int)threadIdx.x < count) differ |= (uint32_t)(entry[i] >> 32) ^ some;
+    differ = __reduce_or_sync(kAll, differ);
+    if constexpr (kTeam > 32) {
+      const int lane = threadIdx.x & 31;
+      turn ^= 1;
+      if (lane == 0) s->sums[turn][threadIdx.x >> 5][3] = differ;
+      __syncthreads();
+      differ = __reduce_or_sync(kAll, lane < kWarps ? (uint32_t)s->sums[turn][lane][3] : 0u);
+    }
+    const int bits = 32 - __clz(differ);
+    const uint32_t upper = largest<kWeights>(bits, bits < 32 ? some >> bits << bits : 0, need - 1,
+                                             [&](int i, uint32_t x) { return (uint32_t)(entry[i] >> 32) < x; });
+    const auto equal = [&](int i) { return (uint32_t)(entry[i] >> 32) == upper; };
+    if (sum_where<false>(equal) == 1) return (u64)upper << 32 | 0x7FFFFFFFu;
+    const u64 before = sum_where<kWeights>([&](int i) { return (uint32_t)(entry[i] >> 32) < upper; });
+    const uint32_t id = largest<kWeights>(id_bits, 0, need - 1 - before, [&](int i, uint32_t x) { return equal(i) && (uint32_t)entry[i] < x; });
+    return (u64)upper << 32 | id;
+  }
+};
 
 // The largest b <= 65535 that at least k of the block's cells reach (0: fewer are that many), of the upper 16
 // bits of their keys.
@@ -296,6 +418,9 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t (&upper)[kEach], i
   return found;
 }
 
+// floor(64 t), t below 2^16: the last bits of 2^23 and that.  (A conversion takes four times an addition.)
+__device__ __forceinline__ uint32_t step_of(float t) { return __float_as_uint(__fmaf_rd(t, (float)kBinsOfOne, 8388608.0f)) & 0xFFFFu; }
+
 struct Cut {  // tokens are kept from the largest down to this one: key, and id among equal ones
   uint32_t key;
   int id;
@@ -307,8 +432,6 @@ __device__ __forceinline__ u64 place_of(float u, u64 total) {
   const u64 r = (u64)(u * 2147483648.0f);
   return (total >> 31) * r + (((total & 0x7FFFFFFFull) * r) >> 31);
 }
-
-__device__ __forceinline__ int power_of_two(int n) { return n <= 2 ? 2 : 1 << (32 - __clz(n - 1)); }
 
 // A row's problem and its steps; every step is called by all threads of the group.
 template <typename T>
@@ -342,16 +465,16 @@ struct Sampler {
   __device__ int collect(float nearest, float beyond, float near, u64 *sum) {
     if (threadIdx.x == 0) s->collected = 0;
     g.sync();
-    const uint32_t counter = remote(smem_addr(&s->collected), 0), to = remote(smem_addr(list), 0);
     u64 v[1] = {0};
     Weights w;
     for_row(row, g, [&](int piece, const uint4 &p, int) {
       const float first = t_of(R::value(R::largest(R::none, p)));
       if (kSum && first < near) {
 #pragma unroll
-        for (int e = 0; e < R::kN; ++e) {
-          const float t = t_of(R::element(p, e));
-          w.add(t, t < near);
+        for (int e = 0; e < R::kN; e += 2) {
+          const Pair minus = minus_t(R::element(p, e), R::element(p, e + 1), m, c);
+          const float2 t = floats_of(minus);
+          w.add(minus, -t.x < near, -t.y < near);
         }
       }
       if (!(first < beyond)) return;
@@ -359,10 +482,11 @@ struct Sampler {
       for (int e = 0; e < R::kN; ++e) {
         const float x = R::element(p, e), t = t_of(x);
         if (t < nearest || !(t < beyond)) continue;
-        int at;
-        asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(counter) : "memory");
-        const u64 entry = (u64)~R::key(x) << 32 | (uint32_t)(row.id(piece) + e);
-        if (at < kList) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to + 8u * (uint32_t)at), "l"(entry) : "memory");
+        const unsigned here = __activemask(), lane = threadIdx.x & 31;
+        int at = 0;
+        if (lane == __ffs(here) - 1u) at = atomicAdd(&s->collected, __popc(here));
+        at = __shfl_sync(here, at, __ffs(here) - 1) + __popc(here & ((1u << lane) - 1));
+        if (at < kList) list[at] = (u64)~R::key(x) << 32 | (uint32_t)(row.id(piece) + e);
       }
     }, [&](int) {
       if (!kSum) return;
@@ -374,59 +498,75 @@ struct Sampler {
       *sum = v[0];
     }
     g.sync();
-    int count;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(count) : "r"(counter) : "memory");
+    int count = s->collected;
+    if (g.size > 1) {
+      int at[kMaxCluster + 1] = {};
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        int more = 0;
+        if (r < g.size) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(more) : "r"(remote(smem_addr(&s->collected), r)) : "memory");
+        at[r + 1] = at[r] + more;
+      }
+      count = at[kMaxCluster];
+      if (g.rank == 0 && count <= kList)
+        for (int r = 1; r < g.size; ++r) {
+          const uint32_t from = remote(smem_addr(list), r);
+          for (int i = threadIdx.x; i < at[r + 1] - at[r]; i += kThreads) {
+            u64 entry;
+            asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(entry) : "r"(from + 8u * (uint32_t)i) : "memory");
+            list[at[r] + i] = entry;
+          }
+        }
+    }
+    if (g.rank == 0 && threadIdx.x == 0 && count > 0 && count <= kList) s->first = (uint32_t)(list[0] >> 32);
+    __syncthreads();
     return count;
   }
 
-  // The first block: the list in order, and weights of its tokens.
-  __device__ void order(int count) {
-    const int n = power_of_two(count);
-    for (int i = count + threadIdx.x; i < n; i += kThreads) list[i] = ~0ull;
-    sort_list(list, n);
-    for (int i = threadIdx.x; i < count; i += kThreads) weights[i] = weight_of(t_of(list[i]));
-    __syncthreads();
+  __device__ __forceinline__ int id_bits() const { return 32 - __clz(a.vocab); }
+
+  // The list's items, in a warp where they fit, and what f(items) gives, in the block's first thread at least.
+  template <typename F>
+  __device__ __forceinline__ void with_items(int count, const F &f) const {
+    const auto weight = [&](u64 entry) { return weight_of(t_of(entry)); };
+    if (count <= 32 * Items<32>::kEvery) {
+      if (threadIdx.x < 32) {
+        Items<32> items(list, count, s, weight);
+        f(items);
+      }
+    } else {
+      Items<kThreads> items(list, count, s, weight);
+      f(items);
+    }
   }
 
-  // The first block: cuts the ordered list, which begins with the row's largest, and draws from it.  False where
-  // it does not hold top_p of `total` (0: of its first top_k).
-  __device__ bool draw_from_list(int count, u64 total) {
-    const int each = (count - 1) / kThreads + 1, first = min(count, (int)threadIdx.x * each), last = min(count, first + each);
-    const int most = a.top_k ? min(a.top_k, count) : count;
-    u64 mine = 0, all;
-    for (int i = first; i < min(last, most); ++i) mine += weights[i];
-    u64 before = block_scan(mine, s, &all);
-    if (a.top_k) total = all;
-    const u64 need = a.top_p < 1.0f ? (u64)ceil((double)total * (double)a.top_p) : ~0ull;
-    if (!a.top_k && all < need) return false;
-    u64 kept = 0, held = 0, kept_all, held_all;
-    for (int i = first; i < min(last, most) && before < need; ++i) {
-      if (t_of(list[i]) > farthest) break;
-      ++kept;
-      held += weights[i];
-      before += weights[i];
-    }
-    block_scan(kept, s, &kept_all);
-    block_scan(held, s, &held_all);
-    // by id, with the place of the weight
-    const int n = power_of_two((int)kept_all);
-    for (int i = threadIdx.x; i < n; i += kThreads)
-      list[i] = i < (int)kept_all ? list[i] << 32 | (uint32_t)i : ~0ull;
-    sort_list(list, n);
-    const u64 place = place_of(a.u[index], held_all);
-    const int per = (n - 1) / kThreads + 1, from = min((int)kept_all, (int)threadIdx.x * per), to = min((int)kept_all, from + per);
-    mine = 0;
-    for (int i = from; i < to; ++i) mine += weights[(uint32_t)list[i]];
-    before = block_scan(mine, s, &all);
-    for (int i = from; i < to; ++i) {
-      const u64 w = weights[(uint32_t)list[i]];
-      if (before <= place && place < before + w) {
-        const int id = (int)(list[i] >> 32);
-        write_token(id, t_of(row.at(id)), held_all, (int)kept_all);
+  // The first block: cuts the list, which holds all tokens down to some one, and draws from it.  s->total says whether
+  // it holds top_p of `total` (0: of its first top_k).
+  __device__ void draw_from_list(int count, u64 total) const {
+    with_items(count, [&](auto &items) {
+      u64 last = ~0ull;  // of the entries that are kept
+      if (a.top_k && a.top_k < count) last = items.template reach<false>((u64)a.top_k, id_bits());
+      const auto first = [&](int i) { return items.entry[i] <= last; };
+      u64 all = items.template sum_where<true>(first);
+      if (a.top_k) total = all;
+      const u64 need = a.top_p < 1.0f ? (u64)ceil((double)total * (double)a.top_p) : 0;
+      if (need > all) {
+        if (threadIdx.x == 0) s->total = 0;
+        return;
       }
-      before += w;
-    }
-    return true;
+      if (a.top_p < 1.0f) last = min(last, items.template reach<true>(need, id_bits()));
+#pragma unroll
+      for (int i = 0; i < items.kEvery; ++i)
+        if (items.entry[i] > last || !(t_of(items.entry[i]) <= farthest)) items.weight[i] = 0;
+      const auto any = [&](int i) { return items.weight[i] != 0; };
+      const u64 kept = items.template sum_where<false>(any);
+      all = items.template sum_where<true>(any);
+      const uint32_t id = items.template largest<true>(id_bits(), 0, place_of(a.u[index], all),
+                                                       [&](int i, uint32_t x) { return (uint32_t)items.entry[i] < x; });
+      if (threadIdx.x != 0) return;
+      write_token((int)id, t_of(row.at((int)id)), all, (int)kept);
+      s->total = 1;
+    });
   }
 
   // What the first block put in s->total, in all blocks.
@@ -438,21 +578,19 @@ struct Sampler {
     return v;
   }
 
-  // The first block: of the collected tokens, in order, the one at which the sum (of weights, or of ones) from `above`
-  // reaches `need`, into s->total as an entry; all ones where none does.
+  // The first block: of the list, the token at which the sum (of weights, or of ones) reaches `need`, into s->total as
+  // an entry; all ones where none does.
   template <bool kWeights>
-  __device__ void find_in_list(int count, u64 above, u64 need) {
-    if (count > 0) order(count);
-    if (threadIdx.x == 0) s->total = ~0ull;
-    const int each = count / kThreads + 1, first = min(count, (int)threadIdx.x * each), last = min(count, first + each);
-    u64 mine = 0, all;
-    for (int i = first; i < last; ++i) mine += kWeights ? weights[i] : 1;
-    u64 before = above + block_scan(mine, s, &all);
-    for (int i = first; i < last; ++i) {
-      const u64 w = kWeights ? weights[i] : 1;
-      if (before < need && need <= before + w) s->total = list[i];
-      before += w;
+  __device__ void find_in_list(int count, u64 need) const {
+    if (count == 0) {
+      if (threadIdx.x == 0) s->total = ~0ull;
+      return;
     }
+    with_items(count, [&](auto &items) {
+      const bool reaches = items.template sum_where<kWeights>([&](int i) { return i * items.kWidth + (int)threadIdx.x < count; }) >= need;
+      const u64 entry = reaches ? items.template reach<kWeights>(need, id_bits()) : ~0ull;
+      if (threadIdx.x == 0) s->total = entry;
+    });
   }
 
   // The cut at the token at which the sum (of weights, or of ones) from the largest down reaches `need`, where the
@@ -469,7 +607,7 @@ struct Sampler {
 #pragma unroll
       for (int e = 0; e < R::kN; ++e) {
         const float t = t_of(R::element(p, e));
-        if (t <= kFarthest) atomicAdd(&bins[(int)(t * kBinsOfOne)], 1u);
+        if (t <= kFarthest) atomicAdd(&bins[step_of(t)], 1u);
       }
     }, [](int) {});
     g.sync();
@@ -521,7 +659,7 @@ struct Sampler {
     const float nearest = (float)bin[0] / kBinsOfOne, beyond = (float)(bin[1] + 1) / kBinsOfOne;
     const int count = collect<kWeights>(nearest, beyond, nearest, &above);
     if (count <= kList && (!kWeights || above < need)) {
-      if (g.rank == 0) find_in_list<kWeights>(count, above, need);
+      if (g.rank == 0) find_in_list<kWeights>(count, need - above);
       const u64 entry = told();
       if (entry != ~0ull) return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
     }
@@ -658,14 +796,16 @@ struct Sampler {
     Weights w;
     for_row(row, g, [&](int piece, const uint4 &p, int) {
 #pragma unroll
-      for (int e = 0; e < R::kN; ++e) {
-        const float x = R::element(p, e), t = t_of(x);
-        w.add(t, keeps(x, t, row.id(piece) + e));
+      for (int e = 0; e < R::kN; e += 2) {
+        const float x = R::element(p, e), y = R::element(p, e + 1);
+        const Pair minus = minus_t(x, y, m, c);
+        const float2 t = floats_of(minus);
+        w.add(minus, keeps(x, -t.x, row.id(piece) + e), keeps(y, -t.y, row.id(piece) + e + 1));
       }
     }, [&](int chunk) {
       const u64 sum = w.sum();
       v[0] += sum;
-      v[1] += w.n;
+      v[1] += w.tokens();
       put_chunk(chunk, sum);
       w = Weights();
     });
@@ -717,11 +857,7 @@ struct Sampler {
       const float t = t_of(R::value_of(bound)), beyond = t < kFarthest ? __uint_as_float(__float_as_uint(t) + 1) : past;
       const int count = top_k ? collect<false>(0.0f, beyond, 0.0f, nullptr) : collect<true>(0.0f, beyond, past, &total);
       if (count <= kList) {
-        if (g.rank == 0) {
-          order(count);
-          const bool done = draw_from_list(count, total);
-          if (threadIdx.x == 0) s->total = done;
-        }
+        if (g.rank == 0) draw_from_list(count, total);
         if (told()) return;
       }
     }
@@ -741,9 +877,12 @@ struct Sampler {
         Weights w;
         for_row(row, g, [&](int piece, const uint4 &p, int) {
 #pragma unroll
-          for (int e = 0; e < R::kN; ++e) {
-            const float x = R::element(p, e), t = t_of(x);
-            w.add(t, t <= kFarthest && cut.keeps(R::key(x), row.id(piece) + e));
+          for (int e = 0; e < R::kN; e += 2) {
+            const float x = R::element(p, e), y = R::element(p, e + 1);
+            const Pair minus = minus_t(x, y, m, c);
+            const float2 t = floats_of(minus);
+            w.add(minus, -t.x <= kFarthest && cut.keeps(R::key(x), row.id(piece) + e),
+                  -t.y <= kFarthest && cut.keeps(R::key(y), row.id(piece) + e + 1));
           }
         }, [&](int) {
           sum[0] += w.sum();
