@@ -35,7 +35,8 @@ constexpr unsigned kAll = 0xffffffffu;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kEach = 4;                   // pieces of 16 bytes of a lane in a chunk, and cells of a thread
 constexpr int kChunkPieces = 32 * kEach;
-constexpr int kList = 4096;                // logits that can be collected
+constexpr int kList = 2048;                // logits that can be collected
+constexpr int kChunksMost = 8192;          // sums of chunks, in the place of the list and what is beside it
 constexpr int kMaxCluster = 8;
 constexpr float kFarthest = 40.0f;         // the weight is 0 past it
 constexpr int kBinsOfOne = 64, kBins = 40 * kBinsOfOne + 1;
@@ -218,11 +219,13 @@ struct Row {
 struct Shared {
   u64 sums[2][kWarps][4];        // of warps, by turns
   u64 peers[2][kMaxCluster][4];  // of the blocks of a cluster
+  u64 items[2][kWarps][3];
   u64 scan[kWarps];
   uint32_t counts[2][kWarps];
   int collected;
   uint32_t first;  // upper half of the list's first entry
   u64 total;
+  u64 held;  // the list's weight, where it is not all that was sought
   int chunk;
   int bins[2];  // first and last
 };
@@ -280,20 +283,33 @@ struct Group {
   }
 };
 
-// Runs f(piece number, piece) over this block's share of the row: chunk c is its where c % size == rank.
-// after(c) follows the pieces of chunk c, in all lanes of the warp that has it.
-template <typename T, typename F, typename After>
-__device__ __forceinline__ void for_row(const Row<T> &row, const Group &g, const F &f, const After &after) {
+// Runs f(chunk, its pieces of this lane) over this block's share of the row: chunk c is its where c % size ==
+// rank, and a warp's as a whole.
+template <typename T, typename F>
+__device__ __forceinline__ void for_row(const Row<T> &row, const Group &g, const F &f) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int chunks = (row.pieces - 1) / kChunkPieces + 1;
   for (int c = g.rank + g.size * warp; c < chunks; c += g.size * kWarps) {
     uint4 p[kEach];
+    const int first = c * kChunkPieces + lane;
+    if (row.id(c * kChunkPieces) >= 0 && row.id((c + 1) * kChunkPieces) <= row.vocab) {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) p[j] = row.load(c * kChunkPieces + j * 32 + lane);
+      for (int j = 0; j < kEach; ++j) p[j] = row.base[first + j * 32];
+    } else {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) f(c * kChunkPieces + j * 32 + lane, p[j], j);
-    after(c);
+      for (int j = 0; j < kEach; ++j) p[j] = row.load(first + j * 32);
+    }
+    f(c, p);
   }
+}
+// f(element, its id) for all of a lane's.
+template <typename T, typename F>
+__device__ __forceinline__ void for_chunk(const Row<T> &row, int chunk, const uint4 (&p)[kEach], const F &f) {
+#pragma unroll
+  for (int j = 0; j < kEach; ++j)
+#pragma unroll
+    for (int e = 0; e < Row<T>::kN; ++e)
+      f(Row<T>::element(p[j], e), row.id(chunk * kChunkPieces + j * 32 + (int)(threadIdx.x & 31)) + e);
 }
 
 // Exclusive sums of v over the block's threads, and the total.
@@ -318,18 +334,18 @@ __device__ __forceinline__ u64 block_scan(u64 v, Shared *s, u64 *total) {
   return before + x - v;
 }
 
-// Sums of v < 2^48 over a warp.
+// Sums of v < 2^50 over a warp.
 __device__ __forceinline__ u64 warp_sum(u64 v) {
-  const uint32_t a = __reduce_add_sync(kAll, (uint32_t)v & 0xFFFFFu), b = __reduce_add_sync(kAll, (uint32_t)(v >> 20) & 0xFFFFFu);
-  return a + ((u64)b << 20) + ((u64)__reduce_add_sync(kAll, (uint32_t)(v >> 40)) << 40);
+  const uint32_t a = __reduce_add_sync(kAll, (uint32_t)v & 0x1FFFFFFu), b = __reduce_add_sync(kAll, (uint32_t)(v >> 25));
+  return a + ((u64)b << 25);
 }
 
-// Collected tokens in the registers of a team, a warp or the block: entries, which ascend in the order of the
-// tokens (keys falling, then ids rising), and weights.  Everything about them is found by searching for the bits
-// of an answer one after the other, each by a sum over the team, which sorts nothing.
-template <int kTeam>
+// Collected tokens in the block's registers, kEvery of them in each thread's: entries, which ascend in
+// the order of the tokens (keys falling, then ids rising), and weights.  Everything about them is found by
+// searching for an answer two bits at a time, by three sums over the block, which sorts nothing.
+template <int kEvery_>
 struct Items {
-  static constexpr int kWidth = kTeam, kEvery = kTeam == 32 ? 8 : kList / kTeam;
+  static constexpr int kEvery = kEvery_;
   u64 entry[kEvery], weight[kEvery];
   int count, turn = 0;
   Shared *s;
@@ -338,64 +354,80 @@ struct Items {
   __device__ Items(const u64 *list, int n, Shared *shared, const F &weight_at) : count(n), s(shared) {
 #pragma unroll
     for (int i = 0; i < kEvery; ++i) {
-      const int at = i * kTeam + (int)threadIdx.x;
+      const int at = i * kThreads + (int)threadIdx.x;
       entry[i] = at < n ? list[at] : ~0ull;
       weight[i] = at < n ? weight_at(list[at]) : 0;
     }
   }
-  __device__ __forceinline__ u64 sum(u64 v) {
-    v = warp_sum(v);
-    if constexpr (kTeam > 32) {
-      const int lane = threadIdx.x & 31;
-      turn ^= 1;
-      if (lane == 0) s->sums[turn][threadIdx.x >> 5][3] = v;
-      __syncthreads();
-      v = warp_sum(lane < kWarps ? s->sums[turn][lane][3] : 0);
-    }
-    return v;
+  template <int kM>
+  __device__ __forceinline__ void sums(u64 (&v)[kM]) {
+#pragma unroll
+    for (int j = 0; j < kM; ++j) v[j] = warp_sum(v[j]);
+    const int lane = threadIdx.x & 31;
+    turn ^= 1;
+#pragma unroll
+    for (int j = 0; j < kM; ++j)
+      if (lane == 0) s->items[turn][threadIdx.x >> 5][j] = v[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kM; ++j) v[j] = warp_sum(lane < kWarps ? s->items[turn][lane][j] : 0);
   }
   // Over the items i that f takes: of weights, or of ones.
   template <bool kWeights, typename F>
   __device__ __forceinline__ u64 sum_where(const F &f) {
-    u64 v = 0;
+    u64 v[1] = {0};
 #pragma unroll
     for (int i = 0; i < kEvery; ++i)
-      if (f(i)) v += kWeights ? weight[i] : 1;
-    return sum(v);
+      if (f(i)) v[0] += kWeights ? weight[i] : 1;
+    sums<1>(v);
+    return v[0];
   }
-  // The largest x below 2^bits, of what f(item, x) asks, for which the sum over f is not more than `most`.
+  // The largest x, of x and any lower bits, for which the sum over the items where f(item) < x is not more than
+  // `most`; f takes no item that it is ~0 of.
   template <bool kWeights, typename F>
   __device__ __forceinline__ uint32_t largest(int bits, uint32_t x, u64 most, const F &f) {
-    for (int bit = bits - 1; bit >= 0; --bit) {
-      const uint32_t next = x | 1u << bit;
-      if (sum_where<kWeights>([&](int i) { return f(i, next); }) <= most) x = next;
+    for (int bit = (bits + 1) / 2 * 2 - 2; bit >= 0; bit -= 2) {
+      u64 v[3] = {0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kEvery; ++i) {
+        const uint32_t y = f(i);
+        if (y == ~0u) continue;
+        const u64 w = kWeights ? weight[i] : 1;
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (y < x + ((uint32_t)(j + 1) << bit)) v[j] += w;
+      }
+      sums<3>(v);
+      x += (uint32_t)((v[0] <= most) + (v[1] <= most) + (v[2] <= most)) << bit;
     }
     return x;
   }
   // The entry at which the sum, in order, reaches `need`; that of all items does.
   template <bool kWeights>
   __device__ u64 reach(u64 need, int id_bits) {
+    const auto upper_of = [&](int i) { return (uint32_t)(entry[i] >> 32); };
     uint32_t differ = 0;
-    const uint32_t some = s->first;
 #pragma unroll
     for (int i = 0; i < kEvery; ++i)
-      if (i * kTeam + (int)threadIdx.x < count) differ |= (uint32_t)(entry[i] >> 32) ^ some;
+      if (i * kThreads + (int)threadIdx.x < count) differ |= upper_of(i) ^ s->first;
     differ = __reduce_or_sync(kAll, differ);
-    if constexpr (kTeam > 32) {
-      const int lane = threadIdx.x & 31;
-      turn ^= 1;
-      if (lane == 0) s->sums[turn][threadIdx.x >> 5][3] = differ;
-      __syncthreads();
-      differ = __reduce_or_sync(kAll, lane < kWarps ? (uint32_t)s->sums[turn][lane][3] : 0u);
+    const int lane = threadIdx.x & 31;
+    turn ^= 1;
+    if (lane == 0) s->items[turn][threadIdx.x >> 5][0] = differ;
+    __syncthreads();
+    differ = __reduce_or_sync(kAll, lane < kWarps ? (uint32_t)s->items[turn][lane][0] : 0u);
+    const int bits = (33 - __clz(differ)) / 2 * 2;
+    const uint32_t upper = largest<kWeights>(bits, bits < 32 ? s->first >> bits << bits : 0, need - 1, upper_of);
+    const auto equal = [&](int i) { return upper_of(i) == upper; };
+    u64 v[2] = {0, 0};  // how many are equal, and what comes before them
+#pragma unroll
+    for (int i = 0; i < kEvery; ++i) {
+      v[0] += equal(i);
+      if (upper_of(i) < upper) v[1] += kWeights ? weight[i] : 1;
     }
-    const int bits = 32 - __clz(differ);
-    const uint32_t upper = largest<kWeights>(bits, bits < 32 ? some >> bits << bits : 0, need - 1,
-                                             [&](int i, uint32_t x) { return (uint32_t)(entry[i] >> 32) < x; });
-    const auto equal = [&](int i) { return (uint32_t)(entry[i] >> 32) == upper; };
-    if (sum_where<false>(equal) == 1) return (u64)upper << 32 | 0x7FFFFFFFu;
-    const u64 before = sum_where<kWeights>([&](int i) { return (uint32_t)(entry[i] >> 32) < upper; });
-    const uint32_t id = largest<kWeights>(id_bits, 0, need - 1 - before, [&](int i, uint32_t x) { return equal(i) && (uint32_t)entry[i] < x; });
-    return (u64)upper << 32 | id;
+    sums<2>(v);
+    if (v[0] == 1) return (u64)upper << 32 | 0x7FFFFFFFu;
+    return (u64)upper << 32 | largest<kWeights>(id_bits, 0, need - 1 - v[1], [&](int i) { return equal(i) ? (uint32_t)entry[i] : ~0u; });
   }
 };
 
@@ -441,7 +473,7 @@ struct Sampler {
   const R &row;
   Group &g;
   Shared *s;
-  u64 *list, *weights;  // kList each; together the chunks' sums
+  u64 *list, *weights;  // of kList, and what is beside it; together the chunks' sums
   float m, c, farthest;
   int index;
 
@@ -467,31 +499,44 @@ struct Sampler {
     g.sync();
     u64 v[1] = {0};
     Weights w;
-    for_row(row, g, [&](int piece, const uint4 &p, int) {
-      const float first = t_of(R::value(R::largest(R::none, p)));
-      if (kSum && first < near) {
+    for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+      uint32_t found = 0;  // by piece and element
 #pragma unroll
-        for (int e = 0; e < R::kN; e += 2) {
-          const Pair minus = minus_t(R::element(p, e), R::element(p, e + 1), m, c);
+      for (int j = 0; j < kEach; ++j) {
+        const bool any = t_of(R::value(R::largest(R::none, p[j]))) < beyond;
+#pragma unroll
+        for (int e = 0; kSum && e < R::kN; e += 2) {
+          const Pair minus = minus_t(R::element(p[j], e), R::element(p[j], e + 1), m, c);
           const float2 t = floats_of(minus);
           w.add(minus, -t.x < near, -t.y < near);
         }
-      }
-      if (!(first < beyond)) return;
+        if (!any) continue;
 #pragma unroll
-      for (int e = 0; e < R::kN; ++e) {
-        const float x = R::element(p, e), t = t_of(x);
-        if (t < nearest || !(t < beyond)) continue;
-        const unsigned here = __activemask(), lane = threadIdx.x & 31;
-        int at = 0;
-        if (lane == __ffs(here) - 1u) at = atomicAdd(&s->collected, __popc(here));
-        at = __shfl_sync(here, at, __ffs(here) - 1) + __popc(here & ((1u << lane) - 1));
-        if (at < kList) list[at] = (u64)~R::key(x) << 32 | (uint32_t)(row.id(piece) + e);
+        for (int e = 0; e < R::kN; e += 2) {
+          const float2 t = floats_of(minus_t(R::element(p[j], e), R::element(p[j], e + 1), m, c));
+          if (-t.x >= nearest && -t.x < beyond) found |= 1u << (j * R::kN + e);
+          if (-t.y >= nearest && -t.y < beyond) found |= 1u << (j * R::kN + e + 1);
+        }
       }
-    }, [&](int) {
-      if (!kSum) return;
-      v[0] += w.sum();
-      w = Weights();
+      if (kSum) {
+        v[0] += w.sum();
+        w = Weights();
+      }
+      // one addition to the counter for a warp (one for each token took ten times as long as all else)
+      if (!__any_sync(kAll, found)) return;
+      const int lane = threadIdx.x & 31, mine = __popc(found);
+      int before = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(kAll, before, d);
+        if (lane >= d) before += y;
+      }
+      int at = lane == 31 ? atomicAdd(&s->collected, before) : 0;
+      at = __shfl_sync(kAll, at, 31) + before - mine;
+      for (; found; found &= found - 1, ++at) {
+        const int bit = __ffs(found) - 1, id = row.id(chunk * kChunkPieces + bit / R::kN * 32 + lane) + bit % R::kN;
+        if (at < kList) list[at] = (u64)~R::key(row.at(id)) << 32 | (uint32_t)id;
+      }
     });
     if (kSum) {
       g.template all<1>(v);
@@ -508,16 +553,20 @@ struct Sampler {
         at[r + 1] = at[r] + more;
       }
       count = at[kMaxCluster];
-      if (g.rank == 0 && count <= kList)
-        for (int r = 1; r < g.size; ++r) {
+      if (g.rank == 0 && count <= kList) {
+#pragma unroll
+        for (int r = 1; r < kMaxCluster; ++r) {
+          if ((int)(threadIdx.x >> 5) % kMaxCluster != r || r >= g.size) continue;  // two warps for a block's tokens
           const uint32_t from = remote(smem_addr(list), r);
-          for (int i = threadIdx.x; i < at[r + 1] - at[r]; i += kThreads) {
+          for (int i = threadIdx.x / 32 / kMaxCluster * 32 + threadIdx.x % 32; i < at[r + 1] - at[r]; i += kThreads / kMaxCluster) {
             u64 entry;
             asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(entry) : "r"(from + 8u * (uint32_t)i) : "memory");
             list[at[r] + i] = entry;
           }
         }
+      }
     }
+    __syncthreads();
     if (g.rank == 0 && threadIdx.x == 0 && count > 0 && count <= kList) s->first = (uint32_t)(list[0] >> 32);
     __syncthreads();
     return count;
@@ -529,20 +578,85 @@ struct Sampler {
   template <typename F>
   __device__ __forceinline__ void with_items(int count, const F &f) const {
     const auto weight = [&](u64 entry) { return weight_of(t_of(entry)); };
-    if (count <= 32 * Items<32>::kEvery) {
-      if (threadIdx.x < 32) {
-        Items<32> items(list, count, s, weight);
-        f(items);
-      }
+    if (count <= 2 * kThreads) {
+      Items<2> items(list, count, s, weight);
+      f(items);
     } else {
-      Items<kThreads> items(list, count, s, weight);
+      Items<kList / kThreads> items(list, count, s, weight);
       f(items);
     }
+  }
+
+  // draw_from_list for up to kThreads tokens, one of a thread's: each against all others, which gives its place and the
+  // weight before it, in the order of the tokens and, of those kept, by id.
+  __device__ void draw_from_short_list(int count, u64 total) const {
+    struct alignas(16) Item {
+      u64 entry, weight;
+    };
+    Item *items = reinterpret_cast<Item *>(weights);
+    const int i = threadIdx.x;
+    const bool mine = i < count;
+    const Item item{mine ? list[i] : ~0ull, mine ? weight_of(t_of(list[i])) : 0};
+    if (mine) items[i] = item;
+    u64 all[1] = {item.weight};
+    sum_in_block(all);
+    if (!a.top_k && all[0] < (u64)ceil((double)total * (double)a.top_p)) {
+      if (i == 0) {
+        s->total = 0;
+        s->held = all[0];
+      }
+      return;
+    }
+    int place = 0;
+    u64 before = 0;
+    if (i / 32 * 32 < count)
+#pragma unroll 4
+      for (int j = 0; j < count; ++j) {
+        const Item other = items[j];
+        if (other.entry < item.entry) {
+          ++place;
+          before += other.weight;
+        }
+      }
+    const bool first = mine && (!a.top_k || place < a.top_k);
+    u64 v[1] = {first ? item.weight : 0};
+    sum_in_block(v);
+    if (a.top_k) total = v[0];
+    const u64 need = a.top_p < 1.0f ? (u64)ceil((double)total * (double)a.top_p) : 0;
+    const bool keep = first && (a.top_p >= 1.0f || before < need) && t_of(item.entry) <= farthest;
+    u64 w[2] = {keep ? item.weight : 0, keep};
+    sum_in_block(w);
+    const u64 at = place_of(a.u[index], w[0]);
+    if (keep) items[place] = Item{(uint32_t)item.entry, item.weight};  // all read the old ones before the sums
+    __syncthreads();
+    if (!keep) return;
+    before = 0;
+#pragma unroll 4
+    for (int j = 0; j < (int)w[1]; ++j)
+      if (items[j].entry < (uint32_t)item.entry) before += items[j].weight;
+    if (before <= at && at < before + item.weight) {
+      write_token((int)(uint32_t)item.entry, t_of(item.entry), w[0], (int)w[1]);
+      s->total = 1;
+    }
+  }
+  template <int kM>
+  __device__ void sum_in_block(u64 (&v)[kM]) const {
+    const int lane = threadIdx.x & 31;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kM; ++j) {
+      v[j] = warp_sum(v[j]);
+      if (lane == 0) s->items[0][threadIdx.x >> 5][j] = v[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kM; ++j) v[j] = warp_sum(lane < kWarps ? s->items[0][lane][j] : 0);
   }
 
   // The first block: cuts the list, which holds all tokens down to some one, and draws from it.  s->total says whether
   // it holds top_p of `total` (0: of its first top_k).
   __device__ void draw_from_list(int count, u64 total) const {
+    if (count <= kThreads) return draw_from_short_list(count, total);
     with_items(count, [&](auto &items) {
       u64 last = ~0ull;  // of the entries that are kept
       if (a.top_k && a.top_k < count) last = items.template reach<false>((u64)a.top_k, id_bits());
@@ -551,7 +665,10 @@ struct Sampler {
       if (a.top_k) total = all;
       const u64 need = a.top_p < 1.0f ? (u64)ceil((double)total * (double)a.top_p) : 0;
       if (need > all) {
-        if (threadIdx.x == 0) s->total = 0;
+        if (threadIdx.x == 0) {
+          s->total = 0;
+          s->held = all;
+        }
         return;
       }
       if (a.top_p < 1.0f) last = min(last, items.template reach<true>(need, id_bits()));
@@ -562,7 +679,7 @@ struct Sampler {
       const u64 kept = items.template sum_where<false>(any);
       all = items.template sum_where<true>(any);
       const uint32_t id = items.template largest<true>(id_bits(), 0, place_of(a.u[index], all),
-                                                       [&](int i, uint32_t x) { return (uint32_t)items.entry[i] < x; });
+                                                       [&](int i) { return (uint32_t)items.entry[i]; });
       if (threadIdx.x != 0) return;
       write_token((int)id, t_of(row.at((int)id)), all, (int)kept);
       s->total = 1;
@@ -579,89 +696,117 @@ struct Sampler {
   }
 
   // The first block: of the list, the token at which the sum (of weights, or of ones) reaches `need`, into s->total as
-  // an entry; all ones where none does.
+  // an entry, all ones where none does; and the sum of all, into s->held.
   template <bool kWeights>
   __device__ void find_in_list(int count, u64 need) const {
     if (count == 0) {
-      if (threadIdx.x == 0) s->total = ~0ull;
+      if (threadIdx.x == 0) {
+        s->total = ~0ull;
+        s->held = 0;
+      }
       return;
     }
     with_items(count, [&](auto &items) {
-      const bool reaches = items.template sum_where<kWeights>([&](int i) { return i * items.kWidth + (int)threadIdx.x < count; }) >= need;
-      const u64 entry = reaches ? items.template reach<kWeights>(need, id_bits()) : ~0ull;
-      if (threadIdx.x == 0) s->total = entry;
+      const u64 all = items.template sum_where<kWeights>([&](int i) { return i * kThreads + (int)threadIdx.x < count; });
+      const u64 entry = all >= need ? items.template reach<kWeights>(need, id_bits()) : ~0ull;
+      if (threadIdx.x == 0) {
+        s->total = entry;
+        s->held = all;
+      }
     });
+  }
+
+  // The first block: the steps of distance, in s->bins, among whose tokens a sum reaches `need` that is `above` for
+  // all tokens nearer than step `from`; and, of ones, the sum before it in s->total.
+  template <bool kWeights>
+  __device__ void find_steps(const uint32_t *bins, u64 need, int from, u64 above) const {
+    constexpr int kOf = (kBins - 1) / kThreads + 1;
+    const int first = min(kBins, (int)threadIdx.x * kOf), last = min(kBins, first + kOf);
+    const auto mass = [&](int i) { return kWeights ? weight_of((i + 0.5f) / kBinsOfOne) * bins[i] : (u64)bins[i]; };
+    u64 mine = 0, all;
+    for (int i = first; i < last; ++i) mine += mass(i);
+    const u64 begin = block_scan(mine, s, &all);
+    u64 before = begin;
+    for (int i = first; i < last; ++i) {
+      if (i == from) s->total = before;
+      before += mass(i);
+    }
+    if (threadIdx.x == 0) s->bins[0] = s->bins[1] = need > above ? kBins - 1 : 0;
+    __syncthreads();
+    const u64 sought = s->total + need - above;  // of the sums here, which differ from those that are meant
+    __syncthreads();
+    before = begin;
+    for (int i = first; i < last && (int64_t)sought > 0; ++i) {
+      const u64 w = mass(i);
+      if (before < sought && sought <= before + w) {
+        s->bins[0] = s->bins[1] = i;
+        if (!kWeights) s->total = before;
+      }
+      before += w;
+    }
+    __syncthreads();
+    if (kWeights && threadIdx.x == 0) {  // a step to either side, where the list has room
+      const int at = s->bins[0];
+      const uint32_t held = bins[at], nearer = at > 0 ? bins[at - 1] : 0, farther = at + 1 < kBins ? bins[at + 1] : 0;
+      if (held + nearer + farther <= kList) {
+        s->bins[0] = max(at - 1, 0);
+        s->bins[1] = min(at + 1, kBins - 1);
+      }
+    }
+    __syncthreads();
   }
 
   // The cut at the token at which the sum (of weights, or of ones) from the largest down reaches `need`, where the
   // weights, or the tokens at t <= 40, come to that.  Tokens are counted by their distance in steps of 1/64: of
-  // ones that gives the step of the cut, and of weights, which differ by 2^(1/64) in a step, one near it.  The step, or
-  // some on either side, are collected, and the rest is exact.
+  // ones that gives the step of the cut, and of weights, which differ by 2^(1/64) in a step, one near it from
+  // where the sum is known (the first block's `above` for tokens nearer than step `from`).  Its tokens and its
+  // neighbours' are collected, and the rest is exact.
   template <bool kWeights>
-  __device__ Cut find_cut(u64 need) {
+  __device__ Cut find_cut(u64 need, int from, u64 above) {
     uint32_t *bins = reinterpret_cast<uint32_t *>(weights);
     g.sync();  // the weights were read
     for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
     __syncthreads();
-    for_row(row, g, [&](int, const uint4 &p, int) {
-#pragma unroll
-      for (int e = 0; e < R::kN; ++e) {
-        const float t = t_of(R::element(p, e));
+    for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+      for_chunk(row, chunk, p, [&](float x, int) {
+        const float t = t_of(x);
         if (t <= kFarthest) atomicAdd(&bins[step_of(t)], 1u);
-      }
-    }, [](int) {});
+      });
+    });
     g.sync();
-    u64 above = 0;
-    if (g.rank == 0) {
-      constexpr int kOf = (kBins - 1) / kThreads + 1;
-      const int first = threadIdx.x * kOf;
-      for (int r = 1; r < g.size; ++r)
-        for (int i = first; i < min(kBins, first + kOf); ++i) {
-          uint32_t more;
-          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(more) : "r"(remote(smem_addr(bins + i), r)) : "memory");
-          bins[i] += more;
+    if (g.rank == 0 && g.size > 1) {
+      for (int i = threadIdx.x; i < kBins; i += kThreads) {
+        uint32_t more[kMaxCluster - 1];
+#pragma unroll
+        for (int r = 1; r < kMaxCluster; ++r) {
+          more[r - 1] = 0;
+          if (r < g.size)
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(more[r - 1]) : "r"(remote(smem_addr(bins + i), r)) : "memory");
         }
-      const auto mass = [&](int i) { return kWeights ? weight_of((i + 0.5f) / kBinsOfOne) * bins[i] : (u64)bins[i]; };
-      u64 mine = 0, all;
-      for (int i = first; i < min(kBins, first + kOf); ++i) mine += mass(i);
-      if (threadIdx.x == 0) s->bins[0] = s->bins[1] = kBins - 1;
-      u64 before = block_scan(mine, s, &all);
-      for (int i = first; i < min(kBins, first + kOf); ++i) {
-        const u64 w = mass(i);
-        if (before < need && need <= before + w) {
-          s->bins[0] = s->bins[1] = i;
-          if (!kWeights) s->total = before;
-        }
-        before += w;
-      }
-      __syncthreads();
-      if (kWeights && threadIdx.x == 0) {  // as far to either side as goes in the list with room to spare
-        int lo = s->bins[0], hi = lo;
-        uint32_t held = bins[lo];
-        for (int d = 0; d < 8; ++d) {
-          const uint32_t more = (lo > 0 ? bins[lo - 1] : 0) + (hi + 1 < kBins ? bins[hi + 1] : 0);
-          if (held + more > kList) break;
-          held += more;
-          lo = max(lo - 1, 0);
-          hi = min(hi + 1, kBins - 1);
-        }
-        s->bins[0] = lo;
-        s->bins[1] = hi;
+#pragma unroll
+        for (int r = 1; r < kMaxCluster; ++r) bins[i] += more[r - 1];
       }
       __syncthreads();
     }
-    if (!kWeights) above = told();
-    else g.sync();
-    int bin[2];
+    for (int turn = 0; turn < 6; ++turn) {
+      if (g.rank == 0) find_steps<kWeights>(bins, need, from, above);
+      if (!kWeights) above = told();
+      else g.sync();
+      int bin[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(bin[j]) : "r"(remote(smem_addr(&s->bins[j]), 0)) : "memory");
-    const float nearest = (float)bin[0] / kBinsOfOne, beyond = (float)(bin[1] + 1) / kBinsOfOne;
-    const int count = collect<kWeights>(nearest, beyond, nearest, &above);
-    if (count <= kList && (!kWeights || above < need)) {
+      for (int j = 0; j < 2; ++j)
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(bin[j]) : "r"(remote(smem_addr(&s->bins[j]), 0)) : "memory");
+      const float nearest = (float)bin[0] / kBinsOfOne, beyond = (float)(bin[1] + 1) / kBinsOfOne;
+      const int count = collect<kWeights>(nearest, beyond, nearest, &above);
+      if (count > kList) break;
+      from = bin[0];
+      if (kWeights && above >= need) continue;  // the cut is nearer
       if (g.rank == 0) find_in_list<kWeights>(count, need - above);
       const u64 entry = told();
       if (entry != ~0ull) return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
+      from = bin[1] + 1;
+      if (g.rank == 0) above += s->held;
+      g.sync();
     }
     return bracket_cut<kWeights>(need);
   }
@@ -676,16 +821,15 @@ struct Sampler {
 #pragma unroll
       for (int j = 0; j < 3; ++j) key[j] = min(max(hi - (uint32_t)(((u64)(hi - lo) * (j + 1)) >> 2), lo + 1), hi - 1);
       u64 v[3] = {0, 0, 0};
-      for_row(row, g, [&](int, const uint4 &p, int) {
-#pragma unroll
-        for (int e = 0; e < R::kN; ++e) {
-          const float x = R::element(p, e), t = t_of(x);
+      for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+        for_chunk(row, chunk, p, [&](float x, int) {
+          const float t = t_of(x);
           const u64 w = kWeights ? weight_of(t) : t <= kFarthest;
 #pragma unroll
           for (int j = 0; j < 3; ++j)
             if (R::key(x) >= key[j]) v[j] += w;
-        }
-      }, [](int) {});
+        });
+      });
       g.template all<3>(v);
       uint32_t new_lo = lo, new_hi = hi;
 #pragma unroll
@@ -708,8 +852,7 @@ struct Sampler {
 
   // Sums of chunks into the first block's shared memory.
   __device__ __forceinline__ void put_chunk(int chunk, u64 sum) const {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kAll, sum, d);
+    sum = warp_sum(sum);
     if ((threadIdx.x & 31) == 0)
       asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(smem_addr(list), 0) + 8u * (uint32_t)chunk), "l"(sum) : "memory");
   }
@@ -763,13 +906,10 @@ struct Sampler {
   __device__ void id_of_rank(uint32_t key, u64 rank) {
     const auto equal = [&](float x, int) -> u64 { return R::key(x) == key; };
     g.sync();
-    u64 mine = 0;
-    for_row(row, g, [&](int piece, const uint4 &p, int) {
-#pragma unroll
-      for (int e = 0; e < R::kN; ++e) mine += equal(R::element(p, e), 0);
-    }, [&](int chunk) {
+    for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+      u64 mine = 0;
+      for_chunk(row, chunk, p, [&](float x, int id) { mine += equal(x, id); });
       put_chunk(chunk, mine);
-      mine = 0;
     });
     g.sync();
     if (g.rank != 0) return;
@@ -787,27 +927,51 @@ struct Sampler {
     __syncthreads();
   }
 
+  // The weights of a chunk's tokens that keeps(x, t, id) takes.
+  template <typename F>
+  __device__ __forceinline__ Weights weigh(int chunk, const uint4 (&p)[kEach], const F &keeps) const {
+    Weights w;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int id = row.id(chunk * kChunkPieces + j * 32 + (int)(threadIdx.x & 31));
+#pragma unroll
+      for (int e = 0; e < R::kN; e += 2) {
+        const float x = R::element(p[j], e), y = R::element(p[j], e + 1);
+        const Pair minus = minus_t(x, y, m, c);
+        const float2 t = floats_of(minus);
+        w.add(minus, keeps(x, -t.x, id + e), keeps(y, -t.y, id + e + 1));
+      }
+    }
+    return w;
+  }
+
   // Draws from all tokens that the cut and min_p keep.
   template <bool kCut>
   __device__ void draw_from_row(const Cut &cut) {
     const auto keeps = [&](float x, float t, int id) { return t <= farthest && (!kCut || cut.keeps(R::key(x), id)); };
+    // Of a chunk whose ids are all up to the cut's, or all past it, tokens above one key are kept.
+    const float above = R::value_of(cut.key);
+    float from = R::value_of(cut.key - 1);
+    if (from == 0.0f) from = R::value_of(cut.key - 2);  // past -0, which is +0
     g.sync();  // the list was read
     u64 v[2] = {0, 0};
-    Weights w;
-    for_row(row, g, [&](int piece, const uint4 &p, int) {
-#pragma unroll
-      for (int e = 0; e < R::kN; e += 2) {
-        const float x = R::element(p, e), y = R::element(p, e + 1);
-        const Pair minus = minus_t(x, y, m, c);
-        const float2 t = floats_of(minus);
-        w.add(minus, keeps(x, -t.x, row.id(piece) + e), keeps(y, -t.y, row.id(piece) + e + 1));
+    for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+      Weights w;
+      if constexpr (kCut) {
+        const int first = row.id(chunk * kChunkPieces), past = row.id((chunk + 1) * kChunkPieces);
+        if (past - 1 <= cut.id || first > cut.id) {
+          const float limit = first > cut.id ? above : from;
+          w = weigh(chunk, p, [&](float x, float t, int) { return t <= farthest && x > limit; });
+        } else {
+          w = weigh(chunk, p, keeps);
+        }
+      } else {
+        w = weigh(chunk, p, keeps);
       }
-    }, [&](int chunk) {
       const u64 sum = w.sum();
       v[0] += sum;
       v[1] += w.tokens();
       put_chunk(chunk, sum);
-      w = Weights();
     });
     g.template all<2>(v);
     g.sync();
@@ -824,7 +988,10 @@ struct Sampler {
     uint32_t cell[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) cell[j] = R::none;
-    for_row(row, g, [&](int, const uint4 &p, int j) { cell[j] = R::largest(cell[j], p); }, [](int) {});
+    for_row(row, g, [&](int, const uint4 (&p)[kEach]) {
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) cell[j] = R::largest(cell[j], p[j]);
+    });
     float top = -INFINITY;
     uint32_t upper[kEach];
 #pragma unroll
@@ -848,50 +1015,44 @@ struct Sampler {
     if (!top_k && !top_p) return draw_from_row<false>(Cut{0, 0});
     // what the cells' bound collects
     const float past = __uint_as_float(__float_as_uint(kFarthest) + 1);
-    const int want = top_k ? a.top_k : 512, share = (want - 1) / g.size + 1;
-    u64 total = 0;
+    const int want = top_k ? a.top_k : 256, share = (want - 1) / g.size + 1;
+    u64 total = 0, held = 0;  // of the row, and of what was listed, of weights
+    int listed = 0;           // the steps of these
     if (share <= kThreads * kEach / 2) {
       u64 least[1] = {0xFFFFull - cell_bound(upper, share, s)};
       g.template all<1, true>(least);
       const uint32_t bound = max((uint32_t)(0xFFFFull - least[0]) << (R::kBits - 16), R::kNothing + 1);
-      const float t = t_of(R::value_of(bound)), beyond = t < kFarthest ? __uint_as_float(__float_as_uint(t) + 1) : past;
+      const float t = t_of(R::value_of(bound));
+      const int step = t < kFarthest ? (int)step_of(t) + 1 : kBins;  // whole steps, so that what they hold is known later
+      const float beyond = step < kBins ? (float)step / kBinsOfOne : past;
       const int count = top_k ? collect<false>(0.0f, beyond, 0.0f, nullptr) : collect<true>(0.0f, beyond, past, &total);
       if (count <= kList) {
         if (g.rank == 0) draw_from_list(count, total);
         if (told()) return;
+        listed = step;
+        if (g.rank == 0) held = s->held;
+        g.sync();
       }
     }
     Cut cut{R::kNothing + 1, 0x7FFFFFFF};
     if (top_k) {
       u64 tokens[1] = {0};
-      for_row(row, g, [&](int, const uint4 &p, int) {
-#pragma unroll
-        for (int e = 0; e < R::kN; ++e) tokens[0] += t_of(R::element(p, e)) <= kFarthest;
-      }, [](int) {});
+      for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+        for_chunk(row, chunk, p, [&](float x, int) { tokens[0] += t_of(x) <= kFarthest; });
+      });
       g.template all<1>(tokens);
-      if (tokens[0] > (u64)a.top_k) cut = find_cut<false>((u64)a.top_k);
+      if (tokens[0] > (u64)a.top_k) cut = find_cut<false>((u64)a.top_k, 0, 0);
     }
     if (top_p) {
       u64 sum[1] = {total};
       if (top_k) {
-        Weights w;
-        for_row(row, g, [&](int piece, const uint4 &p, int) {
-#pragma unroll
-          for (int e = 0; e < R::kN; e += 2) {
-            const float x = R::element(p, e), y = R::element(p, e + 1);
-            const Pair minus = minus_t(x, y, m, c);
-            const float2 t = floats_of(minus);
-            w.add(minus, -t.x <= kFarthest && cut.keeps(R::key(x), row.id(piece) + e),
-                  -t.y <= kFarthest && cut.keeps(R::key(y), row.id(piece) + e + 1));
-          }
-        }, [&](int) {
-          sum[0] += w.sum();
-          w = Weights();
+        for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
+          sum[0] += weigh(chunk, p, [&](float x, float t, int id) { return t <= kFarthest && cut.keeps(R::key(x), id); }).sum();
         });
         g.template all<1>(sum);
       }
       // among the first top_k, whose weight is at least what is needed
-      cut = find_cut<true>((u64)ceil((double)sum[0] * (double)a.top_p));
+      cut = find_cut<true>((u64)ceil((double)sum[0] * (double)a.top_p), listed, held);
     }
     draw_from_row<true>(cut);
   }
@@ -903,7 +1064,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleArgs a, float
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   u64 *list = reinterpret_cast<u64 *>(smem);
-  Shared *s = reinterpret_cast<Shared *>(list + 2 * kList);
+  Shared *s = reinterpret_cast<Shared *>(list + kChunksMost);
   Group g{size, (int)blockIdx.x % size, 0, s};
   const int index = (int)blockIdx.x / size;
   const Row<T> row(a.logits, a.row, index, a.vocab);
@@ -915,7 +1076,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleArgs a, float
 
 template <typename T>
 cudaError_t launch(const SampleArgs &a, cudaStream_t s) {
-  constexpr int kSmem = 2 * kList * 8 + (int)sizeof(Shared);
+  static_assert((COPES_MAX_SAMPLE_VOCAB - 1) / (kChunkPieces * 4) + 2 <= kChunksMost, "room for fp32's chunks");
+  constexpr int kSmem = kChunksMost * 8 + (int)sizeof(Shared);
   static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two blocks of an SM");
   cudaError_t e = allow_smem((const void *)sample_kernel<T>, kSmem, kSmem);
   if (e != cudaSuccess) return e;
