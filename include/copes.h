@@ -626,7 +626,7 @@ int copes_sample_tokens(const void *logits, int dtype, int n, int vocab, int64_t
 /* The residual sum after a block with the norms before and after it, for n rows of hidden values of dtype
  * (row i of x at x + i x_row elements, and so on).  With rms(a) = sqrt(mean a^2 + eps):
  *   z = y / rms(y) * out_weight     (y where out_weight is NULL),
- *   s = x + scale * gate * z        (without gate where that is NULL),
+ *   s = x + (scale * gate) * z      (without gate where that is NULL),
  *   sum = round(s),  normed = round(s / rms(s) * weight).
  * s itself, not its rounding, is what is normed; everything between is fp32 (a square past it counts as it
  * should).  y NULL: s is x, and out_weight, gate and sum are NULL.  Otherwise one of sum and normed may be

@@ -91,7 +91,7 @@ struct Shape {
   static constexpr int kFit = 228 * 1024 / (kSmem + 1280);
   // (Three variants spill all the same: fp32 heads of 256 20 bytes of a thread, of 128 with two column
   // tiles 40, of 64 side by side 16.)
-  static constexpr int kByRegs = 65536 / (kThreads * (DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
+  static constexpr int kByRegs = 65536 / (kThreads * (kFp8 ? (DP > 128 || DP * NT > 128 ? 248 : DP * NT > 64 ? 168 : 128) : DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
   static constexpr int kPerSm = kFit < kByRegs ? kFit : kByRegs;
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
 };

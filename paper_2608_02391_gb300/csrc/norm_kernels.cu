@@ -60,6 +60,10 @@ struct Piece {
   }
 };
 
+__device__ __forceinline__ void copy_async(void *to, const void *from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
 // Sums over the threads of a row: `team` of them, a power of two below a warp's 32, or the whole block.
 struct RowSum {
   int team;
@@ -108,8 +112,11 @@ __device__ __forceinline__ Unit unit_of(const Value &value, float eps, int hidde
 }
 
 // A team of threads for each row, kP pieces of kBytes each; a block has blockDim.x / team rows.
+template <int kBytes, int kP>
+constexpr int kMostThreads = kBytes < 16 && kP <= 4 ? 1024 : 512;
 template <typename T, int kBytes, int kP>
-__global__ void __launch_bounds__(512) residual_norm_kernel(NormArgs a, int team) {
+__global__ void __launch_bounds__(kMostThreads<kBytes, kP>, kP <= 2 ? 1024 / kMostThreads<kBytes, kP> : 1)
+    residual_norm_kernel(NormArgs a, int team) {
   using P = Piece<T, kBytes>;
   constexpr int kN = P::kN;
   __shared__ alignas(256) float s_sum[64];
@@ -148,8 +155,7 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(NormArgs a, int team
       for (int e = 0; e < kN; ++e) {
         float z = y[p][e];
         if (a.out_weight) z = z * u.first * u.second * w[e];
-        if (a.gate) z *= gate[p][e];
-        s[p][e] = fmaf(a.scale, z, s[p][e]);
+        s[p][e] = fmaf(a.gate ? a.scale * gate[p][e] : a.scale, z, s[p][e]);
       }
       if (a.sum) P::store((T *)a.sum + row * a.sum_row + at(p), s[p]);
     }
@@ -164,6 +170,83 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(NormArgs a, int team
 #pragma unroll
     for (int e = 0; e < kN; ++e) s[p][e] = s[p][e] * u.first * u.second * w[e];
     P::store((T *)a.normed + row * a.normed_row + at(p), s[p]);
+  }
+}
+
+// The same for more rows than the GPU works on at once: a block takes row after row, and each of its threads has its
+// pieces of the next rows on their way to shared memory, where it alone reads them, so that HBM is not left waiting
+// while a row's sums are formed.  16,384 rows of 4,096 with a norm after the block and a gate for every channel,
+// bf16: see launch_rows.
+constexpr int kStages = 3;
+template <typename T, int kP>
+__global__ void __launch_bounds__(512, 2) residual_norm_rows_kernel(NormArgs a) {
+  using P = Piece<T, 16>;
+  constexpr int kN = P::kN;
+  extern __shared__ __align__(16) uint4 s_rows[];  // [stage][x, y, gate][piece][thread]
+  __shared__ alignas(256) float s_sum[64];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int threads = blockDim.x, mine = threadIdx.x;
+  const bool gates = a.gate && a.gate_row;
+  const int arrays = 2 + gates;
+  RowSum sum{threads, s_sum};
+  const auto at = [&](int p) { return (p * threads + mine) * kN; };
+  const auto slot = [&](int stage, int array, int p) { return s_rows + ((stage * arrays + array) * kP + p) * threads + mine; };
+  const auto ask = [&](int64_t row, int stage) {
+    if (row < a.n)
+#pragma unroll
+      for (int p = 0; p < kP; ++p) {
+        if (at(p) >= a.hidden) continue;
+        copy_async(slot(stage, 0, p), (const T *)a.x + row * a.x_row + at(p));
+        copy_async(slot(stage, 1, p), (const T *)a.y + row * a.y_row + at(p));
+        if (gates) copy_async(slot(stage, 2, p), (const T *)a.gate + row * a.gate_row + at(p));
+      }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  for (int i = 0; i < kStages - 1; ++i) ask(blockIdx.x + (int64_t)i * gridDim.x, i);
+  int stage = 0;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    ask(row + (int64_t)(kStages - 1) * gridDim.x, stage == 0 ? kStages - 1 : stage - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    P y[kP];
+    float s[kP][kN];
+#pragma unroll
+    for (int p = 0; p < kP; ++p) {
+      y[p].clear();
+      if (at(p) < a.hidden) y[p].load((const T *)slot(stage, 1, p));
+    }
+    Unit u{1.0f, 1.0f};
+    if (a.out_weight) u = unit_of<kP, kN>([&](int p, int e) { return y[p][e]; }, a.eps, a.hidden, sum);
+#pragma unroll
+    for (int p = 0; p < kP; ++p) {
+#pragma unroll
+      for (int e = 0; e < kN; ++e) s[p][e] = 0.0f;
+      if (at(p) >= a.hidden) continue;
+      P x, w, gate;
+      x.load((const T *)slot(stage, 0, p));
+      if (a.out_weight) w.load((const T *)a.out_weight + at(p));
+      if (a.gate) gate.load(gates ? (const T *)slot(stage, 2, p) : (const T *)a.gate + at(p));
+#pragma unroll
+      for (int e = 0; e < kN; ++e) {
+        float z = y[p][e];
+        if (a.out_weight) z = z * u.first * u.second * w[e];
+        s[p][e] = fmaf(a.gate ? a.scale * gate[e] : a.scale, z, x[e]);
+      }
+      if (a.sum) P::store((T *)a.sum + row * a.sum_row + at(p), s[p]);
+    }
+    if (a.normed) {
+      const Unit v = unit_of<kP, kN>([&](int p, int e) { return s[p][e]; }, a.eps, a.hidden, sum);
+#pragma unroll
+      for (int p = 0; p < kP; ++p) {
+        if (at(p) >= a.hidden) continue;
+        P w;
+        w.load((const T *)a.weight + at(p));
+#pragma unroll
+        for (int e = 0; e < kN; ++e) s[p][e] = s[p][e] * v.first * v.second * w[e];
+        P::store((T *)a.normed + row * a.normed_row + at(p), s[p]);
+      }
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
   }
 }
 
@@ -215,13 +298,9 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < kN; ++e) v[e] = v[e] * u.first * u.second * w[e];
     }
-    if (a.gate) {
-      w.load((const T *)a.gate + row * a.gate_row + at);
+    if (a.gate) w.load((const T *)a.gate + row * a.gate_row + at);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) v[e] *= w[e];
-    }
-#pragma unroll
-    for (int e = 0; e < kN; ++e) v[e] = fmaf(a.scale, v[e], x[e]);
+    for (int e = 0; e < kN; ++e) v[e] = fmaf(a.gate ? a.scale * w[e] : a.scale, v[e], x[e]);
   };
   Unit whole{1.0f, 1.0f};
   if (a.normed) whole = unit(total);
@@ -241,7 +320,7 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
 namespace {
 
 template <typename... Params, typename... Args>
-cudaError_t launch_after(unsigned blocks, unsigned threads, cudaStream_t s, void (*kernel)(Params...), Args... args) {
+cudaError_t launch_after(unsigned blocks, unsigned threads, int smem, cudaStream_t s, void (*kernel)(Params...), Args... args) {
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -251,7 +330,20 @@ cudaError_t launch_after(unsigned blocks, unsigned threads, cudaStream_t s, void
   cfg.stream = s;
   cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Row after row where blocks take four at least.
+template <typename T>
+bool launch_rows(const NormArgs &a, int pieces, cudaStream_t s, cudaError_t *e) {
+  constexpr int kP = 2, kMost = kStages * 3 * kP * 512 * 16;
+  const int threads = ((pieces - 1) / kP / 32 + 1) * 32, smem = kStages * (2 + (a.gate && a.gate_row)) * kP * threads * 16;
+  const int by_smem = 228 * 1024 / (smem + 1280), by_threads = 1024 / threads, blocks = 152 * (by_smem < by_threads ? by_smem : by_threads);
+  if (!a.y || pieces <= 128 || pieces > kP * 512 || a.n < 4 * blocks) return false;
+  *e = allow_smem((const void *)residual_norm_rows_kernel<T, kP>, smem + (int)sizeof(float) * 64, kMost);
+  if (*e == cudaSuccess) *e = launch_after(blocks, threads, smem, s, residual_norm_rows_kernel<T, kP>, a);
+  return true;
 }
 
 // kP pieces for each thread of a team: a part of a warp or a warp of a block of 256, or a block.
@@ -261,7 +353,7 @@ cudaError_t launch(const NormArgs &a, int pieces, cudaStream_t s) {
   while (team < 32 && team * kP < pieces) team <<= 1;
   if (team * kP < pieces) team = ((pieces - 1) / kP / 32 + 1) * 32;
   const int threads = team <= 32 ? 256 : team, rows = threads / team;
-  return launch_after((unsigned)((a.n - 1) / rows + 1), threads, s, residual_norm_kernel<T, kBytes, kP>, a, team);
+  return launch_after((unsigned)((a.n - 1) / rows + 1), threads, 0, s, residual_norm_kernel<T, kBytes, kP>, a, team);
 }
 
 template <typename T, int kBytes>
@@ -269,11 +361,15 @@ cudaError_t by_width(const NormArgs &a, cudaStream_t s) {
   constexpr int kN = kBytes / (int)sizeof(T);
   const int pieces = (a.hidden - 1) / kN + 1;
   if (pieces <= 32) return launch<T, kBytes, 1>(a, pieces, s);
+  if constexpr (kBytes == 16) {
+    cudaError_t e;
+    if (launch_rows<T>(a, pieces, s, &e)) return e;
+  }
   if (pieces <= 2 * 512) return launch<T, kBytes, 2>(a, pieces, s);
-  if (pieces <= 4 * 512) return launch<T, kBytes, 4>(a, pieces, s);
+  if (pieces <= 4 * kMostThreads<kBytes, 4>) return launch<T, kBytes, 4>(a, pieces, s);
   if constexpr (kBytes < 16)
     if (pieces <= 16 * 512) return launch<T, kBytes, 16>(a, pieces, s);
-  return launch_after((unsigned)a.n, 1024, s, residual_norm_long_kernel<T, kBytes>, a);
+  return launch_after((unsigned)a.n, 1024, 0, s, residual_norm_long_kernel<T, kBytes>, a);
 }
 
 }  // namespace

@@ -43,19 +43,31 @@ def check_norm(got_s, got_h, x, weight, y, out_weight, gate, scale, eps):
     squares (h / 1024 in rows that are read again), then over threads 10 and up to 32 warps: (74 + h / 1024) 2^-24 of
     itself at most, of which a root has half; the root's reciprocal and the division add 2^-22.  z has three more
     roundings, s one of its two terms and one of itself; what s is off by moves its norm by as much, and its
-    rms by the 2-norm of that."""
+    rms by the 2-norm of that.  An s past the largest number of its type is infinite there (or not, within 2^-7 of
+    it), and one past fp32 makes its norm NaN and the rest of its row's 0."""
     u = 2.0**-8 if x.dtype == torch.bfloat16 else 2.0**-24
     d = lambda t: None if t is None else f64(t)
     s, h = model.norm(d(x), d(weight), d(y), d(out_weight), d(gate), scale, eps)
     root = (74 + x.shape[1] / 1024) * 2.0**-25 + 2.0**-22
     off = 0.0 if y is None else np.abs(s - d(x)) * (root + 2.0**-22) + 2.0**-24 * (np.abs(s) + np.abs(d(x)))
+    size, most = np.abs(s), torch.finfo(torch.float32).max
+    near = np.abs(size / most - 1) <= 2.0**-7
+    past = (size > most) & ~near
     if got_s is not None and y is not None:
-        assert (np.abs(f64(got_s) - s) <= 1.01 * u * np.abs(s) + off + 1e-38).all()
+        got = f64(got_s)
+        assert np.array_equal(got[past], np.copysign(np.inf, s[past]))
+        with np.errstate(invalid="ignore"):
+            assert (near | past | (np.abs(got - s) <= 1.01 * u * size + off + 1e-38)).all()
     if got_h is not None:
+        got = f64(got_h)
+        rows = past.any(1)
+        assert np.isnan(got[past]).all() and not got[rows][~past[rows] & ~near[rows]].any()
+        rows |= near.any(1)
         rms = np.sqrt((s * s).mean(1, keepdims=True) + eps)
         moved = np.sqrt((np.square(off) * np.ones_like(s)).mean(1, keepdims=True)) / rms
         tol = np.abs(h) * (1.01 * u + root + 2.0**-22 + moved) + off / rms * np.abs(d(weight)) + 1e-38
-        assert (np.abs(f64(got_h) - h) <= tol).all(), (np.abs(f64(got_h) - h) / tol).max()
+        with np.errstate(invalid="ignore"):
+            assert (rows[:, None] | (np.abs(got - h) <= tol)).all(), (np.abs(got - h) / tol)[~rows].max()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -118,6 +130,30 @@ def test_norms_of_extreme_rows(copes, hidden, dtype):
     rest = h[6].clone()
     rest[hidden // 2] = 0
     assert not rest.any() and torch.isfinite(h[[i for i in range(n) if i not in (6, 7)]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,hidden", [(6100, 1032), (2600, 2560), (1900, 4096), (1250, 8192)])
+def test_norms_of_many_rows(copes, n, hidden, dtype):
+    """More rows than the GPU works on at once, among them ones whose squares are past fp32, in place too."""
+    g = torch.Generator("cuda").manual_seed(n)
+    rand = lambda *shape: torch.randn(*shape, device="cuda", generator=g)
+    w, ow = (rand(hidden) * 0.2 + 1).to(DT[dtype]), (rand(hidden) * 0.2 + 1).to(DT[dtype])
+    x, y, gate = (rand(n, hidden + 16).to(DT[dtype])[:, 8:8 + hidden] for _ in range(3))
+    x[n // 2] = 2e38
+    y[n - 3] = 3e38
+    for args in (dict(out_weight=ow), dict(gate=gate[0].contiguous(), scale=0.7), dict(out_weight=ow, gate=gate, scale=-0.3)):
+        full = {**dict(out_weight=None, gate=None, scale=1.0), **args}
+        s, h = copes.residual_norm(x, w, y=y, eps=1e-6, **args)
+        rows = torch.tensor(sorted({0, 1, 607, 608, 1216, n // 2, n - 3, n - 1} & set(range(n))) + list(range(5, n, 97)), device="cuda")
+        token = full["gate"] if full["gate"] is None or full["gate"].dim() == 1 else full["gate"][rows]
+        check_norm(s[rows], h[rows], x[rows], w, y[rows], full["out_weight"], token, full["scale"], 1e-6)
+        x2, y2 = x.clone(), y.clone()
+        copes.residual_norm(x2, w, y=y2, eps=1e-6, out=x2, normed=y2, **args)
+        bits = lambda t: t.contiguous().view(torch.int16)  # NaN among them
+        assert torch.equal(bits(x2), bits(s)) and torch.equal(bits(y2), bits(h))
+        only, none = copes.residual_norm(x, None, y=y, eps=1e-6, **args)
+        assert none is None and torch.equal(bits(only), bits(s))
 
 
 def test_norms_of_no_rows_and_of_rows_past_32_bits(copes):
