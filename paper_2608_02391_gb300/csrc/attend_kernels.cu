@@ -79,9 +79,10 @@ struct Shape {
   static constexpr int kStages = 2;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kTeam = kBeside ? 1 : kWarps, kSides = kWarps / kTeam;  // warps on a head, heads
-  static constexpr int kTile = kTeam * 16;                // tokens
+  static constexpr int kOwn = kFp8 && DP <= 128 ? 32 : 16;  // tokens of a warp
+  static constexpr int kTile = kTeam * kOwn;
   static constexpr int kChunks = DP * (int)sizeof(T) / 16;  // 16-byte pieces of a token's row
-  static constexpr int kPart = 16 * kChunks * 16;         // a warp's keys (or values) of a tile, bytes
+  static constexpr int kPart = kOwn * kChunks * 16;       // a warp's keys (or values) of a tile, bytes
   static constexpr int kStage = 2 * kPart * kWarps;
   static constexpr int kHeads = 8 * NT;                   // query heads of a block at a time
   static constexpr int kRow = DP + 4;                     // row of s_o: heads 2j begin 8 banks apart
@@ -91,7 +92,7 @@ struct Shape {
   static constexpr int kFit = 228 * 1024 / (kSmem + 1280);
   // (Three variants spill all the same: fp32 heads of 256 20 bytes of a thread, of 128 with two column
   // tiles 40, of 64 side by side 16.)
-  static constexpr int kByRegs = 65536 / (kThreads * (kFp8 ? (DP > 128 || DP * NT > 128 ? 248 : DP * NT > 64 ? 168 : 128) : DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
+  static constexpr int kByRegs = 65536 / (kThreads * (kFp8 ? (DP * NT > 64 ? 248 : 168) : DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
   static constexpr int kPerSm = kFit < kByRegs ? kFit : kByRegs;
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
 };
@@ -380,43 +381,14 @@ __device__ __forceinline__ void to_units(Queries<S> &q) {
 }
 
 // One warp's 16 tokens: scores, the running maximum and sum, and the weighted values.
-// `left`: how many of the 16 are tokens.  8 bits: `power` is 127 more than the exponent of the key, or in the upper
-// half of the warp of the value, of token lane % 16.
+// `left`: how many of the 16 are tokens.
 template <typename S>
 __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int left, float scale, const Queries<S> &q,
-                                          Running<S> &r, uint32_t power) {
+                                          Running<S> &r) {
   constexpr int NT = S::NT, KS = S::DP / 16, kPitch = S::kChunks * 16;
   const int lane = threadIdx.x & 31;
   float s[NT][4];
-  if constexpr (S::kFp8) {
-    float part[NT][2][4] = {};
-    const int row = lane >> 2;
-    const uint32_t at = keys + row_at<S>(row) * kPitch;
-    const int x = swizzle<S>(row);
-#pragma unroll
-    for (int g = 0; g < KS / 4; ++g) {
-      const uint32_t off = (uint32_t)(((g * 4 + (lane & 3)) ^ x) * 16);
-      uint32_t u[4], v[4];
-      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(at + off) : "memory");
-      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                   : "r"(at + off + 8 * kPitch) : "memory");
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t a[4];
-        codes_to_f16(u[w], a[0], a[2]);
-        codes_to_f16(v[w], a[1], a[3]);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) mma_f16(part[j][w & 1], a, q.b[g * 4 + w][j][0], q.b[g * 4 + w][j][1]);
-      }
-    }
-    const float first = __uint_as_float(__shfl_sync(kAll, power, row) << 23);
-    const float second = __uint_as_float(__shfl_sync(kAll, power, row + 8) << 23);
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s[j][e] = (part[j][0][e] + part[j][1][e]) * q.unit[j][e & 1] * (e < 2 ? first : second);
-  } else if constexpr (S::kFp32) {
+  if constexpr (S::kFp32) {
     constexpr int kSums = NT == 1 ? 2 : 1;  // one for each of the two products of a piece, registers permitting
     float part[NT][kSums][3][4] = {};
     const int row = lane >> 2;
@@ -496,70 +468,7 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
         for (int e = 0; e < 4; ++e) r.o[i][j][e] *= keep[j][e & 1];
   }
 
-  if constexpr (S::kFp8) {
-    // The weights times their values' powers of two, in units that bring the tile's largest of a head into
-    // [2^14, 2^15), in two fp16 terms: 2^-22 of one, or 2^-39 of the largest, lost.
-    const float first = __uint_as_float(__shfl_sync(kAll, power, 16 + (lane >> 2)) << 23);
-    const float second = __uint_as_float(__shfl_sync(kAll, power, 24 + (lane >> 2)) << 23);
-    uint32_t p[NT][2], rest[NT][2];
-    float unit[NT][2];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      uint32_t most = 0;  // two exponents
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        s[j][e] *= first;
-        s[j][2 + e] *= second;
-        most |= max(__float_as_uint(s[j][e]) >> 23, __float_as_uint(s[j][2 + e]) >> 23) << 16 * e;
-      }
-      most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 4));
-      most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 8));
-      most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 16));
-      float over[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t up = min(268u - (most >> 16 * e & 0xFFu), 253u);
-        over[e] = __uint_as_float(up << 23);
-        unit[j][e] = __uint_as_float((254u - up) << 23);
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float u = s[j][2 * e] * over[0], v = s[j][2 * e + 1] * over[1];
-        const uint32_t hi = pack_f16(u, v);
-        const float2 held = unpack_f16(hi);
-        p[j][e] = transpose8(hi);
-        rest[j][e] = transpose8(pack_f16(u - held.x, v - held.y));
-      }
-    }
-    const int row = (lane & 3) * 2, x = swizzle<S>(row), y = swizzle<S>(row + 1);
-#pragma unroll
-    for (int g = 0; g < KS / 4; ++g) {
-      const int piece = g * 4 + (lane >> 3), half = (lane >> 2 & 1) * 8;  // d = 64 g + 8 (lane / 4) + 0 .. 7
-      const uint32_t at = values + row_at<S>(row) * kPitch + (piece ^ x) * 16 + half;
-      const uint32_t next = values + row_at<S>(row + 1) * kPitch + (piece ^ y) * 16 + half;
-      uint32_t u[2][2], v[2][2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[e][0]), "=r"(u[e][1]) : "r"(at + e * 8 * kPitch) : "memory");
-        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v[e][0]), "=r"(v[e][1]) : "r"(next + e * 8 * kPitch) : "memory");
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {  // d + 2 i and d + 2 i + 1
-        const unsigned pick = i & 1 ? 0x7362 : 0x5140;
-        uint32_t a[4];
-        codes_to_f16(__byte_perm(u[0][i / 2], v[0][i / 2], pick), a[0], a[1]);
-        codes_to_f16(__byte_perm(u[1][i / 2], v[1][i / 2], pick), a[2], a[3]);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          float sum[4] = {};  // of the tile
-          mma_f16(sum, a, rest[j][0], rest[j][1]);
-          mma_f16(sum, a, p[j][0], p[j][1]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) r.o[g * 4 + i][j][e] = fmaf(unit[j][e & 1], sum[e], r.o[g * 4 + i][j][e]);
-        }
-      }
-    }
-  } else if constexpr (S::kFp32) {
+  if constexpr (S::kFp32) {
     // P^T: 8 tokens x 8 heads at a time, in 16-bit halves.  A lane then has tokens 2j and 2j + 1
     // (j = lane % 4) as the k of one product: its values are read from those rows.
     uint32_t p[NT][2][2];
@@ -625,6 +534,151 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
 #pragma unroll
         for (int e = 0; e < 4; ++e) r.o[i][j][e] += sum[e];
       }
+    }
+  }
+}
+
+// The same in 8 bits, of kOwn tokens: 32, as many bytes as 16 in 16 (with 16 of 128 components, 128 rows of up to 16,384
+// took 433 us, and 408 so), or 16 of 256.  `power`: 127 more than the exponents of the key and, in the next byte,
+// the value of token lane % kOwn.
+// Codes become fp16 on their way from shared memory to the matrix unit, exactly; what they are to be multiplied
+// by multiplies scores and weights instead.  Which d a lane's share of a product stands for is free, if it is the
+// same for both factors: lanes take whole pieces of 16 bytes of keys, and of values 8 bytes of two tokens at a time.
+template <typename S>
+__device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int left, float scale, const Queries<S> &q,
+                                           Running<S> &r, uint32_t power) {
+  constexpr int NT = S::NT, KS = S::DP / 16, kPitch = S::kChunks * 16, kHalves = S::kOwn / 16, kOf = 2 * kHalves;
+  const int lane = threadIdx.x & 31, row = lane >> 2;
+  float s[NT][2 * kOf];  // tokens lane / 4 + 8 (e / 2), heads 2 (lane % 4) + e % 2
+#pragma unroll
+  for (int half = 0; half < kHalves; ++half) {
+    float part[NT][2][4] = {};
+    const uint32_t at = keys + (half * 16 + row_at<S>(row)) * kPitch;
+    const int x = swizzle<S>(row);
+#pragma unroll
+    for (int g = 0; g < KS / 4; ++g) {
+      const uint32_t off = (uint32_t)(((g * 4 + (lane & 3)) ^ x) * 16);
+      uint32_t u[4], v[4];
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(at + off) : "memory");
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                   : "r"(at + off + 8 * kPitch) : "memory");
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t a[4];
+        codes_to_f16(u[w], a[0], a[2]);
+        codes_to_f16(v[w], a[1], a[3]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mma_f16(part[j][w & 1], a, q.b[g * 4 + w][j][0], q.b[g * 4 + w][j][1]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][half * 4 + e] = part[j][0][e] + part[j][1][e];
+  }
+
+  float key_unit[kOf], value_unit[kOf];  // of the lane's tokens
+#pragma unroll
+  for (int e = 0; e < kOf; ++e) {
+    const uint32_t both = __shfl_sync(kAll, power, row + 8 * e);
+    key_unit[e] = __uint_as_float((both & 0xFFu) << 23);
+    value_unit[e] = __uint_as_float((both >> 8) << 23);
+  }
+  bool grown = false;
+  float keep[NT][2], over[NT][2], unit[NT][2];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    uint32_t most = 0;  // the exponents of the two heads' largest weighted units
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < kOf; ++t) {
+        s[j][2 * t + e] = row + 8 * t < left ? s[j][2 * t + e] * q.unit[j][e] * key_unit[t] * scale : -INFINITY;
+        top = fmaxf(top, s[j][2 * t + e]);
+      }
+      top = fmaxf(top, __shfl_xor_sync(kAll, top, 4));
+      top = fmaxf(top, __shfl_xor_sync(kAll, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(kAll, top, 16));
+      const float m = fmaxf(r.m[j][e], top);
+      keep[j][e] = m == r.m[j][e] ? 1.0f : exp2_fast(r.m[j][e] - m);
+      grown |= m != r.m[j][e];
+      r.m[j][e] = m;
+      const float base = m == -INFINITY ? 0.0f : m;
+      float sum = 0.0f, largest = 0.0f;
+#pragma unroll
+      for (int t = 0; t < kOf; ++t) {
+        const float p = exp2_fast(s[j][2 * t + e] - base);
+        sum += p;
+        s[j][2 * t + e] = p * value_unit[t];
+        largest = fmaxf(largest, s[j][2 * t + e]);
+      }
+      r.l[j][e] = r.l[j][e] * keep[j][e] + sum;
+      most |= __float_as_uint(largest) >> 23 << 16 * e;
+    }
+    // The weights times their values' powers of two, in units that bring the tile's largest of a head into
+    // [2^14, 2^15), in two fp16 terms: 2^-22 of one, or 2^-39 of the largest, lost.
+    most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 4));
+    most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 8));
+    most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 16));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t up = min(268u - (most >> 16 * e & 0xFFu), 253u);
+      over[j][e] = __uint_as_float(up << 23);
+      unit[j][e] = __uint_as_float((254u - up) << 23);
+    }
+  }
+  if (__any_sync(kAll, grown)) {
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.o[i][j][e] *= keep[j][e & 1];
+  }
+  uint32_t p[NT][kOf], rest[NT][kOf];  // of 8 tokens each
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int t = 0; t < kOf; ++t) {
+      const float u = s[j][2 * t] * over[j][0], v = s[j][2 * t + 1] * over[j][1];
+      const uint32_t hi = pack_f16(u, v);
+      const float2 held = unpack_f16(hi);
+      p[j][t] = transpose8(hi);
+      rest[j][t] = transpose8(pack_f16(u - held.x, v - held.y));
+    }
+
+  const int even = (lane & 3) * 2, x = swizzle<S>(even), y = swizzle<S>(even + 1);
+#pragma unroll
+  for (int g = 0; g < KS / 4; ++g) {
+    const int piece = g * 4 + (lane >> 3), low = (lane >> 2 & 1) * 8;  // d = 64 g + 8 (lane / 4) + 0 .. 7
+    const uint32_t at = values + row_at<S>(even) * kPitch + (piece ^ x) * 16 + low;
+    const uint32_t next = values + row_at<S>(even + 1) * kPitch + (piece ^ y) * 16 + low;
+    uint32_t u[kOf][2], v[kOf][2];
+#pragma unroll
+    for (int t = 0; t < kOf; ++t) {
+      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[t][0]), "=r"(u[t][1]) : "r"(at + t * 8 * kPitch) : "memory");
+      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v[t][0]), "=r"(v[t][1]) : "r"(next + t * 8 * kPitch) : "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // d + 2 i and d + 2 i + 1
+      const unsigned pick = i & 1 ? 0x7362 : 0x5140;
+      float sum[NT][4] = {};  // of the tile
+#pragma unroll
+      for (int half = 0; half < kHalves; ++half) {
+        uint32_t a[4];
+        codes_to_f16(__byte_perm(u[2 * half][i / 2], v[2 * half][i / 2], pick), a[0], a[1]);
+        codes_to_f16(__byte_perm(u[2 * half + 1][i / 2], v[2 * half + 1][i / 2], pick), a[2], a[3]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          mma_f16(sum[j], a, rest[j][2 * half], rest[j][2 * half + 1]);
+          mma_f16(sum[j], a, p[j][2 * half], p[j][2 * half + 1]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.o[g * 4 + i][j][e] = fmaf(unit[j][e & 1], sum[j][e], r.o[g * 4 + i][j][e]);
     }
   }
 }
@@ -787,7 +841,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   const uint64_t head_bytes = (uint64_t)c.head_elems * sizeof(T), to_values = c.n_kv_heads * head_bytes;
   const char *pool = c.pool + a.layer * c.layer_bytes + side * head_bytes;
 
-  // Where token (16 member + lane % 16) of a tile is: its page (-1 for none, -2 for one outside the
+  // Where token (kOwn member + lane % kOwn) of a tile is: its page (-1 for none, -2 for one outside the
   // pool), its place there and the tile's key-value head.  Tables are read two tiles ahead of the
   // tile that is asked for, so that nothing waits for them.
   struct Place {
@@ -797,7 +851,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   const auto look_up = [&]() {
     Place p{-1, 0, ahead.kv};
     if (looked == count) return p;
-    const int t = ahead.tile * TILE + member * 16 + (lane & 15);
+    const int t = ahead.tile * TILE + member * S::kOwn + (lane & (S::kOwn - 1));
     if (ahead.tile < ahead.tiles && t < ahead.tokens) {
       const int at_page = by_page.quotient(t);
       p.place = t - at_page * c.page_size;
@@ -813,14 +867,16 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     const char *from = nullptr;
     if (p.page >= 0) from = pool + (uint64_t)p.page * c.page_bytes + p.kv * S::kSides * head_bytes + (uint64_t)p.place * D * sizeof(T);
     else if (p.page == -2) flag_error(kErrCacheId);
-    uint32_t power = 127;
+    uint32_t power = 0x7F7F;
     if constexpr (S::kFp8)
-      if (from)
-        power = *reinterpret_cast<const uint8_t *>(c.pool + (uint64_t)p.page * c.page_bytes + a.layer * c.layer_bytes + c.layer_elems +
-                                                   (uint64_t)(((lane >> 4) * c.n_kv_heads + p.kv * S::kSides + side) * c.page_size + p.place));
+      if (from) {
+        const uint8_t *at = reinterpret_cast<const uint8_t *>(c.pool + (uint64_t)p.page * c.page_bytes + a.layer * c.layer_bytes + c.layer_elems +
+                                                              (uint64_t)((p.kv * S::kSides + side) * c.page_size + p.place));
+        power = at[0] | (uint32_t)at[(uint64_t)c.n_kv_heads * c.page_size] << 8;
+      }
     const uint32_t to = stages + stage * S::kStage;
 #pragma unroll
-    for (int i = 0; i < S::kChunks / 2; ++i) {
+    for (int i = 0; i < S::kChunks * S::kOwn / 32; ++i) {
       const int row = (i * 32 + lane) / S::kChunks, piece = (i * 32 + lane) % S::kChunks;
       const char *src = reinterpret_cast<const char *>(__shfl_sync(kAll, (unsigned long long)from, row));
       const int bytes = src && piece * 16 < D * (int)sizeof(T) ? 16 : 0;  // 0: zeros
@@ -881,9 +937,12 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     asm volatile("cp.async.commit_group;" ::: "memory");
     asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
     __syncwarp();
-    const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - member * 16 : 0;
+    const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - member * S::kOwn : 0;
     const uint32_t tile = stages + j % S::kStages * S::kStage;
-    if (left > 0) warp_tile<S>(tile, tile + S::kPart, left, scale, q, r, powers[0]);
+    if (left > 0) {
+      if constexpr (S::kFp8) warp_tile8<S>(tile, tile + S::kPart, left, scale, q, r, powers[0]);
+      else warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
+    }
 #pragma unroll
     for (int s = 0; s + 1 < S::kStages; ++s) powers[s] = powers[s + 1];
     __syncwarp();

@@ -379,81 +379,121 @@ struct Rows {
   int64_t row, head;
 };
 
-// 8 bits: a team of lanes, a power of two of at least head_dim / 8, per (row, key-value head, key or value), 8 values
-// each.  The row's unit is the power of two that brings its largest finite value into (224, 448]; as codes are
+// 8 bits.  A team of lanes, a power of two of at least head_dim / 8, for each (row, key or value, key-value head), 8
+// values a lane.  The row's unit is the power of two that brings its largest finite value into (224, 448]; as codes are
 // floats, a power of two costs no precision that a finer factor would keep.  `wide`: all rows are 16-byte aligned.
+//
+// Where a row's token is takes a chain of three loads, so a block looks up its kRows rows first, all at once, and
+// each thread then has kJobs pieces on their way.  Bound by HBM: 32,000 tokens of 8 heads of 128 are written in 33 us
+// and read back in 33 (looked up by each team, with a piece of a thread on its way: 87 each).
+constexpr int kCodeThreads = 256, kJobs = 4;
+struct Place {
+  int page, place;  // page -1: no token
+};
 template <bool kWrite>
-__global__ void __launch_bounds__(256) codes_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position, int n,
-                                                    Rows k, Rows v, int team, bool wide) {
+__global__ void __launch_bounds__(kCodeThreads) codes_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position, int n,
+                                                             Rows k, Rows v, int team, int rows, bool wide) {
+  __shared__ Place s_place[kCodeThreads];
   after_the_last();
-  const int64_t job = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / team;
-  const int d = (int)(threadIdx.x & (team - 1)) * 8;
-  const bool there = job < (int64_t)n * c.n_kv_heads * 2;
-  const int h = (int)(job % c.n_kv_heads), which = (int)(job / c.n_kv_heads & 1), i = (int)(job / c.n_kv_heads / 2);
-  int page = 0, place = 0;
-  bool token = there && find_token(c, slots, position, i, page, place);
-  if (there && !token && d == 0) flag_error(kErrCacheId);
-  const bool mine = there && d < c.head_dim;
-  const Rows &rows = which ? v : k;
-  uint16_t *outside = mine ? rows.at + i * rows.row + h * rows.head + d : nullptr;
-  char *base = c.pool + (uint64_t)page * c.page_bytes + layer * c.layer_bytes;
-  const int head = which * c.n_kv_heads + h;
-  uint2 *codes = reinterpret_cast<uint2 *>(base + (uint64_t)head * c.head_elems + (uint64_t)place * c.head_dim + d);
-  uint8_t *power = reinterpret_cast<uint8_t *>(base + c.layer_elems + (uint64_t)head * c.page_size + place);
-  uint32_t w[4] = {};  // 8 values of bf16
-  if constexpr (kWrite) {
-    if (mine && token) {
-      if (wide) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(outside);
-        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+  const int row0 = blockIdx.x * rows, here = min(rows, n - row0);
+  for (int r = threadIdx.x; r < here; r += kCodeThreads) {
+    Place p{-1, 0};
+    if (!find_token(c, slots, position, row0 + r, p.page, p.place)) {
+      p.page = -1;
+      flag_error(kErrCacheId);
+    }
+    s_place[r] = p;
+  }
+  __syncthreads();
+  const int d = (int)(threadIdx.x & (team - 1)) * 8, teams = kCodeThreads / team, heads = 2 * c.n_kv_heads;
+  const int64_t jobs = (int64_t)here * heads;
+  for (int64_t first = threadIdx.x / team; first - (int)(threadIdx.x / team) < jobs; first += (int64_t)teams * kJobs) {
+    uint32_t w[kJobs][4];  // 8 values of bf16
+    uint16_t *outside[kJobs];
+    uint2 *codes[kJobs];
+    uint8_t *power[kJobs];
+    uint2 held[kJobs];
+    uint32_t held_power[kJobs];
+#pragma unroll
+    for (int u = 0; u < kJobs; ++u) {
+      const int64_t job = first + (int64_t)u * teams;
+      const int head = (int)(job % heads), r = (int)(job / heads), which = head >= c.n_kv_heads, h = head - which * c.n_kv_heads;
+      outside[u] = nullptr;
+      codes[u] = nullptr;
+      if (job < jobs && d < c.head_dim) {
+        const Rows &to = which ? v : k;
+        outside[u] = to.at + (row0 + r) * to.row + h * to.head + d;
+        if (s_place[r].page >= 0) {
+          char *base = c.pool + (uint64_t)s_place[r].page * c.page_bytes + layer * c.layer_bytes;
+          codes[u] = reinterpret_cast<uint2 *>(base + (uint64_t)head * c.head_elems + (uint64_t)s_place[r].place * c.head_dim + d);
+          power[u] = reinterpret_cast<uint8_t *>(base + c.layer_elems + (uint64_t)head * c.page_size + s_place[r].place);
+        }
+      }
+      if constexpr (kWrite) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[u][e] = 0;
+        if (codes[u] && wide) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(outside[u]);
+          w[u][0] = x.x, w[u][1] = x.y, w[u][2] = x.z, w[u][3] = x.w;
+        } else if (codes[u]) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[u][e] = outside[u][2 * e] | (uint32_t)outside[u][2 * e + 1] << 16;
+        }
       } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = outside[2 * e] | (uint32_t)outside[2 * e + 1] << 16;
+        held[u] = make_uint2(0, 0);
+        held_power[u] = 127;
+        if (codes[u]) {
+          held[u] = *codes[u];
+          held_power[u] = *power[u];
+        }
       }
     }
-    uint32_t most = 0;  // as bits of bf16
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t x = w[e / 2] >> 16 * (e & 1) & 0x7FFFu;
-      if (x < 0x7F80u) most = max(most, x);
-    }
-    for (int s = team >> 1; s; s >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
-    // 127 more than the exponent e: 448 is 1.75 2^8
-    const int biased = max((int)(most >> 7) - 8 + ((most & 0x7Fu) > 0x60u), 1);
-    const float over = __uint_as_float((uint32_t)(254 - biased) << 23);
-    if (!mine || !token) return;
-    uint32_t pair[4];
+    for (int u = 0; u < kJobs; ++u) {
+      if constexpr (kWrite) {
+        uint32_t most = 0;  // as bits of bf16
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float lo = __uint_as_float(w[e] << 16) * over, hi = __uint_as_float(w[e] & 0xFFFF0000u) * over;
-      if (isinf(lo)) lo = NAN;  // the type has no infinity
-      if (isinf(hi)) hi = NAN;
-      uint16_t two;
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
-      pair[e] = two;
-    }
-    *codes = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
-    if (d == 0) *power = (uint8_t)biased;
-  } else {
-    if (!mine) return;
-    if (token) {
-      const uint2 x = *codes;
-      const float unit = __uint_as_float((uint32_t)*power << 23);
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t x = w[u][e / 2] >> 16 * (e & 1) & 0x7FFFu;
+          if (x < 0x7F80u) most = max(most, x);
+        }
+        for (int s = team >> 1; s; s >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
+        // 127 more than the exponent e: 448 is 1.75 2^8
+        const int biased = max((int)(most >> 7) - 8 + ((most & 0x7Fu) > 0x60u), 1);
+        const float over = __uint_as_float((uint32_t)(254 - biased) << 23);
+        if (!codes[u]) continue;
+        uint32_t pair[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint16_t two = (uint16_t)((e < 2 ? x.x : x.y) >> 16 * (e & 1));
-        uint32_t both;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(both) : "h"(two));
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&both));
-        const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * unit, f.y * unit);
-        w[e] = *reinterpret_cast<const uint32_t *>(&b);
+        for (int e = 0; e < 4; ++e) {
+          float lo = __uint_as_float(w[u][e] << 16) * over, hi = __uint_as_float(w[u][e] & 0xFFFF0000u) * over;
+          if (isinf(lo)) lo = NAN;  // the type has no infinity
+          if (isinf(hi)) hi = NAN;
+          uint16_t two;
+          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
+          pair[e] = two;
+        }
+        *codes[u] = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
+        if (d == 0) *power[u] = (uint8_t)biased;
+      } else {
+        if (!outside[u]) continue;
+        const float unit = __uint_as_float(held_power[u] << 23);
+        uint32_t out[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint16_t two = (uint16_t)((e < 2 ? held[u].x : held[u].y) >> 16 * (e & 1));
+          uint32_t both;
+          asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(both) : "h"(two));
+          const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&both));
+          const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * unit, f.y * unit);
+          out[e] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        if (wide) {
+          *reinterpret_cast<uint4 *>(outside[u]) = make_uint4(out[0], out[1], out[2], out[3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) outside[u][e] = (uint16_t)(out[e / 2] >> 16 * (e & 1));
+        }
       }
-    }
-    if (wide) {
-      *reinterpret_cast<uint4 *>(outside) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) outside[e] = (uint16_t)(w[e / 2] >> 16 * (e & 1));
     }
   }
 }
@@ -543,8 +583,12 @@ static cudaError_t launch_codes(const Cache &c, int layer, const int32_t *slots,
   while (team * 8 < c.head_dim) team *= 2;
   uintptr_t all = 0;
   for (const Rows &r : {k, v}) all |= (uintptr_t)r.at | (uintptr_t)r.row * 2 | (uintptr_t)r.head * 2;
-  const unsigned blocks = (unsigned)(((int64_t)n * c.n_kv_heads * 2 * team + 255) / 256);
-  return launch_after(blocks, 256, s, codes_kernel<kWrite>, c, layer, slots, position, n, k, v, team, all % 16 == 0);
+  // rows of a block: kJobs pieces for each thread twice over, or fewer where that leaves SMs without a block
+  const int64_t a_row = 2 * (int64_t)c.n_kv_heads * team;
+  const int64_t most = n / (152 * 4), fit = 2 * kJobs * kCodeThreads / a_row;
+  const int64_t rows = most < 1 || fit < 1 ? 1 : most < fit ? most : fit;
+  const unsigned blocks = (unsigned)((n - 1) / rows + 1);
+  return launch_after(blocks, kCodeThreads, s, codes_kernel<kWrite>, c, layer, slots, position, n, k, v, team, (int)rows, all % 16 == 0);
 }
 
 cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n,
