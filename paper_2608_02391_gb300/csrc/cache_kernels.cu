@@ -387,8 +387,8 @@ struct Rows {
 // each thread then has kJobs pieces on their way.  Bound by HBM: 32,000 tokens of 8 heads of 128 are written in 33 us
 // and read back in 33 (looked up by each team, with a piece of a thread on its way: 87 each).
 constexpr int kCodeThreads = 256, kJobs = 4;
-struct Place {
-  int page, place;  // page -1: no token
+struct alignas(16) Place {
+  char *codes, *power;  // of the token's first head; NULL: no token
 };
 template <bool kWrite>
 __global__ void __launch_bounds__(kCodeThreads) codes_kernel(Cache c, int layer, const int32_t *slots, const int32_t *position, int n,
@@ -397,17 +397,21 @@ __global__ void __launch_bounds__(kCodeThreads) codes_kernel(Cache c, int layer,
   after_the_last();
   const int row0 = blockIdx.x * rows, here = min(rows, n - row0);
   for (int r = threadIdx.x; r < here; r += kCodeThreads) {
-    Place p{-1, 0};
-    if (!find_token(c, slots, position, row0 + r, p.page, p.place)) {
-      p.page = -1;
+    Place p{nullptr, nullptr};
+    int page, place;
+    if (find_token(c, slots, position, row0 + r, page, place)) {
+      char *base = c.pool + (uint64_t)page * c.page_bytes + layer * c.layer_bytes;
+      p = Place{base + (uint64_t)place * c.head_dim, base + c.layer_elems + place};
+    } else {
       flag_error(kErrCacheId);
     }
     s_place[r] = p;
   }
   __syncthreads();
   const int d = (int)(threadIdx.x & (team - 1)) * 8, teams = kCodeThreads / team, heads = 2 * c.n_kv_heads;
-  const int64_t jobs = (int64_t)here * heads;
-  for (int64_t first = threadIdx.x / team; first - (int)(threadIdx.x / team) < jobs; first += (int64_t)teams * kJobs) {
+  const int jobs = here * heads, step_rows = teams / heads, step_heads = teams % heads;
+  int row = threadIdx.x / team / heads, head = threadIdx.x / team % heads;  // of the next job
+  for (int begun = 0; begun < jobs; begun += teams * kJobs) {
     uint32_t w[kJobs][4];  // 8 values of bf16
     uint16_t *outside[kJobs];
     uint2 *codes[kJobs];
@@ -416,18 +420,23 @@ __global__ void __launch_bounds__(kCodeThreads) codes_kernel(Cache c, int layer,
     uint32_t held_power[kJobs];
 #pragma unroll
     for (int u = 0; u < kJobs; ++u) {
-      const int64_t job = first + (int64_t)u * teams;
-      const int head = (int)(job % heads), r = (int)(job / heads), which = head >= c.n_kv_heads, h = head - which * c.n_kv_heads;
       outside[u] = nullptr;
       codes[u] = nullptr;
-      if (job < jobs && d < c.head_dim) {
-        const Rows &to = which ? v : k;
-        outside[u] = to.at + (row0 + r) * to.row + h * to.head + d;
-        if (s_place[r].page >= 0) {
-          char *base = c.pool + (uint64_t)s_place[r].page * c.page_bytes + layer * c.layer_bytes;
-          codes[u] = reinterpret_cast<uint2 *>(base + (uint64_t)head * c.head_elems + (uint64_t)s_place[r].place * c.head_dim + d);
-          power[u] = reinterpret_cast<uint8_t *>(base + c.layer_elems + (uint64_t)head * c.page_size + s_place[r].place);
+      if (row < here && d < c.head_dim) {
+        // (A reference to one of the two would make the kernel's parameters an array in memory.)
+        const bool value = head >= c.n_kv_heads;
+        outside[u] = value ? v.at + (row0 + row) * v.row + (head - c.n_kv_heads) * v.head + d : k.at + (row0 + row) * k.row + head * k.head + d;
+        const Place at = s_place[row];
+        if (at.codes) {
+          codes[u] = reinterpret_cast<uint2 *>(at.codes + (uint64_t)head * c.head_elems + d);
+          power[u] = reinterpret_cast<uint8_t *>(at.power + (uint64_t)head * c.page_size);
         }
+      }
+      row += step_rows;
+      head += step_heads;
+      if (head >= heads) {
+        head -= heads;
+        ++row;
       }
       if constexpr (kWrite) {
 #pragma unroll
@@ -583,12 +592,8 @@ static cudaError_t launch_codes(const Cache &c, int layer, const int32_t *slots,
   while (team * 8 < c.head_dim) team *= 2;
   uintptr_t all = 0;
   for (const Rows &r : {k, v}) all |= (uintptr_t)r.at | (uintptr_t)r.row * 2 | (uintptr_t)r.head * 2;
-  // rows of a block: kJobs pieces for each thread twice over, or fewer where that leaves SMs without a block
-  const int64_t a_row = 2 * (int64_t)c.n_kv_heads * team;
-  const int64_t most = n / (152 * 4), fit = 2 * kJobs * kCodeThreads / a_row;
-  const int64_t rows = most < 1 || fit < 1 ? 1 : most < fit ? most : fit;
-  const unsigned blocks = (unsigned)((n - 1) / rows + 1);
-  return launch_after(blocks, kCodeThreads, s, codes_kernel<kWrite>, c, layer, slots, position, n, k, v, team, (int)rows, all % 16 == 0);
+  const int each = (n - 1) / (152 * 4) + 1, rows = each < kCodeThreads ? each : kCodeThreads;  // of a block, of as many as run at once
+  return launch_after((n - 1) / rows + 1, kCodeThreads, s, codes_kernel<kWrite>, c, layer, slots, position, n, k, v, team, rows, all % 16 == 0);
 }
 
 cudaError_t launch_cache_append(const Cache &c, int layer, const int32_t *slots, const int32_t *position, int n,
