@@ -710,13 +710,13 @@ def cache_append(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, s
                  position: Optional[torch.Tensor] = None, stream=None) -> None:
     """copes_cache_append: rows of k and v [n, n_kv_heads, head_dim] (any strides over rows and
     heads) into tokens `position` (default: the last ones) of `slots` (default: 0 .. n-1)."""
-    n, (kv, _, d) = k.shape[0], cache.heads
-    for t in (k, v):
-        assert t.shape == (n, kv, d) and t.dtype == cache.io_dtype and t.device == cache.pool.device
-        assert t.stride(2) == 1
+    shape, (kv, _, d) = k.shape, cache.heads
+    n, (k_row, k_head, k_each), (v_row, v_head, v_each) = shape[0], k.stride(), v.stride()
+    dtype, device = cache.io_dtype, cache.pool.device
+    assert shape == (n, kv, d) and v.shape == shape and k.dtype == dtype and v.dtype == dtype
+    assert k.device == device and v.device == device and k_each == 1 and v_each == 1
     _check(load().copes_cache_append(cache.ref, layer, cache._ids(slots, n), cache._ids(position, n), n, k.data_ptr(),
-                                     k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                     cache._stream(stream)))
+                                     k_row, k_head, v.data_ptr(), v_row, v_head, cache._stream(stream)))
 
 
 def cache_read(cache: KVCache, layer: int, slots: Optional[torch.Tensor] = None, position: Optional[torch.Tensor] = None,
@@ -835,12 +835,14 @@ def sample_tokens(logits: torch.Tensor, u: torch.Tensor, top_k: int = 0, top_p: 
     """copes_sample_tokens: a token of each row of logits [n, vocab] (bf16 or fp32, any stride over rows) under
     softmax(scale * logits) cut by top_k, top_p and min_p, by the random numbers u (fp32 [n], in [0, 1))."""
     n, vocab = logits.shape
+    row, each = logits.stride()
     device = logits.device
-    assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
+    assert logits.is_cuda and (each == 1 or vocab == 1)
     assert u.shape == (n,) and u.dtype == torch.float32 and u.device == device and u.is_contiguous()
     dtype = _DTYPE_CODES[logits.dtype]
-    ids, logprob, kept = (_empty(like, stream) for like in _sample_templates(n, device))
-    _check(load().copes_sample_tokens(logits.data_ptr(), dtype, n, vocab, logits.stride(0), u.data_ptr(), scale, top_k, top_p,
+    like_ids, like_logprob, like_kept = _sample_templates(n, device)
+    ids, logprob, kept = _empty(like_ids, stream), _empty(like_logprob, stream), _empty(like_kept, stream)
+    _check(load().copes_sample_tokens(logits.data_ptr(), dtype, n, vocab, row, u.data_ptr(), scale, top_k, top_p,
                                       min_p, ids.data_ptr(), logprob.data_ptr(), kept.data_ptr(), _stream(stream)))
     return SampledTokens(ids, logprob, kept)
 
@@ -858,27 +860,44 @@ def residual_norm(x: torch.Tensor, weight: Optional[torch.Tensor], y: Optional[t
     [n, hidden] (any stride over rows), weights [hidden], gate [hidden] or [n, hidden], all of one type.  Without y, s is x;
     without out_weight y is not normed; without weight there is no second result.  Returns (s, normed): new
     tensors, or `out` (which may be x) and `normed` (which may be y)."""
-    n, hidden = x.shape
+    shape = n, hidden = x.shape
     dtype, device = x.dtype, x.device
-    assert x.is_cuda
-    for t in (x, y, out, normed):
-        assert t is None or (t.shape == (n, hidden) and t.dtype == dtype and t.device == device and (t.stride(1) == 1 or hidden == 1))
-    for t in (weight, out_weight):
-        assert t is None or (t.shape == (hidden,) and t.dtype == dtype and t.device == device and t.is_contiguous())
-    gate_row = 0
+    x_row, each = x.stride()
+    assert x.is_cuda and (each == 1 or hidden == 1)
+    like = _rows_template(n, hidden, dtype, device)
+    y_row = gate_row = out_row = normed_row = 0
+    y_at = gate_at = out_at = normed_at = weight_at = out_weight_at = None
+    if y is not None:
+        y_row, each = y.stride()
+        assert y.shape == shape and y.dtype == dtype and y.device == device and (each == 1 or hidden == 1)
+        y_at = y.data_ptr()
+        if out is None:
+            out = _empty(like, stream)
+            out_row = hidden
+        else:
+            out_row, each = out.stride()
+            assert out.shape == shape and out.dtype == dtype and out.device == device and (each == 1 or hidden == 1)
+        out_at = out.data_ptr()
+    if out_weight is not None:
+        assert out_weight.shape == (hidden,) and out_weight.dtype == dtype and out_weight.device == device and out_weight.is_contiguous()
+        out_weight_at = out_weight.data_ptr()
     if gate is not None:
-        assert gate.shape in ((hidden,), (n, hidden)) and gate.dtype == dtype and gate.device == device
+        assert gate.shape in ((hidden,), shape) and gate.dtype == dtype and gate.device == device
         assert gate.stride(-1) == 1 or hidden == 1
         gate_row = gate.stride(0) if gate.dim() == 2 else 0
-    like = _rows_template(n, hidden, dtype, device)
-    if y is not None and out is None:
-        out = _empty(like, stream)
-    if weight is not None and normed is None:
-        normed = _empty(like, stream)
-    row = lambda t: 0 if t is None else t.stride(0)
-    _check(load().copes_residual_norm(_DTYPE_CODES[dtype], n, hidden, x.data_ptr(), row(x), _ptr(y), row(y), _ptr(out_weight),
-                                      _ptr(gate), gate_row, scale, _ptr(weight), eps, _ptr(out), row(out), _ptr(normed),
-                                      row(normed), _stream(stream)))
+        gate_at = gate.data_ptr()
+    if weight is not None:
+        assert weight.shape == (hidden,) and weight.dtype == dtype and weight.device == device and weight.is_contiguous()
+        weight_at = weight.data_ptr()
+        if normed is None:
+            normed = _empty(like, stream)
+            normed_row = hidden
+        else:
+            normed_row, each = normed.stride()
+            assert normed.shape == shape and normed.dtype == dtype and normed.device == device and (each == 1 or hidden == 1)
+        normed_at = normed.data_ptr()
+    _check(load().copes_residual_norm(_DTYPE_CODES[dtype], n, hidden, x.data_ptr(), x_row, y_at, y_row, out_weight_at, gate_at,
+                                      gate_row, scale, weight_at, eps, out_at, out_row, normed_at, normed_row, _stream(stream)))
     return x if y is None else out, normed
 
 
