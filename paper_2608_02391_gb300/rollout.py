@@ -9,6 +9,8 @@ and the library's cache, attention and log probabilities:
 score   mean log probability of given answers, the answers of one prompt sharing the prompt's pages
         (cache_fork): a dense reward that needs no sampling
 greedy  the likeliest continuation of each prompt, for a verifier to judge
+sample  continuations drawn from given random numbers, the rollouts of one prompt sharing its pages: the
+        same numbers and weights give the same rollouts
 
 One visit with answers as rewards:
 
@@ -32,7 +34,8 @@ from . import copes, workloads
 
 @dataclass(frozen=True)
 class Shape:
-    """The arguments of workloads.decoder_tensors, and the base of the rotary frequencies."""
+    """The arguments of workloads.decoder_tensors, the base of the rotary frequencies, and what a block's output is
+    multiplied by on its way to the residual sum."""
     layers: int
     hidden: int
     mlp: int
@@ -45,10 +48,14 @@ class Shape:
     tied: bool = True
     rope_base: float = 1e6
     eps: float = 1e-6
+    out_norms: bool = False
+    block_gates: bool = False
+    residual_scale: float = 1.0
 
     def tensors(self) -> List[workloads.Tensor]:
         return workloads.decoder_tensors(self.layers, self.hidden, self.mlp, self.vocab, self.q_heads, self.kv_heads,
-                                         self.head_dim, self.qkv_bias, self.qk_norm, self.tied)
+                                         self.head_dim, self.qkv_bias, self.qk_norm, self.tied, self.out_norms,
+                                         self.block_gates)
 
 
 def _rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float) -> torch.Tensor:
@@ -57,10 +64,13 @@ def _rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float) -> torch.Tensor
 
 
 class Decoder:
-    """A decoder over flat weight buffers with the layout of shape.tensors()."""
+    """A decoder over flat weight buffers with the layout of shape.tensors().  fused: norms and residual sums by
+    copes.residual_norm, which holds a sum in 32 bits until it is normed (the default rounds it before, and a norm
+    before its weight); shapes with more than that between their blocks are always so."""
 
-    def __init__(self, shape: Shape, device="cuda"):
+    def __init__(self, shape: Shape, device="cuda", fused: bool = False):
         self.shape = shape
+        self.fused = fused or shape.out_norms or shape.block_gates or shape.residual_scale != 1.0
         self.tensors = shape.tensors()
         self.offsets = workloads.layout_offsets(self.tensors)
         half = torch.arange(0, shape.head_dim, 2, device=device, dtype=torch.float64) / shape.head_dim
@@ -83,7 +93,7 @@ class Decoder:
     def cache(self, n_slots: int, max_tokens: int, page_size: int = 16, n_pages: int = 0, dtype=torch.bfloat16,
               device="cuda") -> copes.KVCache:
         """An empty cache of n_slots sequences of up to max_tokens (n_pages: fewer pages than all of
-        them need, where many share a prompt)."""
+        them need, where many share a prompt).  dtype torch.float8_e4m3fn: one in 8 bits, for weights in bf16."""
         s, width = self.shape, -(-max_tokens // page_size)
         return copes.KVCache.empty(n_pages or n_slots * width, s.layers, s.kv_heads, page_size, s.head_dim, n_slots, width,
                                    dtype=dtype, device=device)
@@ -93,6 +103,20 @@ class Decoder:
         cos, sin = (f(angles).float()[:, None] for f in (torch.cos, torch.sin))
         a, b = x.float().chunk(2, -1)
         return torch.cat((a * cos - b * sin, b * cos + a * sin), -1).to(x.dtype)
+
+    def _norm(self, x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+        """The norm of x over its last dimension."""
+        if not self.fused:
+            return _rms_norm(x, weight, self.shape.eps)
+        return copes.residual_norm(x.reshape(-1, x.shape[-1]), weight, eps=self.shape.eps)[1].view(x.shape)
+
+    def _add(self, x: torch.Tensor, y: torch.Tensor, get, block: str, weight):
+        """The residual sum after a block with output y, and its norm by `weight` (None: that is not wanted)."""
+        if not self.fused:
+            x = x + y
+            return x, None if weight is None else _rms_norm(x, weight, self.shape.eps)
+        return copes.residual_norm(x, weight, y=y, out_weight=get(block + "_out_norm"), gate=get(block + "_gate"),
+                                   scale=self.shape.residual_scale, eps=self.shape.eps, out=x)
 
     def step(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: torch.Tensor, tokens: torch.Tensor,
              logits: bool = True):
@@ -104,20 +128,20 @@ class Decoder:
         place = cache.length[slots.long().clamp_(0, cache.desc.n_slots - 1)] - 1  # a slot past the cache is the calls' to report
         angles = place.double()[:, None] * self.frequencies
         x = weights["embed"][tokens]
+        h = self._norm(x, weights["l0.in_norm"])
         for l in range(s.layers):
             get = lambda name: weights.get(f"l{l}.{name}")
-            h = _rms_norm(x, get("in_norm"), s.eps)
             q, k, v = (torch.nn.functional.linear(h, get(m), get(m + "_bias")).view(n, -1, s.head_dim) for m in "qkv")
             if s.qk_norm:
-                q, k = _rms_norm(q, get("q_norm"), s.eps), _rms_norm(k, get("k_norm"), s.eps)
+                q, k = self._norm(q, get("q_norm")), self._norm(k, get("k_norm"))
             copes.cache_append(cache, l, self._rotate(k, angles), v, slots=slots)
             out, _ = copes.paged_attention(cache, l, self._rotate(q, angles), slots=slots)
-            x = x + out.flatten(1) @ get("o").T
-            h = _rms_norm(x, get("post_norm"), s.eps)
-            x = x + (torch.nn.functional.silu(h @ get("gate").T) * (h @ get("up").T)) @ get("down").T
-        if not logits:
-            return None
-        return _rms_norm(x, weights["final_norm"], s.eps) @ weights["embed" if s.tied else "lm_head"].T
+            x, h = self._add(x, out.flatten(1) @ get("o").T, get, "attn", get("post_norm"))
+            y = (torch.nn.functional.silu(h @ get("gate").T) * (h @ get("up").T)) @ get("down").T
+            last = l + 1 == s.layers
+            after = weights["final_norm"] if last and logits else None if last else weights[f"l{l + 1}.in_norm"]
+            x, h = self._add(x, y, get, "mlp", after)
+        return h @ weights["embed" if s.tied else "lm_head"].T if logits else None
 
     def _check_tokens(self, what: str, sequences: Sequence[Sequence[int]]) -> None:
         """Raises for no sequences, for one without tokens, whose reward would be 0 / 0, and for an id outside the
@@ -159,6 +183,10 @@ class Decoder:
         if used + pages > d.n_pages:
             raise ValueError(f"{pages} pages are needed, and {d.n_pages - used} of the cache's {d.n_pages} are free")
 
+    def _fork_pages(self, size: int, prompt: int, length: int) -> int:
+        """Pages of its own that a fork of a prompt has when it has grown to `length` tokens."""
+        return -(-length // size) - prompt // size
+
     def _check_score(self, cache: copes.KVCache, prompts: Sequence[Sequence[int]],
                      answers: Sequence[Sequence[Sequence[int]]]) -> None:
         self._check_tokens("prompt", prompts)
@@ -171,7 +199,7 @@ class Decoder:
         for p, group in zip(prompt, answers):
             for a in group:  # its last token is not written; the prompt's full pages are shared
                 lengths.append(p + len(a) - 1)
-                pages += -(-lengths[-1] // size) - p // size
+                pages += self._fork_pages(size, p, lengths[-1])
         self._check_room(cache, lengths, pages)
 
     def score(self, w: torch.Tensor, cache: copes.KVCache, prompts: Sequence[Sequence[int]],
@@ -224,3 +252,46 @@ class Decoder:
         copes.cache_free(cache, slots)
         copes.check()
         return torch.stack(out, 1)
+
+    def sample(self, w: torch.Tensor, cache: copes.KVCache, prompts: Sequence[Sequence[int]], n_tokens: int, u: torch.Tensor,
+               rollouts: int = 1, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
+        """n_tokens drawn tokens of each of `rollouts` continuations of each prompt (those of prompt 0, then those of prompt 1,
+        ...), and their log probabilities among the tokens that the cuts keep: int64 and fp32 [prompts * rollouts,
+        n_tokens].  u: fp32 [n_tokens, prompts * rollouts], random numbers in [0, 1); temperature and cuts as
+        copes.sample_tokens' (scale 1 / temperature).  The cache's first slots, one for each prompt and, where a prompt has
+        several, each rollout, are empty before and after; errors as score's, and RuntimeError for logits that
+        nothing can be drawn from."""
+        self._check_tokens("prompt", prompts)
+        if n_tokens < 1 or rollouts < 1 or not 1e-38 <= temperature <= 1e30:
+            raise ValueError(f"{rollouts} continuations of {n_tokens} tokens at temperature {temperature}")
+        if top_k < 0 or not 0 < top_p <= 1 or not 0 <= min_p <= 1:
+            raise ValueError(f"cuts to top_k {top_k}, top_p {top_p} and min_p {min_p}")
+        first, n = len(prompts), len(prompts) * rollouts
+        if u.shape != (n_tokens, n) or u.dtype != torch.float32 or u.device != cache.pool.device:
+            raise ValueError(f"random numbers {tuple(u.shape)} of {u.dtype} on {u.device} for {n_tokens} tokens of {n} continuations")
+        size, prompt = cache.desc.page_size, [len(p) for p in prompts]
+        ends = [p + n_tokens - 1 for p in prompt for _ in range(rollouts)]  # the last token is not written
+        if rollouts == 1:
+            self._check_room(cache, ends, sum(-(-k // size) for k in ends))
+        else:
+            self._check_room(cache, prompt + ends, sum(-(-p // size) + rollouts * self._fork_pages(size, p, p + n_tokens - 1)
+                                                       for p in prompt))
+        weights, device = self.weights(w), cache.pool.device
+        slots = torch.arange(first, dtype=torch.int32, device=device)
+        logits = self.read(weights, cache, list(range(first)), prompts)
+        if rollouts > 1:
+            parents, slots = slots.repeat_interleave(rollouts), torch.arange(first, first + n, dtype=torch.int32, device=device)
+            copes.cache_fork(cache, parents, slots)
+            logits = logits.repeat_interleave(rollouts, 0)
+        tokens = torch.empty((n, n_tokens), dtype=torch.int64, device=device)
+        logprob = torch.empty((n, n_tokens), dtype=torch.float32, device=device)
+        for t in range(n_tokens):
+            r = copes.sample_tokens(logits, u[t].contiguous(), top_k=top_k, top_p=top_p, min_p=min_p, scale=1.0 / temperature)
+            tokens[:, t], logprob[:, t] = r.ids, r.logprob
+            if t + 1 < n_tokens:
+                logits = self.step(weights, cache, slots, r.ids.clamp(min=0))
+        copes.cache_free(cache, torch.arange(n if rollouts == 1 else first + n, dtype=torch.int32, device=device))
+        copes.check()
+        if bool((tokens < 0).any()):
+            raise RuntimeError("logits that nothing can be drawn from")
+        return tokens, logprob

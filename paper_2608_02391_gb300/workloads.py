@@ -42,7 +42,8 @@ def layout_offsets(tensors: Sequence[Tensor]) -> List[int]:
 
 
 def decoder_tensors(layers, hidden, mlp, vocab, q_heads, kv_heads, head_dim, qkv_bias,
-                    qk_norm, tied) -> List[Tensor]:
+                    qk_norm, tied, out_norms=False, block_gates=False) -> List[Tensor]:
+    """out_norms: a norm of each block's output, too; block_gates: a factor for each of its channels."""
     q_out, kv_out = q_heads * head_dim, kv_heads * head_dim
     ts = [Tensor("embed", vocab * hidden, "embed")]
     for l in range(layers):
@@ -60,6 +61,8 @@ def decoder_tensors(layers, hidden, mlp, vocab, q_heads, kv_heads, head_dim, qkv
             ts.append(Tensor(f"l{l}.q_norm", head_dim, "norm", l))
             ts.append(Tensor(f"l{l}.k_norm", head_dim, "norm", l))
         ts.append(Tensor(f"l{l}.in_norm", hidden, "norm", l))
+        ts += [Tensor(f"l{l}.{block}_{what}", hidden, "norm", l) for block in ("attn", "mlp")
+               for what, there in (("out_norm", out_norms), ("gate", block_gates)) if there]
         ts.append(Tensor(f"l{l}.gate", hidden * mlp, "mlp", l))
         ts.append(Tensor(f"l{l}.up", hidden * mlp, "mlp", l))
         ts.append(Tensor(f"l{l}.down", mlp * hidden, "mlp", l))
