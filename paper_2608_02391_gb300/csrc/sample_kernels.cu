@@ -33,6 +33,7 @@ namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
+static_assert((kWarps & (kWarps - 1)) == 0 && kWarps <= 32, "sums over warps by halves");
 constexpr int kEach = 4;                   // pieces of 16 bytes of a lane in a chunk, and cells of a thread
 constexpr int kChunkPieces = 32 * kEach;
 constexpr int kList = 2048;                // logits that can be collected
@@ -862,6 +863,7 @@ struct Sampler {
     const int from = min(chunks, (int)threadIdx.x * per), to = min(chunks, from + per);
     u64 mine = 0, all;
     for (int i = from; i < to; ++i) mine += list[i];
+    if (threadIdx.x == 0) s->chunk = 0;
     u64 before = block_scan(mine, s, &all);
     for (int i = from; i < to; ++i) {
       if (before <= place && place < before + list[i]) {
@@ -1058,8 +1060,9 @@ struct Sampler {
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleArgs a, float c, float farthest, int size) {
+// kPerSm: blocks that an SM holds, two where rows alone fill the GPU; one has twice the registers.
+template <typename T, int kPerSm>
+__global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(SampleArgs a, float c, float farthest, int size) {
   extern __shared__ __align__(16) char smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1074,16 +1077,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleArgs a, float
   if (size > 1) g.sync();  // or to one that has ended
 }
 
-template <typename T>
-cudaError_t launch(const SampleArgs &a, cudaStream_t s) {
+template <typename T, int kPerSm>
+cudaError_t launch(const SampleArgs &a, int size, cudaStream_t s) {
   static_assert((COPES_MAX_SAMPLE_VOCAB - 1) / (kChunkPieces * 4) + 2 <= kChunksMost, "room for fp32's chunks");
   constexpr int kSmem = kChunksMost * 8 + (int)sizeof(Shared);
   static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two blocks of an SM");
-  cudaError_t e = allow_smem((const void *)sample_kernel<T>, kSmem, kSmem);
+  cudaError_t e = allow_smem((const void *)sample_kernel<T, kPerSm>, kSmem, kSmem);
   if (e != cudaSuccess) return e;
-  // as many blocks as an SM holds of a row where there are few
-  int size = 1;
-  while (size < kMaxCluster && (int64_t)a.n * size * 2 <= 152 * 2) size *= 2;
   const float c = a.scale * 1.44269504088896340736f;
   const float farthest = a.min_p > 0.0f ? fminf((float)-log2((double)a.min_p), kFarthest) : kFarthest;
   cudaLaunchConfig_t cfg{};
@@ -1099,15 +1099,24 @@ cudaError_t launch(const SampleArgs &a, cudaStream_t s) {
   cfg.gridDim = dim3((unsigned)a.n * size);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
-  return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, c, farthest, size);
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T, kPerSm>, a, c, farthest, size);
 }
 
 }  // namespace
 
+// Blocks of a row: as many as SMs there are for it.  96 rows of 151,936 in bf16, us with a block on an SM and with two
+// blocks of a row (two to an SM): uncut 22 and 26, the first 50 17 and 19, top_p of flat rows 98 and 110.
+template <typename T>
+static cudaError_t by_rows(const SampleArgs &a, cudaStream_t s) {
+  int size = 1;
+  while (size < kMaxCluster && (int64_t)a.n * size * 2 <= 152) size *= 2;
+  return a.n <= 152 ? launch<T, 1>(a, size, s) : launch<T, 2>(a, 1, s);
+}
+
 cudaError_t launch_sample_tokens(int dtype, const SampleArgs &a, cudaStream_t s) {
   if (a.n == 0) return cudaSuccess;
   g_used = true;
-  return dtype == COPES_BF16 ? launch<__nv_bfloat16>(a, s) : launch<float>(a, s);
+  return dtype == COPES_BF16 ? by_rows<__nv_bfloat16>(a, s) : by_rows<float>(a, s);
 }
 
 unsigned read_and_clear_sample_errors() {
