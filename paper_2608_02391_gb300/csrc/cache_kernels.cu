@@ -460,11 +460,19 @@ __global__ void __launch_bounds__(kCodeThreads) codes_kernel(Cache c, int layer,
 #pragma unroll
     for (int u = 0; u < kJobs; ++u) {
       if constexpr (kWrite) {
-        uint32_t most = 0;  // as bits of bf16
+        uint32_t two = 0;  // the largest, as bits of bf16, of even and of odd ones
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t x = w[u][e / 2] >> 16 * (e & 1) & 0x7FFFu;
-          if (x < 0x7F80u) most = max(most, x);
+        for (int e = 0; e < 4; ++e) two = __vmaxu2(two, w[u][e] & 0x7FFF7FFFu);
+        uint32_t most = max(two & 0xFFFFu, two >> 16);
+        const bool finite = most < 0x7F80u;
+        if (!finite) {
+          most = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t x = w[u][e / 2] >> 16 * (e & 1) & 0x7FFFu;
+            if (x < 0x7F80u) most = max(most, x);
+            else w[u][e / 2] |= 0x7FFFu << 16 * (e & 1);  // the type has no infinity
+          }
         }
         for (int s = team >> 1; s; s >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, s));
         // 127 more than the exponent e: 448 is 1.75 2^8
@@ -474,12 +482,10 @@ __global__ void __launch_bounds__(kCodeThreads) codes_kernel(Cache c, int layer,
         uint32_t pair[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float lo = __uint_as_float(w[u][e] << 16) * over, hi = __uint_as_float(w[u][e] & 0xFFFF0000u) * over;
-          if (isinf(lo)) lo = NAN;  // the type has no infinity
-          if (isinf(hi)) hi = NAN;
-          uint16_t two;
-          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
-          pair[e] = two;
+          const float lo = __uint_as_float(w[u][e] << 16) * over, hi = __uint_as_float(w[u][e] & 0xFFFF0000u) * over;
+          uint16_t code;
+          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(code) : "f"(hi), "f"(lo));
+          pair[e] = code;
         }
         *codes[u] = make_uint2(pair[0] | pair[1] << 16, pair[2] | pair[3] << 16);
         if (d == 0) *power[u] = (uint8_t)biased;

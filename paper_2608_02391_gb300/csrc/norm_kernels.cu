@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include "answer.h"
+#include "copes_device.cuh"
 
 namespace copes {
 
@@ -85,21 +86,29 @@ struct RowSum {
   }
 };
 
-// a / rms(a) = (a first) second.  Squares past fp32 are summed again of values 2^-80 as large, where eps is
-// nothing.
-struct Unit {
-  float first, second;
-};
+// 1 / rms(a).  Squares past fp32 are summed again of values 2^-80 as large, where eps is nothing.
 template <int kP, int kN, typename Value>
-__device__ __forceinline__ Unit unit_of(const Value &value, float eps, int hidden, RowSum &sum) {
+__device__ __forceinline__ float unit_of(const Value &value, float eps, int hidden, RowSum &sum) {
   float mine = 0.0f;
+  if constexpr (kN > 1) {
+    unsigned long long two = 0;
 #pragma unroll
-  for (int p = 0; p < kP; ++p)
+    for (int p = 0; p < kP; ++p)
 #pragma unroll
-    for (int e = 0; e < kN; ++e) mine = fmaf(value(p, e), value(p, e), mine);
+      for (int e = 0; e < kN; e += 2) {
+        const unsigned long long v = pack_f32x2(value(p, e), value(p, e + 1));
+        two = fma_f32x2(v, v, two);
+      }
+    float odd;
+    unpack_f32x2(two, mine, odd);
+    mine += odd;
+  } else {
+#pragma unroll
+    for (int p = 0; p < kP; ++p) mine = fmaf(value(p, 0), value(p, 0), mine);
+  }
   const float squares = sum(mine);
   const bool fine = squares <= FLT_MAX;
-  const Unit u{1.0f, rsqrtf(squares / (float)hidden + eps)};
+  const float u = rsqrtf(squares / (float)hidden + eps);
   if (__all_sync(kAll, fine)) return u;  // the same in all warps of a row
   const float less = 0x1p-80f;
   mine = 0.0f;
@@ -108,7 +117,33 @@ __device__ __forceinline__ Unit unit_of(const Value &value, float eps, int hidde
 #pragma unroll
     for (int e = 0; e < kN; ++e) mine = fmaf(value(p, e) * less, value(p, e) * less, mine);
   const float again = rsqrtf(sum(mine) / (float)hidden);
-  return fine ? u : Unit{less, again};
+  return fine ? u : less * again;  // 2^-128 at least, which has 21 bits
+}
+
+// v = (factor w) v, and to = scale (gate) v + to, of a piece's values.
+template <int kN, typename W>
+__device__ __forceinline__ void multiply(float (&v)[kN], float factor, const W &w) {
+  if constexpr (kN > 1) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+      const unsigned long long two = mul_f32x2(mul_f32x2(pack_f32x2(v[e], v[e + 1]), splat_f32x2(factor)), pack_f32x2(w[e], w[e + 1]));
+      unpack_f32x2(two, v[e], v[e + 1]);
+    }
+  } else {
+    v[0] = v[0] * factor * w[0];
+  }
+}
+template <int kN, typename W>
+__device__ __forceinline__ void add(float (&to)[kN], const float (&v)[kN], float scale, const W *gate) {
+  if constexpr (kN > 1) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 2) {
+      const unsigned long long f = gate ? mul_f32x2(splat_f32x2(scale), pack_f32x2((*gate)[e], (*gate)[e + 1])) : splat_f32x2(scale);
+      unpack_f32x2(fma_f32x2(f, pack_f32x2(v[e], v[e + 1]), pack_f32x2(to[e], to[e + 1])), to[e], to[e + 1]);
+    }
+  } else {
+    to[0] = fmaf(gate ? scale * (*gate)[0] : scale, v[0], to[0]);
+  }
 }
 
 // A team of threads for each row, kP pieces of kBytes each; a block has blockDim.x / team rows.
@@ -144,31 +179,31 @@ __global__ void __launch_bounds__(kMostThreads<kBytes, kP>, kP <= 2 ? 1024 / kMo
 #pragma unroll
     for (int e = 0; e < kN; ++e) s[p][e] = x[p][e];
   if (a.y) {
-    Unit u{1.0f, 1.0f};
+    float u = 1.0f;
     if (a.out_weight) u = unit_of<kP, kN>([&](int p, int e) { return y[p][e]; }, a.eps, a.hidden, sum);
 #pragma unroll
     for (int p = 0; p < kP; ++p) {
       if (!here(p)) continue;
-      P w;
-      if (a.out_weight) w.load((const T *)a.out_weight + at(p));
+      float z[kN];
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        float z = y[p][e];
-        if (a.out_weight) z = z * u.first * u.second * w[e];
-        s[p][e] = fmaf(a.gate ? a.scale * gate[p][e] : a.scale, z, s[p][e]);
+      for (int e = 0; e < kN; ++e) z[e] = y[p][e];
+      if (a.out_weight) {
+        P w;
+        w.load((const T *)a.out_weight + at(p));
+        multiply(z, u, w);
       }
+      add(s[p], z, a.scale, a.gate ? &gate[p] : nullptr);
       if (a.sum) P::store((T *)a.sum + row * a.sum_row + at(p), s[p]);
     }
   }
   if (!a.normed) return;
-  const Unit u = unit_of<kP, kN>([&](int p, int e) { return s[p][e]; }, a.eps, a.hidden, sum);
+  const float u = unit_of<kP, kN>([&](int p, int e) { return s[p][e]; }, a.eps, a.hidden, sum);
 #pragma unroll
   for (int p = 0; p < kP; ++p) {
     if (!here(p)) continue;
     P w;
     w.load((const T *)a.weight + at(p));
-#pragma unroll
-    for (int e = 0; e < kN; ++e) s[p][e] = s[p][e] * u.first * u.second * w[e];
+    multiply(s[p], u, w);
     P::store((T *)a.normed + row * a.normed_row + at(p), s[p]);
   }
 }
@@ -215,7 +250,7 @@ __global__ void __launch_bounds__(512, 2) residual_norm_rows_kernel(NormArgs a) 
       y[p].clear();
       if (at(p) < a.hidden) y[p].load((const T *)slot(stage, 1, p));
     }
-    Unit u{1.0f, 1.0f};
+    float u = 1.0f;
     if (a.out_weight) u = unit_of<kP, kN>([&](int p, int e) { return y[p][e]; }, a.eps, a.hidden, sum);
 #pragma unroll
     for (int p = 0; p < kP; ++p) {
@@ -224,25 +259,28 @@ __global__ void __launch_bounds__(512, 2) residual_norm_rows_kernel(NormArgs a) 
       if (at(p) >= a.hidden) continue;
       P x, w, gate;
       x.load((const T *)slot(stage, 0, p));
-      if (a.out_weight) w.load((const T *)a.out_weight + at(p));
       if (a.gate) gate.load(gates ? (const T *)slot(stage, 2, p) : (const T *)a.gate + at(p));
+      float z[kN];
 #pragma unroll
       for (int e = 0; e < kN; ++e) {
-        float z = y[p][e];
-        if (a.out_weight) z = z * u.first * u.second * w[e];
-        s[p][e] = fmaf(a.gate ? a.scale * gate[e] : a.scale, z, x[e]);
+        s[p][e] = x[e];
+        z[e] = y[p][e];
       }
+      if (a.out_weight) {
+        w.load((const T *)a.out_weight + at(p));
+        multiply(z, u, w);
+      }
+      add(s[p], z, a.scale, a.gate ? &gate : nullptr);
       if (a.sum) P::store((T *)a.sum + row * a.sum_row + at(p), s[p]);
     }
     if (a.normed) {
-      const Unit v = unit_of<kP, kN>([&](int p, int e) { return s[p][e]; }, a.eps, a.hidden, sum);
+      const float v = unit_of<kP, kN>([&](int p, int e) { return s[p][e]; }, a.eps, a.hidden, sum);
 #pragma unroll
       for (int p = 0; p < kP; ++p) {
         if (at(p) >= a.hidden) continue;
         P w;
         w.load((const T *)a.weight + at(p));
-#pragma unroll
-        for (int e = 0; e < kN; ++e) s[p][e] = s[p][e] * v.first * v.second * w[e];
+        multiply(s[p], v, w);
         P::store((T *)a.normed + row * a.normed_row + at(p), s[p]);
       }
     }
@@ -271,8 +309,8 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
         for (int e = 0; e < kN; ++e) mine = fmaf(v[e] * first, v[e] * first, mine);
       }
       const float squares = sum(mine);
-      if (first != 1.0f) return Unit{first, rsqrtf(squares / (float)a.hidden)};
-      if (squares <= FLT_MAX) return Unit{1.0f, rsqrtf(squares / (float)a.hidden + a.eps)};
+      if (first != 1.0f) return first * rsqrtf(squares / (float)a.hidden);
+      if (squares <= FLT_MAX) return rsqrtf(squares / (float)a.hidden + a.eps);
       first = 0x1p-80f;
     }
   };
@@ -282,7 +320,7 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
 #pragma unroll
     for (int e = 0; e < kN; ++e) v[e] = y[e];
   };
-  Unit u{1.0f, 1.0f};
+  float u = 1.0f;
   if (a.y && a.out_weight) u = unit(block);
   const auto total = [&](int at, float (&v)[kN]) {
     P x, y, w;
@@ -296,13 +334,13 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
     if (a.out_weight) {
       w.load((const T *)a.out_weight + at);
 #pragma unroll
-      for (int e = 0; e < kN; ++e) v[e] = v[e] * u.first * u.second * w[e];
+      for (int e = 0; e < kN; ++e) v[e] = v[e] * u * w[e];
     }
     if (a.gate) w.load((const T *)a.gate + row * a.gate_row + at);
 #pragma unroll
     for (int e = 0; e < kN; ++e) v[e] = fmaf(a.gate ? a.scale * w[e] : a.scale, v[e], x[e]);
   };
-  Unit whole{1.0f, 1.0f};
+  float whole = 1.0f;
   if (a.normed) whole = unit(total);
   for (int at = threadIdx.x * kN; at < a.hidden; at += blockDim.x * kN) {
     float v[kN];
@@ -312,7 +350,7 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
     P w;
     w.load((const T *)a.weight + at);
 #pragma unroll
-    for (int e = 0; e < kN; ++e) v[e] = v[e] * whole.first * whole.second * w[e];
+    for (int e = 0; e < kN; ++e) v[e] = v[e] * whole * w[e];
     P::store((T *)a.normed + row * a.normed_row + at, v);
   }
 }
