@@ -85,14 +85,16 @@ struct Shape {
   static constexpr int kPart = kOwn * kChunks * 16;       // a warp's keys (or values) of a tile, bytes
   static constexpr int kStage = 2 * kPart * kWarps;
   static constexpr int kHeads = 8 * NT;                   // query heads of a block at a time
-  static constexpr int kRow = DP + 4;                     // row of s_o: heads 2j begin 8 banks apart
+  // Values that the warps of a block put together at a time: half of 128 where that lets a third block on an SM.
+  static constexpr int kAtOnce = kFp8 && DP == 128 && NT == 1 ? DP / 2 : DP;
+  static constexpr int kRow = kAtOnce + 4;                // row of s_o: heads 2j begin 8 banks apart
   static constexpr int kFixed = (kWarps * 8 * kRow + kWarps * 16) * 4;
   static constexpr int kSmem = kStages * kStage + kFixed;
   // blocks of an SM by its 228 KB, 1 KB of them taken for each block, and by its registers
   static constexpr int kFit = 228 * 1024 / (kSmem + 1280);
   // (Three variants spill all the same: fp32 heads of 256 20 bytes of a thread, of 128 with two column
   // tiles 40, of 64 side by side 16.)
-  static constexpr int kByRegs = 65536 / (kThreads * (kFp8 ? (DP * NT > 64 ? 248 : 168) : DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
+  static constexpr int kByRegs = 65536 / (kThreads * (kFp8 ? (DP > 128 || NT > 1 ? 248 : 168) : DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
   static constexpr int kPerSm = kFit < kByRegs ? kFit : kByRegs;
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
 };
@@ -890,7 +892,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   Place next = look_up();
   // The queries of a (row, head group), and, registers permitting, of the next one, asked for a
   // (row, head group) before they are used.
-  constexpr bool kNextToo = S::NT == 1 && (S::kFp32 ? S::DP <= 64 : S::DP <= 128);
+  constexpr bool kNextToo = S::NT == 1 && (S::kFp32 || S::kFp8 ? S::DP <= 64 : S::DP <= 128);
   const int64_t q_bytes = sizeof(typename Beside<T>::type), q_wide = S::kFp32 ? 16 : 4;
   const bool wide = (uintptr_t)a.q % q_wide == 0 && a.q_row * q_bytes % q_wide == 0 && a.q_head * q_bytes % q_wide == 0;
   Queries<S> q, q_next;
@@ -924,7 +926,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   Running<S> r;
   r.clear();
   const float scale = a.scale * 1.44269504088896340736f;  // of log2
-  constexpr int kD4 = S::DP / 4;
+  constexpr int kD4 = S::kAtOnce / 4;
   const int slot_floats = S::kHeads * (D + 2);
   Split begun{-1, 0, 0, 0};
   for (int j = 0; j < count; ++j) {
@@ -993,38 +995,42 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
         }
       }
 #pragma unroll
-      for (int i = 0; i < S::DP / 16; ++i)
+      for (int from = 0; from < S::DP; from += S::kAtOnce) {
+        if (from) team_sync();
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          s_o[(member * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1)] = r.o[i][nt][e] * factor[e & 1];
-      team_sync();
-      for (int v = rank; v < 8 * kD4; v += kTeamThreads) {
-        const int h = v / kD4, d = v % kD4 * 4;
-        if (nt * 8 + h >= heads || d >= D) continue;
-        float4 o;
-        if constexpr (S::kTeam > 1) {
-          float M = -INFINITY, L = 0.0f;
+        for (int i = from / 16; i < (from + S::kAtOnce) / 16; ++i)
 #pragma unroll
-          for (int w = 0; w < S::kTeam; ++w) M = fmaxf(M, s_m[w * 8 + h]);
-          o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int e = 0; e < 4; ++e)
+            s_o[(member * 8 + (lane & 3) * 2 + (e & 1)) * S::kRow + output_d<S>(i, e >> 1) - from] = r.o[i][nt][e] * factor[e & 1];
+        team_sync();
+        for (int v = rank; v < 8 * kD4; v += kTeamThreads) {
+          const int h = v / kD4, at = v % kD4 * 4, d = from + at;
+          if (nt * 8 + h >= heads || d >= D) continue;
+          float4 o;
+          if constexpr (S::kTeam > 1) {
+            float M = -INFINITY, L = 0.0f;
 #pragma unroll
-          for (int w = 0; w < S::kTeam; ++w) {
-            const float weight = part_weight(s_m[w * 8 + h], M);
-            L = fmaf(weight, s_l[w * 8 + h], L);
-            fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + d));
+            for (int w = 0; w < S::kTeam; ++w) M = fmaxf(M, s_m[w * 8 + h]);
+            o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < S::kTeam; ++w) {
+              const float weight = part_weight(s_m[w * 8 + h], M);
+              L = fmaf(weight, s_l[w * 8 + h], L);
+              fma4(o, weight, *reinterpret_cast<const float4 *>(s_o + (w * 8 + h) * S::kRow + at));
+            }
+            if (whole) o = normalised(o, L);
+            if (d == 0 && !whole) {
+              mine_part[nt * 8 + h] = M;
+              mine_part[S::kHeads + nt * 8 + h] = L;
+            } else if (d == 0 && a.lse) {
+              a.lse[first + nt * 8 + h] = log_sum(M, L);
+            }
+          } else {
+            o = *reinterpret_cast<const float4 *>(s_o + h * S::kRow + at);
           }
-          if (whole) o = normalised(o, L);
-          if (d == 0 && !whole) {
-            mine_part[nt * 8 + h] = M;
-            mine_part[S::kHeads + nt * 8 + h] = L;
-          } else if (d == 0 && a.lse) {
-            a.lse[first + nt * 8 + h] = log_sum(M, L);
-          }
-        } else {
-          o = *reinterpret_cast<const float4 *>(s_o + h * S::kRow + d);
+          if (whole) store(o, (typename Beside<T>::type *)a.out + (first + nt * 8 + h) * D + d);
+          else *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
         }
-        if (whole) store(o, (typename Beside<T>::type *)a.out + (first + nt * 8 + h) * D + d);
-        else *reinterpret_cast<float4 *>(mine_part + 2 * S::kHeads + (nt * 8 + h) * D + d) = o;
       }
     }
     if (!whole && lo <= x0) begun = Split{was.row, was.kv, was.sub, shares.owner(x1)};
