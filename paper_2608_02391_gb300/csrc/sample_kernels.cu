@@ -32,12 +32,9 @@ __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_sample_er
 namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-static_assert((kWarps & (kWarps - 1)) == 0 && kWarps <= 32, "sums over warps by halves");
 constexpr int kEach = 4;                   // pieces of 16 bytes of a lane in a chunk, and cells of a thread
 constexpr int kChunkPieces = 32 * kEach;
 constexpr int kList = 2048;                // logits that can be collected
-constexpr int kChunksMost = 8192;          // sums of chunks, in the place of the list and what is beside it
 constexpr int kMaxCluster = 8;
 constexpr float kFarthest = 40.0f;         // the weight is 0 past it
 constexpr int kBinsOfOne = 64, kBins = 40 * kBinsOfOne + 1;
@@ -218,11 +215,11 @@ struct Row {
 
 // What is in shared memory beside the list.
 struct Shared {
-  u64 sums[2][kWarps][4];        // of warps, by turns
+  u64 sums[2][32][4];        // of warps, by turns
   u64 peers[2][kMaxCluster][4];  // of the blocks of a cluster
-  u64 items[2][kWarps][3];
-  u64 scan[kWarps];
-  uint32_t counts[2][kWarps];
+  u64 items[2][32][3];
+  u64 scan[32];
+  uint32_t counts[2][32];
   int collected;
   uint32_t first;  // upper half of the list's first entry
   u64 total;
@@ -240,7 +237,10 @@ __device__ __forceinline__ uint32_t remote(uint32_t at, int rank) {
 }
 
 // The blocks that share a row: one, or a cluster.
+template <int kWarps_>
 struct Group {
+  static constexpr int kWarps = kWarps_;
+  static_assert((kWarps & (kWarps - 1)) == 0 && kWarps <= 32, "sums over warps by halves");
   int size, rank, turn;
   Shared *s;
   __device__ __forceinline__ void sync() const {
@@ -286,8 +286,8 @@ struct Group {
 
 // Runs f(chunk, its pieces of this lane) over this block's share of the row: chunk c is its where c % size ==
 // rank, and a warp's as a whole.
-template <typename T, typename F>
-__device__ __forceinline__ void for_row(const Row<T> &row, const Group &g, const F &f) {
+template <typename T, int kWarps, typename F>
+__device__ __forceinline__ void for_row(const Row<T> &row, const Group<kWarps> &g, const F &f) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int chunks = (row.pieces - 1) / kChunkPieces + 1;
   for (int c = g.rank + g.size * warp; c < chunks; c += g.size * kWarps) {
@@ -314,6 +314,7 @@ __device__ __forceinline__ void for_chunk(const Row<T> &row, int chunk, const ui
 }
 
 // Exclusive sums of v over the block's threads, and the total.
+template <int kWarps>
 __device__ __forceinline__ u64 block_scan(u64 v, Shared *s, u64 *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   u64 x = v;
@@ -344,9 +345,9 @@ __device__ __forceinline__ u64 warp_sum(u64 v) {
 // Collected tokens in the block's registers, kEvery of them in each thread's: entries, which ascend in
 // the order of the tokens (keys falling, then ids rising), and weights.  Everything about them is found by
 // searching for an answer two bits at a time, by three sums over the block, which sorts nothing.
-template <int kEvery_>
+template <int kEvery_, int kThreads>
 struct Items {
-  static constexpr int kEvery = kEvery_;
+  static constexpr int kEvery = kEvery_, kWarps = kThreads / 32;
   u64 entry[kEvery], weight[kEvery];
   int count, turn = 0;
   Shared *s;
@@ -434,6 +435,7 @@ struct Items {
 
 // The largest b <= 65535 that at least k of the block's cells reach (0: fewer are that many), of the upper 16
 // bits of their keys.
+template <int kWarps>
 __device__ __forceinline__ uint32_t cell_bound(const uint32_t (&upper)[kEach], int k, Shared *s) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t found = 0;
@@ -467,16 +469,22 @@ __device__ __forceinline__ u64 place_of(float u, u64 total) {
 }
 
 // A row's problem and its steps; every step is called by all threads of the group.
-template <typename T>
+template <typename T, int kThreads>
 struct Sampler {
   using R = Row<T>;
+  static constexpr int kWarps = kThreads / 32, kShort = 512;
   const SampleArgs &a;
   const R &row;
-  Group &g;
+  Group<kWarps> &g;
   Shared *s;
-  u64 *list, *weights;  // of kList, and what is beside it; together the chunks' sums
+  u64 *list, *weights, *sums;  // of kList, what is beside it, and the chunks' sums
   float m, c, farthest;
   int index;
+  // After find_cut: of what was collected last, the number, where it begins, and the weight and number of all nearer;
+  // the chunks' sums are of these.
+  int last_count = -1;
+  float last_nearest;
+  u64 last_above[2];
 
   __device__ __forceinline__ float t_of(float x) const { return __fmul_rn(__fsub_rn(m, x), c); }
   __device__ __forceinline__ float t_of(u64 entry) const { return t_of(R::value_of(~(uint32_t)(entry >> 32))); }
@@ -492,13 +500,13 @@ struct Sampler {
     write(id, 0.0f - (t * 0.69314718055994531f + log1pf((float)(total - (1ull << 40)) * 0x1p-40f)), kept);
   }
 
-  // Tokens with nearest <= t < beyond into the first block's list; how many there were.  The weights of all tokens
-  // with t < near are summed over the group into *sum.
-  template <bool kSum>
-  __device__ int collect(float nearest, float beyond, float near, u64 *sum) {
+  // Tokens with nearest <= t < beyond into the first block's list; how many there were.  The weights and the number of all
+  // tokens with t < near are summed over the group into sum; kChunks: the weights by chunks, too.
+  template <bool kSum, bool kChunks>
+  __device__ int collect(float nearest, float beyond, float near, u64 (*sum)[2]) {
     if (threadIdx.x == 0) s->collected = 0;
     g.sync();
-    u64 v[1] = {0};
+    u64 v[2] = {0, 0};
     Weights w;
     for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
       uint32_t found = 0;  // by piece and element
@@ -520,7 +528,10 @@ struct Sampler {
         }
       }
       if (kSum) {
-        v[0] += w.sum();
+        const u64 all = w.sum();
+        v[0] += all;
+        v[1] += w.tokens();
+        if (kChunks) put_chunk(chunk, all);
         w = Weights();
       }
       // one addition to the counter for a warp (one for each token took ten times as long as all else)
@@ -540,8 +551,9 @@ struct Sampler {
       }
     });
     if (kSum) {
-      g.template all<1>(v);
-      *sum = v[0];
+      g.template all<2>(v);
+      (*sum)[0] = v[0];
+      (*sum)[1] = v[1];
     }
     g.sync();
     int count = s->collected;
@@ -579,16 +591,16 @@ struct Sampler {
   template <typename F>
   __device__ __forceinline__ void with_items(int count, const F &f) const {
     const auto weight = [&](u64 entry) { return weight_of(t_of(entry)); };
-    if (count <= 2 * kThreads) {
-      Items<2> items(list, count, s, weight);
+    if (count <= kList / 2) {
+      Items<kList / 2 / kThreads, kThreads> items(list, count, s, weight);
       f(items);
     } else {
-      Items<kList / kThreads> items(list, count, s, weight);
+      Items<kList / kThreads, kThreads> items(list, count, s, weight);
       f(items);
     }
   }
 
-  // draw_from_list for up to kThreads tokens, one of a thread's: each against all others, which gives its place and the
+  // draw_from_list for up to kShort tokens, one of a thread's: each against all others, which gives its place and the
   // weight before it, in the order of the tokens and, of those kept, by id.
   __device__ void draw_from_short_list(int count, u64 total) const {
     struct alignas(16) Item {
@@ -657,7 +669,7 @@ struct Sampler {
   // The first block: cuts the list, which holds all tokens down to some one, and draws from it.  s->total says whether
   // it holds top_p of `total` (0: of its first top_k).
   __device__ void draw_from_list(int count, u64 total) const {
-    if (count <= kThreads) return draw_from_short_list(count, total);
+    if (count <= kShort) return draw_from_short_list(count, total);
     with_items(count, [&](auto &items) {
       u64 last = ~0ull;  // of the entries that are kept
       if (a.top_k && a.top_k < count) last = items.template reach<false>((u64)a.top_k, id_bits());
@@ -726,7 +738,7 @@ struct Sampler {
     const auto mass = [&](int i) { return kWeights ? weight_of((i + 0.5f) / kBinsOfOne) * bins[i] : (u64)bins[i]; };
     u64 mine = 0, all;
     for (int i = first; i < last; ++i) mine += mass(i);
-    const u64 begin = block_scan(mine, s, &all);
+    const u64 begin = block_scan<kWarps>(mine, s, &all);
     u64 before = begin;
     for (int i = first; i < last; ++i) {
       if (i == from) s->total = before;
@@ -798,13 +810,23 @@ struct Sampler {
       for (int j = 0; j < 2; ++j)
         asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(bin[j]) : "r"(remote(smem_addr(&s->bins[j]), 0)) : "memory");
       const float nearest = (float)bin[0] / kBinsOfOne, beyond = (float)(bin[1] + 1) / kBinsOfOne;
-      const int count = collect<kWeights>(nearest, beyond, nearest, &above);
+      u64 sum[2] = {0, 0};
+      const int count = collect<kWeights, kWeights>(nearest, beyond, nearest, &sum);
+      if (kWeights) above = sum[0];
       if (count > kList) break;
       from = bin[0];
       if (kWeights && above >= need) continue;  // the cut is nearer
       if (g.rank == 0) find_in_list<kWeights>(count, need - above);
       const u64 entry = told();
-      if (entry != ~0ull) return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
+      if (entry != ~0ull) {
+        if (kWeights) {
+          last_count = count;
+          last_nearest = nearest;
+          last_above[0] = sum[0];
+          last_above[1] = sum[1];
+        }
+        return Cut{~(uint32_t)(entry >> 32), (int)(uint32_t)entry};
+      }
       from = bin[1] + 1;
       if (g.rank == 0) above += s->held;
       g.sync();
@@ -855,22 +877,22 @@ struct Sampler {
   __device__ __forceinline__ void put_chunk(int chunk, u64 sum) const {
     sum = warp_sum(sum);
     if ((threadIdx.x & 31) == 0)
-      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(smem_addr(list), 0) + 8u * (uint32_t)chunk), "l"(sum) : "memory");
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(smem_addr(sums), 0) + 8u * (uint32_t)chunk), "l"(sum) : "memory");
   }
   // The first block: the chunk in which the sum passes `place`, and the sum before it, in s->chunk and s->total.
   __device__ void find_chunk(u64 place) const {
     const int chunks = (row.pieces - 1) / kChunkPieces + 1, per = (chunks - 1) / kThreads + 1;
     const int from = min(chunks, (int)threadIdx.x * per), to = min(chunks, from + per);
     u64 mine = 0, all;
-    for (int i = from; i < to; ++i) mine += list[i];
+    for (int i = from; i < to; ++i) mine += sums[i];
     if (threadIdx.x == 0) s->chunk = 0;
-    u64 before = block_scan(mine, s, &all);
+    u64 before = block_scan<kWarps>(mine, s, &all);
     for (int i = from; i < to; ++i) {
-      if (before <= place && place < before + list[i]) {
+      if (before <= place && place < before + sums[i]) {
         s->chunk = i;
         s->total = before;
       }
-      before += list[i];
+      before += sums[i];
     }
     __syncthreads();
   }
@@ -947,6 +969,33 @@ struct Sampler {
     return w;
   }
 
+  // draw_from_row after a find_cut that collected the cut's tokens: all nearer ones are kept, and some of these.
+  __device__ void draw_from_parts(const Cut &cut) {
+    if (g.rank != 0) return;
+    u64 v[2] = {0, 0};
+    for (int i = threadIdx.x; i < last_count; i += kThreads) {
+      const int id = (int)(uint32_t)list[i];
+      if (t_of(list[i]) > farthest || !cut.keeps(~(uint32_t)(list[i] >> 32), id)) continue;
+      const u64 w = weight_of(t_of(list[i]));
+      v[0] += w;
+      ++v[1];
+      atomicAdd(&sums[(id + row.shift) / R::kN / kChunkPieces], w);
+    }
+    sum_in_block(v);  // and no sum is added to any more
+    const u64 place = place_of(a.u[index], last_above[0] + v[0]);
+    draw_at(place, last_above[0] + v[0], (int)(last_above[1] + v[1]),
+            [&](float x, float t, int id) { return t <= farthest && cut.keeps(R::key(x), id); });
+  }
+  // The first block: the token at which the sum, by the chunks' sums and then that of what keeps(x, t, id) takes, passes
+  // `place`.
+  template <typename F>
+  __device__ void draw_at(u64 place, u64 total, int kept, const F &keeps) {
+    find_chunk(place);
+    if (threadIdx.x < 32)
+      find_token(place, [&](float x, int id) { return keeps(x, t_of(x), id) ? weight_of(t_of(x)) : 0; },
+                 [&](int id, float x) { write_token(id, t_of(x), total, kept); });
+  }
+
   // Draws from all tokens that the cut and min_p keep.
   template <bool kCut>
   __device__ void draw_from_row(const Cut &cut) {
@@ -955,7 +1004,7 @@ struct Sampler {
     const float above = R::value_of(cut.key);
     float from = R::value_of(cut.key - 1);
     if (from == 0.0f) from = R::value_of(cut.key - 2);  // past -0, which is +0
-    g.sync();  // the list was read
+    g.sync();  // the chunks' sums were read
     u64 v[2] = {0, 0};
     for_row(row, g, [&](int chunk, const uint4 (&p)[kEach]) {
       Weights w;
@@ -978,11 +1027,7 @@ struct Sampler {
     g.template all<2>(v);
     g.sync();
     if (g.rank != 0) return;
-    const u64 place = place_of(a.u[index], v[0]);
-    find_chunk(place);
-    if (threadIdx.x < 32)
-      find_token(place, [&](float x, int id) { return keeps(x, t_of(x), id) ? weight_of(t_of(x)) : 0; },
-                 [&](int id, float x) { write_token(id, t_of(x), v[0], (int)v[1]); });
+    draw_at(place_of(a.u[index], v[0]), v[0], (int)v[1], keeps);
   }
 
   __device__ void run() {
@@ -1020,14 +1065,16 @@ struct Sampler {
     const int want = top_k ? a.top_k : 256, share = (want - 1) / g.size + 1;
     u64 total = 0, held = 0;  // of the row, and of what was listed, of weights
     int listed = 0;           // the steps of these
-    if (share <= kThreads * kEach / 2) {
-      u64 least[1] = {0xFFFFull - cell_bound(upper, share, s)};
+    if (share <= kList / 2) {
+      u64 least[1] = {0xFFFFull - cell_bound<kWarps>(upper, share, s)};
       g.template all<1, true>(least);
       const uint32_t bound = max((uint32_t)(0xFFFFull - least[0]) << (R::kBits - 16), R::kNothing + 1);
       const float t = t_of(R::value_of(bound));
       const int step = t < kFarthest ? (int)step_of(t) + 1 : kBins;  // whole steps, so that what they hold is known later
       const float beyond = step < kBins ? (float)step / kBinsOfOne : past;
-      const int count = top_k ? collect<false>(0.0f, beyond, 0.0f, nullptr) : collect<true>(0.0f, beyond, past, &total);
+      u64 sum[2] = {0, 0};
+      const int count = top_k ? collect<false, false>(0.0f, beyond, 0.0f, nullptr) : collect<true, false>(0.0f, beyond, past, &sum);
+      total = sum[0];
       if (count <= kList) {
         if (g.rank == 0) draw_from_list(count, total);
         if (told()) return;
@@ -1056,33 +1103,39 @@ struct Sampler {
       // among the first top_k, whose weight is at least what is needed
       cut = find_cut<true>((u64)ceil((double)sum[0] * (double)a.top_p), listed, held);
     }
-    draw_from_row<true>(cut);
+    if (top_p && last_count >= 0 && farthest >= last_nearest) draw_from_parts(cut);
+    else draw_from_row<true>(cut);
   }
 };
 
+constexpr int kSharedBytes = ((int)sizeof(Shared) + 15) / 16 * 16;
+template <typename T>
+constexpr int smem_of(int vocab) {  // and one chunk more, as a row may begin within a piece
+  return kSharedBytes + 8 * (2 * kList + (vocab - 1) / (kChunkPieces * Row<T>::kN) + 2);
+}
+
 // kPerSm: blocks that an SM holds, two where rows alone fill the GPU; one has twice the registers.
-template <typename T, int kPerSm>
+template <typename T, int kThreads, int kPerSm>
 __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(SampleArgs a, float c, float farthest, int size) {
   extern __shared__ __align__(16) char smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  u64 *list = reinterpret_cast<u64 *>(smem);
-  Shared *s = reinterpret_cast<Shared *>(list + kChunksMost);
-  Group g{size, (int)blockIdx.x % size, 0, s};
+  Shared *s = reinterpret_cast<Shared *>(smem);
+  u64 *list = reinterpret_cast<u64 *>(smem + kSharedBytes);
+  Group<kThreads / 32> g{size, (int)blockIdx.x % size, 0, s};
   const int index = (int)blockIdx.x / size;
   const Row<T> row(a.logits, a.row, index, a.vocab);
   if (size > 1) g.sync();  // no block writes to one that has not begun
-  Sampler<T> sampler{a, row, g, s, list, list + kList, 0.0f, c, farthest, index};
+  Sampler<T, kThreads> sampler{a, row, g, s, list, list + kList, list + 2 * kList, 0.0f, c, farthest, index};
   sampler.run();
   if (size > 1) g.sync();  // or to one that has ended
 }
 
-template <typename T, int kPerSm>
+template <typename T, int kThreads, int kPerSm>
 cudaError_t launch(const SampleArgs &a, int size, cudaStream_t s) {
-  static_assert((COPES_MAX_SAMPLE_VOCAB - 1) / (kChunkPieces * 4) + 2 <= kChunksMost, "room for fp32's chunks");
-  constexpr int kSmem = kChunksMost * 8 + (int)sizeof(Shared);
-  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two blocks of an SM");
-  cudaError_t e = allow_smem((const void *)sample_kernel<T, kPerSm>, kSmem, kSmem);
+  constexpr int kMost = smem_of<T>(COPES_MAX_SAMPLE_VOCAB);
+  static_assert(kPerSm * (kMost + 1024) <= 228 * 1024, "as many blocks on an SM");
+  cudaError_t e = allow_smem((const void *)sample_kernel<T, kThreads, kPerSm>, kMost, kMost);
   if (e != cudaSuccess) return e;
   const float c = a.scale * 1.44269504088896340736f;
   const float farthest = a.min_p > 0.0f ? fminf((float)-log2((double)a.min_p), kFarthest) : kFarthest;
@@ -1098,8 +1151,8 @@ cudaError_t launch(const SampleArgs &a, int size, cudaStream_t s) {
   cfg.stream = s;
   cfg.gridDim = dim3((unsigned)a.n * size);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
-  return cudaLaunchKernelEx(&cfg, sample_kernel<T, kPerSm>, a, c, farthest, size);
+  cfg.dynamicSmemBytes = smem_of<T>(a.vocab);
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads, kPerSm>, a, c, farthest, size);
 }
 
 }  // namespace
@@ -1110,7 +1163,7 @@ template <typename T>
 static cudaError_t by_rows(const SampleArgs &a, cudaStream_t s) {
   int size = 1;
   while (size < kMaxCluster && (int64_t)a.n * size * 2 <= 152) size *= 2;
-  return a.n <= 152 ? launch<T, 1>(a, size, s) : launch<T, 2>(a, 1, s);
+  return a.n <= 152 ? launch<T, 512, 1>(a, size, s) : launch<T, 512, 2>(a, 1, s);
 }
 
 cudaError_t launch_sample_tokens(int dtype, const SampleArgs &a, cudaStream_t s) {
