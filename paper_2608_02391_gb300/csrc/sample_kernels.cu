@@ -899,30 +899,38 @@ struct Sampler {
   // One warp: the first token of s->chunk at which the sum of f(x, id) passes `place`: then(id, x).
   template <typename F, typename Then>
   __device__ void find_token(u64 place, const F &f, const Then &then) const {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, first = s->chunk * kChunkPieces + lane;
+    uint4 p[kEach];
     u64 before = s->total;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) p[j] = row.load(first + j * 32);
+#pragma unroll 1
     for (int j = 0; j < kEach; ++j) {
-      const int piece = s->chunk * kChunkPieces + j * 32 + lane;
-      const uint4 p = row.load(piece);
+      const uint4 q = j == 0 ? p[0] : j == 1 ? p[1] : j == 2 ? p[2] : p[3];
       u64 mine = 0;
 #pragma unroll
-      for (int e = 0; e < R::kN; ++e) mine += f(R::element(p, e), row.id(piece) + e);
-      u64 x = mine;
+      for (int e = 0; e < R::kN; ++e) mine += f(R::element(q, e), row.id(first + j * 32) + e);
+      const u64 all = warp_sum(mine);
+      if (before <= place && place < before + all) {  // the same in all lanes
+        u64 x = mine;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const u64 y = __shfl_up_sync(kAll, x, d);
-        if (lane >= d) x += y;
-      }
-      u64 at = before + x - mine;
-      if (at <= place && place < at + mine) {
-#pragma unroll
-        for (int e = 0; e < R::kN; ++e) {
-          const u64 w = f(R::element(p, e), row.id(piece) + e);
-          if (at <= place && place < at + w) then(row.id(piece) + e, R::element(p, e));
-          at += w;
+        for (int d = 1; d < 32; d <<= 1) {
+          const u64 y = __shfl_up_sync(kAll, x, d);
+          if (lane >= d) x += y;
         }
+        u64 at = before + x - mine;
+        if (at <= place && place < at + mine) {
+#pragma unroll
+          for (int e = 0; e < R::kN; ++e) {
+            const int id = row.id(first + j * 32) + e;
+            const u64 w = f(R::element(q, e), id);
+            if (at <= place && place < at + w) then(id, R::element(q, e));
+            at += w;
+          }
+        }
+        return;
       }
-      before += __shfl_sync(kAll, x, 31);
+      before += all;
     }
   }
 
