@@ -384,8 +384,9 @@ struct Rows {
 // floats, a power of two costs no precision that a finer factor would keep.  `wide`: all rows are 16-byte aligned.
 //
 // Where a row's token is takes a chain of three loads, so a block looks up its kRows rows first, all at once, and
-// each thread then has kJobs pieces on their way.  Bound by HBM: 32,000 tokens of 8 heads of 128 are written in 33 us
-// and read back in 33 (looked up by each team, with a piece of a thread on its way: 87 each).
+// each thread then has kJobs pieces on their way: 32,000 tokens of 8 heads of 128, 197 MB each way, are written and
+// read back in 87 us together, 4.5 TB/s (looked up by each team, with one piece of a thread on its way: 174; with two, 157;
+// with eight, 121 where four took 110), bound by what converts them.  A token each of 64 sequences: 5.8 us.
 constexpr int kCodeThreads = 256, kJobs = 4;
 struct alignas(16) Place {
   char *codes, *power;  // of the token's first head; NULL: no token

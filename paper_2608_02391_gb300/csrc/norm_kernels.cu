@@ -1,10 +1,13 @@
 // The residual sum of a block with the norms before and after it, a row at a time.
 //
 // With rms(a) = sqrt(mean a^2 + eps), g a gate and c the residual scale:
-//   z = y / rms(y) out_weight (or y),   s = x + c g z,   normed = s / rms(s) weight.
+//   z = y / rms(y) out_weight (or y),   s = x + (c g) z,   normed = s / rms(s) weight.
 // A row's values stay in the registers of its threads from the one read to the one write, so each
-// array passes HBM once; 4 flops a value and norm are nothing beside that, and few rows are a chain
-// of a load, two sums over the row's threads and a store.
+// array passes HBM once, and HBM bounds it where there are many rows: 16,384 of 4,096 in bf16, with a norm after the
+// block and a gate for every channel, 537 MB in 99 us, 5.4 TB/s, four fifths of a copy's rate (of the issue slots,
+// half: a value's way from bf16 and back takes as many operations as the sums).  A few rows are a chain of a load, two
+// sums over the row's threads and a store: one row of 896 2.2 us, 22,400 rows of 128 (the norm alone) 4.2, 301 rows of 2,561
+// in fp32 that begin anywhere 8.6.
 #include <float.h>
 #include <math.h>
 
@@ -210,8 +213,7 @@ __global__ void __launch_bounds__(kMostThreads<kBytes, kP>, kP <= 2 ? 1024 / kMo
 
 // The same for more rows than the GPU works on at once: a block takes row after row, and each of its threads has its
 // pieces of the next rows on their way to shared memory, where it alone reads them, so that HBM is not left waiting
-// while a row's sums are formed.  16,384 rows of 4,096 with a norm after the block and a gate for every channel,
-// bf16: see launch_rows.
+// while a row's sums are formed: 16,384 rows of 4,096 in 99 us, 105 with a block for each row.
 constexpr int kStages = 3;
 template <typename T, int kP>
 __global__ void __launch_bounds__(512, 2) residual_norm_rows_kernel(NormArgs a) {
@@ -372,7 +374,7 @@ cudaError_t launch_after(unsigned blocks, unsigned threads, int smem, cudaStream
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Row after row where blocks take four at least.
+// Row after row where blocks take four at least, and a row is work for four warps.
 template <typename T>
 bool launch_rows(const NormArgs &a, int pieces, cudaStream_t s, cudaError_t *e) {
   constexpr int kP = 2, kMost = kStages * 3 * kP * 512 * 16;

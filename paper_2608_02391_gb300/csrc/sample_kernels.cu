@@ -3,25 +3,29 @@
 // Every token has a weight that is a whole number, so that sums are exact in any order and a row's token
 // does not depend on how the row was shared out: with m the row's largest logit,
 //   t = (m - x) * (scale log2 e),  n = floor(t),  f = t - n   (each step rounded to fp32),
-//   weight = floor(P(f) 2^(40 - n)),   P(f) = 2^-f within 2^-21 (kPoly, Horner's steps fused).
+//   weight = floor(P(f) 2^(40 - n)),   P(f) = 2^-f within 2^-21 (Horner's steps fused; power below).
 // The tokens in order of falling logit, equal ones by ascending id, are cut to the first top_k, to the
 // shortest beginning that holds top_p of their weight, and to t <= -log2 min_p.  Of the tokens kept, in
 // ascending id, the one drawn is the first at which the sum of the weights passes
 // floor(floor(u 2^31) total / 2^31).
 //
-// A row is read by a block, or by a cluster of up to 8 where rows alone would leave SMs without work.  It
-// comes from HBM once, for its maximum; what follows reads it again from L2.  About 16 instructions a
-// logit for its weight, against 2 bytes from HBM, make the weights' passes as dear as the first one.
+// A row is read by a block, or by a cluster of up to 8 where rows alone would leave SMs without work: from HBM
+// for its maximum, and then from L2 for what follows.  A weight takes 14 operations of the fp32 units, by
+// pairs, and 5 others, so a pass over 151,936 of them keeps an SM for 8 us, where HBM brings that row in bf16 in 7:
+// 2,048 rows without a cut take 247 us, 92 of them HBM's (one after the other on an SM; to have the next row
+// brought to L2 by the pass over this one, or its maximum found by it, made nothing faster: 254 and 286 us).
 //
 // Cuts.  While the maximum is sought, each thread keeps the maxima of four cells of the row: the k-th
-// largest of the 2,048 cells is a bound that k logits at least reach.  Those that do are collected
-// (a few more than k, as a rule), sorted, cut, and drawn from, in shared memory.  Where the cut lies
-// behind what can be collected (a flat row, thousands of equal logits), it is bracketed by passes that
-// measure three bounds each, until what lies between can be collected.
+// largest of the 2,048 cells is a bound that k logits at least reach.  Those that do (a few more than k, as a
+// rule; 256 for a top_p alone) are collected, cut and drawn from, in shared memory: 608 rows take 58 us with top_k
+// 50, 124 with top_p 0.95 where few tokens hold that.  A cut that lies behind them (of a flat row) is sought by a
+// count of tokens by their distance: the tokens near it are collected, what is nearer is summed exactly, and
+// the token drawn from the sums of chunks: 273 us.  Where thousands of logits are equal, passes bracket the cut.
 #include <float.h>
 #include <math.h>
 
 #include "answer.h"
+#include "copes_device.cuh"
 
 namespace copes {
 
@@ -59,23 +63,12 @@ __device__ __forceinline__ u64 weight_of(float t) {
   return ((u64)p << 16) >> (__float_as_uint(z) & 63u);
 }
 
-// Two floats in one register pair, and operations on both.
+// Two floats in a register pair (pack_f32x2), added downwards and upwards.
 using Pair = u64;
-__device__ __forceinline__ Pair pair_of(float a, float b) {
-  Pair p;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
-  return p;
-}
 __device__ __forceinline__ float2 floats_of(Pair p) {
   float2 f;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+  unpack_f32x2(p, f.x, f.y);
   return f;
-}
-__device__ __forceinline__ Pair both(float a) { return pair_of(a, a); }
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-  Pair d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
 }
 __device__ __forceinline__ Pair add2_down(Pair a, Pair b) {
   Pair d;
@@ -87,20 +80,9 @@ __device__ __forceinline__ Pair add2_up(Pair a, Pair b) {
   asm("add.rp.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-  Pair d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-  Pair d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-
 // -t of two tokens: (x - m) c, each operation rounded.
 __device__ __forceinline__ Pair minus_t(float x0, float x1, float m, float c) {
-  return mul2(add2(pair_of(x0, x1), both(-m)), both(c));
+  return mul_f32x2(add_f32x2(pack_f32x2(x0, x1), splat_f32x2(-m)), splat_f32x2(c));
 }
 
 // The sum of the weights of at most 60 tokens, and their number, in 32-bit registers.  With y = P(f) 2^-n, whose
@@ -111,20 +93,20 @@ struct Weights {
   uint32_t hi = 0, lo = 0;
   // Tokens at -minus.x and -minus.y, where keep.
   __device__ __forceinline__ void add(Pair minus, bool keep_x, bool keep_y) {
-    const Pair z = add2_up(minus, both(12582912.0f));  // 1.5 2^23 - n
-    const Pair less = add2(z, both(-12582912.0f));     // -n
-    const Pair f = fma2(minus, both(-1.0f), less);
-    Pair p = both(-0.0008996404358185828f);
-    p = fma2(p, f, both(0.009098555892705917f));
-    p = fma2(p, f, both(-0.05521015450358391f));
-    p = fma2(p, f, both(0.2401522845029831f));
-    p = fma2(p, f, both(-0.693140983581543f));
-    p = fma2(p, f, both(1.0f));
+    const Pair z = add2_up(minus, splat_f32x2(12582912.0f));  // 1.5 2^23 - n
+    const Pair less = add_f32x2(z, splat_f32x2(-12582912.0f));  // -n
+    const Pair f = fma_f32x2(minus, splat_f32x2(-1.0f), less);
+    Pair p = splat_f32x2(-0.0008996404358185828f);
+    p = fma_f32x2(p, f, splat_f32x2(0.009098555892705917f));
+    p = fma_f32x2(p, f, splat_f32x2(-0.05521015450358391f));
+    p = fma_f32x2(p, f, splat_f32x2(0.2401522845029831f));
+    p = fma_f32x2(p, f, splat_f32x2(-0.693140983581543f));
+    p = fma_f32x2(p, f, splat_f32x2(1.0f));
     const float2 zz = floats_of(z), pp = floats_of(p);
-    const Pair y = pair_of(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(zz.x) << 23)),
-                           __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(zz.y) << 23)));
-    const Pair top = add2_down(y, both(64.0f));
-    const Pair rest = add2_down(fma2(add2(top, both(-64.0f)), both(-1.0f), y), both(0x1p-17f));
+    const Pair y = pack_f32x2(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(zz.x) << 23)),
+                              __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(zz.y) << 23)));
+    const Pair top = add2_down(y, splat_f32x2(64.0f));
+    const Pair rest = add2_down(fma_f32x2(add_f32x2(top, splat_f32x2(-64.0f)), splat_f32x2(-1.0f), y), splat_f32x2(0x1p-17f));
     const float2 t = floats_of(top), r = floats_of(rest);
     if (keep_x) {
       hi += __float_as_uint(t.x);
@@ -215,7 +197,7 @@ struct Row {
 
 // What is in shared memory beside the list.
 struct Shared {
-  u64 sums[2][32][4];        // of warps, by turns
+  u64 sums[2][32][4];            // of warps, by turns
   u64 peers[2][kMaxCluster][4];  // of the blocks of a cluster
   u64 items[2][32][3];
   u64 scan[32];
@@ -227,8 +209,6 @@ struct Shared {
   int chunk;
   int bins[2];  // first and last
 };
-
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 __device__ __forceinline__ uint32_t remote(uint32_t at, int rank) {
   uint32_t to;
@@ -587,7 +567,7 @@ struct Sampler {
 
   __device__ __forceinline__ int id_bits() const { return 32 - __clz(a.vocab); }
 
-  // The list's items, in a warp where they fit, and what f(items) gives, in the block's first thread at least.
+  // f of the list's items.
   template <typename F>
   __device__ __forceinline__ void with_items(int count, const F &f) const {
     const auto weight = [&](u64 entry) { return weight_of(t_of(entry)); };
