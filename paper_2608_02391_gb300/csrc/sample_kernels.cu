@@ -17,10 +17,10 @@
 //
 // Cuts.  While the maximum is sought, each thread keeps the maxima of four cells of the row: the k-th
 // largest of the 2,048 cells is a bound that k logits at least reach.  Those that do (a few more than k, as a
-// rule; 256 for a top_p alone) are collected, cut and drawn from, in shared memory: 608 rows take 58 us with top_k
-// 50, 124 with top_p 0.95 where few tokens hold that.  A cut that lies behind them (of a flat row) is sought by a
+// rule; 128 for a top_p alone) are collected, cut and drawn from, in shared memory: 608 rows take 60 us with top_k
+// 50, 103 with top_p 0.95 where few tokens hold that.  A cut that lies behind them (of a flat row) is sought by a
 // count of tokens by their distance: the tokens near it are collected, what is nearer is summed exactly, and
-// the token drawn from the sums of chunks: 273 us.  Where thousands of logits are equal, passes bracket the cut.
+// the token drawn from the sums of chunks: 265 us.  Where thousands of logits are equal, passes bracket the cut.
 #include <float.h>
 #include <math.h>
 
@@ -1050,7 +1050,7 @@ struct Sampler {
     if (!top_k && !top_p) return draw_from_row<false>(Cut{0, 0});
     // what the cells' bound collects
     const float past = __uint_as_float(__float_as_uint(kFarthest) + 1);
-    const int want = top_k ? a.top_k : 256, share = (want - 1) / g.size + 1;
+    const int want = top_k ? a.top_k : 128, share = (want - 1) / g.size + 1;
     u64 total = 0, held = 0;  // of the row, and of what was listed, of weights
     int listed = 0;           // the steps of these
     if (share <= kList / 2) {
@@ -1146,7 +1146,8 @@ cudaError_t launch(const SampleArgs &a, int size, cudaStream_t s) {
 }  // namespace
 
 // Blocks of a row: as many as SMs there are for it.  96 rows of 151,936 in bf16, us with a block on an SM and with two
-// blocks of a row (two to an SM): uncut 22 and 26, the first 50 17 and 19, top_p of flat rows 98 and 110.
+// blocks of a row, two to an SM, as the kernel was then: uncut 22 and 26, the first 50 17 and 19, top_p of flat rows 98
+// and 110.  (1,024 threads on an SM: one row 15.5 instead of 12.7, 96 rows the same.)
 template <typename T>
 static cudaError_t by_rows(const SampleArgs &a, cudaStream_t s) {
   int size = 1;
