@@ -10,10 +10,11 @@
 // floor(floor(u 2^31) total / 2^31).
 //
 // A row is read by a block, or by a cluster of up to 8 where rows alone would leave SMs without work: from HBM
-// for its maximum, and then from L2 for what follows.  A weight takes 14 operations of the fp32 units, by
-// pairs, and 5 others, so a pass over 151,936 of them keeps an SM for 8 us, where HBM brings that row in bf16 in 7:
-// 2,048 rows without a cut take 247 us, 92 of them HBM's (one after the other on an SM; to have the next row
-// brought to L2 by the pass over this one, or its maximum found by it, made nothing faster: 254 and 286 us).
+// for its maximum, and then from L2 for what follows.  A weight takes 13 operations of the fp32 units, by
+// pairs, and 5 others, so a pass over 151,936 of them keeps an SM for 14 us, where HBM brings that row in bf16 in 7:
+// 2,048 rows without a cut take 237 us, 190 of them these passes, in which one of an SM's two blocks computes while the
+// other reads (to have the next row brought to L2 by the pass over this one, or its maximum found by it, or the second
+// blocks begin later, made nothing faster).
 //
 // Cuts.  While the maximum is sought, each thread keeps the maxima of four cells of the row: the k-th
 // largest of the 2,048 cells is a bound that k logits at least reach.  Those that do (a few more than k, as a
@@ -87,8 +88,9 @@ __device__ __forceinline__ Pair minus_t(float x0, float x1, float m, float c) {
 
 // The sum of the weights of at most 60 tokens, and their number, in 32-bit registers.  With y = P(f) 2^-n, whose
 // bits are P's less n in the exponent, a weight is floor(y 2^40): 2^23 floor(y 2^17), which is what adding 64
-// downwards leaves in the last bits, and floor(rest 2^40), by 2^-17 likewise.  The upper 9 bits of 64's, 133 each,
-// count the tokens.  (With 64-bit shifts and additions, and each token for itself, 2,048 rows of 151,936 took 377 us.)
+// downwards leaves in the last bits, and floor(rest 2^40), by 2^-17 likewise (2^-17 less the upper part is exact).
+// The upper 9 bits of 64's, 133 each, count the tokens.  (With 64-bit shifts and additions, and each token for itself,
+// 2,048 rows of 151,936 took 377 us; with the upper part taken from y first, and then 2^-17 added, 250.)
 struct Weights {
   uint32_t hi = 0, lo = 0;
   // Tokens at -minus.x and -minus.y, where keep.
@@ -106,7 +108,7 @@ struct Weights {
     const Pair y = pack_f32x2(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(zz.x) << 23)),
                               __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(zz.y) << 23)));
     const Pair top = add2_down(y, splat_f32x2(64.0f));
-    const Pair rest = add2_down(fma_f32x2(add_f32x2(top, splat_f32x2(-64.0f)), splat_f32x2(-1.0f), y), splat_f32x2(0x1p-17f));
+    const Pair rest = add2_down(fma_f32x2(top, splat_f32x2(-1.0f), splat_f32x2(64.0f + 0x1p-17f)), y);
     const float2 t = floats_of(top), r = floats_of(rest);
     if (keep_x) {
       hi += __float_as_uint(t.x);
