@@ -864,6 +864,7 @@ def residual_norm(x: torch.Tensor, weight: Optional[torch.Tensor], y: Optional[t
     dtype, device = x.dtype, x.device
     x_row, each = x.stride()
     assert x.is_cuda and (each == 1 or hidden == 1)
+    assert (out is None or y is not None) and (normed is None or weight is not None)
     like = _rows_template(n, hidden, dtype, device)
     y_row = gate_row = out_row = normed_row = 0
     y_at = gate_at = out_at = normed_at = weight_at = out_weight_at = None

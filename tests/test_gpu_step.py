@@ -156,6 +156,16 @@ def test_norms_of_many_rows(copes, n, hidden, dtype):
         assert none is None and torch.equal(bits(only), bits(s))
 
 
+def test_outputs_that_a_norm_would_not_write_are_refused(copes):
+    x, w = torch.ones(2, 8, device="cuda"), torch.ones(8, device="cuda")
+    for kw in (dict(out=x.clone()), dict(weight=None, y=x, normed=x.clone())):
+        with pytest.raises(AssertionError):
+            copes.residual_norm(**{**dict(x=x, weight=w), **kw})
+    with pytest.raises(copes.CopesError):
+        copes.residual_norm(x, None)  # nothing to write
+    assert error_bits(copes) == 0
+
+
 def test_norms_of_no_rows_and_of_rows_past_32_bits(copes):
     w = torch.ones(64, device="cuda", dtype=torch.bfloat16)
     s, h = copes.residual_norm(torch.empty(0, 64, device="cuda", dtype=torch.bfloat16), w,
