@@ -842,8 +842,8 @@ def sample_tokens(logits: torch.Tensor, u: torch.Tensor, top_k: int = 0, top_p: 
     dtype = _DTYPE_CODES[logits.dtype]
     like_ids, like_logprob, like_kept = _sample_templates(n, device)
     ids, logprob, kept = _empty(like_ids, stream), _empty(like_logprob, stream), _empty(like_kept, stream)
-    _check(load().copes_sample_tokens(logits.data_ptr(), dtype, n, vocab, row, u.data_ptr(), scale, top_k, top_p,
-                                      min_p, ids.data_ptr(), logprob.data_ptr(), kept.data_ptr(), _stream(stream)))
+    _check(load().copes_sample_tokens(logits.data_ptr(), dtype, n, vocab, row, u.data_ptr(), scale,
+                                      max(-1, min(top_k, vocab)), top_p, min_p, ids.data_ptr(), logprob.data_ptr(), kept.data_ptr(), _stream(stream)))
     return SampledTokens(ids, logprob, kept)
 
 

@@ -273,6 +273,15 @@ def test_drawn_tokens_of_rows_that_nothing_can_be_drawn_from(copes):
     assert r.ids.numel() == 0 and error_bits(copes) == 0
 
 
+def test_a_top_k_past_32_bits_keeps_all(copes):
+    logits, u = torch.randn(3, 500, device="cuda"), torch.rand(3, device="cuda")
+    for top_k in (500, 2**31, 2**32, 2**32 + 5):
+        assert copes.sample_tokens(logits, u, top_k=top_k).kept.tolist() == [500] * 3
+    for top_k in (-1, -2**32):
+        with pytest.raises(copes.CopesError):
+            copes.sample_tokens(logits, u, top_k=top_k)
+
+
 def test_drawn_tokens_do_not_depend_on_the_batch(copes):
     """A row alone, by a cluster of eight blocks, and among hundreds, by one."""
     g = torch.Generator("cuda").manual_seed(8)
