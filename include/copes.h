@@ -522,7 +522,8 @@ int copes_cache_grow(const copes_kv_cache *c, const int32_t *slots, int n, const
  * likewise v; head_dim values in a row) goes to token position[i] of slots[i]; where position
  * is NULL, to the slot's last token, and where slots is NULL, to slot i.  Slots may repeat
  * (a prompt's tokens); of rows that name one token (through a shared page, or twice) each value
- * is one of theirs.  A row that is not a token of its slot is skipped and reported (bit 32). */
+ * is one of theirs (of COPES_E4M3 each code, and each byte: of rows that differ, none may be kept whole).  A row
+ * that is not a token of its slot is skipped and reported (bit 32). */
 int copes_cache_append(const copes_kv_cache *c, int layer, const int32_t *slots, const int32_t *position, int n,
                        const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
                        int64_t v_head, cudaStream_t stream);

@@ -431,6 +431,20 @@ def test_attention_over_8_bits_of_extreme_units(copes):
     assert error_bits(copes) == 0
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_bytes_past_a_sequence_are_not_read(copes, d):
+    cache = cache8(copes, [3, 33], 1, 2, 16, d, seed=d, spare=0, poison=False)
+    q = torch.randn(2, 4, d, device="cuda").bfloat16()
+    out, lse = copes.paged_attention(cache, 0, q, scale=0.01)
+    size, table = 2 * 2 * 16 * d, cache.table.tolist()
+    for page, begin in ((table[0][0], 3), (table[1][2], 1)):
+        cache.pool[page, 0, :size].view(4, 16, d)[:, begin:] = 0xFF
+        cache.pool[page, 0, size:size + 64].view(4, 16)[:, begin:] = 0xFF
+    again = copes.paged_attention(cache, 0, q, scale=0.01)
+    assert torch.isfinite(out).all() and torch.equal(again[0], out) and torch.equal(again[1], lse)
+    assert error_bits(copes) == 0
+
+
 @pytest.mark.parametrize("kv,d,ps", [(2, 64, 16), (3, 16, 5), (5, 80, 7), (8, 128, 16), (1, 256, 33), (2, 48, 1)])
 def test_what_is_written_in_8_bits_is_read_back(copes, kv, d, ps):
     layers, lens = 3, [0, 1, ps, ps + 1, 5 * ps + 2, 40]
@@ -483,6 +497,25 @@ def test_what_is_written_in_8_bits_is_read_back(copes, kv, d, ps):
     assert error_bits(copes) == 32 and not last[0][0].any()  # slot 0 has no token
     want = copes.cache_read(cache, 1, slots=ids(range(1, 6)), position=ids(x - 1 for x in lens[1:]))
     assert torch.equal(last[0][1:].view(torch.int16), want[0].view(torch.int16))
+
+
+def test_rows_that_name_one_token_of_8_bits(copes):
+    """Equal ones are kept, of others each code and byte is one of theirs; read, each gives the token."""
+    cache = cache8(copes, [20, 20], 1, 2, 16, 64, seed=1)
+    x = (torch.randn(300, 2, 2, 64, device="cuda") * 2.0 ** torch.randint(-5, 5, (300, 1, 1, 1), device="cuda")).bfloat16()
+    x[150:] = x[150]
+    slots, position = ids([0] * 150 + [1] * 150), ids([7] * 150 + [19] * 150)
+    copes.cache_append(cache, 0, x[:, 0], x[:, 1], slots=slots, position=position)
+    k, v = copes.cache_read(cache, 0, slots=slots, position=position)
+    assert torch.equal(k, k[[0] * 150 + [150] * 150]) and torch.equal(v, v[[0] * 150 + [150] * 150])
+    assert np.array_equal(f64(k[150]), model.stored(f64(x[150, 0]))[0]) and np.array_equal(f64(v[150]), model.stored(f64(x[150, 1]))[0])
+    size, page = 2 * 2 * 16 * 64, int(cache.table[0, 0])
+    raw = cache.pool[page, 0].cpu().numpy()
+    for which in (0, 1):
+        _, code, power = model.stored(f64(x[:150, which]))
+        there, byte = raw[:size].reshape(2, 2, 16, 64)[which, :, 7], raw[size:size + 64].reshape(2, 2, 16)[which, :, 7]
+        assert (code == there).any(0).all() and (power == byte).any(0).all()
+    assert error_bits(copes) == 0
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
