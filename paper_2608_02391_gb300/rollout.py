@@ -128,7 +128,7 @@ class Decoder:
         place = cache.length[slots.long().clamp_(0, cache.desc.n_slots - 1)] - 1  # a slot past the cache is the calls' to report
         angles = place.double()[:, None] * self.frequencies
         x = weights["embed"][tokens]
-        h = self._norm(x, weights["l0.in_norm"])
+        h = self._norm(x, weights["l0.in_norm" if s.layers else "final_norm"])
         for l in range(s.layers):
             get = lambda name: weights.get(f"l{l}.{name}")
             q, k, v = (torch.nn.functional.linear(h, get(m), get(m + "_bias")).view(n, -1, s.head_dim) for m in "qkv")

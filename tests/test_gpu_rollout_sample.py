@@ -176,3 +176,20 @@ def test_a_visit_rewarded_by_drawn_answers():
     es.round_robin_visit(arena, sub, 0, 0, cfg, layout.d_pad, rewards, evaluate=evaluate)
     copes.check()
     assert ((rewards >= 0) & (rewards <= 1)).all() and not torch.equal(arena.master, before)
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_a_decoder_without_layers(fused):
+    from paper_2608_02391_gb300 import copes, rollout
+    decoder = rollout.Decoder(rollout.Shape(0, 48, 80, 301, 4, 2, 16), fused=fused)
+    cache = copes.KVCache.empty(4, 1, 2, 16, 16, 2, 2, dtype=torch.float32)
+    w = torch.randn(decoder.offsets[-1] + 48, device="cuda")
+    weights = decoder.weights(w)
+    slots, tokens = torch.arange(2, dtype=torch.int32, device="cuda"), torch.tensor([7, 300], device="cuda")
+    logits = decoder.step(weights, cache, slots, tokens)
+    x = w[:301 * 48].view(301, 48).double()
+    h = x[tokens] / torch.sqrt((x[tokens] ** 2).mean(-1, keepdim=True) + 1e-6) * weights["final_norm"].double()
+    # a product off by 10 half steps of 2^-24 at most, its norm among them, and 48 roundings of their sum
+    assert ((logits - h @ x.T).abs() <= 60 * 2.0**-24 * (h.abs() @ x.abs().T)).all()
+    assert decoder.step(weights, cache, slots, tokens, logits=False) is None
+    copes.check()
