@@ -12,16 +12,16 @@
 // A row is read by a block, or by a cluster of up to 8 where rows alone would leave SMs without work: from HBM
 // for its maximum, and then from L2 for what follows.  A weight takes 13 operations of the fp32 units, by
 // pairs, and 5 others, so a pass over 151,936 of them keeps an SM for 14 us, where HBM brings that row in bf16 in 7:
-// 2,048 rows without a cut take 237 us, 190 of them these passes, in which one of an SM's two blocks computes while the
+// 2,048 rows without a cut take 236 us, 190 of them these passes, in which one of an SM's two blocks computes while the
 // other reads (to have the next row brought to L2 by the pass over this one, or its maximum found by it, or the second
 // blocks begin later, made nothing faster).
 //
 // Cuts.  While the maximum is sought, each thread keeps the maxima of four cells of the row: the k-th
 // largest of the 2,048 cells is a bound that k logits at least reach.  Those that do (a few more than k, as a
-// rule; 128 for a top_p alone) are collected, cut and drawn from, in shared memory: 608 rows take 60 us with top_k
-// 50, 103 with top_p 0.95 where few tokens hold that.  A cut that lies behind them (of a flat row) is sought by a
+// rule; 128 for a top_p alone) are collected, cut and drawn from, in shared memory: 608 rows take 57 us with top_k
+// 50, 98 with top_p 0.95 where few tokens hold that.  A cut that lies behind them (of a flat row) is sought by a
 // count of tokens by their distance: the tokens near it are collected, what is nearer is summed exactly, and
-// the token drawn from the sums of chunks: 265 us.  Where thousands of logits are equal, passes bracket the cut.
+// the token drawn from the sums of chunks: 253 us.  Where thousands of logits are equal, passes bracket the cut.
 #include <float.h>
 #include <math.h>
 
@@ -191,6 +191,23 @@ struct Row {
     }
     return before;
   }
+  // Bits of a piece's elements in [low, high], those of its pieces j = 0 .. kEach - 1 apart, and a bit's j kN + e.
+  __device__ __forceinline__ static uint32_t within(const uint4 &p, int j, float low, float high) {
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+    uint32_t found = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 4) {
+        const float x = __uint_as_float(w[e]);
+        if (x >= low && x <= high) found |= 1u << (4 * j + e);
+      } else {
+        const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&w[e]);
+        found |= __hge2_mask(x, __float2bfloat162_rn(low)) & __hle2_mask(x, __float2bfloat162_rn(high)) & 0x10001u << (4 * j + e);
+      }
+    }
+    return found;
+  }
+  __device__ __forceinline__ static int place(int bit) { return sizeof(T) == 4 ? bit : (bit & 15) * 2 + (bit >> 4); }
   __device__ __forceinline__ static float value(uint32_t largest) {
     if constexpr (sizeof(T) == 4) return __uint_as_float(largest);
     else return max_nan(__uint_as_float(largest << 16), __uint_as_float(largest & 0xFFFF0000u));
@@ -482,10 +499,30 @@ struct Sampler {
     write(id, 0.0f - (t * 0.69314718055994531f + log1pf((float)(total - (1ull << 40)) * 0x1p-40f)), kept);
   }
 
+  // The least key with t < bound, of the row's largest or before, sought by a warp's lanes around where it would be without
+  // roundings and then between what that leaves; t falls as keys rise.  (Elements are then compared as they are, in bf16
+  // by pairs: 608 rows with top_k 1,000 110 -> 97 us, flat rows with top_p 0.95 262 -> 253.)
+  __device__ uint32_t first_within(float bound) const {
+    uint32_t lo = R::kNothing, hi = R::key(m);  // not so at lo
+    const uint32_t near = R::key(m - bound / c) - 16;
+    for (bool around = true; hi - lo > 1; around = false) {
+      const auto probe = [&](int i) {
+        return around ? min(max(near + i, lo), hi) : lo + 1 + (uint32_t)((u64)(hi - lo - 1) * i >> 5);
+      };
+      const uint32_t yes = __ballot_sync(kAll, t_of(R::value_of(probe(threadIdx.x & 31))) < bound);
+      const int first = yes ? __ffs(yes) - 1 : 32;
+      const uint32_t above = yes ? probe(first) : hi;
+      if (first) lo = probe(first - 1);
+      hi = above;
+    }
+    return hi;
+  }
+
   // Tokens with nearest <= t < beyond into the first block's list; how many there were.  The weights and the number of all
   // tokens with t < near are summed over the group into sum; kChunks: the weights by chunks, too.
   template <bool kSum, bool kChunks>
   __device__ int collect(float nearest, float beyond, float near, u64 (*sum)[2]) {
+    const float low = R::value_of(first_within(beyond)), high = nearest > 0.0f ? R::value_of(first_within(nearest) - 1) : m;
     if (threadIdx.x == 0) s->collected = 0;
     g.sync();
     u64 v[2] = {0, 0};
@@ -494,20 +531,13 @@ struct Sampler {
       uint32_t found = 0;  // by piece and element
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
-        const bool any = t_of(R::value(R::largest(R::none, p[j]))) < beyond;
 #pragma unroll
         for (int e = 0; kSum && e < R::kN; e += 2) {
           const Pair minus = minus_t(R::element(p[j], e), R::element(p[j], e + 1), m, c);
           const float2 t = floats_of(minus);
           w.add(minus, -t.x < near, -t.y < near);
         }
-        if (!any) continue;
-#pragma unroll
-        for (int e = 0; e < R::kN; e += 2) {
-          const float2 t = floats_of(minus_t(R::element(p[j], e), R::element(p[j], e + 1), m, c));
-          if (-t.x >= nearest && -t.x < beyond) found |= 1u << (j * R::kN + e);
-          if (-t.y >= nearest && -t.y < beyond) found |= 1u << (j * R::kN + e + 1);
-        }
+        if (R::value(R::largest(R::none, p[j])) >= low) found |= R::within(p[j], j, low, high);
       }
       if (kSum) {
         const u64 all = w.sum();
@@ -528,7 +558,7 @@ struct Sampler {
       int at = lane == 31 ? atomicAdd(&s->collected, before) : 0;
       at = __shfl_sync(kAll, at, 31) + before - mine;
       for (; found; found &= found - 1, ++at) {
-        const int bit = __ffs(found) - 1, id = row.id(chunk * kChunkPieces + bit / R::kN * 32 + lane) + bit % R::kN;
+        const int bit = R::place(__ffs(found) - 1), id = row.id(chunk * kChunkPieces + bit / R::kN * 32 + lane) + bit % R::kN;
         if (at < kList) list[at] = (u64)~R::key(row.at(id)) << 32 | (uint32_t)id;
       }
     });
