@@ -607,15 +607,16 @@ class KVCache:
         if heads is None:
             assert pool.dim() == 6 and pool.shape[2] == 2
             heads = tuple(pool.shape[3:])
+            self.dtype = _DTYPE_CODES[pool.dtype]  # bytes without `heads` would have no room for their exponents
         else:
             assert pool.dim() == 3 and pool.dtype == torch.uint8 and pool.shape[2] == self.layer_bytes(*heads)
+            self.dtype = E4M3
         assert table.dim() == 2
         assert length.shape == (table.shape[0],) and refs.shape == (pool.shape[0],)
         for t in (pool, table, length, refs):
             assert t.is_cuda and t.is_contiguous() and t.device == pool.device
         assert all(t.dtype == torch.int32 for t in (table, length, refs))
         self.pool, self.table, self.length, self.refs = pool, table, length, refs
-        self.dtype = E4M3 if pool.dtype == torch.uint8 else _DTYPE_CODES[pool.dtype]
         self.io_dtype = torch.bfloat16 if self.dtype == E4M3 else pool.dtype  # of q, k, v and out
         n_pages, n_layers = pool.shape[:2]
         self.heads = kv, ps, d = heads
