@@ -205,8 +205,9 @@ __device__ __forceinline__ void rebase(float &s, float &h, float m, float M, flo
   s = f * s;
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+// (Not .aligned: that asks for warps whose lanes are together, which after branches by lane nothing but the compiler sees to.)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 // The address of the cluster's first block's copy of a shared variable.
 __device__ __forceinline__ uint32_t in_first(const void *p) {
   uint32_t r;

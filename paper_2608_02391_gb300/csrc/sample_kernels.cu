@@ -246,8 +246,9 @@ struct Group {
     if (size == 1) {
       __syncthreads();
     } else {
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      // (not .aligned: lanes come here from branches of their own, and need not be together)
+      asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
   }
   // v[j] over all threads, by adding or, kMax, as the largest; the same in every thread.

@@ -1,6 +1,8 @@
 """Calls at the edges of a generating step that the host decides: pools of another form, weights of another type than
 the cache, cuts that fp32 rounds away, and what a decoder leaves in a cache where a step fails."""
+import glob
 import os
+import re
 
 import pytest
 import torch
@@ -52,3 +54,12 @@ def test_bytes_are_a_pool_only_with_room_for_their_exponents(copes, monkeypatch)
     for n in (room - 16, 2 * 16 * 16, room + 16):
         with pytest.raises(AssertionError):
             handle(copes, OnGpu(0x1000000, torch.uint8, 4, 1, n), heads=(1, 16, 16))
+
+
+def test_cluster_barriers_take_lanes_one_by_one():
+    """barrier.cluster with .aligned is undefined where a warp's lanes are not together, and lanes come to the kernels' barriers
+    from loops and branches of their own.  Which barrier a kernel asks for is in its source alone."""
+    root = os.path.join(os.path.dirname(__file__), "..", "paper_2608_02391_gb300", "csrc")
+    asked = [b for f in glob.glob(os.path.join(root, "*.cu*")) + glob.glob(os.path.join(root, "*.h"))
+             for b in re.findall(r"barrier\.cluster\.(?:arrive|wait)[.a-z]*", open(f).read())]
+    assert len(asked) >= 4 and not [b for b in asked if "aligned" in b]
