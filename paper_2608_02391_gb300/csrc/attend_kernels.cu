@@ -881,7 +881,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     if constexpr (S::kFp8)
       if (from) {
         const uint8_t *at = reinterpret_cast<const uint8_t *>(c.pool + (uint64_t)p.page * c.page_bytes + a.layer * c.layer_bytes + c.layer_elems +
-                                                              (uint64_t)((p.kv * S::kSides + side) * c.page_size + p.place));
+                                                              (uint64_t)(p.kv * S::kSides + side) * c.page_size + p.place);
         power = at[0] | (uint32_t)at[(uint64_t)c.n_kv_heads * c.page_size] << 8;
       }
     const uint32_t to = stages + stage * S::kStage;
