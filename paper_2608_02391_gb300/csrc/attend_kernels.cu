@@ -58,6 +58,7 @@ __device__ __forceinline__ void flag_error(unsigned bit) { atomicOr(&g_attend_er
 
 constexpr int kSMs = 152;
 constexpr unsigned kAll = 0xffffffffu;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // An element of an 8-bit cache, and what queries and outputs are beside a cache of T.
 struct E4m3 {
@@ -306,6 +307,7 @@ template <typename S>
 struct Queries {
   uint32_t b[S::DP / 16][S::NT][S::kFp32 ? 4 : 2];
   float unit[S::NT][2];
+  bool plain;  // all of these are from 2^-63 to 2^63, with the scale, too, which is in them then
 };
 
 // `wide`: rows of q are aligned to what a lane loads at a time, 4 bytes of bf16 and 16 of fp32.
@@ -360,10 +362,13 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, bool wide, int
 }
 
 // Queries for codes: the largest of a head comes to lie in [2^14, 2^15), so that fp16 holds all of a value of 8 bits
-// down to 2^-32 of it, and 2^-39 of it is lost at most of a smaller one.
+// down to 2^-32 of it, and 2^-39 of it is lost at most of a smaller one.  (From 2^-100 down the unit stays 2^-114, of
+// which bf16's least value is 2^-19: nothing is lost.)
 template <typename S>
-__device__ __forceinline__ void to_units(Queries<S> &q) {
+__device__ __forceinline__ void to_units(Queries<S> &q, float scale) {
+  scale *= kLog2e;
   const int lane = threadIdx.x & 31;
+  bool plain = true;
 #pragma unroll
   for (int j = 0; j < S::NT; ++j) {
     uint32_t most = 0;  // of the finite ones
@@ -377,6 +382,8 @@ __device__ __forceinline__ void to_units(Queries<S> &q) {
     most = max(most, __shfl_xor_sync(kAll, most, 1));
     most = max(most, __shfl_xor_sync(kAll, most, 2));
     const uint32_t power = max(most >> 7, 27u) - 14;  // 127 more than the unit's
+    const float scaled = fabsf(scale * __uint_as_float(power << 23));
+    plain = plain && (!most || (power - 64 <= 126 && scaled >= 0x1p-63f && scaled <= 0x1p63f));
     const float over = __uint_as_float((254 - power) << 23);
 #pragma unroll
     for (int k = 0; k < S::DP / 16; ++k)
@@ -388,6 +395,10 @@ __device__ __forceinline__ void to_units(Queries<S> &q) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) q.unit[j][e] = __uint_as_float(__shfl_sync(kAll, power, ((lane & 3) * 2 + e) * 4) << 23);
   }
+  q.plain = __all_sync(kAll, plain);
+  if (q.plain)
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) q.unit[j][0] *= scale, q.unit[j][1] *= scale;
 }
 
 // One warp's 16 tokens: scores, the running maximum and sum, and the weighted values.
@@ -594,6 +605,24 @@ __device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int l
     key_unit[e] = __uint_as_float((both & 0xFFu) << 23);
     value_unit[e] = __uint_as_float((both >> 8) << 23);
   }
+  // Sums of codes are 0 or between 2^-33 and 2^32, which plain units do not take out of fp32 on the way.  Others may where
+  // the key's, too, would not: one above 1 and one below are multiplied first, exactly.
+  if (q.plain) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int t = 0; t < 2 * kOf; ++t) s[j][t] = s[j][t] * q.unit[j][t & 1] * key_unit[t >> 1];
+  } else {
+    asm volatile("" : "+f"(scale));  // (not to be kept in a register from tile to tile for this)
+    scale *= kLog2e;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int t = 0; t < 2 * kOf; ++t) {
+        const float a = q.unit[j][t & 1], b = key_unit[t >> 1];
+        s[j][t] = ((a < 1.0f) == (b < 1.0f) ? s[j][t] * a * b : s[j][t] * (a * b)) * scale;
+      }
+  }
   bool grown = false;
   float keep[NT][2], over[NT][2], unit[NT][2];
 #pragma unroll
@@ -604,7 +633,7 @@ __device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int l
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < kOf; ++t) {
-        s[j][2 * t + e] = row + 8 * t < left ? s[j][2 * t + e] * q.unit[j][e] * key_unit[t] * scale : -INFINITY;
+        s[j][2 * t + e] = row + 8 * t < left ? s[j][2 * t + e] : -INFINITY;
         top = fmaxf(top, s[j][2 * t + e]);
       }
       top = fmaxf(top, __shfl_xor_sync(kAll, top, 4));
@@ -897,6 +926,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     }
     return power;
   };
+  const float scale = a.scale * kLog2e;  // of log2
   Place next = look_up();
   // The queries of a (row, head group), and, registers permitting, of the next one, asked for a
   // (row, head group) before they are used.
@@ -912,7 +942,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
   Cursor asking = at;  // whose queries were asked for last
   if (at.tile >= at.tiles) next_unit(asking);
   queries_of(asking, q);
-  if constexpr (S::kFp8) to_units(q);
+  if constexpr (S::kFp8) to_units(q, a.scale);
   if constexpr (kNextToo) {
     next_unit(asking);
     if (count > at.tiles - at.tile) queries_of(asking, q_next);
@@ -933,7 +963,6 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
 
   Running<S> r;
   r.clear();
-  const float scale = a.scale * 1.44269504088896340736f;  // of log2
   constexpr int kD4 = S::kAtOnce / 4;
   const int slot_floats = S::kHeads * (D + 2);
   Split begun{-1, 0, 0, 0};
@@ -950,7 +979,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - member * S::kOwn : 0;
     const uint32_t tile = stages + j % S::kStages * S::kStage;
     if (left > 0) {
-      if constexpr (S::kFp8) warp_tile8<S>(tile, tile + S::kPart, left, scale, q, r, powers[0]);
+      if constexpr (S::kFp8) warp_tile8<S>(tile, tile + S::kPart, left, a.scale, q, r, powers[0]);
       else warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
     }
 #pragma unroll
@@ -964,7 +993,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
       if constexpr (kNextToo) q = q_next;
       next_unit(asking);
       queries_of(asking, kNextToo ? q_next : q);
-      if constexpr (S::kFp8) to_units(q);
+      if constexpr (S::kFp8) to_units(q, a.scale);
     }
 
     // the warps' states together

@@ -1,9 +1,10 @@
-"""A generating step's calls at the edges of what they allow: heads of a page past 2^31 tokens."""
+"""A generating step's calls at the edges of what they allow: heads of a page past 2^31 tokens, queries and keys of any size."""
 import numpy as np
 import pytest
 import torch
 
 import step_model as model
+from test_gpu_step import cache8, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,30 @@ def test_heads_of_a_page_past_2_to_31_tokens(copes):
     finally:
         cache = None
         torch.cuda.empty_cache()
+
+
+# log2 of the queries, of the keys' powers of two, of the scale: scores of some units each
+SIZES = [(0, -3, -9), (60, -66, -6), (120, -120, -12), (110, -113, -9), (100, -100, -12), (-110, 100, -2), (-125, 118, -5), (-129, 118, -1),
+         (-121, -1, 110), (-128, 0, 116), (60, 50, -122), (-60, -50, 98)]
+
+
+@pytest.mark.parametrize("heads,kv,d", [(6, 2, 64), (32, 2, 64), (12, 4, 128), (10, 5, 256)])
+@pytest.mark.parametrize("query,key,scale", SIZES)
+def test_queries_and_keys_of_any_size(copes, query, key, scale, heads, kv, d):
+    """Products of queries and keys that fp32 holds, of factors that are as large and as small as their types hold: a query's
+    values of at least 2^-32 of its largest count whole, in bf16's subnormal numbers, too."""
+    ps, lens = 16, [1, 16, 40, 333, 0, 700]
+    cache = cache8(copes, lens, 1, kv, ps, d, seed=d + heads)
+    size, rng = 2 * kv * ps * d, np.random.default_rng(heads)
+    powers = rng.integers(116, 122, (cache.desc.n_pages, 1, 2, kv, ps))
+    powers[:, :, 0] = key + 127 - rng.integers(0, 6, powers[:, :, 0].shape)
+    powers = np.maximum(powers, 1)
+    cache.pool[:, :, size:size + 2 * kv * ps] = torch.from_numpy(powers.reshape(cache.desc.n_pages, 1, -1).astype(np.uint8)).cuda()
+    g = torch.Generator("cuda").manual_seed(heads)
+    q = (torch.randn(len(lens), heads, d, device="cuda", generator=g, dtype=torch.float64) * 2.0**query).bfloat16()
+    q[:, 0] = 0
+    q[:, 1, 5:] = (q[:, 1, 5:].double() * 2.0**-20).bfloat16()
+    q[1, 2:4] = (q[1, 2:4].double() * 2.0**-30).bfloat16()  # beside others of its kind
+    scale = 2.0**scale
+    check_attention(cache, 0, q, range(len(lens)), scale, *copes.paged_attention(cache, 0, q, scale=scale))
+    copes.check()
