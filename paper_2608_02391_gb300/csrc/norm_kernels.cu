@@ -89,7 +89,7 @@ struct RowSum {
   }
 };
 
-// 1 / rms(a).  Squares past fp32 are summed again of values 2^-80 as large, where eps is nothing.
+// 1 / rms(a).  Squares past fp32 are summed again of values 2^-80 as large, with eps 2^-160 as large.
 template <int kP, int kN, typename Value>
 __device__ __forceinline__ float unit_of(const Value &value, float eps, int hidden, RowSum &sum) {
   float mine = 0.0f;
@@ -119,7 +119,7 @@ __device__ __forceinline__ float unit_of(const Value &value, float eps, int hidd
   for (int p = 0; p < kP; ++p)
 #pragma unroll
     for (int e = 0; e < kN; ++e) mine = fmaf(value(p, e) * less, value(p, e) * less, mine);
-  const float again = rsqrtf(sum(mine) / (float)hidden);
+  const float again = rsqrtf(sum(mine) / (float)hidden + eps * less * less);
   return fine ? u : less * again;  // 2^-128 at least, which has 21 bits
 }
 
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(1024) residual_norm_long_kernel(NormArgs a) {
         for (int e = 0; e < kN; ++e) mine = fmaf(v[e] * first, v[e] * first, mine);
       }
       const float squares = sum(mine);
-      if (first != 1.0f) return first * rsqrtf(squares / (float)a.hidden);
+      if (first != 1.0f) return first * rsqrtf(squares / (float)a.hidden + a.eps * first * first);
       if (squares <= FLT_MAX) return rsqrtf(squares / (float)a.hidden + a.eps);
       first = 0x1p-80f;
     }

@@ -1,10 +1,11 @@
-"""A generating step's calls at the edges of what they allow: heads of a page past 2^31 tokens, queries and keys of any size."""
+"""A generating step's calls at the edges of what they allow: heads of a page past 2^31 tokens, queries and keys of any size,
+norms whose eps counts beside squares past fp32."""
 import numpy as np
 import pytest
 import torch
 
 import step_model as model
-from test_gpu_step import cache8, check_attention
+from test_gpu_step import cache8, check_attention, check_norm
 
 pytestmark = pytest.mark.gpu
 
@@ -74,4 +75,23 @@ def test_queries_and_keys_of_any_size(copes, query, key, scale, heads, kv, d):
     q[1, 2:4] = (q[1, 2:4].double() * 2.0**-30).bfloat16()  # beside others of its kind
     scale = 2.0**scale
     check_attention(cache, 0, q, range(len(lens)), scale, *copes.paged_attention(cache, 0, q, scale=scale))
+    copes.check()
+
+
+@pytest.mark.parametrize("n,hidden", [(3, 64), (2, 4096), (2500, 4096), (2, 8192), (2, 8190), (2, 300_000), (2, 1 << 24)])
+def test_eps_counts_beside_squares_past_fp32(copes, n, hidden):
+    """Squares whose sum is just past fp32, so that their mean is 2e31 and more, and the largest eps, 1e30."""
+    eps = 1e30
+    sign = torch.randint(0, 2, (n, hidden), device="cuda", generator=torch.Generator("cuda").manual_seed(hidden)).float() * 2 - 1
+    x = sign * (1.02 * (torch.finfo(torch.float32).max / hidden) ** 0.5)
+    x[n // 2] *= 0.5  # its sum is not
+    w = torch.linspace(0.5, 1.5, hidden, device="cuda")
+    rows = torch.tensor(sorted({0, n // 2, n - 1} | set(range(0, n, 200))), device="cuda")
+    _, h = copes.residual_norm(x, w, eps=eps)
+    check_norm(None, h[rows], x[rows], w, None, None, None, 1.0, eps)
+    zeros = torch.zeros_like(x)
+    s, h = copes.residual_norm(zeros, w, y=x, out_weight=w, scale=0.5, eps=eps)
+    check_norm(s[rows], h[rows], zeros[rows], w, x[rows], w, None, 0.5, eps)
+    s, h = copes.residual_norm(zeros, w, y=x, eps=eps)
+    check_norm(s[rows], h[rows], zeros[rows], w, x[rows], None, None, 1.0, eps)
     copes.check()
