@@ -153,10 +153,20 @@ class Decoder:
         if min(map(min, sequences)) < 0 or max(map(max, sequences)) >= self.shape.vocab:
             raise ValueError(f"a token outside the vocabulary of {self.shape.vocab} in the {what}s")
 
+    def _check_cache(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache) -> None:
+        """Raises for a cache whose first append would refuse these weights' keys, when it has grown already."""
+        s, (kv, _, d), dtype = self.shape, cache.heads, weights["embed"].dtype
+        if dtype != cache.io_dtype:
+            raise ValueError(f"weights of {dtype} with a cache for {cache.io_dtype}")
+        if s.layers and ((kv, d) != (s.kv_heads, s.head_dim) or cache.desc.n_layers < s.layers):
+            raise ValueError(f"a cache of {cache.desc.n_layers} layers of {kv} heads of {d} for {s.layers} of {s.kv_heads} of {s.head_dim}")
+
     def read(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: Sequence[int],
              prompts: Sequence[Sequence[int]]) -> torch.Tensor:
-        """Writes prompts (one token at least each) into empty slots and returns the logits after each."""
+        """Writes prompts (one token at least each) into empty slots and returns the logits after each.  ValueError, before
+        any work, for a cache that is not one of weights of this type and shape."""
         self._check_tokens("prompt", prompts)
+        self._check_cache(weights, cache)
         device = cache.pool.device
         last = [None] * len(prompts)
         for t in range(max(map(len, prompts))):
@@ -207,8 +217,8 @@ class Decoder:
         """Mean log probability of every answer under the weights w: fp32, the answers of prompt 0,
         then those of prompt 1, ...  The cache's first slots, one for each prompt and each answer, are
         empty before and after.  Prompts or answers without tokens, ids outside the vocabulary, answers without
-        a prompt and what the cache has no room for raise ValueError before any work; what a kernel reports
-        (copes.check), CopesError."""
+        a prompt, a cache for weights of another type or shape and what the cache has no room for raise ValueError
+        before any work; what a kernel reports (copes.check), CopesError."""
         self._check_score(cache, prompts, answers)
         weights, device = self.weights(w), cache.pool.device
         flat = [(i, a) for i, group in enumerate(answers) for a in group]

@@ -3,6 +3,7 @@ the cache, cuts that fp32 rounds away, and what a decoder leaves in a cache wher
 import glob
 import os
 import re
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -63,3 +64,51 @@ def test_cluster_barriers_take_lanes_one_by_one():
     asked = [b for f in glob.glob(os.path.join(root, "*.cu*")) + glob.glob(os.path.join(root, "*.h"))
              for b in re.findall(r"barrier\.cluster\.(?:arrive|wait)[.a-z]*", open(f).read())]
     assert len(asked) >= 4 and not [b for b in asked if "aligned" in b]
+
+
+SHAPE = dict(layers=2, hidden=48, mlp=80, vocab=301, q_heads=6, kv_heads=2, head_dim=16)
+
+
+def decoder_and_weights(dtype, **kw):
+    from paper_2608_02391_gb300 import rollout
+    d = rollout.Decoder(rollout.Shape(**{**SHAPE, **kw}), device="cpu")
+    return d, torch.zeros(d.offsets[-1] + d.tensors[-1].numel, dtype=dtype)
+
+
+def cache_of(copes, dtype, heads=(2, 16, 16), layers=2):
+    code, io = (copes.E4M3, torch.bfloat16) if dtype is None else (copes._DTYPE_CODES[dtype], dtype)
+    return SimpleNamespace(desc=copes.KVCacheDesc(1, code, 100, layers, *heads, 1, 9, 9, 1, 1), pool=torch.zeros(1), heads=heads, io_dtype=io,
+                           length=torch.zeros(9, dtype=torch.int32), refs=torch.zeros(100, dtype=torch.int32))
+
+
+def calls_of(d, w, cache):
+    prompts, u = [[1, 2], [3]], torch.zeros(3, 4)
+    return [lambda: d.score(w, cache, prompts, [[[1]], [[2, 3]]]), lambda: d.greedy(w, cache, prompts, 3),
+            lambda: d.sample(w, cache, prompts, 3, u[:, :2]), lambda: d.sample(w, cache, prompts, 3, u, rollouts=2),
+            lambda: d.read(d.weights(w), cache, [0, 1], prompts)]
+
+
+class Begun(Exception):
+    pass
+
+
+def test_caches_of_other_weights_are_refused_before_any_work(copes, monkeypatch):
+    """None: a cache in 8 bits, for bf16."""
+    def begun(*a, **kw):
+        raise Begun
+
+    monkeypatch.setattr(copes, "cache_grow", begun)
+    monkeypatch.setattr(copes, "cache_free", lambda *a, **kw: None)
+    bf16, fp32 = torch.bfloat16, torch.float32
+    for weights, cache, fine in ((fp32, None, False), (fp32, bf16, False), (bf16, fp32, False), (bf16, None, True), (bf16, bf16, True),
+                                 (fp32, fp32, True)):
+        for call in calls_of(*decoder_and_weights(weights), cache_of(copes, cache)):
+            with pytest.raises(Begun if fine else ValueError, match=None if fine else "cache"):
+                call()
+    for kw in (dict(heads=(4, 16, 16)), dict(heads=(2, 16, 32)), dict(layers=1)):
+        for call in calls_of(*decoder_and_weights(bf16), cache_of(copes, bf16, **kw)):
+            with pytest.raises(ValueError, match="cache"):
+                call()
+    for call in calls_of(*decoder_and_weights(bf16), cache_of(copes, bf16, layers=3)):
+        with pytest.raises(Begun):
+            call()
