@@ -24,6 +24,7 @@ One visit with answers as rewards:
 """
 from __future__ import annotations
 
+import ctypes
 from dataclasses import dataclass
 from typing import Dict, List, Sequence
 
@@ -274,7 +275,7 @@ class Decoder:
         self._check_tokens("prompt", prompts)
         if n_tokens < 1 or rollouts < 1 or not 1e-38 <= temperature <= 1e30:
             raise ValueError(f"{rollouts} continuations of {n_tokens} tokens at temperature {temperature}")
-        if top_k < 0 or not 0 < top_p <= 1 or not 0 <= min_p <= 1:
+        if top_k < 0 or not 0 < top_p <= 1 or not 0 <= min_p <= 1 or not ctypes.c_float(top_p).value > 0:  # in fp32, the calls' type
             raise ValueError(f"cuts to top_k {top_k}, top_p {top_p} and min_p {min_p}")
         first, n = len(prompts), len(prompts) * rollouts
         if u.shape != (n_tokens, n) or u.dtype != torch.float32 or u.device != cache.pool.device:

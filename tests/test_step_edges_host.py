@@ -112,3 +112,16 @@ def test_caches_of_other_weights_are_refused_before_any_work(copes, monkeypatch)
     for call in calls_of(*decoder_and_weights(bf16), cache_of(copes, bf16, layers=3)):
         with pytest.raises(Begun):
             call()
+
+
+def test_cuts_that_fp32_rounds_away_are_refused_before_any_work(copes, monkeypatch):
+    def begun(*a, **kw):
+        raise Begun
+
+    monkeypatch.setattr(copes, "cache_grow", begun)
+    monkeypatch.setattr(copes, "cache_free", lambda *a, **kw: None)
+    d, w = decoder_and_weights(torch.bfloat16)
+    for kw, fine in ((dict(top_p=1e-46), False), (dict(top_p=5e-324), False), (dict(top_p=2e-45), True), (dict(min_p=1e-46), True),
+                     (dict(top_p=1 - 1e-12), True), (dict(temperature=1e-38), True), (dict(temperature=1e30), True)):
+        with pytest.raises(Begun if fine else ValueError, match=None if fine else "cuts"):
+            d.sample(w, cache_of(copes, torch.bfloat16), [[1, 2]], 3, torch.zeros(3, 1), **kw)
