@@ -24,6 +24,7 @@ One visit with answers as rewards:
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from dataclasses import dataclass
 from typing import Dict, List, Sequence
@@ -194,6 +195,14 @@ class Decoder:
         if used + pages > d.n_pages:
             raise ValueError(f"{pages} pages are needed, and {d.n_pages - used} of the cache's {d.n_pages} are free")
 
+    @contextlib.contextmanager
+    def _in_slots(self, cache: copes.KVCache, n: int):
+        """The first n slots of the cache are empty afterwards, of work that fails, too."""
+        try:
+            yield
+        finally:
+            copes.cache_free(cache, torch.arange(n, dtype=torch.int32, device=cache.pool.device))
+
     def _fork_pages(self, size: int, prompt: int, length: int) -> int:
         """Pages of its own that a fork of a prompt has when it has grown to `length` tokens."""
         return -(-length // size) - prompt // size
@@ -222,25 +231,26 @@ class Decoder:
         before any work; what a kernel reports (copes.check), CopesError."""
         self._check_score(cache, prompts, answers)
         weights, device = self.weights(w), cache.pool.device
+        self._check_cache(weights, cache)
         flat = [(i, a) for i, group in enumerate(answers) for a in group]
         n, first = len(flat), len(prompts)
-        slots = list(range(first))
-        logits = self.read(weights, cache, slots, prompts)
-        parents = torch.tensor([i for i, _ in flat], dtype=torch.int32, device=device)
-        children = torch.arange(first, first + n, dtype=torch.int32, device=device)
-        copes.cache_fork(cache, parents, children)
-        width = max(len(a) for _, a in flat)
-        table = torch.full((width, n), -1, dtype=torch.int64)
-        for j, (_, a) in enumerate(flat):
-            table[:len(a), j] = torch.tensor(a)
-        table = table.to(device)
-        total = copes.token_logprobs(logits[parents.long()], table[0]).logprob
-        lengths = torch.tensor([len(a) for _, a in flat])
-        for t in range(1, width):  # after token t - 1, for the answers that have a token t
-            rows = (lengths > t).nonzero()[:, 0].to(device)
-            logits = self.step(weights, cache, children[rows], table[t - 1, rows])
-            total[rows] += copes.token_logprobs(logits, table[t, rows]).logprob
-        copes.cache_free(cache, torch.arange(first + n, dtype=torch.int32, device=device))
+        with self._in_slots(cache, first + n):
+            slots = list(range(first))
+            logits = self.read(weights, cache, slots, prompts)
+            parents = torch.tensor([i for i, _ in flat], dtype=torch.int32, device=device)
+            children = torch.arange(first, first + n, dtype=torch.int32, device=device)
+            copes.cache_fork(cache, parents, children)
+            width = max(len(a) for _, a in flat)
+            table = torch.full((width, n), -1, dtype=torch.int64)
+            for j, (_, a) in enumerate(flat):
+                table[:len(a), j] = torch.tensor(a)
+            table = table.to(device)
+            total = copes.token_logprobs(logits[parents.long()], table[0]).logprob
+            lengths = torch.tensor([len(a) for _, a in flat])
+            for t in range(1, width):  # after token t - 1, for the answers that have a token t
+                rows = (lengths > t).nonzero()[:, 0].to(device)
+                logits = self.step(weights, cache, children[rows], table[t - 1, rows])
+                total[rows] += copes.token_logprobs(logits, table[t, rows]).logprob
         copes.check()
         return total / lengths.to(device)
 
@@ -253,14 +263,15 @@ class Decoder:
         lengths = [len(p) + n_tokens - 1 for p in prompts]  # the last token is not written
         self._check_room(cache, lengths, sum(-(-k // cache.desc.page_size) for k in lengths))
         weights, device = self.weights(w), cache.pool.device
-        slots = torch.arange(len(prompts), dtype=torch.int32, device=device)
-        none = torch.full((len(prompts),), -1, dtype=torch.int64, device=device)
-        logits, out = self.read(weights, cache, list(range(len(prompts))), prompts), []
-        for t in range(n_tokens):
-            out.append(copes.token_logprobs(logits, none, top=1).top_ids[:, 0])
-            if t + 1 < n_tokens:
-                logits = self.step(weights, cache, slots, out[-1])
-        copes.cache_free(cache, slots)
+        self._check_cache(weights, cache)
+        with self._in_slots(cache, len(prompts)):
+            slots = torch.arange(len(prompts), dtype=torch.int32, device=device)
+            none = torch.full((len(prompts),), -1, dtype=torch.int64, device=device)
+            logits, out = self.read(weights, cache, list(range(len(prompts))), prompts), []
+            for t in range(n_tokens):
+                out.append(copes.token_logprobs(logits, none, top=1).top_ids[:, 0])
+                if t + 1 < n_tokens:
+                    logits = self.step(weights, cache, slots, out[-1])
         copes.check()
         return torch.stack(out, 1)
 
@@ -288,20 +299,21 @@ class Decoder:
             self._check_room(cache, prompt + ends, sum(-(-p // size) + rollouts * self._fork_pages(size, p, p + n_tokens - 1)
                                                        for p in prompt))
         weights, device = self.weights(w), cache.pool.device
-        slots = torch.arange(first, dtype=torch.int32, device=device)
-        logits = self.read(weights, cache, list(range(first)), prompts)
-        if rollouts > 1:
-            parents, slots = slots.repeat_interleave(rollouts), torch.arange(first, first + n, dtype=torch.int32, device=device)
-            copes.cache_fork(cache, parents, slots)
-            logits = logits.repeat_interleave(rollouts, 0)
-        tokens = torch.empty((n, n_tokens), dtype=torch.int64, device=device)
-        logprob = torch.empty((n, n_tokens), dtype=torch.float32, device=device)
-        for t in range(n_tokens):
-            r = copes.sample_tokens(logits, u[t].contiguous(), top_k=top_k, top_p=top_p, min_p=min_p, scale=1.0 / temperature)
-            tokens[:, t], logprob[:, t] = r.ids, r.logprob
-            if t + 1 < n_tokens:
-                logits = self.step(weights, cache, slots, r.ids.clamp(min=0))
-        copes.cache_free(cache, torch.arange(n if rollouts == 1 else first + n, dtype=torch.int32, device=device))
+        self._check_cache(weights, cache)
+        with self._in_slots(cache, n if rollouts == 1 else first + n):
+            slots = torch.arange(first, dtype=torch.int32, device=device)
+            logits = self.read(weights, cache, list(range(first)), prompts)
+            if rollouts > 1:
+                parents, slots = slots.repeat_interleave(rollouts), torch.arange(first, first + n, dtype=torch.int32, device=device)
+                copes.cache_fork(cache, parents, slots)
+                logits = logits.repeat_interleave(rollouts, 0)
+            tokens = torch.empty((n, n_tokens), dtype=torch.int64, device=device)
+            logprob = torch.empty((n, n_tokens), dtype=torch.float32, device=device)
+            for t in range(n_tokens):
+                r = copes.sample_tokens(logits, u[t].contiguous(), top_k=top_k, top_p=top_p, min_p=min_p, scale=1.0 / temperature)
+                tokens[:, t], logprob[:, t] = r.ids, r.logprob
+                if t + 1 < n_tokens:
+                    logits = self.step(weights, cache, slots, r.ids.clamp(min=0))
         copes.check()
         if bool((tokens < 0).any()):
             raise RuntimeError("logits that nothing can be drawn from")

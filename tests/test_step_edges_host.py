@@ -125,3 +125,30 @@ def test_cuts_that_fp32_rounds_away_are_refused_before_any_work(copes, monkeypat
                      (dict(top_p=1 - 1e-12), True), (dict(temperature=1e-38), True), (dict(temperature=1e30), True)):
         with pytest.raises(Begun if fine else ValueError, match=None if fine else "cuts"):
             d.sample(w, cache_of(copes, torch.bfloat16), [[1, 2]], 3, torch.zeros(3, 1), **kw)
+
+
+@pytest.mark.parametrize("fails", ["read", "step", "cache_fork"])
+def test_slots_are_empty_after_work_that_fails(copes, monkeypatch, fails):
+    """Each call frees the slots that it was to use, once, whether reading, forking or a later step fails."""
+    def failing(*a, **kw):
+        raise Begun
+
+    freed = []
+    monkeypatch.setattr(copes, "cache_free", lambda cache, slots, **kw: freed.append(slots.tolist()))
+    monkeypatch.setattr(copes, "cache_fork", failing if fails == "cache_fork" else lambda *a, **kw: None)
+    ones = lambda logits, *a, **kw: SimpleNamespace(logprob=torch.zeros(len(logits)), top_ids=torch.zeros(len(logits), 1, dtype=torch.int64),
+                                                    ids=torch.zeros(len(logits), dtype=torch.int64))
+    monkeypatch.setattr(copes, "token_logprobs", ones)
+    monkeypatch.setattr(copes, "sample_tokens", ones)
+    d, w = decoder_and_weights(torch.bfloat16)
+    monkeypatch.setattr(d, "read", failing if fails == "read" else lambda weights, cache, slots, prompts: torch.zeros(len(prompts), 301))
+    monkeypatch.setattr(d, "step", failing)
+    prompts, u, cache = [[1, 2], [3]], torch.zeros(3, 4), cache_of(copes, torch.bfloat16)
+    for n, call in ((5, lambda: d.score(w, cache, prompts, [[[1]], [[2, 3], [4, 5, 6]]])), (2, lambda: d.greedy(w, cache, prompts, 3)),
+                    (2, lambda: d.sample(w, cache, prompts, 3, u[:, :2])), (6, lambda: d.sample(w, cache, prompts, 3, u, rollouts=2))):
+        if fails == "cache_fork" and n == 2:
+            continue
+        freed.clear()
+        with pytest.raises(Begun):
+            call()
+        assert freed == [list(range(n))]
