@@ -565,9 +565,17 @@ __device__ __forceinline__ void warp_tile(uint32_t keys, uint32_t values, int le
 // Codes become fp16 on their way from shared memory to the matrix unit, exactly; what they are to be multiplied
 // by multiplies scores and weights instead.  Which d a lane's share of a product stands for is free, if it is the
 // same for both factors: lanes take whole pieces of 16 bytes of keys, and of values 8 bytes of two tokens at a time.
-template <typename S>
+//
+// kPlain: q.plain.  Sums of codes are 0 or between 2^-33 and 2^32, which plain units do not take out of fp32 before the
+// key's brings them where they belong.  Another unit may: where it is above 1 and the key's below, or the other way round, the
+// product of the two is taken first, which is exact.  (A branch within one form cost 2% of 128 rows of up to 16,384.)
+template <typename S, bool kPlain>
 __device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int left, float scale, const Queries<S> &q,
                                            Running<S> &r, uint32_t power) {
+  if constexpr (!kPlain) {
+    asm volatile("" : "+f"(scale));  // (else it is kept in a register from tile to tile: 1% with 24/1 heads of 64)
+    scale *= kLog2e;
+  }
   constexpr int NT = S::NT, KS = S::DP / 16, kPitch = S::kChunks * 16, kHalves = S::kOwn / 16, kOf = 2 * kHalves;
   const int lane = threadIdx.x & 31, row = lane >> 2;
   float s[NT][2 * kOf];  // tokens lane / 4 + 8 (e / 2), heads 2 (lane % 4) + e % 2
@@ -605,24 +613,6 @@ __device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int l
     key_unit[e] = __uint_as_float((both & 0xFFu) << 23);
     value_unit[e] = __uint_as_float((both >> 8) << 23);
   }
-  // Sums of codes are 0 or between 2^-33 and 2^32, which plain units do not take out of fp32 on the way.  Others may where
-  // the key's, too, would not: one above 1 and one below are multiplied first, exactly.
-  if (q.plain) {
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int t = 0; t < 2 * kOf; ++t) s[j][t] = s[j][t] * q.unit[j][t & 1] * key_unit[t >> 1];
-  } else {
-    asm volatile("" : "+f"(scale));  // (not to be kept in a register from tile to tile for this)
-    scale *= kLog2e;
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int t = 0; t < 2 * kOf; ++t) {
-        const float a = q.unit[j][t & 1], b = key_unit[t >> 1];
-        s[j][t] = ((a < 1.0f) == (b < 1.0f) ? s[j][t] * a * b : s[j][t] * (a * b)) * scale;
-      }
-  }
   bool grown = false;
   float keep[NT][2], over[NT][2], unit[NT][2];
 #pragma unroll
@@ -633,7 +623,11 @@ __device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int l
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < kOf; ++t) {
-        s[j][2 * t + e] = row + 8 * t < left ? s[j][2 * t + e] : -INFINITY;
+        const float u = q.unit[j][e], k = key_unit[t];
+        float score = s[j][2 * t + e];
+        if constexpr (kPlain) score = score * u * k;
+        else score = ((u < 1.0f) == (k < 1.0f) ? score * u * k : score * (u * k)) * scale;
+        s[j][2 * t + e] = row + 8 * t < left ? score : -INFINITY;
         top = fmaxf(top, s[j][2 * t + e]);
       }
       top = fmaxf(top, __shfl_xor_sync(kAll, top, 4));
@@ -979,8 +973,12 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) attend_kernel(AttendAr
     const int left = at.tile < at.tiles ? at.tokens - at.tile * TILE - member * S::kOwn : 0;
     const uint32_t tile = stages + j % S::kStages * S::kStage;
     if (left > 0) {
-      if constexpr (S::kFp8) warp_tile8<S>(tile, tile + S::kPart, left, a.scale, q, r, powers[0]);
-      else warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
+      if constexpr (S::kFp8) {
+        if (q.plain) warp_tile8<S, true>(tile, tile + S::kPart, left, a.scale, q, r, powers[0]);
+        else warp_tile8<S, false>(tile, tile + S::kPart, left, a.scale, q, r, powers[0]);
+      } else {
+        warp_tile<S>(tile, tile + S::kPart, left, scale, q, r);
+      }
     }
 #pragma unroll
     for (int s = 0; s + 1 < S::kStages; ++s) powers[s] = powers[s + 1];
