@@ -44,7 +44,7 @@
 // unit as fp16, which holds them exactly, one conversion for two; a key's power of two multiplies its scores, a
 // value's its weights; queries and weights are scaled by powers of two into fp16's range (to_units, warp_tile8).
 // A warp takes 32 tokens at a time, as many bytes as 16 of bf16, and three blocks fit on an SM.  128 rows of up to
-// 16,384 tokens, 32/8 heads of 128: 2.11 GB in 371 us, 5.7 TB/s (one row of 131,071 57 us, 32 of up to 4,096 34, 64 of up
+// 16,384 tokens, 32/8 heads of 128: 2.11 GB in 368 us, 5.7 TB/s (one row of 131,071 56 us, 32 of up to 4,096 33, 64 of up
 // to 8,000 with 14/2 heads of 64 27, 32 of up to 8,000 with 12/4 heads of 256 59).
 #include <math.h>
 
@@ -101,8 +101,8 @@ struct Shape {
   static constexpr int kSmem = kStages * kStage + kFixed;
   // blocks of an SM by its 228 KB, 1 KB of them taken for each block, and by its registers
   static constexpr int kFit = 228 * 1024 / (kSmem + 1280);
-  // (Three variants spill all the same: fp32 heads of 256 20 bytes of a thread, of 128 with two column
-  // tiles 40, of 64 side by side 16.)
+  // (Four variants spill all the same: fp32 heads of 256 16 bytes of a thread, of 128 with two column
+  // tiles 8, of 64 side by side 16, and 8 bits with heads of 128 and two column tiles 8.)
   static constexpr int kByRegs = 65536 / (kThreads * (kFp8 ? (DP > 128 || NT > 1 ? 248 : 168) : DP > 64 || NT > 1 ? 248 : kFp32 ? 200 : 168));
   static constexpr int kPerSm = kFit < kByRegs ? kFit : kByRegs;
   static_assert(kSmem <= 227 * 1024, "more shared memory than an SM has");
@@ -650,7 +650,8 @@ __device__ __forceinline__ void warp_tile8(uint32_t keys, uint32_t values, int l
       most |= __float_as_uint(largest) >> 23 << 16 * e;
     }
     // The weights times their values' powers of two, in units that bring the tile's largest of a head into
-    // [2^14, 2^15), in two fp16 terms: 2^-22 of one, or 2^-39 of the largest, lost.
+    // [2^14, 2^15), in two fp16 terms: 2^-22 of one, or 2^-39 of the largest, lost (2^-25 of one below 2^-112, which
+    // fp32's powers of two bring no further than 1).
     most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 4));
     most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 8));
     most = __vmaxu2(most, __shfl_xor_sync(kAll, most, 16));

@@ -383,10 +383,12 @@ struct Rows {
 // values a lane.  The row's unit is the power of two that brings its largest finite value into (224, 448]; as codes are
 // floats, a power of two costs no precision that a finer factor would keep.  `wide`: all rows are 16-byte aligned.
 //
-// Where a row's token is takes a chain of three loads, so a block looks up its kRows rows first, all at once, and
+// Where a row's token is takes a chain of three loads, so a block looks up its rows first, all at once, and
 // each thread then has kJobs pieces on their way: 32,000 tokens of 8 heads of 128, 197 MB each way, are written and
 // read back in 87 us together, 4.5 TB/s (looked up by each team, with one piece of a thread on its way: 174; with two, 157;
-// with eight, 121 where four took 110), bound by what converts them.  A token each of 64 sequences: 5.8 us.
+// with eight, 121 where four took 110), bound by HBM and by instructions: 148 of a lane to write 8 values and 101 to read
+// them, of which unpacking, scaling, converting and packing are some 30; the rest is a piece's place, address and
+// predicates and the maximum's shuffles.  A token each of 64 sequences: 5.7 us.
 constexpr int kCodeThreads = 256, kJobs = 4;
 struct alignas(16) Place {
   char *codes, *power;  // of the token's first head; NULL: no token

@@ -5,7 +5,7 @@
 // A row's values stay in the registers of its threads from the one read to the one write, so each
 // array passes HBM once, and HBM bounds it where there are many rows: 16,384 of 4,096 in bf16, with a norm after the
 // block and a gate for every channel, 537 MB in 99 us, 5.4 TB/s, four fifths of a copy's rate (of the issue slots,
-// half: a value's way from bf16 and back takes as many operations as the sums).  A few rows are a chain of a load, two
+// two thirds: a value's way from bf16 and back takes as many operations as the sums).  A few rows are a chain of a load, two
 // sums over the row's threads and a store: one row of 896 2.2 us, 22,400 rows of 128 (the norm alone) 4.2, 301 rows of 2,561
 // in fp32 that begin anywhere 8.6.
 #include <float.h>
@@ -149,7 +149,8 @@ __device__ __forceinline__ void add(float (&to)[kN], const float (&v)[kN], float
   }
 }
 
-// A team of threads for each row, kP pieces of kBytes each; a block has blockDim.x / team rows.
+// A team of threads for each row, kP pieces of kBytes each; a block has blockDim.x / team rows.  (In bf16 two forms spill: 2 pieces
+// of 16 bytes 40 bytes of a thread stored and 12 loaded, 16 pieces of 4 112 and 56.)
 template <int kBytes, int kP>
 constexpr int kMostThreads = kBytes < 16 && kP <= 4 ? 1024 : 512;
 template <typename T, int kBytes, int kP>

@@ -1135,7 +1135,8 @@ constexpr int smem_of(int vocab) {  // and one chunk more, as a row may begin wi
   return kSharedBytes + 8 * (2 * kList + (vocab - 1) / (kChunkPieces * Row<T>::kN) + 2);
 }
 
-// kPerSm: blocks that an SM holds, two where rows alone fill the GPU; one has twice the registers.
+// kPerSm: blocks that an SM holds, two where rows alone fill the GPU; one has twice the registers.  (All but fp32 with one spill: bf16
+// with two 28 bytes of a thread, with one 8 stored and 48 loaded, fp32 with two 8.)
 template <typename T, int kThreads, int kPerSm>
 __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(SampleArgs a, float c, float farthest, int size) {
   extern __shared__ __align__(16) char smem[];
