@@ -158,9 +158,11 @@ class Decoder:
     def _check_cache(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache) -> None:
         """Raises for a cache whose first append would refuse these weights' keys, when it has grown already."""
         s, (kv, _, d), dtype = self.shape, cache.heads, weights["embed"].dtype
+        if not s.layers:
+            return
         if dtype != cache.io_dtype:
             raise ValueError(f"weights of {dtype} with a cache for {cache.io_dtype}")
-        if s.layers and ((kv, d) != (s.kv_heads, s.head_dim) or cache.desc.n_layers < s.layers):
+        if (kv, d) != (s.kv_heads, s.head_dim) or cache.desc.n_layers < s.layers:
             raise ValueError(f"a cache of {cache.desc.n_layers} layers of {kv} heads of {d} for {s.layers} of {s.kv_heads} of {s.head_dim}")
 
     def read(self, weights: Dict[str, torch.Tensor], cache: copes.KVCache, slots: Sequence[int],

@@ -152,3 +152,12 @@ def test_slots_are_empty_after_work_that_fails(copes, monkeypatch, fails):
         with pytest.raises(Begun):
             call()
         assert freed == [list(range(n))]
+
+
+def test_a_decoder_without_layers_takes_any_cache(copes, monkeypatch):
+    """It writes nothing there."""
+    for name in ("cache_grow", "cache_free"):
+        monkeypatch.setattr(copes, name, lambda *a, **kw: None)
+    d, w = decoder_and_weights(torch.float32, layers=0)
+    logits = d.read(d.weights(w), cache_of(copes, torch.bfloat16, heads=(1, 16, 64), layers=1), [0, 1], [[1, 2], [3]])
+    assert logits.shape == (2, 301)
